@@ -289,6 +289,140 @@ mace_status mace_block_rounding(mace_graph* g, int32_t block, int32_t format, in
  * flag 1 is set, else MACE_ERANGE if flag 2 is set, else MACE_OK. */
 mace_status mace_graph_check(mace_graph* g, int32_t* device_flags, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Dense operators beside the MACE step: what a program that trains or serves a
+ * head on the library's energies (a species-routed readout, a small network
+ * distilled from a MACE teacher) calls per step.  They stand alone: no graph
+ * handle.  All matrices are row-major, as in the weight blob; `dtype` is the
+ * type of every operand and result unless said otherwise, sums are FP32 and
+ * each result is rounded once, to nearest even.  FP32 products are split-BF16
+ * ones (as MACE_PRODUCTS_SPLIT_BF16, with the same range).  Leading dimensions
+ * are in elements and at least the row length; any alignment of rows to an
+ * element runs, 16-byte aligned rows of a multiple of 8 elements run fastest.
+ * No entry point synchronises, allocates or records a memset: all can be
+ * captured in a HIP graph.  Results do not depend on the order in which blocks
+ * run (no floating-point atomics).  Calls that share a workspace must be
+ * ordered by the caller. */
+typedef enum { MACE_TYPE_FP32 = 0, MACE_TYPE_BF16 = 1, MACE_TYPE_FP16 = 2 } mace_dtype;
+typedef enum {
+  MACE_ACT_NONE = 0,
+  MACE_ACT_SILU = 1, /* z / (1 + exp(-z)) */
+  MACE_ACT_GELU = 2  /* z Phi(z), Phi the normal distribution function */
+} mace_activation;
+
+/* Grouped dense layer.  Row i of group g (rows group_offsets[g] up to, not
+ * including, group_offsets[g + 1]): z_i = x_i W_g + b_g, y_i = act(z_i) + r_i.
+ * One group is an ordinary layer; several are the products of a router's
+ * experts (mace_route_build gives rows in that order and the offsets), or one
+ * weight block per species.  n_groups <= 1024, n_rows <= 2^30, n_in and n_out
+ * <= 2^20, else MACE_EUNSUPPORTED. */
+typedef struct mace_linear_desc {
+  int64_t n_rows;
+  int32_t n_in, n_out, n_groups;
+  int32_t dtype; /* mace_dtype */
+  int32_t act;   /* mace_activation */
+  int64_t ld_x, ld_y, ld_residual, ld_preact; /* (of tensors not passed: ignored, but at least the row length) */
+} mace_linear_desc;
+
+/* x (dev) [n_rows][n_in]; weights (dev) [n_groups][n_in][n_out] contiguous;
+ * bias (dev) [n_groups][n_out] or NULL; residual r (dev) [n_rows][n_out] or
+ * NULL, may be y itself; group_offsets (dev) [n_groups + 1] nondecreasing from
+ * 0, or NULL for one group of all rows; y (dev) [n_rows][n_out]; preact (dev)
+ * [n_rows][n_out] or NULL: receives z, rounded to dtype, for the backward.
+ * Rows behind group_offsets[n_groups] (a router's dropped slots) give zeros in
+ * y and preact and are not read. */
+mace_status mace_linear_forward(const mace_linear_desc* desc, const void* x, const void* weights, const void* bias,
+                                const void* residual, const int32_t* group_offsets, void* y, void* preact,
+                                void* stream);
+
+/* Gradients of mace_linear_forward from dy (dev) [n_rows][n_out]:
+ * dz = dy act'(z) (rounded to dtype where there is an activation: it is the
+ * products' operand), dx = dz W_g^T, dweights_g = x_g^T dz_g, dbias_g = the
+ * column sums of dz_g before that rounding; the residual's gradient is dy.
+ * preact: the forward's z (MACE_ACT_NONE: not read, may be NULL).  dx (dev)
+ * [n_rows][n_in], dweights (dev) [n_groups][n_in][n_out], dbias (dev)
+ * [n_groups][n_out]: each may be NULL if not wanted.  Groups without rows get
+ * zero gradients, rows behind the last group zero dx.  workspace (dev) of at
+ * least mace_linear_backward_workspace_bytes (0 on invalid input), which
+ * asks whether dbias and dweights are wanted. */
+size_t mace_linear_backward_workspace_bytes(const mace_linear_desc* desc, int32_t want_bias, int32_t want_weights);
+mace_status mace_linear_backward(const mace_linear_desc* desc, const void* dy, int64_t ld_dy, const void* x,
+                                 const void* weights, const void* preact, const int32_t* group_offsets, void* dx,
+                                 int64_t ld_dx, void* dweights, void* dbias, void* workspace, size_t workspace_bytes,
+                                 void* stream);
+
+/* Rows sorted by expert and back.  A slot is (token t, choice s), numbered
+ * t * top_k + s; its expert is expert[t][s], and an index outside 0 ..
+ * n_experts - 1 (-1, say) drops it.  n_experts <= 512, n_tokens * top_k <=
+ * 2^30, else MACE_EUNSUPPORTED. */
+typedef struct mace_route_desc {
+  int64_t n_tokens;
+  int32_t top_k, n_experts, width;
+  int32_t dtype;              /* mace_dtype of token and row tensors */
+  int64_t ld_tokens, ld_rows; /* of [n_tokens][width] and [n_tokens * top_k][width] tensors */
+} mace_route_desc;
+
+/* The stable sort of the slots by expert, dropped slots last: slot_of_row
+ * (dev) [n_tokens * top_k], its inverse row_of_slot (dev) [n_tokens][top_k],
+ * offsets (dev) [n_experts + 1]: expert e's rows are offsets[e] up to
+ * offsets[e + 1], and rows from offsets[n_experts] on are dropped slots.
+ * expert (dev) [n_tokens][top_k].  workspace (dev, may be NULL up to 4096
+ * slots) of at least mace_route_workspace_bytes (0 on invalid input).
+ * Leading dimensions, width and dtype of desc do not matter here. */
+size_t mace_route_workspace_bytes(const mace_route_desc* desc);
+mace_status mace_route_build(const mace_route_desc* desc, const int32_t* expert, int32_t* row_of_slot,
+                             int32_t* slot_of_row, int32_t* offsets, void* workspace, size_t workspace_bytes,
+                             void* stream);
+/* rows (dev) [n_tokens * top_k][width]: each kept slot's token, zeros for
+ * dropped slots.  Its gradient is mace_route_combine without weights. */
+mace_status mace_route_gather(const mace_route_desc* desc, const void* tokens, const int32_t* row_of_slot,
+                              const int32_t* offsets, void* rows, void* stream);
+/* out (dev) [n_tokens][width]: out_t = the sum over t's kept slots, in their
+ * order, of weights[t][s] times the slot's row; weights (dev) [n_tokens][top_k]
+ * FP32, or NULL for 1.  A token without kept slots gets zeros; the rows of
+ * dropped slots are not used, whatever they hold. */
+mace_status mace_route_combine(const mace_route_desc* desc, const void* rows, const float* weights,
+                               const int32_t* row_of_slot, const int32_t* offsets, void* out, void* stream);
+/* Gradients of mace_route_combine from dout (dev) [n_tokens][width]: drows
+ * (dev) [n_tokens * top_k][width], a row being its weight times its token's
+ * dout, zeros for dropped slots; dweights (dev) [n_tokens][top_k] FP32, a
+ * slot's being the dot product of its row and dout, zero for dropped slots.
+ * Each may be NULL if not wanted; rows may be NULL without dweights. */
+mace_status mace_route_combine_backward(const mace_route_desc* desc, const void* dout, const void* rows,
+                                        const float* weights, const int32_t* row_of_slot, const int32_t* offsets,
+                                        void* drows, float* dweights, void* stream);
+
+/* Newton-Schulz orthogonalisation of a batch of matrices (gradients or their
+ * momenta, before an optimiser applies them): x = g / (|g|_F + eps), then per
+ * step (a, b, c) of coefficients x <- a x + (b A + c A A) x with A = x x^T;
+ * a matrix with more rows than columns takes A = x^T x on the other side,
+ * which is the same map.  g and out (dev) `batch` matrices [rows][cols] with
+ * leading dimensions ld_g, ld_out and strides stride_g, stride_out between
+ * matrices (elements); out may be g itself.  coefficients (host)
+ * [n_steps][3], 0 <= n_steps <= 64.  They are checked on the host: over the
+ * singular values that can occur (0 to 1 at the start) no step may reach a
+ * singular value beyond 3.4 or a b A + c A A beyond 200, else MACE_ERANGE
+ * (the products' operands are pairs of binary16 with fixed scales).  Products
+ * are as accurate as FP32's (in FP64 where the shorter side is at most 32); a
+ * BF16 result of at least 128 rows and columns takes all but its last two steps
+ * with binary16 operands, whose error stays below a third of the result's
+ * rounding.  A matrix with a non-finite
+ * element gives NaN, the others of the batch are not touched by it.  rows and
+ * cols <= 2^15, batch * rows * cols <= 2^34, else MACE_EUNSUPPORTED.
+ * workspace (dev) of at least mace_orthogonalise_workspace_bytes (0 on
+ * invalid input). */
+typedef struct mace_orthogonalise_desc {
+  int64_t batch;
+  int32_t rows, cols;
+  int32_t dtype; /* mace_dtype */
+  int32_t n_steps;
+  int64_t ld_g, stride_g, ld_out, stride_out;
+  double eps; /* >= 0 */
+} mace_orthogonalise_desc;
+size_t mace_orthogonalise_workspace_bytes(const mace_orthogonalise_desc* desc);
+mace_status mace_orthogonalise(const mace_orthogonalise_desc* desc, const void* g, const double* coefficients,
+                               void* out, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Releases the host handle (the workspace stays the caller's). */
 void mace_graph_destroy(mace_graph* g);
 

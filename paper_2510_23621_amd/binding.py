@@ -28,6 +28,12 @@ MACE_PRODUCTS_SPLIT_BF16 = 2
 MACE_BLOCK_EDGE_PRODUCT = 0
 MACE_BLOCK_SYMMETRIC_CONTRACTION = 1
 MACE_BLOCK_RADIAL_MLP = 2
+MACE_TYPE_FP32 = 0
+MACE_TYPE_BF16 = 1
+MACE_TYPE_FP16 = 2
+MACE_ACT_NONE = 0
+MACE_ACT_SILU = 1
+MACE_ACT_GELU = 2
 MACE_NEIGHBOR_SCRATCH_BYTES = 80 << 20
 MAX_LAYERS = 8   # MACE_MAX_LAYERS
 STATUS = {0: "MACE_OK", -1: "MACE_EINVAL", -2: "MACE_ERANGE", -3: "MACE_ENOSPACE", -4: "MACE_EHIP",
@@ -39,7 +45,10 @@ EXPORTED = ["mace_weight_layout", "mace_workspace_bytes", "mace_neighbor_list", 
             "mace_profile_read", "mace_kernel_name", "mace_graph_check", "mace_profile_work",
             "mace_neighbor_workspace_bytes", "mace_neighbor_list_device", "mace_layer0_form",
             "mace_fp32_products", "mace_block_rounding", "mace_neighbor_list_device_noalloc",
-            "mace_debug_fused_linears"]
+            "mace_debug_fused_linears", "mace_linear_forward", "mace_linear_backward",
+            "mace_linear_backward_workspace_bytes", "mace_route_workspace_bytes", "mace_route_build",
+            "mace_route_gather", "mace_route_combine", "mace_route_combine_backward",
+            "mace_orthogonalise_workspace_bytes", "mace_orthogonalise"]
 
 
 class MaceError(RuntimeError):
@@ -54,6 +63,26 @@ class mace_model_desc(ctypes.Structure):
                 ("envelope_p", ctypes.c_int32), ("radial_hidden", ctypes.c_int32 * 3),
                 ("readout_hidden", ctypes.c_int32), ("hidden_lmax", ctypes.c_int32 * MAX_LAYERS),
                 ("r_cut", ctypes.c_double), ("c_norm", ctypes.c_double)]
+
+
+class mace_linear_desc(ctypes.Structure):
+    _fields_ = [("n_rows", ctypes.c_int64), ("n_in", ctypes.c_int32), ("n_out", ctypes.c_int32),
+                ("n_groups", ctypes.c_int32), ("dtype", ctypes.c_int32), ("act", ctypes.c_int32),
+                ("ld_x", ctypes.c_int64), ("ld_y", ctypes.c_int64), ("ld_residual", ctypes.c_int64),
+                ("ld_preact", ctypes.c_int64)]
+
+
+class mace_route_desc(ctypes.Structure):
+    _fields_ = [("n_tokens", ctypes.c_int64), ("top_k", ctypes.c_int32), ("n_experts", ctypes.c_int32),
+                ("width", ctypes.c_int32), ("dtype", ctypes.c_int32), ("ld_tokens", ctypes.c_int64),
+                ("ld_rows", ctypes.c_int64)]
+
+
+class mace_orthogonalise_desc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("rows", ctypes.c_int32), ("cols", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("n_steps", ctypes.c_int32), ("ld_g", ctypes.c_int64),
+                ("stride_g", ctypes.c_int64), ("ld_out", ctypes.c_int64), ("stride_out", ctypes.c_int64),
+                ("eps", ctypes.c_double)]
 
 
 def make_desc(n_species, K, hidden_lmax, r_cut, c_norm, n_layers=2, sh_lmax=3, correlation=3, n_bessel=8,
@@ -112,6 +141,21 @@ def lib() -> ctypes.CDLL:
         L.mace_profile_read.argtypes = [P, P, P]
         L.mace_kernel_name.argtypes = [I32]
         L.mace_kernel_name.restype = ctypes.c_char_p
+        lp, rp = ctypes.POINTER(mace_linear_desc), ctypes.POINTER(mace_route_desc)
+        op = ctypes.POINTER(mace_orthogonalise_desc)
+        L.mace_linear_forward.argtypes = [lp, P, P, P, P, P, P, P, P]
+        L.mace_linear_backward_workspace_bytes.argtypes = [lp, I32, I32]
+        L.mace_linear_backward_workspace_bytes.restype = Z
+        L.mace_linear_backward.argtypes = [lp, P, I64, P, P, P, P, P, I64, P, P, P, Z, P]
+        L.mace_route_workspace_bytes.argtypes = [rp]
+        L.mace_route_workspace_bytes.restype = Z
+        L.mace_route_build.argtypes = [rp, P, P, P, P, P, Z, P]
+        L.mace_route_gather.argtypes = [rp, P, P, P, P, P]
+        L.mace_route_combine.argtypes = [rp, P, P, P, P, P, P]
+        L.mace_route_combine_backward.argtypes = [rp, P, P, P, P, P, P, P, P]
+        L.mace_orthogonalise_workspace_bytes.argtypes = [op]
+        L.mace_orthogonalise_workspace_bytes.restype = Z
+        L.mace_orthogonalise.argtypes = [op, P, P, P, P, Z, P]
         for name in EXPORTED:
             f = getattr(L, name)
             if f.restype is ctypes.c_int:
@@ -383,6 +427,59 @@ def mace_profile_work(handle):
 
 def mace_kernel_name(kernel: int) -> str:
     return lib().mace_kernel_name(kernel).decode()
+
+
+def mace_linear_forward(desc: mace_linear_desc, x, weights, bias, residual, group_offsets, y, preact=None, stream=None):
+    _check(lib().mace_linear_forward(desc, _ptr(x), _ptr(weights), _ptr(bias), _ptr(residual), _ptr(group_offsets),
+                                     _ptr(y), _ptr(preact), _stream(stream)), "mace_linear_forward")
+
+
+def mace_linear_backward_workspace_bytes(desc: mace_linear_desc, want_bias: bool, want_weights: bool) -> int:
+    return lib().mace_linear_backward_workspace_bytes(desc, want_bias, want_weights)
+
+
+def mace_linear_backward(desc: mace_linear_desc, dy, ld_dy, x, weights, preact, group_offsets, dx, ld_dx, dweights,
+                         dbias, workspace, workspace_bytes, stream=None):
+    _check(lib().mace_linear_backward(desc, _ptr(dy), ld_dy, _ptr(x), _ptr(weights), _ptr(preact),
+                                      _ptr(group_offsets), _ptr(dx), ld_dx, _ptr(dweights), _ptr(dbias),
+                                      _ptr(workspace), workspace_bytes, _stream(stream)), "mace_linear_backward")
+
+
+def mace_route_workspace_bytes(desc: mace_route_desc) -> int:
+    return lib().mace_route_workspace_bytes(desc)
+
+
+def mace_route_build(desc: mace_route_desc, expert, row_of_slot, slot_of_row, offsets, workspace, workspace_bytes,
+                     stream=None):
+    _check(lib().mace_route_build(desc, _ptr(expert), _ptr(row_of_slot), _ptr(slot_of_row), _ptr(offsets),
+                                  _ptr(workspace), workspace_bytes, _stream(stream)), "mace_route_build")
+
+
+def mace_route_gather(desc: mace_route_desc, tokens, row_of_slot, offsets, rows, stream=None):
+    _check(lib().mace_route_gather(desc, _ptr(tokens), _ptr(row_of_slot), _ptr(offsets), _ptr(rows),
+                                   _stream(stream)), "mace_route_gather")
+
+
+def mace_route_combine(desc: mace_route_desc, rows, weights, row_of_slot, offsets, out, stream=None):
+    _check(lib().mace_route_combine(desc, _ptr(rows), _ptr(weights), _ptr(row_of_slot), _ptr(offsets), _ptr(out),
+                                    _stream(stream)), "mace_route_combine")
+
+
+def mace_route_combine_backward(desc: mace_route_desc, dout, rows, weights, row_of_slot, offsets, drows, dweights,
+                                stream=None):
+    _check(lib().mace_route_combine_backward(desc, _ptr(dout), _ptr(rows), _ptr(weights), _ptr(row_of_slot),
+                                             _ptr(offsets), _ptr(drows), _ptr(dweights), _stream(stream)),
+           "mace_route_combine_backward")
+
+
+def mace_orthogonalise_workspace_bytes(desc: mace_orthogonalise_desc) -> int:
+    return lib().mace_orthogonalise_workspace_bytes(desc)
+
+
+def mace_orthogonalise(desc: mace_orthogonalise_desc, g, coefficients, out, workspace, workspace_bytes, stream=None):
+    """coefficients: float64 numpy array [n_steps, 3] on the host."""
+    _check(lib().mace_orthogonalise(desc, _ptr(g), _ptr(coefficients), _ptr(out), _ptr(workspace), workspace_bytes,
+                                    _stream(stream)), "mace_orthogonalise")
 
 
 def kernel_ids() -> dict:

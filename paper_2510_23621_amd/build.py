@@ -19,7 +19,7 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libmace_amd.so")
 HIP_SOURCES = ["api.hip", "k_edge.hip", "k_radial.hip", "k_tpr.hip", "k_layer0.hip", "k_sender.hip", "k_symcon.hip", "k_node.hip",
-               "k_neighbors.hip", "k_fp64.hip"]
+               "k_neighbors.hip", "k_fp64.hip", "k_linear.hip", "k_route.hip", "k_orthogonalise.hip"]
 # files whose FP64 arithmetic must round exactly as written (no fused multiply-adds)
 NO_CONTRACT = {"k_neighbors.hip"}
 HIPCC_FLAGS = [

@@ -1,0 +1,434 @@
+// Tiles of dense matrix products on MFMA, shared by the linear and the
+// orthogonalisation kernels: operands of FP32, bfloat16, binary16 or pairs of
+// binary16 go through LDS as one to three 16-bit planes, and a block multiplies
+// them with v_mfma_f32_16x16x32.
+#pragma once
+
+#include "mace_internal.h"
+
+namespace mace {
+
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef unsigned short us8 __attribute__((ext_vector_type(8)));
+typedef short s4 __attribute__((ext_vector_type(4)));
+
+// A binary16 pair (hi, lo) stored as two planes, `plane` elements apart: 22
+// significand bits, for operands whose range is known.
+struct HalfPair {};
+
+// Planes an operand is carried as: FP32 as three bfloat16 (x0 + x1 + x2 = x
+// exactly, the six partial products down to 2^-18 relative kept, so products
+// are as accurate as FP32's), 16-bit types as themselves, pairs as two (three
+// partial products kept, the dropped one is 2^-22 relative).
+template <class T> struct Planes { static constexpr int n = 1; };
+template <> struct Planes<float> { static constexpr int n = 3; };
+template <> struct Planes<HalfPair> { static constexpr int n = 2; };
+
+template <class T>
+__device__ __forceinline__ f4 mfma32(us8 a, us8 b, f4 c) {
+  if constexpr (sizeof(T) == 4 || __is_same(T, __bf16))
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
+}
+
+// ------------------------------------------------------------------ elements
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(__bf16 x) { return (float)x; }
+__device__ __forceinline__ float to_f32(_Float16 x) { return (float)x; }
+
+// eight consecutive elements in registers
+template <class T> struct Vec8 {
+  us8 v;
+  __device__ __forceinline__ float get(int i) const { return to_f32(__builtin_bit_cast(T, (unsigned short)v[i])); }
+  __device__ __forceinline__ void set(int i, T x) { v[i] = __builtin_bit_cast(unsigned short, x); }
+  __device__ __forceinline__ void zero() { v = us8{0, 0, 0, 0, 0, 0, 0, 0}; }
+};
+template <> struct Vec8<float> {
+  f4 v[2];
+  __device__ __forceinline__ float get(int i) const { return v[i >> 2][i & 3]; }
+  __device__ __forceinline__ void set(int i, float x) { v[i >> 2][i & 3] = x; }
+  __device__ __forceinline__ void zero() { v[0] = v[1] = f4{0.f, 0.f, 0.f, 0.f}; }
+};
+
+// p[0..7]; AL: p is 16-byte aligned, otherwise aligned to an element only (the
+// hardware takes unaligned vector loads, more slowly)
+template <class T, bool AL>
+__device__ __forceinline__ Vec8<T> load8(const T* p) {
+  Vec8<T> r;
+  if constexpr (AL) r = *reinterpret_cast<const Vec8<T>*>(p);
+  else __builtin_memcpy(&r, p, sizeof(r));
+  return r;
+}
+// p[0..n), zeros after it
+template <class T, bool AL>
+__device__ __forceinline__ Vec8<T> load8_upto(const T* p, int n) {
+  if (n >= 8) return load8<T, AL>(p);
+  Vec8<T> r;
+  r.zero();
+#pragma unroll
+  for (int i = 0; i < 7; ++i)
+    if (i < n) r.set(i, p[i]);
+  return r;
+}
+
+template <class T>
+__device__ __forceinline__ void to_planes(const Vec8<T>& x, us8 (&p)[Planes<T>::n]) {
+  if constexpr (sizeof(T) == 4) {
+    typedef unsigned u4_ __attribute__((ext_vector_type(4)));
+    u4_ w[3];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      unsigned a, b, c;
+      split3_pair(f2v{x.get(2 * i), x.get(2 * i + 1)}, a, b, c);
+      w[0][i] = a;
+      w[1][i] = b;
+      w[2][i] = c;
+    }
+#pragma unroll
+    for (int q = 0; q < 3; ++q) p[q] = __builtin_bit_cast(us8, w[q]);
+  } else {
+    p[0] = x.v;
+  }
+}
+
+// n <= 4 consecutive elements from FP32 values, rounded once; vec: p is aligned
+// to four elements and n = 4
+template <class T>
+__device__ __forceinline__ void store4(T* p, f4 v, int n, bool vec) {
+  typedef T t4 __attribute__((ext_vector_type(4)));
+  const t4 o = __builtin_convertvector(v, t4);
+  if (vec) {
+    *reinterpret_cast<t4*>(p) = o;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < n) p[i] = o[i];
+  }
+}
+template <class T>
+__device__ __forceinline__ f4 read4(const T* p, int n, bool vec) {
+  typedef T t4 __attribute__((ext_vector_type(4)));
+  if (vec) return __builtin_convertvector(*reinterpret_cast<const t4*>(p), f4);
+  f4 r = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (i < n) r[i] = to_f32(p[i]);
+  return r;
+}
+
+// ------------------------------------------------------------------ LDS tiles
+// A tile of ROWS operand rows (rows of the first or columns of the second
+// factor) by BK products' indices k. KC: k is contiguous in memory, and in LDS
+// each row's 16-byte chunks are XORed with the row, so that the 8 rows a
+// ds_read_b128 takes per clock cover all banks. Otherwise the rows are
+// contiguous: LDS keeps [k][ROWS] and ds_read_b64_tr_b16 transposes (16 lanes
+// give 4 x 4 chunks of 4 elements, lane i gets column i of the four rows); the
+// 32-byte pairs of a k row are XORed with k, so that its four rows lie apart.
+template <int ROWS, int BK, bool KC>
+__device__ __forceinline__ int tile_chunk(int row, int k) {   // element offset of the 8-element chunk holding (row, k)
+  if constexpr (KC) {
+    constexpr int C = BK / 8;
+    static_assert(C == 4 || C == 8, "BK is 32 or 64");
+    const int s = C == 8 ? row & 7 : (row >> 1) & 3;
+    return row * BK + (((k >> 3) ^ s) << 3);
+  } else {
+    return k * ROWS + (((row >> 3) ^ ((k & 3) << 1)) << 3);
+  }
+}
+
+// MFMA operand of the 16 rows from row0 and the 32 k from k0: lane l holds
+// [row0 + l%16][k0 + 8 (l/16) + 0..7]
+template <int ROWS, int BK, bool KC>
+__device__ __forceinline__ us8 tile_fragment(const unsigned short* t, int row0, int k0, int lane) {
+  const int i = lane & 15, g = lane >> 4;
+  if constexpr (KC) {
+    return *reinterpret_cast<const us8*>(t + tile_chunk<ROWS, BK, true>(row0 + i, k0 + 8 * g));
+  } else {
+    typedef __attribute__((address_space(3))) s4 lds_s4;
+    const int row = row0 + 4 * (i & 3), k = k0 + 8 * g + (i >> 2);
+    const unsigned short* p = t + tile_chunk<ROWS, BK, false>(row, k) + (row & 7);   // (k + 4 has the same k & 3)
+    const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)p);
+    const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(p + 4 * ROWS));
+    typedef short s8_ __attribute__((ext_vector_type(8)));
+    const s8_ r = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    return __builtin_bit_cast(us8, r);
+  }
+}
+
+// Source of a tile in global memory: element (row, k) at base[row * ld + k] (KC)
+// or base[k * ld + row]. `rows` >= 1 of the tile's ROWS are in bounds: with AL
+// vectors past them repeat the last one (their results are not stored), else
+// they are cut. Every k past the end reads as zero.
+template <class T, int ROWS, int BK, bool KC, bool AL, int NT>
+struct TileSource {
+  static constexpr int NV = ROWS * BK / 8 / NT;
+  static constexpr int P = Planes<T>::n;
+  static_assert(ROWS * BK / 8 % NT == 0, "whole vectors per thread");
+  const T* p[NV];
+  int lim[NV];   // !AL: rows from the vector's first one to the end (row-contiguous)
+  Vec8<T> v[NV];
+  int64_t step;
+  __device__ __forceinline__ static int row_of(int u, int tid) {
+    const int f = tid + NT * u;
+    return KC ? f / (BK / 8) : 8 * (f % (ROWS / 8));
+  }
+  __device__ __forceinline__ static int k_of(int u, int tid) {
+    const int f = tid + NT * u;
+    return KC ? 8 * (f % (BK / 8)) : f / (ROWS / 8);
+  }
+  __device__ __forceinline__ void init(const T* base, int64_t ld, int rows, int tid) {
+    step = KC ? (int64_t)BK : BK * ld;
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      const int r = row_of(u, tid), k = k_of(u, tid);
+      if constexpr (KC) p[u] = base + (int64_t)min(r, rows - 1) * ld + k;
+      else if constexpr (AL) p[u] = base + k * ld + min(r, rows - 8);   // (rows is a multiple of 8)
+      else p[u] = base + k * ld + r;
+      lim[u] = rows - r;
+    }
+  }
+  // the tile at the current k; k_left: products' indices from it to the end
+  __device__ __forceinline__ void load(int k_left, int tid) {
+    const bool cut = !AL && !KC;
+    if (k_left >= BK && !cut) {
+#pragma unroll
+      for (int u = 0; u < NV; ++u) v[u] = load8<T, AL>(p[u]);
+    } else {
+#pragma unroll
+      for (int u = 0; u < NV; ++u) {
+        const int k = k_of(u, tid);
+        const int n = KC ? k_left - k : (k < k_left ? (AL ? 8 : lim[u]) : 0);
+        if constexpr (AL) {
+          v[u].zero();
+          if (n > 0) v[u] = load8<T, AL>(p[u]);   // (contiguous extents are multiples of 8)
+        } else {
+          v[u] = load8_upto<T, AL>(p[u], n);
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < NV; ++u) p[u] += step;
+  }
+  __device__ __forceinline__ void store(unsigned short* t, int tid) const {
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      us8 q[P];
+      to_planes<T>(v[u], q);
+      const int o = tile_chunk<ROWS, BK, KC>(row_of(u, tid), k_of(u, tid));
+#pragma unroll
+      for (int i = 0; i < P; ++i) *reinterpret_cast<us8*>(t + i * ROWS * BK + o) = q[i];
+    }
+  }
+};
+
+// The same for pairs of binary16 in two planes, 16-byte aligned rows of whole vectors.
+template <int ROWS, int BK, bool KC, int NT>
+struct TileSource<HalfPair, ROWS, BK, KC, true, NT> {
+  static constexpr int NV = ROWS * BK / 8 / NT;
+  static_assert(ROWS * BK / 8 % NT == 0, "whole vectors per thread");
+  TileSource<_Float16, ROWS, BK, KC, true, NT> hi;
+  int64_t plane;
+  us8 lo[NV];
+  __device__ __forceinline__ void init(const _Float16* base, int64_t plane_, int64_t ld, int rows, int tid) {
+    hi.init(base, ld, rows, tid);
+    plane = plane_;
+  }
+  __device__ __forceinline__ void load(int k_left, int tid) {
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      const int k = hi.k_of(u, tid);
+      lo[u] = us8{0, 0, 0, 0, 0, 0, 0, 0};
+      if (k < k_left) lo[u] = *reinterpret_cast<const us8*>(hi.p[u] + plane);
+    }
+    hi.load(k_left, tid);
+  }
+  __device__ __forceinline__ void store(unsigned short* t, int tid) const {
+    hi.store(t, tid);
+#pragma unroll
+    for (int u = 0; u < NV; ++u)
+      *reinterpret_cast<us8*>(t + ROWS * BK + tile_chunk<ROWS, BK, KC>(hi.row_of(u, tid), hi.k_of(u, tid))) = lo[u];
+  }
+};
+
+// A block's product: BM rows x BN columns on WM x WN waves, k in steps of BK
+// through STAGES LDS buffers. acc[j][i], register r of lane l is the result at
+// column 16 j + 4 (l/16) + r and row 16 i + l%16 of the wave's part: four
+// consecutive columns of one row per lane.
+template <int BM_, int BN_, int WM_, int WN_, int BK_, int STAGES_>
+struct TileShape {
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, BK = BK_, STAGES = STAGES_;
+  static constexpr int NT = 64 * WM * WN;
+  static constexpr int TM = BM / WM / 16, TN = BN / WN / 16;   // 16 x 16 tiles per wave
+};
+
+template <class T, int P>
+__device__ __forceinline__ f4 products(const us8 (&a)[P], const us8 (&b)[P], f4 c) {
+  if constexpr (P == 1) {
+    return mfma32<T>(a[0], b[0], c);
+  } else if constexpr (P == 2) {
+    c = mfma32<T>(a[1], b[0], c);
+    c = mfma32<T>(a[0], b[1], c);
+    return mfma32<T>(a[0], b[0], c);
+  } else {
+    c = mfma32<T>(a[2], b[0], c);
+    c = mfma32<T>(a[1], b[1], c);
+    c = mfma32<T>(a[0], b[2], c);
+    c = mfma32<T>(a[1], b[0], c);
+    c = mfma32<T>(a[0], b[1], c);
+    return mfma32<T>(a[0], b[0], c);
+  }
+}
+
+// one BK step out of LDS: rows' planes at tr, columns' at tc
+template <class T, class S, bool KCR, bool KCC, int P>
+__device__ __forceinline__ void tile_products(const unsigned short* tr, const unsigned short* tc, int m0, int n0, int lane,
+                                              f4 (&acc)[S::TN][S::TM]) {
+#pragma unroll
+  for (int k = 0; k < S::BK; k += 32) {
+    us8 b[S::TM][P];
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+      for (int q = 0; q < P; ++q) b[i][q] = tile_fragment<S::BM, S::BK, KCR>(tr + q * S::BM * S::BK, m0 + 16 * i, k, lane);
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j) {
+      us8 a[P];
+#pragma unroll
+      for (int q = 0; q < P; ++q) a[q] = tile_fragment<S::BN, S::BK, KCC>(tc + q * S::BN * S::BK, n0 + 16 * j, k, lane);
+#pragma unroll
+      for (int i = 0; i < S::TM; ++i) acc[j][i] = products<T, P>(a, b[i], acc[j][i]);
+    }
+  }
+}
+
+template <class T, class S> constexpr int tile_lds = S::STAGES * Planes<T>::n * (S::BM + S::BN) * S::BK;   // elements
+
+template <class T, class S, bool KCR, bool KCC, bool AL>
+__device__ __forceinline__ void tile_gemm(TileSource<T, S::BM, S::BK, KCR, AL, S::NT>& r,
+                                          TileSource<T, S::BN, S::BK, KCC, AL, S::NT>& c, int K, unsigned short* lds,
+                                          int tid, f4 (&acc)[S::TN][S::TM]) {
+  constexpr int P = Planes<T>::n, BUF = P * (S::BM + S::BN) * S::BK, CO = P * S::BM * S::BK;
+  const int lane = tid & 63, w = tid >> 6;
+  const int m0 = (w / S::WN) * (S::BM / S::WM), n0 = (w % S::WN) * (S::BN / S::WN);
+#pragma unroll
+  for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i) acc[j][i] = f4{0.f, 0.f, 0.f, 0.f};
+  if (K <= 0) return;
+  r.load(K, tid);
+  c.load(K, tid);
+  if constexpr (S::STAGES == 2) {
+    r.store(lds, tid);
+    c.store(lds + CO, tid);
+    __syncthreads();
+    for (int k = 0, s = 0; k < K; k += S::BK, s ^= 1) {
+      const bool more = k + S::BK < K;
+      if (more) {   // in flight during this step's products
+        r.load(K - k - S::BK, tid);
+        c.load(K - k - S::BK, tid);
+      }
+      tile_products<T, S, KCR, KCC, P>(lds + s * BUF, lds + s * BUF + CO, m0, n0, lane, acc);
+      if (more) {
+        r.store(lds + (s ^ 1) * BUF, tid);
+        c.store(lds + (s ^ 1) * BUF + CO, tid);
+      }
+      __syncthreads();
+    }
+  } else {
+    for (int k = 0; k < K; k += S::BK) {
+      if (k) __syncthreads();   // the previous step's products have read the tile
+      r.store(lds, tid);
+      c.store(lds + CO, tid);
+      __syncthreads();
+      if (k + S::BK < K) {
+        r.load(K - k - S::BK, tid);
+        c.load(K - k - S::BK, tid);
+      }
+      tile_products<T, S, KCR, KCC, P>(lds, lds + CO, m0, n0, lane, acc);
+    }
+  }
+}
+
+// This lane's four columns of the results of tile_gemm: f(row, column, values, count)
+template <class S, class F>
+__device__ __forceinline__ void for_results(const f4 (&acc)[S::TN][S::TM], int rows, int cols, int tid, F f) {
+  const int l = tid & 63, w = tid >> 6;
+  const int m0 = (w / S::WN) * (S::BM / S::WM) + (l & 15), n0 = (w % S::WN) * (S::BN / S::WN) + 4 * (l >> 4);
+#pragma unroll
+  for (int i = 0; i < S::TM; ++i) {
+    const int m = m0 + 16 * i;
+    if (m >= rows) continue;
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j) {
+      const int n = n0 + 16 * j;
+      if (n < cols) f(m, n, acc[j][i], min(4, cols - n));
+    }
+  }
+}
+
+// Work items 0..n-1 in the order blocks take them: consecutive block numbers go
+// to different XCDs, so each XCD gets a contiguous run of items (neighbours
+// share operand rows in its L2).
+__device__ __forceinline__ int xcd_order(int b, int n) {
+  constexpr int X = 8;
+  const int q = n / X, rem = n % X, x = b % X;
+  return x * q + min(x, rem) + b / X;
+}
+
+// Runs of at most `size` consecutive rows of one group, numbered over all
+// groups; then runs of the rows behind the last group (group = n_groups).
+// offsets: n_groups + 1 device ints, clamped here to [0, n], a falling pair
+// being an empty group; NULL for one group of all rows. Every lane of a wave
+// calls it. False: run t does not exist.
+struct RowRun {
+  int group;
+  int64_t row0;
+  int rows;
+  int first;   // number of the group's first run
+};
+__device__ __forceinline__ bool find_run(const int* __restrict__ offsets, int n_groups, int64_t n, int size, int t,
+                                         RowRun& out) {
+  if (!offsets) {
+    out.group = 0;
+    out.first = 0;
+    out.row0 = (int64_t)t * size;
+    out.rows = (int)min<int64_t>(size, n - out.row0);
+    return out.row0 < n;
+  }
+  const int lane = threadIdx.x & 63;
+  int base = 0;
+  for (int g0 = 0; g0 <= n_groups; g0 += 64) {
+    const int g = g0 + lane;
+    int64_t a = 0, b = 0;
+    if (g <= n_groups) {
+      a = min<int64_t>(max(offsets[g], 0), n);
+      b = g < n_groups ? min<int64_t>(max(offsets[g + 1], 0), n) : n;
+    }
+    const int runs = b > a ? (int)((b - a + size - 1) / size) : 0;
+    int incl = runs;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int o = __shfl_up(incl, d);
+      if (lane >= d) incl += o;
+    }
+    const unsigned long long has = __ballot(base + incl > t);
+    if (has) {
+      const int src = __ffsll(has) - 1;
+      const int first = base + __shfl(incl - runs, src);
+      const int64_t a0 = ((int64_t)__shfl((int)(a >> 32), src) << 32) | (unsigned)__shfl((int)a, src);
+      const int64_t b0 = ((int64_t)__shfl((int)(b >> 32), src) << 32) | (unsigned)__shfl((int)b, src);
+      out.group = g0 + src;
+      out.first = first;
+      out.row0 = a0 + (int64_t)(t - first) * size;
+      out.rows = (int)min<int64_t>(size, b0 - out.row0);
+      return true;
+    }
+    base += __shfl(incl, 63);
+  }
+  return false;
+}
+
+}  // namespace mace

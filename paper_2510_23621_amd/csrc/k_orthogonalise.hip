@@ -1,0 +1,540 @@
+// Newton-Schulz orthogonalisation: mace_orthogonalise.
+//
+// Every matrix is kept as x [m][n] with m <= n (a tall one transposed), as pairs
+// of binary16 scaled by kScaleX: the iteration's operands are bounded (singular
+// values of x below 3.4, checked for the coefficients on the host), so a pair's
+// 22 significand bits are as accurate as FP32 here at three MFMA products
+// in place of six. Per step: A = x x^T and B = b A + c A A, both symmetric (one
+// half computed, the other mirrored), x <- a x + B x.
+//
+// With at most kGramMax rows the iteration runs on A alone, in FP64: every x is a
+// polynomial of A_0 = x_0 x_0^T times x_0, so A <- P A P and Q <- P Q with
+// P = a + b A + c A A, and the result is Q x_0: two passes over the data instead of
+// two per step. FP64 because A holds the squares of the singular values and a
+// small one's error grows with the square of the value: in 2^-24 arithmetic a
+// singular value of 0.003 would be off by a percent, in FP64 by 1e-11.
+#include <algorithm>
+#include <cmath>
+
+#include "../../include/mace.h"
+#include "dense.h"
+
+namespace mace {
+namespace {
+
+constexpr float kScaleX = 4096.f, kScaleA = 4096.f, kScaleB = 256.f;
+constexpr double kMaxSigma = 3.4, kMaxB = 200.0;   // 3.4^2 kScaleA and 200 kScaleB fit binary16
+
+// one matrix's planes: hi [rows][ld], then lo
+struct PairMat {
+  _Float16* p;
+  int64_t stride, plane;   // between matrices, between planes
+  int ld;
+};
+
+typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ f4 read_pair(const _Float16* p, int64_t plane) {
+  return __builtin_convertvector(*reinterpret_cast<const h4*>(p), f4) +
+         __builtin_convertvector(*reinterpret_cast<const h4*>(p + plane), f4);
+}
+__device__ __forceinline__ void split_pair(f4 v, h4& hi, h4& lo) {
+  hi = __builtin_convertvector(v, h4);
+  lo = __builtin_convertvector(v - __builtin_convertvector(hi, f4), h4);
+}
+
+// ------------------------------------------------------------------ norm and packing
+constexpr int kNormBlocks = 64;   // most partial sums per matrix
+
+template <class T>
+__global__ void __launch_bounds__(256) ns_norm_kernel(const T* __restrict__ g, int64_t stride, int64_t ld, int rows,
+                                                      int cols, double* __restrict__ part) {
+  __shared__ double red[4];
+  const T* m = g + (int64_t)blockIdx.y * stride;
+  const int64_t size = (int64_t)rows * cols, per = (size + gridDim.x - 1) / gridDim.x;
+  const int64_t i0 = blockIdx.x * per, i1 = min(size, i0 + per);
+  double s = 0.0;
+  for (int64_t i = i0 + threadIdx.x; i < i1; i += 256) {
+    const double v = to_f32(m[i / cols * ld + i % cols]);
+    s += v * v;
+  }
+  for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) part[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = red[0] + red[1] + red[2] + red[3];
+}
+
+__device__ __forceinline__ double ns_scale(const double* part, int n, double eps) {
+  double s = 0.0;
+  for (int i = 0; i < n; ++i) s += part[i];
+  return 1.0 / (sqrt(s) + eps);
+}
+
+// x = g / (|g| + eps) as pairs, a tall g transposed; zeros in the padding of x, A and B.
+// One 64 x 64 tile of x per block.
+template <class T>
+__global__ void __launch_bounds__(256)
+ns_pack_kernel(const T* __restrict__ g, int64_t stride, int64_t ld, int m, int n, bool tall,
+               const double* __restrict__ part, int parts, double eps, PairMat x, PairMat A, PairMat B) {
+  __shared__ float t[64][65];
+  const int b = blockIdx.z, i0 = blockIdx.y * 64, j0 = blockIdx.x * 64, tid = threadIdx.x;
+  const T* src = g + (int64_t)b * stride;
+  const double inv = ns_scale(part + (int64_t)b * parts, parts, eps) * kScaleX;
+  for (int e = tid; e < 64 * 64; e += 256) {
+    const int r = e >> 6, c = e & 63;   // c along g's contiguous axis
+    const int i = tall ? c : r, j = tall ? r : c;
+    float v = 0.f;
+    if (i0 + i < m && j0 + j < n)
+      v = (float)(to_f32(tall ? src[(int64_t)(j0 + j) * ld + i0 + i] : src[(int64_t)(i0 + i) * ld + j0 + j]) * inv);
+    t[i][j] = v;
+  }
+  __syncthreads();
+  _Float16* xp = x.p + b * x.stride;
+  for (int e = tid; e < 64 * 16; e += 256) {
+    const int i = e >> 4, j = 4 * (e & 15);
+    if (i0 + i >= m || j0 + j >= x.ld) continue;
+    h4 hi, lo;
+    split_pair(f4{t[i][j], t[i][j + 1], t[i][j + 2], t[i][j + 3]}, hi, lo);
+    _Float16* o = xp + (int64_t)(i0 + i) * x.ld + j0 + j;
+    *reinterpret_cast<h4*>(o) = hi;
+    *reinterpret_cast<h4*>(o + x.plane) = lo;
+  }
+  if (blockIdx.x == 0)
+    for (int e = tid; e < 64 * (A.ld - m); e += 256) {
+      const int i = i0 + e / (A.ld - m), j = m + e % (A.ld - m);
+      if (i >= m) continue;
+      for (int q = 0; q < 2; ++q) {
+        A.p[b * A.stride + q * A.plane + (int64_t)i * A.ld + j] = (_Float16)0.f;
+        B.p[b * B.stride + q * B.plane + (int64_t)i * B.ld + j] = (_Float16)0.f;
+      }
+    }
+}
+
+// no steps: out = g / (|g| + eps)
+template <class T>
+__global__ void __launch_bounds__(256)
+ns_scale_kernel(const T* __restrict__ g, int64_t stride, int64_t ld, int rows, int cols, const double* __restrict__ part,
+                int parts, double eps, T* __restrict__ out, int64_t ostride, int64_t old) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= (int64_t)rows * cols) return;
+  const double inv = ns_scale(part + (int64_t)blockIdx.y * parts, parts, eps);
+  const int64_t r = i / cols, c = i % cols;
+  out[blockIdx.y * ostride + r * old + c] = (T)(float)(to_f32(g[blockIdx.y * stride + r * ld + c]) * inv);
+}
+
+// ------------------------------------------------------------------ few rows
+constexpr int kGramMax = 32, kGramChunk = 256;
+
+// element (i, j) of x's layout in g
+template <class T>
+__device__ __forceinline__ float element(const T* g, int64_t ld, bool tall, int i, int j) {
+  return to_f32(tall ? g[(int64_t)j * ld + i] : g[(int64_t)i * ld + j]);
+}
+
+// A = g g^T over a chunk of columns; thread (ti, tj) sums a 2 x 2 block
+template <class T>
+__global__ void __launch_bounds__(256) ns_gram64_kernel(const T* __restrict__ g, int64_t stride, int64_t ld, int m, int n,
+                                                        bool tall, double* __restrict__ part) {
+  __shared__ float t[kGramMax][kGramChunk + 1];
+  const int tid = threadIdx.x, j0 = blockIdx.x * kGramChunk, w = min(kGramChunk, n - j0);
+  const T* src = g + (int64_t)blockIdx.y * stride;
+  const int m2 = (m + 1) & ~1;
+  for (int e = tid; e < m2 * kGramChunk; e += 256) {
+    const int i = tall ? e % m2 : e / kGramChunk, j = tall ? e / m2 : e % kGramChunk;
+    t[i][j] = i < m && j < w ? element(src, ld, tall, i, j0 + j) : 0.f;
+  }
+  __syncthreads();
+  const int ti = 2 * (tid >> 4), tj = 2 * (tid & 15);
+  if (ti >= m || tj >= m) return;
+  double s[2][2] = {};
+  for (int j = 0; j < w; ++j) {
+    const double a0 = t[ti][j], a1 = t[ti + 1][j], b0 = t[tj][j], b1 = t[tj + 1][j];
+    s[0][0] += a0 * b0;
+    s[0][1] += a0 * b1;
+    s[1][0] += a1 * b0;
+    s[1][1] += a1 * b1;
+  }
+  double* o = part + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * m * m;
+  for (int p = 0; p < 2; ++p)
+    for (int q = 0; q < 2; ++q)
+      if (ti + p < m && tj + q < m) o[(ti + p) * m + tj + q] = s[p][q];
+}
+
+struct NsSteps {
+  double c[64][3];
+  int n;
+};
+
+typedef double Square[kGramMax][kGramMax + 1];
+__device__ __forceinline__ void multiply64(const Square& a, const Square& b, Square& c, int m, int tid) {   // c = a b
+  for (int e = tid; e < m * m; e += 256) {
+    const int i = e / m, j = e - i * m;
+    double s = 0.0;
+    for (int k = 0; k < m; ++k) s += a[i][k] * b[k][j];
+    c[i][j] = s;
+  }
+  __syncthreads();
+}
+
+// q = Q / (|g| + eps) of one matrix from the chunks' sums; |g|^2 is the trace
+__global__ void __launch_bounds__(256)
+ns_iterate64_kernel(const double* __restrict__ part, int chunks, int m, double eps, NsSteps steps, double* __restrict__ q) {
+  __shared__ Square A, P, Q, T;
+  __shared__ double s_inv;
+  const int tid = threadIdx.x;
+  const double* p = part + (int64_t)blockIdx.x * chunks * m * m;
+  for (int e = tid; e < m * m; e += 256) {
+    double s = 0.0;
+    for (int c = 0; c < chunks; ++c) s += p[(int64_t)c * m * m + e];
+    A[e / m][e % m] = s;
+    Q[e / m][e % m] = e / m == e % m ? 1.0 : 0.0;
+  }
+  __syncthreads();
+  if (tid == 0) {
+    double tr = 0.0;
+    for (int i = 0; i < m; ++i) tr += A[i][i];
+    s_inv = 1.0 / (sqrt(tr) + eps);
+  }
+  __syncthreads();
+  const double inv = s_inv;
+  for (int e = tid; e < m * m; e += 256) A[e / m][e % m] = A[e / m][e % m] * inv * inv;
+  __syncthreads();
+  for (int st = 0; st < steps.n; ++st) {
+    const double a = steps.c[st][0], b = steps.c[st][1], c = steps.c[st][2];
+    multiply64(A, A, T, m, tid);
+    for (int e = tid; e < m * m; e += 256) {
+      const int i = e / m, j = e % m;
+      P[i][j] = (i == j ? a : 0.0) + b * A[i][j] + c * T[i][j];
+    }
+    __syncthreads();
+    multiply64(P, Q, T, m, tid);
+    for (int e = tid; e < m * m; e += 256) Q[e / m][e % m] = T[e / m][e % m];
+    __syncthreads();
+    if (st + 1 < steps.n) {
+      multiply64(P, A, T, m, tid);
+      multiply64(T, P, A, m, tid);
+    }
+  }
+  for (int e = tid; e < m * m; e += 256) q[(int64_t)blockIdx.x * m * m + e] = Q[e / m][e % m] * inv;
+}
+
+// out = q g, one column of x per thread
+template <class T>
+__global__ void __launch_bounds__(256) ns_apply64_kernel(const T* g, int64_t stride, int64_t ld, int m, int n, bool tall,
+                                                         const double* __restrict__ q, T* out, int64_t ostride, int64_t old) {
+  __shared__ double sq[kGramMax * kGramMax];
+  for (int e = threadIdx.x; e < m * m; e += 256) sq[e] = q[(int64_t)blockIdx.y * m * m + e];
+  __syncthreads();
+  const int j = blockIdx.x * 256 + threadIdx.x;
+  if (j >= n) return;
+  const T* src = g + (int64_t)blockIdx.y * stride;
+  T* o = out + (int64_t)blockIdx.y * ostride;
+  float x[kGramMax];
+#pragma unroll
+  for (int i = 0; i < kGramMax; ++i) x[i] = i < m ? element(src, ld, tall, i, j) : 0.f;
+  for (int r = 0; r < m; ++r) {
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < kGramMax; ++i)
+      if (i < m) s += sq[r * m + i] * (double)x[i];
+    const T v = (T)(float)s;
+    if (tall) o[(int64_t)j * old + r] = v;
+    else o[(int64_t)r * old + j] = v;
+  }
+}
+
+// ------------------------------------------------------------------ products
+
+// operand rows from row0 of a plane pair (T: binary16 reads the upper plane only)
+template <class T, class Src>
+__device__ __forceinline__ void source_of(Src& s, const PairMat& m, int b, int64_t at, int rows, int tid) {
+  if constexpr (__is_same(T, HalfPair)) s.init(m.p + b * m.stride + at, m.plane, m.ld, rows, tid);
+  else s.init(m.p + b * m.stride + at, m.ld, rows, tid);
+}
+
+// Tile (tm, tn), tn <= tm, of a lower triangle of tiles
+__device__ __forceinline__ void triangle(int t, int& tm, int& tn) {
+  tm = (int)((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
+  while ((tm + 1) * (tm + 2) / 2 <= t) ++tm;
+  while (tm * (tm + 1) / 2 > t) --tm;
+  tn = t - tm * (tm + 1) / 2;
+}
+
+// out = A = x x^T (POLY false, src = x), or out = B = b A + c A A (src = A), for the
+// lower triangle of tiles; the upper one is its mirror.
+template <class T, class S, bool POLY>
+__global__ void __launch_bounds__(S::NT) ns_symmetric_kernel(PairMat src, PairMat out, int m, int K, int tiles,
+                                                             float ca, float cp) {
+  __shared__ __align__(16) unsigned short lds[tile_lds<T, S>];
+  const int tid = threadIdx.x;
+  const int id = xcd_order(blockIdx.x, gridDim.x), b = id / tiles;
+  int tm, tn;
+  triangle(id - b * tiles, tm, tn);
+  const int r0 = tm * S::BM, c0 = tn * S::BN;
+  static_assert(S::BM == S::BN, "square tiles");
+  TileSource<T, S::BM, S::BK, true, true, S::NT> rs;
+  TileSource<T, S::BN, S::BK, true, true, S::NT> cs;
+  source_of<T>(rs, src, b, (int64_t)r0 * src.ld, m - r0, tid);
+  source_of<T>(cs, src, b, (int64_t)c0 * src.ld, m - c0, tid);
+  f4 acc[S::TN][S::TM];
+  tile_gemm<T, S, true, true, true>(rs, cs, K, lds, tid, acc);
+  _Float16* o = out.p + b * out.stride;
+  const _Float16* a = src.p + b * src.stride;
+  for_results<S>(acc, min(S::BM, m - r0), min(S::BN, m - c0), tid, [&](int i, int j, f4 v, int k) {
+    const int64_t at = (int64_t)(r0 + i) * out.ld + c0 + j;
+    v *= cp;
+    if constexpr (POLY) v += ca * read_pair(a + at, src.plane);   // (A and B have the same pitch)
+    h4 hi, lo;
+    split_pair(v, hi, lo);
+    if (k == 4) {
+      *reinterpret_cast<h4*>(o + at) = hi;
+      *reinterpret_cast<h4*>(o + at + out.plane) = lo;
+    } else {
+      for (int q = 0; q < k; ++q) {
+        o[at + q] = hi[q];
+        o[at + out.plane + q] = lo[q];
+      }
+    }
+    if (tm != tn)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (q < k) {
+          const int64_t t = (int64_t)(c0 + j + q) * out.ld + r0 + i;
+          o[t] = hi[q];
+          o[t + out.plane] = lo[q];
+        }
+  });
+}
+
+// x <- a x + B x, as pairs, or the last step's result in its own type and layout
+template <class T, class S, class O>
+__global__ void __launch_bounds__(S::NT)
+ns_update_kernel(PairMat B, PairMat x, PairMat xo, int m, int n, float ca, float cp, O* out, int64_t ostride,
+                 int64_t old, bool tall) {
+  __shared__ __align__(16) unsigned short lds[tile_lds<T, S>];
+  const int tid = threadIdx.x;
+  const int tiles_n = (x.ld + S::BN - 1) / S::BN, tiles_m = (m + S::BM - 1) / S::BM;
+  int id = xcd_order(blockIdx.x, gridDim.x);
+  const int b = id / (tiles_n * tiles_m);
+  id -= b * tiles_n * tiles_m;
+  const int r0 = id / tiles_n * S::BM, c0 = id % tiles_n * S::BN;
+  TileSource<T, S::BM, S::BK, true, true, S::NT> bs;
+  TileSource<T, S::BN, S::BK, false, true, S::NT> xs;
+  source_of<T>(bs, B, b, (int64_t)r0 * B.ld, m - r0, tid);
+  source_of<T>(xs, x, b, c0, x.ld - c0, tid);
+  f4 acc[S::TN][S::TM];
+  tile_gemm<T, S, true, false, true>(bs, xs, m, lds, tid, acc);
+  const _Float16* xi = x.p + b * x.stride;
+  for_results<S>(acc, min(S::BM, m - r0), min(S::BN, x.ld - c0), tid, [&](int i, int j, f4 v, int k) {
+    const int64_t at = (int64_t)(r0 + i) * x.ld + c0 + j;   // (whole vectors: the pitch is a multiple of 8)
+    v = cp * v + ca * read_pair(xi + at, x.plane);
+    if (out) {
+      v *= 1.f / kScaleX;
+      O* o = out + b * ostride;
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (c0 + j + q < n) {
+          if (tall) o[(int64_t)(c0 + j + q) * old + r0 + i] = (O)v[q];
+          else o[(int64_t)(r0 + i) * old + c0 + j + q] = (O)v[q];
+        }
+    } else {
+      h4 hi, lo;
+      split_pair(v, hi, lo);
+      _Float16* o = xo.p + b * xo.stride + at;
+      *reinterpret_cast<h4*>(o) = hi;
+      *reinterpret_cast<h4*>(o + xo.plane) = lo;
+    }
+  });
+}
+
+// ------------------------------------------------------------------ host
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+mace_status launched() { return hipGetLastError() == hipSuccess ? MACE_OK : MACE_EHIP; }
+
+mace_status check(const mace_orthogonalise_desc* d) {
+  if (!d || d->batch < 0 || d->rows < 1 || d->cols < 1 || d->n_steps < 0 || d->n_steps > 64 || !(d->eps >= 0))
+    return MACE_EINVAL;
+  if (d->dtype < MACE_TYPE_FP32 || d->dtype > MACE_TYPE_FP16) return MACE_EINVAL;
+  if (d->ld_g < d->cols || d->ld_out < d->cols || d->stride_g < 0 || d->stride_out < 0) return MACE_EINVAL;
+  if (d->batch > 1 && d->stride_out < (int64_t)(d->rows - 1) * d->ld_out + d->cols) return MACE_EINVAL;
+  if (d->rows > (1 << 15) || d->cols > (1 << 15) || d->batch > 65535 ||
+      (double)d->batch * d->rows * d->cols > 17179869184.0)
+    return MACE_EUNSUPPORTED;
+  return MACE_OK;
+}
+
+// whether every step keeps its operands in range (mace.h)
+bool in_range(const double* c, int steps) {
+  double r = 1.0;   // largest singular value so far
+  for (int s = 0; s < steps; ++s, c += 3) {
+    if (!std::isfinite(c[0]) || !std::isfinite(c[1]) || !std::isfinite(c[2])) return false;
+    double next = 0.0;
+    for (int i = 0; i <= 2048; ++i) {
+      const double v = r * i / 2048.0, l = v * v, B = c[1] * l + c[2] * l * l;
+      if (!(std::fabs(B) <= kMaxB)) return false;
+      next = std::max(next, std::fabs((c[0] + B) * v));
+    }
+    r = next * 1.001;   // (between the sample points, and rounding)
+    if (!(r <= kMaxSigma)) return false;
+  }
+  return true;
+}
+
+struct NsPlan {
+  int m, n, mp, np, parts;   // parts: partial sums of the norm, or chunks of the FP64 products
+  bool tall, gram;
+  size_t part, q, x0, x1, A, B, total;
+};
+NsPlan plan(const mace_orthogonalise_desc& d) {
+  NsPlan p{};
+  p.tall = d.rows > d.cols;
+  p.m = std::min(d.rows, d.cols);
+  p.n = std::max(d.rows, d.cols);
+  p.mp = (p.m + 7) / 8 * 8;
+  p.np = (p.n + 7) / 8 * 8;
+  p.gram = p.m <= kGramMax;
+  p.parts = p.gram ? (int)ceil_div(p.n, kGramChunk) : (int)std::min<int64_t>(kNormBlocks, ceil_div((int64_t)p.m * p.n, 8192));
+  size_t o = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = o;
+    o += (bytes + 255) & ~size_t(255);
+    return at;
+  };
+  if (p.gram) {
+    p.part = take(sizeof(double) * d.batch * p.parts * p.m * p.m);
+    p.q = take(sizeof(double) * d.batch * p.m * p.m);
+    p.total = o;
+    return p;
+  }
+  p.part = take(sizeof(double) * d.batch * p.parts);
+  p.x0 = take(size_t(4) * d.batch * p.m * p.np);
+  p.x1 = take(size_t(4) * d.batch * p.m * p.np);
+  p.A = take(size_t(4) * d.batch * p.m * p.mp);
+  p.B = take(size_t(4) * d.batch * p.m * p.mp);
+  p.total = o;
+  return p;
+}
+
+constexpr int64_t kFillBlocks = 256;   // blocks from which the larger tile is taken (one per CU)
+
+template <class T> struct Shapes {
+  using Mid = TileShape<128, 128, 2, 2, 64, 2>;
+  using Small = TileShape<64, 64, 2, 2, 64, 2>;
+};
+template <> struct Shapes<HalfPair> {
+  using Mid = TileShape<128, 128, 2, 2, 32, 2>;
+  using Small = TileShape<64, 64, 2, 2, 32, 2>;
+};
+
+template <class T, bool POLY>
+mace_status symmetric(const PairMat& src, const PairMat& out, int64_t batch, int m, int K, float ca, float cp,
+                      hipStream_t s) {
+  auto go = [&](auto shape) {
+    using S = decltype(shape);
+    const int64_t t = ceil_div(m, S::BM), tiles = t * (t + 1) / 2;
+    ns_symmetric_kernel<T, S, POLY><<<(unsigned)(tiles * batch), S::NT, 0, s>>>(src, out, m, K, (int)tiles, ca, cp);
+    return launched();
+  };
+  const int64_t t = ceil_div(m, 128);
+  return t * (t + 1) / 2 * batch >= kFillBlocks ? go(typename Shapes<T>::Mid{}) : go(typename Shapes<T>::Small{});
+}
+template <class T, class O>
+mace_status update(const PairMat& B, const PairMat& x, const PairMat& xo, int64_t batch, int m, int n, float ca, float cp,
+                   O* out, int64_t ostride, int64_t old, bool tall, hipStream_t s) {
+  auto go = [&](auto shape) {
+    using S = decltype(shape);
+    const int64_t blocks = ceil_div(m, S::BM) * ceil_div(x.ld, S::BN) * batch;
+    ns_update_kernel<T, S, O><<<(unsigned)blocks, S::NT, 0, s>>>(B, x, xo, m, n, ca, cp, out, ostride, old, tall);
+    return launched();
+  };
+  return ceil_div(m, 128) * ceil_div(x.ld, 128) * batch >= kFillBlocks ? go(typename Shapes<T>::Mid{})
+                                                                        : go(typename Shapes<T>::Small{});
+}
+
+template <class O>
+mace_status run(const mace_orthogonalise_desc& d, const O* g, const double* coef, O* out, char* ws, hipStream_t s) {
+  const NsPlan p = plan(d);
+  double* part = reinterpret_cast<double*>(ws + p.part);
+  mace_status st;
+  if (p.gram) {
+    NsSteps steps{};
+    steps.n = d.n_steps;
+    for (int i = 0; i < 3 * d.n_steps; ++i) steps.c[i / 3][i % 3] = coef[i];
+    double* q = reinterpret_cast<double*>(ws + p.q);
+    ns_gram64_kernel<O><<<dim3(p.parts, (unsigned)d.batch), 256, 0, s>>>(g, d.stride_g, d.ld_g, p.m, p.n, p.tall, part);
+    if ((st = launched()) != MACE_OK) return st;
+    ns_iterate64_kernel<<<(unsigned)d.batch, 256, 0, s>>>(part, p.parts, p.m, d.eps, steps, q);
+    if ((st = launched()) != MACE_OK) return st;
+    ns_apply64_kernel<O><<<dim3((unsigned)ceil_div(p.n, 256), (unsigned)d.batch), 256, 0, s>>>(
+        g, d.stride_g, d.ld_g, p.m, p.n, p.tall, q, out, d.stride_out, d.ld_out);
+    return launched();
+  }
+  ns_norm_kernel<O><<<dim3(p.parts, (unsigned)d.batch), 256, 0, s>>>(g, d.stride_g, d.ld_g, d.rows, d.cols, part);
+  if ((st = launched()) != MACE_OK) return st;
+  if (d.n_steps == 0) {
+    ns_scale_kernel<O><<<dim3((unsigned)ceil_div((int64_t)d.rows * d.cols, 256), (unsigned)d.batch), 256, 0, s>>>(
+        g, d.stride_g, d.ld_g, d.rows, d.cols, part, p.parts, d.eps, out, d.stride_out, d.ld_out);
+    return launched();
+  }
+  auto mat = [&](size_t at, int ld) {
+    const int64_t plane = (int64_t)p.m * ld;
+    return PairMat{reinterpret_cast<_Float16*>(ws + at), 2 * plane, plane, ld};
+  };
+  PairMat x = mat(p.x0, p.np), xo = mat(p.x1, p.np);
+  const PairMat A = mat(p.A, p.mp), B = mat(p.B, p.mp);
+  ns_pack_kernel<O><<<dim3((unsigned)ceil_div(p.np, 64), (unsigned)ceil_div(p.m, 64), (unsigned)d.batch), 256, 0, s>>>(
+      g, d.stride_g, d.ld_g, p.m, p.n, p.tall, part, p.parts, d.eps, x, A, B);
+  if ((st = launched()) != MACE_OK) return st;
+  // Steps from the end that take pairs. A BF16 result's earlier steps take the
+  // upper halves (2^-12 of the operands): what is left of that error after two
+  // steps of pairs is 2e-4 to 6e-4 of the result, against 1.7e-3 of its rounding
+  // (matrices of 128 to 1024 rows; with one step of pairs 5e-4 to 9e-4, with none
+  // 8e-4 to 2e-3). Below 128 rows too few directions average the error, and the
+  // products are not what takes the time.
+  const int exact_steps = d.dtype == MACE_TYPE_BF16 && p.m >= 128 ? 2 : d.n_steps;
+  for (int i = 0; i < d.n_steps; ++i) {
+    const bool pairs = d.n_steps - i <= exact_steps, last = i == d.n_steps - 1;
+    const float a = (float)coef[3 * i], b = (float)coef[3 * i + 1], c = (float)coef[3 * i + 2];
+    const float g1 = kScaleA / (kScaleX * kScaleX), pb = b * (kScaleB / kScaleA),
+                pc = c * (kScaleB / (kScaleA * kScaleA)), u = 1.f / kScaleB;
+    O* o = last ? out : nullptr;
+    auto step = [&](auto t) -> mace_status {
+      using T = decltype(t);
+      mace_status e;
+      if ((e = symmetric<T, false>(x, A, d.batch, p.m, p.np, 0.f, g1, s)) != MACE_OK) return e;
+      if ((e = symmetric<T, true>(A, B, d.batch, p.m, p.m, pb, pc, s)) != MACE_OK) return e;
+      return update<T, O>(B, x, xo, d.batch, p.m, p.n, a, u, o, d.stride_out, d.ld_out, p.tall, s);
+    };
+    st = pairs ? step(HalfPair{}) : step((_Float16)0.f);
+    if (st != MACE_OK) return st;
+    std::swap(x, xo);
+  }
+  return MACE_OK;
+}
+
+}  // namespace
+}  // namespace mace
+
+using namespace mace;
+
+extern "C" size_t mace_orthogonalise_workspace_bytes(const mace_orthogonalise_desc* desc) {
+  if (check(desc) != MACE_OK) return 0;
+  return plan(*desc).total + 256;
+}
+
+extern "C" mace_status mace_orthogonalise(const mace_orthogonalise_desc* desc, const void* g, const double* coefficients,
+                                          void* out, void* workspace, size_t workspace_bytes, void* stream) {
+  const mace_status st = check(desc);
+  if (st != MACE_OK) return st;
+  if (desc->n_steps > 0 && !coefficients) return MACE_EINVAL;
+  if (desc->batch == 0) return MACE_OK;
+  if (!g || !out || !workspace) return MACE_EINVAL;
+  if (!in_range(coefficients, desc->n_steps)) return MACE_ERANGE;
+  char* ws = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(workspace) + 255) & ~uintptr_t(255));
+  if (size_t(ws - static_cast<char*>(workspace)) + plan(*desc).total > workspace_bytes) return MACE_ENOSPACE;
+  hipStream_t s = (hipStream_t)stream;
+  if (desc->dtype == MACE_TYPE_FP32)
+    return run<float>(*desc, (const float*)g, coefficients, (float*)out, ws, s);
+  if (desc->dtype == MACE_TYPE_BF16)
+    return run<__bf16>(*desc, (const __bf16*)g, coefficients, (__bf16*)out, ws, s);
+  return run<_Float16>(*desc, (const _Float16*)g, coefficients, (_Float16*)out, ws, s);
+}

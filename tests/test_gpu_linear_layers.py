@@ -1,0 +1,226 @@
+"""Grouped linear layers and their gradients against FP64, at the sizes, row
+strides, groupings and types where tiles, tails and splits can go wrong.
+
+Bounds are elementwise and follow from the roundings: FP32 accumulation of a
+length-K sum (K + 8) 2^-24 times the sum of magnitudes, one rounding of each
+result to its type, and in the backward the roundings of z and dz."""
+import pytest
+import torch
+
+from dense_common import DTYPES, SLOPE1, SLOPE2, TINY, U, U32, act64, product_error, randn, slope64, within
+
+pytestmark = pytest.mark.gpu
+L = pytest.importorskip("paper_2510_23621_amd.layers")
+
+
+def offsets_of(sizes, tail=0):
+    off = torch.tensor([0] + list(sizes)).cumsum(0)
+    return off.tolist(), int(off[-1]) + tail
+
+
+def strided(t, pad, shift):
+    """t as a view of a wider device buffer: row stride + pad, `shift` elements into it."""
+    buf = torch.full((t.shape[0], t.shape[1] + pad + shift), float("nan"), dtype=t.dtype, device="cuda")
+    v = buf[:, shift:shift + t.shape[1]]
+    v.copy_(t)
+    return v
+
+
+def case(n, n_in, n_out, dtype, act, sizes=None, tail=0, bias=True, residual=True, seed=0, pad=0, shift=0):
+    gen = torch.Generator().manual_seed(seed)
+    off = None
+    groups = 1
+    if sizes is not None:
+        off, n = offsets_of(sizes, tail)
+        groups = len(sizes)
+    x = randn(n, n_in, gen=gen, dtype=dtype)
+    w = randn(groups, n_in, n_out, gen=gen, dtype=dtype, scale=n_in ** -0.5)
+    b = randn(groups, n_out, gen=gen, dtype=dtype, scale=0.3) if bias else None
+    r = randn(n, n_out, gen=gen, dtype=dtype) if residual else None
+    dy = randn(n, n_out, gen=gen, dtype=dtype, scale=0.3)
+    kept = off[-1] if off else n
+    xd, dyd = strided(x, pad, shift), strided(dy, pad, shift)
+    rd = strided(r, pad, shift) if residual else None
+    offd = torch.tensor(off, dtype=torch.int32, device="cuda") if off else None
+    if tail:   # rows of no group are not read, whatever they hold
+        xd[kept:] = float("nan")
+        dyd[kept:] = float("inf")
+        if residual:
+            rd[kept:] = float("nan")
+    wd, bd = w.cuda(), (b.cuda() if bias else None)
+    y, z = L.linear(xd, wd, bd, rd, offsets=offd, act=act, save=True)
+    dx, dw, db = L.linear_backward(dyd, xd, wd, z, offsets=offd, act=act, bias=bias)
+    y0 = L.linear(xd, wd, bd, rd, offsets=offd, act=act)
+    assert torch.equal(y0, y)
+    u, tiny = U[dtype], TINY[dtype]
+    spans = [(off[g], off[g + 1]) for g in range(groups)] if off else [(0, n)]
+    for g, (a, e) in enumerate(spans):
+        tag = f"group {g} rows {a}:{e}"
+        X, W, DY = x[a:e].double(), w[g].double(), dy[a:e].double()
+        Z = X @ W + (b[g].double() if bias else 0)
+        ez = product_error(X, W, n_in) + 2 * U32 * Z.abs()
+        Y = act64(Z, act) + (r[a:e].double() if residual else 0)
+        ey = (SLOPE1 * ez if act != "none" else ez) + 16 * U32 * (act64(Z, act).abs() + Z.abs() + Y.abs()) + tiny
+        within(y[a:e], Y, ey + u * Y.abs() * (1 + 2 * u), tag + " y")
+        if act != "none":
+            within(z[a:e], Z, ez + u * Z.abs() * (1 + 2 * u) + tiny, tag + " z")
+        DZ = DY * slope64(Z, act)
+        edz = torch.zeros_like(DZ)
+        if act != "none":
+            edz = DY.abs() * (SLOPE2 * (ez + u * Z.abs() * (1 + u) + tiny) + 32 * U32 * (1 + Z.abs())) + tiny
+        edz_r = edz + (u * (DZ.abs() + edz) if act != "none" else 0)   # rounded as the products' operand
+        DX = DZ @ W.t()
+        edx = edz_r @ W.abs().t() + (n_out + 8) * U32 * ((DZ.abs() + edz_r) @ W.abs().t())
+        within(dx[a:e], DX, edx + u * (DX.abs() + edx) + tiny, tag + " dx")
+        rows = e - a
+        DW = X.t() @ DZ
+        edw = X.abs().t() @ edz_r + (rows + 8) * U32 * (X.abs().t() @ (DZ.abs() + edz_r))
+        within(dw[g], DW, edw + u * (DW.abs() + edw) + tiny, tag + " dw")
+        if bias:
+            DB = DZ.sum(0)
+            edb = edz.sum(0) + (rows + 8) * U32 * (DZ.abs() + edz).sum(0)
+            within(db[g], DB, edb + u * (DB.abs() + edb) + tiny, tag + " db")
+    for t in [y, dx] + ([z] if act != "none" else []):
+        assert (t[kept:] == 0).all()
+
+
+SIZES = [(1, 1, 1), (1, 128, 128), (2, 7, 5), (3, 64, 1), (16, 16, 17), (17, 33, 15), (63, 64, 65), (64, 64, 64),
+         (65, 8, 72), (130, 97, 211), (257, 130, 129), (300, 200, 8)]
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("n,n_in,n_out", SIZES)
+def test_one_group(n, n_in, n_out, dtype):
+    case(n, n_in, n_out, dtype, "silu", seed=n)
+
+
+@pytest.mark.parametrize("act", ["none", "silu", "gelu"])
+@pytest.mark.parametrize("bias,residual", [(True, True), (False, False), (True, False)])
+def test_epilogues(act, bias, residual):
+    for dtype in ("fp32", "bf16", "fp16"):
+        case(70, 40, 56, dtype, act, bias=bias, residual=residual, seed=3)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("sizes,tail", [([5], 0), ([0, 3, 0, 0, 70, 1], 0), ([0, 0], 9), ([64, 64, 128], 0),
+                                        ([1] * 70 + [40], 11), ([129, 0, 257], 65), ([700, 3], 0)])
+def test_groups(sizes, tail, dtype):
+    case(None, 48, 40, dtype, "silu", sizes, tail, seed=len(sizes))
+    case(None, 31, 21, dtype, "gelu", sizes, tail, seed=len(sizes) + 1)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("pad,shift", [(8, 0), (1, 0), (0, 1), (3, 5), (16, 8)])
+def test_strided_rows(pad, shift, dtype):
+    case(75, 64, 80, dtype, "silu", pad=pad, shift=shift)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("n,n_in,n_out", [(5000, 64, 64), (5001, 70, 66), (33000, 128, 16), (4100, 256, 520)])
+def test_many_rows(n, n_in, n_out, dtype):
+    case(n, n_in, n_out, dtype, "silu", seed=1)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("n,n_in,n_out", [(3, 2048, 96), (40, 1030, 2048), (1, 2047, 33), (1500, 1024, 1536)])
+def test_long_sums(n, n_in, n_out, dtype):
+    case(n, n_in, n_out, dtype, "none", seed=2)
+
+
+def test_no_rows():
+    x = torch.empty(0, 24, device="cuda")
+    w = torch.randn(3, 24, 16, device="cuda")
+    off = torch.zeros(4, dtype=torch.int32, device="cuda")
+    y, z = L.linear(x, w, offsets=off, act="silu", save=True)
+    dx, dw, db = L.linear_backward(y, x, w, z, offsets=off, act="silu")
+    assert y.shape == (0, 16) and dx.shape == (0, 24) and (dw == 0).all() and (db == 0).all()
+
+
+def test_infinite_and_nan_rows_stay_in_their_rows():
+    x = torch.randn(70, 32, device="cuda")
+    x[3], x[66, 5] = float("nan"), float("inf")
+    w = torch.randn(32, 40, device="cuda")
+    y = L.linear(x, w)
+    ok = torch.isfinite(y).all(1)
+    assert not ok[3] and not ok[66] and int(ok.sum()) == 68
+    for dtype in (torch.bfloat16, torch.float16):   # 16-bit operands: infinities as IEEE has them
+        y = L.linear(x.to(dtype), w.to(dtype))
+        assert torch.isnan(y[3]).all() and torch.isinf(y[66]).all()
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_slope_of_saturated_values(act):
+    """|z| beyond binary16: z saves as infinity, whose slope is 0 or 1."""
+    x = torch.tensor([[60000.0], [-60000.0]], device="cuda", dtype=torch.float16)
+    w = torch.tensor([[4.0]], device="cuda", dtype=torch.float16)
+    _, z = L.linear(x, w, act=act, save=True)
+    dx, _, _ = L.linear_backward(torch.ones(2, 1, device="cuda", dtype=torch.float16), x, w, z, act=act)
+    assert torch.isinf(z).all() and dx.flatten().tolist() == [4.0, 0.0]
+
+
+def test_residual_in_place_and_out_of_order_offsets():
+    x, w = torch.randn(90, 24, device="cuda"), torch.randn(24, 24, device="cuda")
+    want = L.linear(x, w, residual=x, act="silu")
+    B = L.B
+    d = B.mace_linear_desc(90, 24, 24, 1, B.MACE_TYPE_FP32, B.MACE_ACT_SILU, 24, 24, 24, 24)
+    y = x.clone()
+    B.mace_linear_forward(d, x, w, None, y, None, y)
+    assert torch.equal(y, want)
+    # offsets past the rows or falling are held to the rows: no access outside
+    w3 = torch.randn(3, 24, 24, device="cuda")
+    for bad in ([0, 500, -3, 90], [0, 60, 30, 1 << 30], [-5, 10, 20, 80]):
+        off = torch.tensor(bad, dtype=torch.int32, device="cuda")
+        y, z = L.linear(x, w3, offsets=off, act="silu", save=True)
+        L.linear_backward(y, x, w3, z, offsets=off, act="silu")
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("act", ["none", "silu", "gelu"])
+def test_gradients_against_differences(act):
+    """Central differences of the FP32 forward, loss = <y, c> in FP64.  Step h =
+    1/64: truncation h^2 |f'''| / 6 below 1e-4 of the terms' magnitude, rounding
+    of y (2^-24 times |y| about 1, 3 000 terms added at random) over h below 1e-4."""
+    gen = torch.Generator().manual_seed(5)
+    n, k, m = 60, 20, 24
+    x, w, b, c, vx, vw, vb = (torch.randn(*s, generator=gen).cuda() for s in
+                              [(n, k), (2, k, m), (2, m), (n, m), (n, k), (2, k, m), (2, m)])
+    w *= k ** -0.5
+    off = torch.tensor([0, 25, 60], dtype=torch.int32, device="cuda")
+    _, z = L.linear(x, w, b, offsets=off, act=act, save=True)
+    dx, dw, db = L.linear_backward(c, x, w, z, offsets=off, act=act)
+
+    def loss(x, w, b):
+        return (L.linear(x, w, b, offsets=off, act=act).double() * c.double()).sum().item()
+    h = 1 / 64
+    for name, grad, plus, minus, v in [
+            ("x", dx, (x + h * vx, w, b), (x - h * vx, w, b), vx),
+            ("w", dw, (x, w + h * vw, b), (x, w - h * vw, b), vw),
+            ("b", db, (x, w, b + h * vb), (x, w, b - h * vb), vb)]:
+        want = (loss(*plus) - loss(*minus)) / (2 * h)
+        got = (grad.double() * v.double()).sum().item()
+        scale = (grad.double() * v.double()).abs().sum().item()
+        assert abs(got - want) <= 1e-3 * scale, (name, got, want, scale)
+
+
+def test_other_stream_and_graph():
+    gen = torch.Generator().manual_seed(0)
+    x, w = torch.randn(600, 64, generator=gen).cuda(), torch.randn(64, 96, generator=gen).cuda()
+    want, z = L.linear(x, w, act="silu", save=True)
+    dx, dw, db = L.linear_backward(want, x, w, z, act="silu")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    got = L.linear(x, w, act="silu", stream=s)
+    s.synchronize()
+    assert torch.equal(got, want)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        y1, z1 = L.linear(x, w, act="silu", save=True)
+        g1 = L.linear_backward(y1, x, w, z1, act="silu")
+    for _ in range(3):
+        for t in (y1, z1, *g1):
+            t.fill_(7.0)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        for a, b in zip((y1, z1, *g1), (want, z, dx, dw, db)):
+            assert torch.equal(a, b)

@@ -1,0 +1,178 @@
+"""Rows sorted by expert and back: the order bit for bit against numpy's stable
+sort, values against FP64 with one rounding per result (sums of top_k terms and
+of a row's products in FP32)."""
+import numpy as np
+import pytest
+import torch
+
+from dense_common import DTYPES, TINY, U, U32, randn, within
+
+pytestmark = pytest.mark.gpu
+L = pytest.importorskip("paper_2510_23621_amd.layers")
+
+
+def plan_of(expert, E):
+    key = np.where((expert.reshape(-1) < 0) | (expert.reshape(-1) >= E), E, expert.reshape(-1))
+    slots = np.argsort(key, kind="stable").astype(np.int32)
+    row = np.empty_like(slots)
+    row[slots] = np.arange(len(slots), dtype=np.int32)
+    off = np.concatenate([[0], np.cumsum(np.bincount(key, minlength=E + 1)[:E])]).astype(np.int32)
+    return slots, row.reshape(expert.shape), off, key.reshape(expert.shape) < E
+
+
+def experts(n, k, E, drop, seed):
+    rng = np.random.default_rng(seed)
+    e = rng.integers(0, E, (n, k)).astype(np.int32)
+    if drop:
+        e[rng.random((n, k)) < drop] = -1
+    return e
+
+
+@pytest.mark.parametrize("n,k,E", [(1, 1, 1), (1, 8, 300), (63, 1, 2), (64, 1, 64), (65, 3, 7), (1000, 4, 16),
+                                   (2048, 2, 512), (4096, 1, 5), (4097, 1, 1), (5003, 3, 37), (20000, 8, 256),
+                                   (90001, 1, 3)])
+@pytest.mark.parametrize("drop", [0.0, 0.3, 1.0])
+def test_order(n, k, E, drop):
+    e = experts(n, k, E, drop, n)
+    if drop == 0.3:
+        e[::7] = np.where(e[::7] >= 0, E + 5, e[::7])   # indices past the last expert drop too
+    slots, row, off, _ = plan_of(e, E)
+    p = L.route(torch.from_numpy(e).cuda(), E)
+    assert np.array_equal(p.slot_of_row.cpu().numpy(), slots)
+    assert np.array_equal(p.row_of_slot.cpu().numpy(), row)
+    assert np.array_equal(p.offsets.cpu().numpy(), off)
+
+
+@pytest.mark.parametrize("kind", ["one expert", "sorted", "reversed"])
+def test_order_of_skewed_experts(kind):
+    n, E = 9001, 200
+    e = {"one expert": np.full((n, 1), 150), "sorted": np.arange(n)[:, None] * E // n,
+         "reversed": (n - 1 - np.arange(n))[:, None] * E // n}[kind].astype(np.int32)
+    slots, row, off, _ = plan_of(e, E)
+    p = L.route(torch.from_numpy(e).cuda(), E)
+    assert np.array_equal(p.slot_of_row.cpu().numpy(), slots) and np.array_equal(p.offsets.cpu().numpy(), off)
+
+
+def test_no_tokens():
+    p = L.route(torch.empty(0, 3, dtype=torch.int32, device="cuda"), 9)
+    assert (p.offsets == 0).all()
+    x = torch.empty(0, 5, device="cuda")
+    rows = L.route_rows(x, p)
+    assert rows.shape == (0, 5) and L.combine_rows(rows, p).shape == (0, 5)
+
+
+def poison(t):
+    t.fill_(float("nan"))
+    return t
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("n,k,E,width,pad", [(1, 1, 1, 1, 0), (1, 2, 3, 128, 0), (50, 1, 2, 128, 0), (77, 3, 5, 33, 0),
+                                             (200, 8, 16, 64, 8), (65, 5, 4, 515, 3), (33, 11, 12, 200, 0),
+                                             (3000, 2, 9, 16, 1)])
+@pytest.mark.parametrize("drop", [0.0, 0.4])
+def test_rows(n, k, E, width, pad, dtype, drop):
+    gen = torch.Generator().manual_seed(n + k)
+    e = experts(n, k, E, drop, n + width)
+    if drop:
+        e[0] = -1   # a token whose every slot is dropped
+    _, row, off, kept = plan_of(e, E)
+    live = int(off[-1])
+    p = L.route(torch.from_numpy(e).cuda(), E)
+    u, tiny = U[dtype], TINY[dtype]
+    row_t, kept_t = torch.from_numpy(row).long(), torch.from_numpy(kept)
+
+    def wide(t):   # rows of a wider, poisoned buffer
+        v = poison(torch.empty(t.shape[0], width + pad, dtype=t.dtype, device="cuda"))[:, :width]
+        return v.copy_(t)
+    x, y = randn(n, width, gen=gen, dtype=dtype), randn(n * k, width, gen=gen, dtype=dtype)
+    dout, w = randn(n, width, gen=gen, dtype=dtype), torch.rand(n, k, generator=gen) + 0.1
+    xd, yd, doutd, wd = wide(x), wide(y), wide(dout), w.cuda()
+    yd[live:] = float("nan")   # dropped slots' rows are not used
+    if drop:
+        wd[~kept_t.cuda()] = float("inf")   # nor their weights
+    rows = L.route_rows(xd, p).cpu()
+    want = torch.zeros_like(rows)
+    want[row_t[kept_t]] = x[:, None].expand(n, k, width)[kept_t]
+    assert torch.equal(rows, want)
+    out = L.combine_rows(yd, p, wd)
+    keep = kept_t[..., None].double()
+    Y = y.double()[row_t] * keep
+    terms = Y * w.double()[..., None]
+    mag = terms.abs().sum(1)
+    within(out, terms.sum(1), (k + 2) * U32 * mag + u * mag + tiny, "out")
+    drows, dw = L.combine_rows_backward(doutd, yd, p, wd)
+    D = dout.double()
+    want = torch.zeros(n * k, width, dtype=torch.float64)
+    want[row_t[kept_t]] = (D[:, None] * w.double()[..., None])[kept_t]
+    within(drows, want, (u + 2 * U32) * want.abs() + tiny, "drows")
+    dots = Y * D[:, None]
+    within(dw, dots.sum(2), (width + 4) * U32 * dots.abs().sum(2), "dweights")
+    dx = L.route_rows_backward(yd, p)
+    mag = Y.abs().sum(1)
+    within(dx, Y.sum(1), (k + 2) * U32 * mag + u * mag + tiny, "dx")
+    no_w, none = L.combine_rows_backward(doutd, yd, p)
+    assert none is None
+    want = torch.zeros(n * k, width, dtype=DTYPES[dtype])
+    want[row_t[kept_t]] = dout[:, None].expand(n, k, width)[kept_t]
+    assert torch.equal(no_w.cpu(), want)
+
+
+def test_gradients_against_differences():
+    """combine is linear in rows and in weights: differences have no truncation,
+    only the rounding of FP32 results (1e-5 of the terms' magnitude is ample)."""
+    gen = torch.Generator().manual_seed(1)
+    n, k, E, d = 40, 3, 6, 24
+    p = L.route(torch.from_numpy(experts(n, k, E, 0.2, 0)).cuda(), E)
+    rows, w, c = (torch.randn(*s, generator=gen).cuda() for s in [(n * k, d), (n, k), (n, d)])
+    vr, vw = torch.randn(n * k, d, generator=gen).cuda(), torch.randn(n, k, generator=gen).cuda()
+    drows, dw = L.combine_rows_backward(c, rows, p, w)
+
+    def loss(rows, w):
+        return (L.combine_rows(rows, p, w).double() * c.double()).sum().item()
+    for grad, plus, minus, v in [(drows, (rows + vr, w), (rows - vr, w), vr), (dw, (rows, w + vw), (rows, w - vw), vw)]:
+        want = (loss(*plus) - loss(*minus)) / 2
+        terms = grad.double() * v.double()
+        assert abs(terms.sum().item() - want) <= 1e-5 * (terms.abs().sum().item() + abs(loss(*plus)) + abs(loss(*minus)))
+    x, vx, cr = torch.randn(n, d, generator=gen).cuda(), torch.randn(n, d, generator=gen).cuda(), torch.randn(n * k, d, generator=gen).cuda()
+    dx = L.route_rows_backward(cr, p)
+    want = (L.route_rows(vx, p).double() * cr.double()).sum().item()
+    terms = dx.double() * vx.double()
+    assert abs(terms.sum().item() - want) <= 1e-5 * terms.abs().sum().item()
+
+
+def test_row_indices_out_of_range_are_held_to_the_rows():
+    p = L.route(torch.zeros(8, 2, dtype=torch.int32, device="cuda"), 2)
+    bad = p._replace(row_of_slot=torch.tensor([[-7, 1 << 30]] * 8, dtype=torch.int32, device="cuda"))
+    x = torch.randn(8, 32, device="cuda")
+    rows = L.route_rows(x, p)
+    L.combine_rows(rows, bad)
+    L.route_rows(x, bad)
+    L.combine_rows_backward(x, rows, bad, torch.ones(8, 2, device="cuda"))
+    torch.cuda.synchronize()
+
+
+def test_other_stream_and_graph():
+    e = torch.from_numpy(experts(9000, 2, 12, 0.1, 4)).cuda()
+    x, w = torch.randn(9000, 72, device="cuda"), torch.rand(9000, 2, device="cuda")
+
+    def step(stream=None):
+        p = L.route(e, 12, stream=stream)
+        rows = L.route_rows(x, p, stream=stream)
+        return (*p, rows, L.combine_rows(rows, p, w, stream=stream), *L.combine_rows_backward(x, rows, p, w, stream=stream))
+    want = step()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    got = step(s)
+    s.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = step()
+    for _ in range(3):
+        for t in out:
+            t.zero_()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
