@@ -30,7 +30,7 @@ struct LinearArgs {
   T *y, *z;
   const int* offsets;
   int64_t n, ldx, ldy, ldr, ldz;
-  int n_in, n_out, groups, act, tiles_m;
+  int n_in, n_out, groups, act;
 };
 template <class T>
 struct RowGradArgs {
@@ -38,7 +38,7 @@ struct RowGradArgs {
   T* dx;
   const int* offsets;
   int64_t n, lddz, lddx;
-  int n_in, n_out, groups, tiles_m;
+  int n_in, n_out, groups;
 };
 template <class T>
 struct WeightGradArgs {
@@ -48,6 +48,14 @@ struct WeightGradArgs {
   const int* offsets;
   int64_t n, ldx, lddz;
   int n_in, n_out, groups, splits;
+};
+template <class T>
+struct BiasGradArgs {
+  const float* sums;
+  T* db;
+  const int* offsets;
+  int64_t n;
+  int n_out, run_rows, max_runs;
 };
 
 // rows behind the last group: zeros
@@ -92,13 +100,10 @@ __global__ void __launch_bounds__(S::NT) linear_fwd_kernel(LinearArgs<T> a) {
   });
 }
 
-// dx = dz W_g^T
+// dx = dz W_g^T: tile `id`
 template <class T, bool AL, class S>
-__global__ void __launch_bounds__(S::NT) linear_row_grad_kernel(RowGradArgs<T> a) {
-  __shared__ __align__(16) unsigned short lds[tile_lds<T, S>];
-  const int tid = threadIdx.x;
+__device__ __forceinline__ void row_grad_tile(const RowGradArgs<T>& a, int id, unsigned short* lds, int tid) {
   const int tiles_n = (a.n_in + S::BN - 1) / S::BN;
-  const int id = xcd_order(blockIdx.x, gridDim.x);
   const int c0 = id % tiles_n * S::BN, cols = min(S::BN, a.n_in - c0);
   RowRun run;
   if (!find_run(a.offsets, a.groups, a.n, S::BM, id / tiles_n, run)) return;
@@ -117,13 +122,10 @@ __global__ void __launch_bounds__(S::NT) linear_row_grad_kernel(RowGradArgs<T> a
                  [&](int m, int n, f4 v, int k) { store4(dx + m * a.lddx + n, v, k, AL && k == 4); });
 }
 
-// dW_g = x_g^T dz_g, the group's rows cut into `splits` parts
+// dW_g = x_g^T dz_g, the group's rows cut into `splits` parts: tile `id`
 template <class T, bool AL, class S>
-__global__ void __launch_bounds__(S::NT) linear_weight_grad_kernel(WeightGradArgs<T> a) {
-  __shared__ __align__(16) unsigned short lds[tile_lds<T, S>];
-  const int tid = threadIdx.x;
+__device__ __forceinline__ void weight_grad_tile(const WeightGradArgs<T>& a, int id, unsigned short* lds, int tid) {
   const int tiles_n = (a.n_out + S::BN - 1) / S::BN, tiles_m = (a.n_in + S::BM - 1) / S::BM;
-  int id = xcd_order(blockIdx.x, gridDim.x);
   const int c0 = id % tiles_n * S::BN;
   id /= tiles_n;
   const int m0 = id % tiles_m * S::BM;
@@ -152,6 +154,57 @@ __global__ void __launch_bounds__(S::NT) linear_weight_grad_kernel(WeightGradArg
     T* o = a.dw + at;
     for_results<S>(acc, rows, cols, tid,
                    [&](int m, int n, f4 v, int k) { store4(o + (int64_t)m * a.n_out + n, v, k, AL && k == 4); });
+  }
+}
+
+// db_g: the column sums of the group's runs (sums, one row per run), four row
+// lanes, then in order: 64 columns of one group
+template <class T>
+__device__ __forceinline__ void bias_grad(const BiasGradArgs<T>& a, int id, float* lds, int tid) {
+  const int blocks = (a.n_out + 63) / 64, g = id / blocks;
+  const int c = tid & 63, y = tid >> 6, col = id % blocks * 64 + c;
+  int first = 0, runs = 0;
+  if (!a.offsets) {
+    runs = (int)((a.n + a.run_rows - 1) / a.run_rows);
+  } else {   // every wave sums the runs of the groups before g
+    for (int e0 = 0; e0 <= g; e0 += 64) {
+      const int e = e0 + c;
+      int64_t p = 0, q = 0;
+      if (e <= g) {
+        p = min<int64_t>(max(a.offsets[e], 0), a.n);
+        q = min<int64_t>(max(a.offsets[e + 1], 0), a.n);
+      }
+      const int r = q > p ? (int)((q - p + a.run_rows - 1) / a.run_rows) : 0;
+      int before = e < g ? r : 0;
+#pragma unroll
+      for (int d = 32; d; d >>= 1) before += __shfl_xor(before, d);
+      first += before;
+      if (g - e0 < 64) runs = __shfl(r, g - e0);
+    }
+  }
+  runs = min(runs, a.max_runs - first);   // (offsets that do not rise could count more runs than there are sums)
+  float s = 0.f;
+  if (col < a.n_out)
+    for (int r = y; r < runs; r += 4) s += a.sums[(int64_t)(first + r) * a.n_out + col];
+  lds[y * 64 + c] = s;
+  __syncthreads();
+  if (y == 0 && col < a.n_out) a.db[(int64_t)g * a.n_out + col] = (T)(s + lds[64 + c] + lds[128 + c] + lds[192 + c]);
+}
+
+// All three gradients in one launch: blocks below row_blocks form dx, the next
+// weight_blocks dW, the rest db.
+template <class T, bool ALX, bool ALW, class S>
+__global__ void __launch_bounds__(S::NT)
+linear_grad_kernel(RowGradArgs<T> a, WeightGradArgs<T> b, BiasGradArgs<T> c, int row_blocks, int weight_blocks) {
+  __shared__ __align__(16) unsigned short lds[tile_lds<T, S>];
+  const int tid = threadIdx.x;
+  int id = blockIdx.x;
+  if (id < row_blocks) {
+    row_grad_tile<T, ALX, S>(a, xcd_order(id, row_blocks), lds, tid);
+  } else if ((id -= row_blocks) < weight_blocks) {
+    weight_grad_tile<T, ALW, S>(b, xcd_order(id, weight_blocks), lds, tid);
+  } else {
+    bias_grad<T>(c, id - weight_blocks, reinterpret_cast<float*>(lds), tid);
   }
 }
 
@@ -216,44 +269,6 @@ linear_slope_kernel(const T* __restrict__ dy, int64_t lddy, const T* __restrict_
   }
 }
 
-// db_g: the column sums of the group's runs, 16 row lanes, then in order
-template <class T>
-__global__ void __launch_bounds__(1024) linear_bias_grad_kernel(const float* __restrict__ sums,
-                                                                const int* __restrict__ offsets, int groups, int64_t n,
-                                                                int n_out, int run_rows, int max_runs, T* __restrict__ db) {
-  __shared__ float red[16][64];
-  const int g = blockIdx.y, c = threadIdx.x & 63, y = threadIdx.x >> 6, col = blockIdx.x * 64 + c;
-  int first = 0, runs = 0;
-  if (!offsets) {
-    runs = (int)((n + run_rows - 1) / run_rows);
-  } else {   // every wave sums the runs of the groups before g
-    for (int e0 = 0; e0 <= g; e0 += 64) {
-      const int e = e0 + c;
-      int64_t a = 0, b = 0;
-      if (e <= g) {
-        a = min<int64_t>(max(offsets[e], 0), n);
-        b = min<int64_t>(max(offsets[e + 1], 0), n);
-      }
-      const int r = b > a ? (int)((b - a + run_rows - 1) / run_rows) : 0;
-      int before = e < g ? r : 0;
-#pragma unroll
-      for (int d = 32; d; d >>= 1) before += __shfl_xor(before, d);
-      first += before;
-      if (g - e0 < 64) runs = __shfl(r, g - e0);
-    }
-  }
-  runs = min(runs, max_runs - first);   // (offsets that do not rise could count more runs than there are sums)
-  float s = 0.f;
-  if (col < n_out)
-    for (int r = y; r < runs; r += 16) s += sums[(int64_t)(first + r) * n_out + col];
-  red[y][c] = s;
-  __syncthreads();
-  if (y == 0 && col < n_out) {
-    for (int r = 1; r < 16; ++r) s += red[r][c];
-    db[(int64_t)g * n_out + col] = (T)s;
-  }
-}
-
 // ------------------------------------------------------------------ host
 constexpr int kMaxLinearGroups = 1024;
 
@@ -283,13 +298,13 @@ int weight_splits(const mace_linear_desc& d, int bm, int bn) {
   return (int)std::max<int64_t>(1, std::min({want, most, (int64_t)64}));
 }
 
+constexpr int64_t kFillBlocks = 256;   // blocks from which the larger tile is taken (one per CU)
+
 struct BackwardPlan {
   int splits;
   int64_t lddz;
   size_t dz, sums, part, total;   // byte offsets
 };
-
-constexpr int64_t kFillBlocks = 256;   // blocks from which the larger tile is taken (one per CU)
 
 bool small_weight_tiles(const mace_linear_desc& d) {
   return ceil_div(d.n_in, 128) * ceil_div(d.n_out, 128) * d.n_groups * std::max<int64_t>(1, d.n_rows / d.n_groups / 512) < kFillBlocks;
@@ -326,7 +341,7 @@ template <class T>
 mace_status forward(const mace_linear_desc& d, const void* x, const void* w, const void* bias, const void* residual,
                     const int* offsets, void* y, void* z, hipStream_t s) {
   LinearArgs<T> a{(const T*)x, (const T*)w, (const T*)bias, (const T*)residual, (T*)y, (T*)z, offsets, d.n_rows,
-                  d.ld_x, d.ld_y, d.ld_residual, d.ld_preact, d.n_in, d.n_out, d.n_groups, d.act, 0};
+                  d.ld_x, d.ld_y, d.ld_residual, d.ld_preact, d.n_in, d.n_out, d.n_groups, d.act};
   const bool al = aligned16(x) && aligned16(w) && aligned16(bias) && aligned16(residual) && aligned16(y) &&
                   aligned16(z) && ((d.n_in | d.n_out | d.ld_x | d.ld_y | d.ld_residual | d.ld_preact) & 7) == 0;
   auto go = [&](auto shape) -> mace_status {
@@ -369,47 +384,43 @@ mace_status backward(const mace_linear_desc& d, const void* dy, int64_t lddy, co
     else go(linear_slope_kernel<T, false>);
     if ((st = launched()) != MACE_OK) return st;
   }
-  if (db) {
-    linear_bias_grad_kernel<T><<<dim3((unsigned)ceil_div(d.n_out, 64), d.n_groups), 1024, 0, s>>>(
-        sums, offsets, d.n_groups, d.n_rows, d.n_out, slope_run(d.n_rows), (int)slope_runs(d), (T*)db);
-    if ((st = launched()) != MACE_OK) return st;
-  }
   const bool al_z = aligned16(dz) && ((d.n_in | d.n_out | lddz) & 7) == 0;
-  if (dx && d.n_rows > 0) {
-    RowGradArgs<T> a{dz, (const T*)w, (T*)dx, offsets, d.n_rows, lddz, lddx, d.n_in, d.n_out, d.n_groups, 0};
-    const bool al = al_z && aligned16(w) && aligned16(dx) && (lddx & 7) == 0;
-    auto go = [&](auto shape) -> mace_status {
-      using S = decltype(shape);
-      const int64_t blocks = (ceil_div(d.n_rows, S::BM) + (offsets ? d.n_groups : 0)) * ceil_div(d.n_in, S::BN);
-      if (blocks > INT32_MAX) return MACE_EUNSUPPORTED;
-      if (al) linear_row_grad_kernel<T, true, S><<<(unsigned)blocks, S::NT, 0, s>>>(a);
-      else linear_row_grad_kernel<T, false, S><<<(unsigned)blocks, S::NT, 0, s>>>(a);
-      return launched();
-    };
-    using Mid = typename Shapes<T>::Mid;
-    st = ceil_div(d.n_rows, Mid::BM) * ceil_div(d.n_in, Mid::BN) >= kFillBlocks ? go(Mid{})
-                                                                             : go(typename Shapes<T>::Small{});
-    if (st != MACE_OK) return st;
+  const bool al_x = al_z && aligned16(w) && aligned16(dx) && (lddx & 7) == 0;
+  const bool al_w = al_z && aligned16(x) && aligned16(dw) && (d.ld_x & 7) == 0;
+  const RowGradArgs<T> ra{dz, (const T*)w, (T*)dx, offsets, d.n_rows, lddz, lddx, d.n_in, d.n_out, d.n_groups};
+  const WeightGradArgs<T> wa{(const T*)x, dz, (T*)dw, p.splits > 1 ? reinterpret_cast<float*>(ws + p.part) : nullptr,
+                             offsets, d.n_rows, d.ld_x, lddz, d.n_in, d.n_out, d.n_groups, p.splits};
+  const BiasGradArgs<T> ba{sums, (T*)db, offsets, d.n_rows, d.n_out, slope_run(d.n_rows), (int)slope_runs(d)};
+  auto go = [&](auto shape, bool rows, bool weights, bool bias) -> mace_status {
+    using S = decltype(shape);
+    static_assert(S::NT == 256, "bias_grad's lanes");
+    const int64_t rb = rows ? (ceil_div(d.n_rows, S::BM) + (offsets ? d.n_groups : 0)) * ceil_div(d.n_in, S::BN) : 0;
+    const int64_t wb = weights ? ceil_div(d.n_in, S::BM) * ceil_div(d.n_out, S::BN) * d.n_groups * p.splits : 0;
+    const int64_t blocks = rb + wb + (bias ? ceil_div(d.n_out, 64) * d.n_groups : 0);
+    if (blocks > INT32_MAX) return MACE_EUNSUPPORTED;
+    if (blocks == 0) return MACE_OK;
+    auto f = al_x && al_w ? linear_grad_kernel<T, true, true, S>
+                          : (al_x ? linear_grad_kernel<T, true, false, S>
+                                  : (al_w ? linear_grad_kernel<T, false, true, S> : linear_grad_kernel<T, false, false, S>));
+    f<<<(unsigned)blocks, S::NT, 0, s>>>(ra, wa, ba, (int)rb, (int)wb);
+    return launched();
+  };
+  using Mid = typename Shapes<T>::Mid;
+  using Small = typename Shapes<T>::Small;
+  const bool want_x = dx && d.n_rows > 0;
+  const bool small_x = ceil_div(d.n_rows, Mid::BM) * ceil_div(d.n_in, Mid::BN) < kFillBlocks;
+  const bool small_w = small_weight_tiles(d);
+  const bool x_big = want_x && !small_x, w_big = dw && !small_w;
+  if (x_big || w_big) {
+    if ((st = go(Mid{}, x_big, w_big, db != nullptr)) != MACE_OK) return st;
+    if ((st = go(Small{}, want_x && small_x, dw && small_w, false)) != MACE_OK) return st;
+  } else {
+    if ((st = go(Small{}, want_x, dw != nullptr, db != nullptr)) != MACE_OK) return st;
   }
-  if (dw) {
-    WeightGradArgs<T> a{(const T*)x, dz, (T*)dw, p.splits > 1 ? reinterpret_cast<float*>(ws + p.part) : nullptr,
-                        offsets, d.n_rows, d.ld_x, lddz, d.n_in, d.n_out, d.n_groups, p.splits};
-    const bool al = al_z && aligned16(x) && aligned16(dw) && (d.ld_x & 7) == 0;
-    auto go = [&](auto shape) -> mace_status {
-      using S = decltype(shape);
-      const int64_t blocks = ceil_div(d.n_in, S::BM) * ceil_div(d.n_out, S::BN) * d.n_groups * p.splits;
-      if (blocks > INT32_MAX) return MACE_EUNSUPPORTED;
-      if (al) linear_weight_grad_kernel<T, true, S><<<(unsigned)blocks, S::NT, 0, s>>>(a);
-      else linear_weight_grad_kernel<T, false, S><<<(unsigned)blocks, S::NT, 0, s>>>(a);
-      return launched();
-    };
-    st = small_weight_tiles(d) ? go(typename Shapes<T>::Small{}) : go(typename Shapes<T>::Mid{});
-    if (st != MACE_OK) return st;
-    if (p.splits > 1) {
-      const int64_t size = (int64_t)d.n_groups * d.n_in * d.n_out;
-      linear_join_kernel<T><<<(unsigned)ceil_div(size, 1024), 256, 0, s>>>(a.part, p.splits, size, (T*)dw);
-      st = launched();
-    }
+  if (dw && p.splits > 1) {
+    const int64_t size = (int64_t)d.n_groups * d.n_in * d.n_out;
+    linear_join_kernel<T><<<(unsigned)ceil_div(size, 1024), 256, 0, s>>>(wa.part, p.splits, size, (T*)dw);
+    st = launched();
   }
   return st;
 }

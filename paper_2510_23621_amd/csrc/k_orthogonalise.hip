@@ -50,13 +50,12 @@ __global__ void __launch_bounds__(256) ns_norm_kernel(const T* __restrict__ g, i
                                                       int cols, double* __restrict__ part) {
   __shared__ double red[4];
   const T* m = g + (int64_t)blockIdx.y * stride;
-  const int64_t size = (int64_t)rows * cols, per = (size + gridDim.x - 1) / gridDim.x;
-  const int64_t i0 = blockIdx.x * per, i1 = min(size, i0 + per);
   double s = 0.0;
-  for (int64_t i = i0 + threadIdx.x; i < i1; i += 256) {
-    const double v = to_f32(m[i / cols * ld + i % cols]);
-    s += v * v;
-  }
+  for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += 4 * gridDim.x)   // a row per wave
+    for (int c = threadIdx.x & 63; c < cols; c += 64) {
+      const double v = to_f32(m[r * ld + c]);
+      s += v * v;
+    }
   for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
   __syncthreads();
@@ -242,6 +241,178 @@ __global__ void __launch_bounds__(256) ns_apply64_kernel(const T* g, int64_t str
   }
 }
 
+// ------------------------------------------------------------------ matrices that fit LDS
+// Up to 128 x 128: one block per matrix does everything, x and A (then B) staying
+// in LDS as pairs, padded to MM x NN. Both products of x read the one layout
+// [i][j]: rows by ds_read_b128, columns by ds_read_b64_tr_b16; the 16-byte chunks
+// of row i are XORed with its three low bits rotated, which keeps eight rows' chunks
+// (b128) and four rows' pairs of chunks (transposed) apart.
+template <int LD>
+__device__ __forceinline__ int fit_chunk(int i, int j) {
+  return i * LD + (((j >> 3) ^ (((i & 3) << 1) | ((i >> 2) & 1))) << 3);
+}
+template <int LD>
+__device__ __forceinline__ us8 fit_rows(const unsigned short* t, int row0, int k0, int lane) {
+  return *reinterpret_cast<const us8*>(t + fit_chunk<LD>(row0 + (lane & 15), k0 + 8 * (lane >> 4)));
+}
+template <int LD>
+__device__ __forceinline__ us8 fit_cols(const unsigned short* t, int col0, int k0, int lane) {
+  typedef __attribute__((address_space(3))) s4 lds_s4;
+  typedef short s8_ __attribute__((ext_vector_type(8)));
+  const int i = lane & 15, k = k0 + 8 * (lane >> 4) + (i >> 2), c = col0 + 4 * (i & 3);
+  const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(t + fit_chunk<LD>(k, c) + (c & 7)));
+  const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(t + fit_chunk<LD>(k + 4, c) + (c & 7)));
+  const s8_ r = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  return __builtin_bit_cast(us8, r);
+}
+
+// D (R x C) = P Q over K on 8 waves as WR x WC parts; the lane's results in
+// acc[j][i]: row 16 i + l%16 and columns 16 j + 4 (l/16) + 0..3 of its wave's
+// part. QC: Q[k][c] is x itself, else Q = src^T and its columns are src's rows.
+template <int R, int C, int K, int LDP, int LDQ, bool QC, int WR, int WC>
+struct FitProduct {
+  static constexpr int TI = R / WR / 16, TJ = C / WC / 16;
+  f4 acc[TJ][TI];
+  int r0, c0;
+  __device__ __forceinline__ void run(const unsigned short* p, int plane_p, const unsigned short* q, int plane_q, int tid) {
+    const int lane = tid & 63, w = tid >> 6;
+    r0 = w / WC * (R / WR);
+    c0 = w % WC * (C / WC);
+#pragma unroll
+    for (int j = 0; j < TJ; ++j)
+#pragma unroll
+      for (int i = 0; i < TI; ++i) acc[j][i] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < K; k += 32) {
+      us8 b[TI][2];
+#pragma unroll
+      for (int i = 0; i < TI; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) b[i][h] = fit_rows<LDP>(p + h * plane_p, r0 + 16 * i, k, lane);
+#pragma unroll
+      for (int j = 0; j < TJ; ++j) {
+        us8 a[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          a[h] = QC ? fit_cols<LDQ>(q + h * plane_q, c0 + 16 * j, k, lane) : fit_rows<LDQ>(q + h * plane_q, c0 + 16 * j, k, lane);
+#pragma unroll
+        for (int i = 0; i < TI; ++i) acc[j][i] = products<HalfPair, 2>(a, b[i], acc[j][i]);
+      }
+    }
+  }
+  // f(row, column, values)
+  template <class F>
+  __device__ __forceinline__ void each(int tid, F f) const {
+    const int lane = tid & 63;
+#pragma unroll
+    for (int i = 0; i < TI; ++i)
+#pragma unroll
+      for (int j = 0; j < TJ; ++j) f(r0 + 16 * i + (lane & 15), c0 + 16 * j + 4 * (lane >> 4), acc[j][i], j * TI + i);
+  }
+};
+
+template <int LD>
+__device__ __forceinline__ f4 fit_read(const unsigned short* t, int plane, int i, int j) {
+  return read_pair(reinterpret_cast<const _Float16*>(t + fit_chunk<LD>(i, j) + (j & 7)), plane);
+}
+template <int LD>
+__device__ __forceinline__ void fit_write(unsigned short* t, int plane, int i, int j, f4 v) {
+  h4 hi, lo;
+  split_pair(v, hi, lo);
+  unsigned short* p = t + fit_chunk<LD>(i, j) + (j & 7);
+  *reinterpret_cast<h4*>(p) = hi;
+  *reinterpret_cast<h4*>(p + plane) = lo;
+}
+
+template <class T, int MM, int NN>
+__global__ void __launch_bounds__(512)
+ns_fit_kernel(const T* g, int64_t stride, int64_t ld, int m, int n, bool tall, double eps, NsSteps steps, T* out,
+              int64_t ostride, int64_t old) {
+  constexpr int PX = MM * NN, PA = MM * MM, QUADS = MM * NN / 4 / 512;
+  extern __shared__ __align__(16) unsigned short fit_lds[];
+  unsigned short *x = fit_lds, *A = fit_lds + 2 * PX;
+  __shared__ double red[8];
+  const int tid = threadIdx.x;
+  const T* src = g + (int64_t)blockIdx.x * stride;
+  T* dst = out + (int64_t)blockIdx.x * ostride;
+  // quads of four columns; lanes run along g's contiguous axis
+  auto place = [&](int u, int& i, int& j) {
+    const int q = tid + 512 * u;
+    i = tall ? q % MM : q / (NN / 4);
+    j = 4 * (tall ? q / MM : q % (NN / 4));
+  };
+  f4 v[QUADS];
+  double s = 0.0;
+#pragma unroll
+  for (int u = 0; u < QUADS; ++u) {
+    int i, j;
+    place(u, i, j);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      v[u][c] = i < m && j + c < n ? element(src, ld, tall, i, j + c) : 0.f;
+      s += (double)v[u][c] * v[u][c];
+    }
+  }
+  for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
+  if ((tid & 63) == 0) red[tid >> 6] = s;
+  __syncthreads();
+  s = 0.0;
+  for (int i = 0; i < 8; ++i) s += red[i];
+  const double inv = kScaleX / (sqrt(s) + eps);
+#pragma unroll
+  for (int u = 0; u < QUADS; ++u) {
+    int i, j;
+    place(u, i, j);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) v[u][c] = (float)(v[u][c] * inv);
+    fit_write<NN>(x, PX, i, j, v[u]);
+  }
+  __syncthreads();
+  constexpr int WC = MM == 64 ? 4 : 2, WR = 8 / WC;
+  for (int st = 0; st < steps.n; ++st) {
+    const float ca = (float)steps.c[st][0], cb = (float)steps.c[st][1] * (kScaleB / kScaleA),
+                cc = (float)steps.c[st][2] * (kScaleB / (kScaleA * kScaleA));
+    {
+      FitProduct<MM, MM, NN, NN, NN, false, WR, WC> p;
+      p.run(x, PX, x, PX, tid);
+      p.each(tid, [&](int i, int j, f4 r, int) { fit_write<MM>(A, PA, i, j, r * (kScaleA / (kScaleX * kScaleX))); });
+    }
+    __syncthreads();
+    {
+      FitProduct<MM, MM, MM, MM, MM, false, WR, WC> p;
+      p.run(A, PA, A, PA, tid);
+      f4 b[p.TI * p.TJ];
+      p.each(tid, [&](int i, int j, f4 r, int e) { b[e] = cc * r + cb * fit_read<MM>(A, PA, i, j); });
+      __syncthreads();
+      p.each(tid, [&](int i, int j, f4, int e) { fit_write<MM>(A, PA, i, j, b[e]); });
+    }
+    __syncthreads();
+    {
+      FitProduct<MM, NN, MM, MM, NN, true, WR, WC> p;
+      p.run(A, PA, x, PX, tid);
+      const bool last = st + 1 == steps.n;
+      f4 b[p.TI * p.TJ];
+      p.each(tid, [&](int i, int j, f4 r, int e) { b[e] = (1.f / kScaleB) * r + ca * fit_read<NN>(x, PX, i, j); });
+      if (!last) {
+        __syncthreads();
+        p.each(tid, [&](int i, int j, f4, int e) { fit_write<NN>(x, PX, i, j, b[e]); });
+        __syncthreads();
+      } else {
+        p.each(tid, [&](int i, int j, f4, int e) {
+          if (i >= m) return;
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            if (j + c < n) {
+              const T r = (T)(b[e][c] * (1.f / kScaleX));
+              if (tall) dst[(int64_t)(j + c) * old + i] = r;
+              else dst[(int64_t)i * old + j + c] = r;
+            }
+        });
+      }
+    }
+  }
+}
+
 // ------------------------------------------------------------------ products
 
 // operand rows from row0 of a plane pair (T: binary16 reads the upper plane only)
@@ -381,7 +552,7 @@ bool in_range(const double* c, int steps) {
 
 struct NsPlan {
   int m, n, mp, np, parts;   // parts: partial sums of the norm, or chunks of the FP64 products
-  bool tall, gram;
+  bool tall, gram, fit;   // which of the kernels above; neither: products by launches of tiles
   size_t part, q, x0, x1, A, B, total;
 };
 NsPlan plan(const mace_orthogonalise_desc& d) {
@@ -392,7 +563,8 @@ NsPlan plan(const mace_orthogonalise_desc& d) {
   p.mp = (p.m + 7) / 8 * 8;
   p.np = (p.n + 7) / 8 * 8;
   p.gram = p.m <= kGramMax;
-  p.parts = p.gram ? (int)ceil_div(p.n, kGramChunk) : (int)std::min<int64_t>(kNormBlocks, ceil_div((int64_t)p.m * p.n, 8192));
+  p.parts = p.gram ? (int)ceil_div(p.n, kGramChunk) : (int)std::min<int64_t>(kNormBlocks, ceil_div(d.rows, 4));
+  p.fit = !p.gram && p.n <= 128;
   size_t o = 0;
   auto take = [&](size_t bytes) {
     const size_t at = o;
@@ -405,6 +577,7 @@ NsPlan plan(const mace_orthogonalise_desc& d) {
     p.total = o;
     return p;
   }
+  if (p.fit && d.n_steps > 0) return p;
   p.part = take(sizeof(double) * d.batch * p.parts);
   p.x0 = take(size_t(4) * d.batch * p.m * p.np);
   p.x1 = take(size_t(4) * d.batch * p.m * p.np);
@@ -450,15 +623,33 @@ mace_status update(const PairMat& B, const PairMat& x, const PairMat& xo, int64_
                                                                         : go(typename Shapes<T>::Small{});
 }
 
+template <class O, int MM, int NN>
+mace_status run_fit(const mace_orthogonalise_desc& d, const NsPlan& p, const NsSteps& steps, const O* g, O* out,
+                    hipStream_t s) {
+  constexpr int bytes = 2 * 2 * (MM * NN + MM * MM);
+  auto f = ns_fit_kernel<O, MM, NN>;
+  if (bytes > 65536 && hipFuncSetAttribute(reinterpret_cast<const void*>(f), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                           bytes) != hipSuccess)
+    return MACE_EHIP;
+  f<<<(unsigned)d.batch, 512, bytes, s>>>(g, d.stride_g, d.ld_g, p.m, p.n, p.tall, d.eps, steps, out, d.stride_out,
+                                          d.ld_out);
+  return launched();
+}
+
 template <class O>
 mace_status run(const mace_orthogonalise_desc& d, const O* g, const double* coef, O* out, char* ws, hipStream_t s) {
   const NsPlan p = plan(d);
   double* part = reinterpret_cast<double*>(ws + p.part);
   mace_status st;
+  NsSteps steps{};
+  steps.n = d.n_steps;
+  for (int i = 0; i < 3 * d.n_steps; ++i) steps.c[i / 3][i % 3] = coef[i];
+  if (p.fit && d.n_steps > 0) {
+    if (p.n <= 64) return run_fit<O, 64, 64>(d, p, steps, g, out, s);
+    if (p.m <= 64) return run_fit<O, 64, 128>(d, p, steps, g, out, s);
+    return run_fit<O, 128, 128>(d, p, steps, g, out, s);
+  }
   if (p.gram) {
-    NsSteps steps{};
-    steps.n = d.n_steps;
-    for (int i = 0; i < 3 * d.n_steps; ++i) steps.c[i / 3][i % 3] = coef[i];
     double* q = reinterpret_cast<double*>(ws + p.q);
     ns_gram64_kernel<O><<<dim3(p.parts, (unsigned)d.batch), 256, 0, s>>>(g, d.stride_g, d.ld_g, p.m, p.n, p.tall, part);
     if ((st = launched()) != MACE_OK) return st;

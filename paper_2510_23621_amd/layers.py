@@ -1,15 +1,18 @@
 """Dense operators on torch tensors: grouped linear layers, rows sorted by
 expert and back, Newton-Schulz orthogonalisation, and the gradients of the
 first two.  torch allocates results and workspaces, the library's kernels do
-the work on ``stream`` (default: the current one).
+the work on ``stream`` (a torch.cuda.Stream; default: the current one).
 
 Tensors are float32, bfloat16 or float16 on one GPU; rows may be strided
 (any row stride, columns adjacent).  Tensors of another stream are the
 caller's to order, as with any torch operation.
+
+The checks are written out in each function: a small layer's call is bound by
+the host, and one costs about as much as its kernel.
 """
 from __future__ import annotations
 
-from contextlib import nullcontext
+from functools import lru_cache, wraps
 from typing import NamedTuple
 
 import numpy as np
@@ -23,90 +26,121 @@ ACTIVATIONS = {"none": B.MACE_ACT_NONE, "silu": B.MACE_ACT_SILU, "gelu": B.MACE_
 NEWTON_SCHULZ = ((3.4445, -4.7750, 2.0315),) * 5
 
 
-def _on(stream):
-    """Allocations belong to the stream that uses them."""
-    return nullcontext() if stream is None else torch.cuda.stream(stream)
+def _streamed(f):
+    """Runs f with `stream` as the current stream, so that what it allocates
+    belongs to the stream that uses it."""
+    @wraps(f)
+    def on(*args, stream=None, **kw):
+        if stream is None:
+            return f(*args, **kw)
+        with torch.cuda.stream(stream):
+            return f(*args, **kw)
+    return on
 
 
-def _need(ok: bool, what: str):
-    if not ok:
-        raise ValueError(what)
+def _current_stream(t) -> int:
+    return torch._C._cuda_getCurrentRawStream(t.get_device())
 
 
-def _rows(t, name: str, shape, like) -> int:
-    """Leading dimension of a [rows, columns] tensor, after checking it."""
-    _need(tuple(t.shape) == tuple(shape), f"{name} must be {tuple(shape)}, not {tuple(t.shape)}")
-    _need(t.dtype == like.dtype and t.device == like.device, f"{name} must have x's dtype and device")
-    n, c = shape
-    if n == 0:
-        return c
-    s = t.stride()
-    if n == 1:
-        _need(c == 1 or s[1] == 1, f"{name}'s columns must be adjacent")
-        return c
-    _need((c == 1 or s[1] == 1) and s[0] >= c, f"{name}'s columns must be adjacent and its rows apart")
-    return s[0]
+def _rows(t, n: int, c: int, like, name: str) -> int:
+    """Leading dimension of t, which has to be [n, c] with adjacent columns and of like's dtype and device."""
+    if t.shape != (n, c):
+        raise ValueError(f"{name} must be {(n, c)}, not {tuple(t.shape)}")
+    if t.dtype != like.dtype or t.get_device() != like.get_device():
+        raise ValueError(f"{name} must have the first tensor's dtype and device")
+    s0, s1 = t.stride()
+    if (s1 != 1 and c > 1 and n > 0) or (s0 < c and n > 1):
+        raise ValueError(f"{name}'s columns must be adjacent and its rows apart")
+    return s0 if n > 1 else c
 
 
-def _whole(t, name: str, shape, dtype, device):
-    _need(tuple(t.shape) == tuple(shape) and t.dtype == dtype and t.device == device and t.is_contiguous(),
-          f"{name} must be contiguous {tuple(shape)} {dtype} on {device}")
+def _whole(t, shape, dtype, like, name: str):
+    if t.shape != shape or t.dtype != dtype or t.get_device() != like.get_device() or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous {tuple(shape)} {dtype} on {like.device}")
 
 
-def _linear_desc(x, w, bias, offsets, act):
-    _need(x.dim() == 2 and x.is_cuda and x.dtype in DTYPES, "x must be a [rows, n_in] GPU tensor of a supported dtype")
-    _need(act in ACTIVATIONS, f"act must be one of {sorted(ACTIVATIONS)}")
-    _need(w.dim() in (2, 3), "w must be [n_in, n_out] or [groups, n_in, n_out]")
+def _gpu_matrix(t, name: str) -> int:
+    """The library's number of t's dtype; t has to be a matrix on a GPU."""
+    dtype = DTYPES.get(t.dtype)
+    if dtype is None or t.dim() != 2 or not t.is_cuda:
+        raise ValueError(f"{name} must be a 2-d GPU tensor of float32, bfloat16 or float16")
+    return dtype
+
+
+def _linear_desc(x, w, offsets, act):
+    dtype, a = _gpu_matrix(x, "x"), ACTIVATIONS.get(act)
+    if a is None:
+        raise ValueError(f"act must be one of {sorted(ACTIVATIONS)}")
     n, n_in = x.shape
-    groups, n_out = (1 if w.dim() == 2 else w.shape[0]), w.shape[-1]
-    _whole(w, "w", (*w.shape[:-2], n_in, n_out), x.dtype, x.device)
-    if bias is not None:
-        _whole(bias, "bias", (*w.shape[:-2], n_out), x.dtype, x.device)
-    if offsets is not None:
-        _whole(offsets, "offsets", (groups + 1,), torch.int32, x.device)
+    shape = w.shape
+    if len(shape) == 3:
+        groups, k, n_out = shape
+    elif len(shape) == 2:
+        groups, (k, n_out) = 1, shape
     else:
-        _need(groups == 1, "more than one group needs offsets")
-    d = B.mace_linear_desc(n, n_in, n_out, groups, DTYPES[x.dtype], ACTIVATIONS[act], _rows(x, "x", x.shape, x), n_out,
-                           n_out, n_out)
-    return d
+        raise ValueError("w must be [n_in, n_out] or [groups, n_in, n_out]")
+    if k != n_in or w.dtype != x.dtype or w.get_device() != x.get_device() or not w.is_contiguous():
+        raise ValueError(f"w must be contiguous with {n_in} input rows, of x's dtype and device")
+    if offsets is not None:
+        _whole(offsets, (groups + 1,), torch.int32, x, "offsets")
+    elif groups != 1:
+        raise ValueError("more than one group needs offsets")
+    s0, s1 = x.stride()
+    if (s1 != 1 and n_in > 1 and n > 0) or (s0 < n_in and n > 1):
+        raise ValueError("x's columns must be adjacent and its rows apart")
+    return B.mace_linear_desc(n, n_in, n_out, groups, dtype, a, s0 if n > 1 else n_in, n_out, n_out, n_out)
 
 
-def linear(x, w, bias=None, residual=None, *, offsets=None, act: str = "none", save: bool = False, stream=None):
+@_streamed
+def linear(x, w, bias=None, residual=None, *, offsets=None, act: str = "none", save: bool = False):
     """y = act(x W_g + b_g) + residual for the rows offsets[g]:offsets[g+1] of
     each group g (int32 offsets on the device; None: one group).  Rows behind
     the last group give zeros.  With save, returns (y, z): z is what
     linear_backward needs, the value before the activation (None without one)."""
-    d = _linear_desc(x, w, bias, offsets, act)
-    shape = (d.n_rows, d.n_out)
+    d = _linear_desc(x, w, offsets, act)
+    n, m = d.n_rows, d.n_out
+    if bias is not None:
+        _whole(bias, (*w.shape[:-2], m), x.dtype, x, "bias")
     if residual is not None:
-        d.ld_residual = _rows(residual, "residual", shape, x)
-    with _on(stream):
-        y = torch.empty(shape, dtype=x.dtype, device=x.device)
-        z = torch.empty(shape, dtype=x.dtype, device=x.device) if save and act != "none" else None
-        B.mace_linear_forward(d, x, w, bias, residual, offsets, y, z, stream)
+        d.ld_residual = _rows(residual, n, m, x, "residual")
+    y = x.new_empty((n, m))
+    z = x.new_empty((n, m)) if save and d.act else None
+    B._check(B.lib().mace_linear_forward(d, x.data_ptr(), w.data_ptr(), None if bias is None else bias.data_ptr(),
+                                         None if residual is None else residual.data_ptr(),
+                                         None if offsets is None else offsets.data_ptr(), y.data_ptr(),
+                                         None if z is None else z.data_ptr(), _current_stream(x)),
+             "mace_linear_forward")
     return (y, z) if save else y
 
 
+@_streamed
 def linear_backward(dy, x, w, z=None, *, offsets=None, act: str = "none", bias: bool = True, need_dx: bool = True,
-                    need_dw: bool = True, stream=None):
+                    need_dw: bool = True):
     """(dx, dw, db) of `linear` from dy; z as `linear` saved it.  The residual's
     gradient is dy itself.  bias, need_dx, need_dw: which ones are wanted (None
     in the others' places)."""
-    d = _linear_desc(x, w, None, offsets, act)
-    shape = (d.n_rows, d.n_out)
-    ld_dy = _rows(dy, "dy", shape, x)
-    if act != "none":
-        _need(z is not None, "an activation's gradient needs z")
-        d.ld_preact = _rows(z, "z", shape, x)
-    with _on(stream):
-        dx = torch.empty((d.n_rows, d.n_in), dtype=x.dtype, device=x.device) if need_dx else None
-        dw = torch.empty_like(w) if need_dw else None
-        db = torch.empty((*w.shape[:-2], d.n_out), dtype=x.dtype, device=x.device) if bias else None
-        nbytes = B.mace_linear_backward_workspace_bytes(d, bias, need_dw)
-        if nbytes == 0:   # sizes the library does not take: the call itself says which way
-            nbytes = 1
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
-        B.mace_linear_backward(d, dy, ld_dy, x, w, z, offsets, dx, d.n_in, dw, db, ws, nbytes, stream)
+    d = _linear_desc(x, w, offsets, act)
+    n, m = d.n_rows, d.n_out
+    ld_dy = _rows(dy, n, m, x, "dy")
+    if d.act:
+        if z is None:
+            raise ValueError("an activation's gradient needs z")
+        d.ld_preact = _rows(z, n, m, x, "z")
+    else:
+        z = None
+    dx = x.new_empty((n, d.n_in)) if need_dx else None
+    dw = torch.empty_like(w) if need_dw else None
+    db = x.new_empty((*w.shape[:-2], m)) if bias else None
+    lib = B.lib()
+    # (0 for sizes the library does not take: the call itself says which error)
+    nbytes = lib.mace_linear_backward_workspace_bytes(d, bias, need_dw) or 1
+    ws = x.new_empty(nbytes, dtype=torch.uint8)
+    B._check(lib.mace_linear_backward(d, dy.data_ptr(), ld_dy, x.data_ptr(), w.data_ptr(),
+                                      None if z is None else z.data_ptr(),
+                                      None if offsets is None else offsets.data_ptr(),
+                                      None if dx is None else dx.data_ptr(), d.n_in,
+                                      None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr(),
+                                      ws.data_ptr(), nbytes, _current_stream(x)), "mace_linear_backward")
     return dx, dw, db
 
 
@@ -117,68 +151,82 @@ class Route(NamedTuple):
     offsets: torch.Tensor       # int32 [n_experts + 1]
 
 
-def route(expert, n_experts: int, *, stream=None) -> Route:
+@_streamed
+def route(expert, n_experts: int) -> Route:
     """The stable sort of the slots of expert (int32 [tokens, top_k]) by expert;
     slots with an index outside 0..n_experts-1 are dropped, behind the others."""
-    _need(expert.dim() == 2 and expert.is_cuda, "expert must be a [tokens, top_k] GPU tensor")
-    _whole(expert, "expert", expert.shape, torch.int32, expert.device)
+    if expert.dim() != 2 or not expert.is_cuda or expert.dtype != torch.int32 or not expert.is_contiguous():
+        raise ValueError("expert must be a contiguous int32 [tokens, top_k] GPU tensor")
     n, k = expert.shape
     d = B.mace_route_desc(n, k, n_experts, 1, B.MACE_TYPE_FP32, 1, 1)
-    with _on(stream):
-        # one allocation: the orders, the offsets
-        buf = torch.empty(2 * n * k + n_experts + 1, dtype=torch.int32, device=expert.device)
-        r = Route(buf[:n * k].view(n, k), buf[n * k:2 * n * k], buf[2 * n * k:])
-        nbytes = B.mace_route_workspace_bytes(d) if n * k > 4096 else 0
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=expert.device) if nbytes else None
-        B.mace_route_build(d, expert, r.row_of_slot, r.slot_of_row, r.offsets, ws, nbytes, stream)
-    return r
+    lib = B.lib()
+    s = n * k
+    buf = expert.new_empty(2 * s + max(n_experts, 0) + 1)   # one allocation
+    rows, slots, offsets = buf[:s].view(n, k), buf[s:2 * s], buf[2 * s:]
+    nbytes = lib.mace_route_workspace_bytes(d) if s > 4096 else 0
+    ws = expert.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
+    at = buf.data_ptr()
+    B._check(lib.mace_route_build(d, expert.data_ptr(), at, at + 4 * s, at + 8 * s,
+                                  None if ws is None else ws.data_ptr(), nbytes, _current_stream(expert)),
+             "mace_route_build")
+    return Route(rows, slots, offsets)
 
 
-def _route_desc(plan: Route, t, name: str, rows: bool):
-    _need(t.dim() == 2 and t.is_cuda and t.dtype in DTYPES, f"{name} must be a 2-d GPU tensor of a supported dtype")
-    n, k = plan.row_of_slot.shape
-    ld = _rows(t, name, (n * k if rows else n, t.shape[1]), t)
-    width = t.shape[1]
-    return B.mace_route_desc(n, k, plan.offsets.shape[0] - 1, width, DTYPES[t.dtype], width if rows else ld,
-                             ld if rows else width)
-
-
-def _weights(weights, plan: Route):
+def _check_weights(weights, plan: Route, like):
     if weights is not None:
-        _whole(weights, "weights", plan.row_of_slot.shape, torch.float32, plan.row_of_slot.device)
+        _whole(weights, plan.row_of_slot.shape, torch.float32, like, "weights")
 
 
-def route_rows(x, plan: Route, *, stream=None):
+@_streamed
+def route_rows(x, plan: Route):
     """[tokens * top_k, width] rows in expert order; zeros for dropped slots."""
-    d = _route_desc(plan, x, "x", False)
-    with _on(stream):
-        rows = torch.empty((plan.slot_of_row.shape[0], d.width), dtype=x.dtype, device=x.device)
-        B.mace_route_gather(d, x, plan.row_of_slot, plan.offsets, rows, stream)
+    dtype = _gpu_matrix(x, "x")
+    n, k = plan.row_of_slot.shape
+    width = x.shape[1]
+    ld = _rows(x, n, width, x, "x")
+    d = B.mace_route_desc(n, k, plan.offsets.shape[0] - 1, width, dtype, ld, width)
+    rows = x.new_empty((n * k, width))
+    B._check(B.lib().mace_route_gather(d, x.data_ptr(), plan.row_of_slot.data_ptr(), plan.offsets.data_ptr(),
+                                       rows.data_ptr(), _current_stream(x)), "mace_route_gather")
     return rows
 
 
-def combine_rows(rows, plan: Route, weights=None, *, stream=None):
+@_streamed
+def combine_rows(rows, plan: Route, weights=None):
     """[tokens, width]: each token's kept rows times their weights (float32
     [tokens, top_k], None: ones), summed."""
-    d = _route_desc(plan, rows, "rows", True)
-    _weights(weights, plan)
-    with _on(stream):
-        out = torch.empty((d.n_tokens, d.width), dtype=rows.dtype, device=rows.device)
-        B.mace_route_combine(d, rows, weights, plan.row_of_slot, plan.offsets, out, stream)
+    dtype = _gpu_matrix(rows, "rows")
+    n, k = plan.row_of_slot.shape
+    width = rows.shape[1]
+    ld = _rows(rows, n * k, width, rows, "rows")
+    _check_weights(weights, plan, rows)
+    d = B.mace_route_desc(n, k, plan.offsets.shape[0] - 1, width, dtype, width, ld)
+    out = rows.new_empty((n, width))
+    B._check(B.lib().mace_route_combine(d, rows.data_ptr(), None if weights is None else weights.data_ptr(),
+                                        plan.row_of_slot.data_ptr(), plan.offsets.data_ptr(), out.data_ptr(),
+                                        _current_stream(rows)), "mace_route_combine")
     return out
 
 
-def combine_rows_backward(dout, rows, plan: Route, weights=None, *, stream=None):
+@_streamed
+def combine_rows_backward(dout, rows, plan: Route, weights=None):
     """(drows, dweights) of `combine_rows`; dweights is None without weights."""
-    d = _route_desc(plan, dout, "dout", False)
-    _weights(weights, plan)
-    d.ld_rows = _rows(rows, "rows", (d.n_tokens * d.top_k, d.width), dout)
-    with _on(stream):
-        # rows and their gradient share a leading dimension
-        buf = torch.empty((d.n_tokens * d.top_k, d.ld_rows), dtype=dout.dtype, device=dout.device)
-        drows = buf if d.ld_rows == d.width else buf[:, :d.width]
-        dw = None if weights is None else torch.empty_like(weights)
-        B.mace_route_combine_backward(d, dout, rows, weights, plan.row_of_slot, plan.offsets, drows, dw, stream)
+    dtype = _gpu_matrix(dout, "dout")
+    n, k = plan.row_of_slot.shape
+    width = dout.shape[1]
+    ld = _rows(dout, n, width, dout, "dout")
+    ld_rows = _rows(rows, n * k, width, dout, "rows")
+    _check_weights(weights, plan, dout)
+    d = B.mace_route_desc(n, k, plan.offsets.shape[0] - 1, width, dtype, ld, ld_rows)
+    drows = dout.new_empty((n * k, ld_rows))   # rows and their gradient share a leading dimension
+    if ld_rows != width:
+        drows = drows[:, :width]
+    dw = None if weights is None else torch.empty_like(weights)
+    B._check(B.lib().mace_route_combine_backward(d, dout.data_ptr(), rows.data_ptr(),
+                                                 None if weights is None else weights.data_ptr(),
+                                                 plan.row_of_slot.data_ptr(), plan.offsets.data_ptr(), drows.data_ptr(),
+                                                 None if dw is None else dw.data_ptr(), _current_stream(dout)),
+             "mace_route_combine_backward")
     return drows, dw
 
 
@@ -187,21 +235,30 @@ def route_rows_backward(drows, plan: Route, *, stream=None):
     return combine_rows(drows, plan, None, stream=stream)
 
 
-def orthogonalise(g, coefficients=NEWTON_SCHULZ, *, eps: float = 1e-7, stream=None):
+@lru_cache(maxsize=64)
+def _coefficients(steps: tuple) -> np.ndarray:
+    return np.ascontiguousarray(steps, dtype=np.float64).reshape(-1, 3)
+
+
+@_streamed
+def orthogonalise(g, coefficients=NEWTON_SCHULZ, *, eps: float = 1e-7):
     """Newton-Schulz steps (a, b, c) on g / (|g|_F + eps), x <- a x + (b A + c A A) x
     with A = x x^T: [rows, cols] or a batch [batch, rows, cols], columns adjacent."""
-    _need(g.dim() in (2, 3) and g.is_cuda and g.dtype in DTYPES,
-          "g must be a [(batch,) rows, cols] GPU tensor of a supported dtype")
-    coef = np.ascontiguousarray(coefficients, dtype=np.float64).reshape(-1, 3)
-    m = g if g.dim() == 3 else g[None]
-    b, rows, cols = m.shape
-    if m.numel() and not ((cols == 1 or m.stride(2) == 1) and (rows == 1 or m.stride(1) >= cols) and m.stride(0) >= 0):
+    dtype = DTYPES.get(g.dtype)
+    if dtype is None or g.dim() not in (2, 3) or not g.is_cuda:
+        raise ValueError("g must be a [(batch,) rows, cols] GPU tensor of float32, bfloat16 or float16")
+    coef = _coefficients(tuple(tuple(float(v) for v in c) for c in coefficients))
+    if g.dim() == 3:
+        (b, rows, cols), (sb, s0, s1) = g.shape, g.stride()
+    else:
+        (rows, cols), (s0, s1), b, sb = g.shape, g.stride(), 1, 0
+    if (s1 != 1 and cols > 1 or s0 < cols and rows > 1 or sb < 0) and g.numel():
         raise ValueError("g's columns must be adjacent and its rows apart")
-    d = B.mace_orthogonalise_desc(b, rows, cols, DTYPES[g.dtype], len(coef), m.stride(1) if rows > 1 else cols,
-                                  m.stride(0), cols, rows * cols, eps)
-    with _on(stream):
-        out = torch.empty(g.shape, dtype=g.dtype, device=g.device)
-        nbytes = B.mace_orthogonalise_workspace_bytes(d) or 1
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=g.device)
-        B.mace_orthogonalise(d, m, coef, out, ws, nbytes, stream)
+    d = B.mace_orthogonalise_desc(b, rows, cols, dtype, len(coef), s0 if rows > 1 else cols, sb, cols, rows * cols, eps)
+    out = g.new_empty(g.shape)
+    lib = B.lib()
+    nbytes = lib.mace_orthogonalise_workspace_bytes(d) or 1
+    ws = g.new_empty(nbytes, dtype=torch.uint8)
+    B._check(lib.mace_orthogonalise(d, g.data_ptr(), coef.ctypes.data, out.data_ptr(), ws.data_ptr(), nbytes,
+                                    _current_stream(g)), "mace_orthogonalise")
     return out
