@@ -224,6 +224,54 @@ struct TileSource {
   }
 };
 
+__device__ __forceinline__ uint64_t uniform64(uint64_t v) {
+  return ((uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32) |
+         (unsigned)__builtin_amdgcn_readfirstlane((int)v);
+}
+
+// The same tile copied from memory to LDS without passing through registers
+// (16-bit elements, 16-byte aligned rows of whole vectors): a wave's 64 lanes
+// fill 1024 consecutive bytes, so each lane reads the chunk that the tile's
+// layout wants at its place. Whole steps of BK only; the rest of a row
+// goes through TileSource, which fills with zeros.
+template <class T, int ROWS, int BK, bool KC, int NT>
+struct DirectSource {
+  static constexpr int NV = ROWS * BK / 8 / NT;
+  static_assert(ROWS * BK / 8 % NT == 0 && BK == 64 && sizeof(T) == 2, "whole vectors per thread");
+  unsigned off[NV];   // bytes from the step's first element (the caller sees to it that they fit)
+  uint64_t base, step;
+  __device__ __forceinline__ void init(const T* base_, int64_t ld, int rows, int tid) {
+    base = uniform64(reinterpret_cast<uint64_t>(base_));
+    step = uniform64(2 * (KC ? (uint64_t)BK : BK * ld));
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      const int f = tid + NT * u;
+      if constexpr (KC) {
+        const int r = f / (BK / 8), c = f % (BK / 8) ^ (r & 7);
+        off[u] = 2 * (unsigned)(min(r, rows - 1) * ld + 8 * c);
+      } else {
+        const int k = f / (ROWS / 8), c = f % (ROWS / 8) ^ ((k & 3) << 1);
+        off[u] = 2 * (unsigned)(k * ld + min(8 * c, rows - 8));
+      }
+    }
+  }
+  // Written as asm: the compiler would wait for these copies before any later LDS
+  // read, having no way to know that it reads the other buffer. They have no
+  // register outputs; tile_gemm_direct waits for them (vmcnt) itself. The s_nop is
+  // the wait state between writing M0 and an LDS copy.
+  __device__ __forceinline__ void issue(const unsigned short* t, int tid) {
+    typedef __attribute__((address_space(3))) const unsigned short las;
+    const unsigned at = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(las*)t + (tid & ~63) * 16);
+#pragma unroll
+    for (int u = 0; u < NV; ++u)
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                   :
+                   : "s"(at + NT * u * 16), "v"(off[u]), "s"(base)
+                   : "memory", "m0");
+    base += step;
+  }
+};
+
 // The same for pairs of binary16 in two planes, 16-byte aligned rows of whole vectors.
 template <int ROWS, int BK, bool KC, int NT>
 struct TileSource<HalfPair, ROWS, BK, KC, true, NT> {
@@ -257,8 +305,9 @@ struct TileSource<HalfPair, ROWS, BK, KC, true, NT> {
 // through STAGES LDS buffers. acc[j][i], register r of lane l is the result at
 // column 16 j + 4 (l/16) + r and row 16 i + l%16 of the wave's part: four
 // consecutive columns of one row per lane.
-template <int BM_, int BN_, int WM_, int WN_, int BK_, int STAGES_>
+template <int BM_, int BN_, int WM_, int WN_, int BK_, int STAGES_, bool DIRECT_ = false>
 struct TileShape {
+  static constexpr bool DIRECT = DIRECT_;   // operands straight to LDS where they are aligned
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, BK = BK_, STAGES = STAGES_;
   static constexpr int NT = 64 * WM * WN;
   static constexpr int TM = BM / WM / 16, TN = BN / WN / 16;   // 16 x 16 tiles per wave
@@ -353,7 +402,8 @@ __device__ __forceinline__ void tile_gemm(TileSource<T, S::BM, S::BK, KCR, AL, S
 }
 
 // This lane's four columns of the results of tile_gemm: f(row, column, values, count)
-template <class S, class F>
+// (AL: columns come in whole vectors)
+template <class S, bool AL, class F>
 __device__ __forceinline__ void for_results(const f4 (&acc)[S::TN][S::TM], int rows, int cols, int tid, F f) {
   const int l = tid & 63, w = tid >> 6;
   const int m0 = (w / S::WN) * (S::BM / S::WM) + (l & 15), n0 = (w % S::WN) * (S::BN / S::WN) + 4 * (l >> 4);
@@ -364,8 +414,59 @@ __device__ __forceinline__ void for_results(const f4 (&acc)[S::TN][S::TM], int r
 #pragma unroll
     for (int j = 0; j < S::TN; ++j) {
       const int n = n0 + 16 * j;
-      if (n < cols) f(m, n, acc[j][i], min(4, cols - n));
+      if (n < cols) f(m, n, acc[j][i], AL ? 4 : min(4, cols - n));
     }
+  }
+}
+
+// tile_gemm with both operands copied straight to LDS: two buffers, the next
+// step's copies in flight during this step's products.
+template <class T, class S, bool KCR, bool KCC>
+__device__ __forceinline__ void tile_gemm_direct(const T* rb, int64_t rld, int rows, const T* cb, int64_t cld, int cols,
+                                                 int K, unsigned short* lds, int tid, f4 (&acc)[S::TN][S::TM]) {
+  constexpr int BUF = (S::BM + S::BN) * S::BK, CO = S::BM * S::BK;
+  const int lane = tid & 63, w = tid >> 6;
+  const int m0 = (w / S::WN) * (S::BM / S::WM), n0 = (w % S::WN) * (S::BN / S::WN);
+#pragma unroll
+  for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i) acc[j][i] = f4{0.f, 0.f, 0.f, 0.f};
+  if (K <= 0) return;
+  const int whole = K / S::BK;
+  DirectSource<T, S::BM, S::BK, KCR, S::NT> r;
+  DirectSource<T, S::BN, S::BK, KCC, S::NT> c;
+  r.init(rb, rld, rows, tid);
+  c.init(cb, cld, cols, tid);
+  if (whole) {
+    r.issue(lds, tid);
+    c.issue(lds + CO, tid);
+    for (int i = 0; i < whole; ++i) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();   // this step's tile is in LDS, the other buffer has been read
+      if (i + 1 < whole) {
+        r.issue(lds + (~i & 1) * BUF, tid);
+        c.issue(lds + (~i & 1) * BUF + CO, tid);
+      }
+      tile_products<T, S, KCR, KCC, 1>(lds + (i & 1) * BUF, lds + (i & 1) * BUF + CO, m0, n0, lane, acc);
+    }
+  }
+  if (K % S::BK) {
+    const int64_t k = (int64_t)whole * S::BK;
+    unsigned short* t = lds + (whole & 1) * BUF;   // (read two steps ago, with a barrier since)
+    {
+      TileSource<T, S::BM, S::BK, KCR, true, S::NT> v;
+      v.init(rb + (KCR ? k : k * rld), rld, rows, tid);
+      v.load(K - (int)k, tid);
+      v.store(t, tid);
+    }
+    {
+      TileSource<T, S::BN, S::BK, KCC, true, S::NT> v;
+      v.init(cb + (KCC ? k : k * cld), cld, cols, tid);
+      v.load(K - (int)k, tid);
+      v.store(t + CO, tid);
+    }
+    __syncthreads();
+    tile_products<T, S, KCR, KCC, 1>(t, t + CO, m0, n0, lane, acc);
   }
 }
 

@@ -9,10 +9,32 @@
 namespace mace {
 namespace {
 
+template <int I> struct Int { static constexpr int value = I; };
+
 // ------------------------------------------------------------------ activations
-__device__ __forceinline__ float activate(float z, int act) {
-  if (act == MACE_ACT_SILU) return silu(z);
-  if (act == MACE_ACT_GELU) return 0.5f * z * erfcf(-0.70710678118654752f * z);   // z Phi(z)
+// Normal distribution: Phi(z), and exp(-z^2 / 2). erfc(x) = t q(t) exp(-x^2), t =
+// 1 / (1 + 0.36 x), with q a degree-9 polynomial fitted to a relative error of
+// 1.6e-7 (evaluated in FP32) over x >= 0: no cancellation in either tail.
+__device__ __forceinline__ float normal_cdf(float z, float& e) {
+  const float x = fminf(fabsf(z), 30.f);
+  const float t = recip_ge1(__builtin_fmaf(x, 0.36f * 0.70710678118654752f, 1.f));
+  e = exp_neg(0.5f * x * x);
+  constexpr float q[10] = {0.20310825109481812f, 0.20310771465301514f, 0.1899440586566925f,  0.16391651332378387f,
+                           0.12292544543743134f, 0.10651545226573944f, -0.02863478660583496f, 0.14342354238033295f,
+                           -0.14196832478046417f, 0.03766215592622757f};
+  float p = q[9];
+#pragma unroll
+  for (int i = 8; i >= 0; --i) p = __builtin_fmaf(p, t, q[i]);
+  const float h = 0.5f * t * p * e;   // Phi(-|z|)
+  return z > 0.f ? 1.f - h : h;
+}
+template <int ACT>
+__device__ __forceinline__ float activate(float z) {
+  if constexpr (ACT == MACE_ACT_SILU) return silu(z);
+  if constexpr (ACT == MACE_ACT_GELU) {
+    float e;
+    return z * normal_cdf(z, e);
+  }
   return z;
 }
 // act'(z); beyond |z| = 88 the slopes are 0 and 1 to FP32, and z (1 - s) would
@@ -20,7 +42,9 @@ __device__ __forceinline__ float activate(float z, int act) {
 __device__ __forceinline__ float activation_slope(float z, int act) {
   z = z > 88.f ? 88.f : (z < -88.f ? -88.f : z);   // (keeps NaN)
   if (act == MACE_ACT_SILU) return silu_grad(z);
-  return 0.5f * erfcf(-0.70710678118654752f * z) + 0.39894228040143268f * z * exp_neg(0.5f * z * z);
+  float e;
+  const float c = normal_cdf(z, e);
+  return __builtin_fmaf(0.39894228040143268f * z, e, c);
 }
 
 // ------------------------------------------------------------------ arguments
@@ -58,6 +82,21 @@ struct BiasGradArgs {
   int n_out, run_rows, max_runs;
 };
 
+// The block's product, by the way its shape and operands allow
+template <class T, class S, bool KCR, bool KCC, bool AL>
+__device__ __forceinline__ void product(const T* rb, int64_t rld, int rows, const T* cb, int64_t cld, int cols, int K,
+                                        unsigned short* lds, int tid, f4 (&acc)[S::TN][S::TM]) {
+  if constexpr (AL && S::DIRECT) {
+    tile_gemm_direct<T, S, KCR, KCC>(rb, rld, rows, cb, cld, cols, K, lds, tid, acc);
+  } else {
+    TileSource<T, S::BM, S::BK, KCR, AL, S::NT> r;
+    TileSource<T, S::BN, S::BK, KCC, AL, S::NT> c;
+    r.init(rb, rld, rows, tid);
+    c.init(cb, cld, cols, tid);
+    tile_gemm<T, S, KCR, KCC, AL>(r, c, K, lds, tid, acc);
+  }
+}
+
 // rows behind the last group: zeros
 template <class T>
 __device__ __forceinline__ void zero_rows(T* y, int64_t ld, int rows, int cols, int tid, int nt) {
@@ -80,24 +119,25 @@ __global__ void __launch_bounds__(S::NT) linear_fwd_kernel(LinearArgs<T> a) {
     if (z) zero_rows(z, a.ldz, run.rows, cols, tid, S::NT);
     return;
   }
-  TileSource<T, S::BM, S::BK, true, AL, S::NT> xr;
-  TileSource<T, S::BN, S::BK, false, AL, S::NT> wc;
-  xr.init(a.x + run.row0 * a.ldx, a.ldx, run.rows, tid);
-  wc.init(a.w + (int64_t)run.group * a.n_in * a.n_out + c0, a.n_out, a.n_out - c0, tid);
   f4 acc[S::TN][S::TM];
-  tile_gemm<T, S, true, false, AL>(xr, wc, a.n_in, lds, tid, acc);
+  product<T, S, true, false, AL>(a.x + run.row0 * a.ldx, a.ldx, run.rows, a.w + (int64_t)run.group * a.n_in * a.n_out + c0,
+                                 a.n_out, a.n_out - c0, a.n_in, lds, tid, acc);
   const T* bias = a.bias ? a.bias + (int64_t)run.group * a.n_out + c0 : nullptr;
   const T* res = a.residual ? a.residual + run.row0 * a.ldr + c0 : nullptr;
-  for_results<S>(acc, run.rows, cols, tid, [&](int m, int n, f4 v, int k) {
-    const bool vec = AL && k == 4;
-    if (bias) v += read4(bias + n, k, vec);
-    if (z) store4(z + m * a.ldz + n, v, k, vec);
-    if (a.act != MACE_ACT_NONE)
+  auto finish = [&](auto act) {
+    for_results<S, AL>(acc, run.rows, cols, tid, [&](int m, int n, f4 v, int k) {
+      const bool vec = AL;
+      if (bias) v += read4(bias + n, k, vec);
+      if (z) store4(z + m * a.ldz + n, v, k, vec);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = activate(v[i], a.act);
-    if (res) v += read4(res + m * a.ldr + n, k, vec);
-    store4(y + m * a.ldy + n, v, k, vec);
-  });
+      for (int i = 0; i < 4; ++i) v[i] = activate<decltype(act)::value>(v[i]);
+      if (res) v += read4(res + m * a.ldr + n, k, vec);
+      store4(y + m * a.ldy + n, v, k, vec);
+    });
+  };
+  if (a.act == MACE_ACT_SILU) finish(Int<MACE_ACT_SILU>{});
+  else if (a.act == MACE_ACT_GELU) finish(Int<MACE_ACT_GELU>{});
+  else finish(Int<MACE_ACT_NONE>{});
 }
 
 // dx = dz W_g^T: tile `id`
@@ -112,14 +152,11 @@ __device__ __forceinline__ void row_grad_tile(const RowGradArgs<T>& a, int id, u
     zero_rows(dx, a.lddx, run.rows, cols, tid, S::NT);
     return;
   }
-  TileSource<T, S::BM, S::BK, true, AL, S::NT> zr;
-  TileSource<T, S::BN, S::BK, true, AL, S::NT> wc;
-  zr.init(a.dz + run.row0 * a.lddz, a.lddz, run.rows, tid);
-  wc.init(a.w + ((int64_t)run.group * a.n_in + c0) * a.n_out, a.n_out, cols, tid);
   f4 acc[S::TN][S::TM];
-  tile_gemm<T, S, true, true, AL>(zr, wc, a.n_out, lds, tid, acc);
-  for_results<S>(acc, run.rows, cols, tid,
-                 [&](int m, int n, f4 v, int k) { store4(dx + m * a.lddx + n, v, k, AL && k == 4); });
+  product<T, S, true, true, AL>(a.dz + run.row0 * a.lddz, a.lddz, run.rows,
+                                a.w + ((int64_t)run.group * a.n_in + c0) * a.n_out, a.n_out, cols, a.n_out, lds, tid, acc);
+  for_results<S, AL>(acc, run.rows, cols, tid,
+                 [&](int m, int n, f4 v, int k) { store4(dx + m * a.lddx + n, v, k, AL); });
 }
 
 // dW_g = x_g^T dz_g, the group's rows cut into `splits` parts: tile `id`
@@ -139,21 +176,18 @@ __device__ __forceinline__ void weight_grad_tile(const WeightGradArgs<T>& a, int
   }
   const int64_t per = ((r1 - r0 + a.splits - 1) / a.splits + S::BK - 1) / S::BK * S::BK;
   const int64_t k0 = min(r1, r0 + split * per), k1 = min(r1, k0 + per);
-  TileSource<T, S::BM, S::BK, false, AL, S::NT> xr;
-  TileSource<T, S::BN, S::BK, false, AL, S::NT> zc;
-  xr.init(a.x + k0 * a.ldx + m0, a.ldx, a.n_in - m0, tid);
-  zc.init(a.dz + k0 * a.lddz + c0, a.lddz, a.n_out - c0, tid);
   f4 acc[S::TN][S::TM];
-  tile_gemm<T, S, false, false, AL>(xr, zc, (int)(k1 - k0), lds, tid, acc);
+  product<T, S, false, false, AL>(a.x + k0 * a.ldx + m0, a.ldx, a.n_in - m0, a.dz + k0 * a.lddz + c0, a.lddz,
+                                  a.n_out - c0, (int)(k1 - k0), lds, tid, acc);
   const int64_t at = ((int64_t)g * a.n_in + m0) * a.n_out + c0;
   if (a.part) {
     float* o = a.part + (int64_t)split * a.groups * a.n_in * a.n_out + at;
-    for_results<S>(acc, rows, cols, tid,
-                   [&](int m, int n, f4 v, int k) { store4(o + (int64_t)m * a.n_out + n, v, k, AL && k == 4); });
+    for_results<S, AL>(acc, rows, cols, tid,
+                   [&](int m, int n, f4 v, int k) { store4(o + (int64_t)m * a.n_out + n, v, k, AL); });
   } else {
     T* o = a.dw + at;
-    for_results<S>(acc, rows, cols, tid,
-                   [&](int m, int n, f4 v, int k) { store4(o + (int64_t)m * a.n_out + n, v, k, AL && k == 4); });
+    for_results<S, AL>(acc, rows, cols, tid,
+                   [&](int m, int n, f4 v, int k) { store4(o + (int64_t)m * a.n_out + n, v, k, AL); });
   }
 }
 
@@ -162,7 +196,7 @@ __device__ __forceinline__ void weight_grad_tile(const WeightGradArgs<T>& a, int
 template <class T>
 __device__ __forceinline__ void bias_grad(const BiasGradArgs<T>& a, int id, float* lds, int tid) {
   const int blocks = (a.n_out + 63) / 64, g = id / blocks;
-  const int c = tid & 63, y = tid >> 6, col = id % blocks * 64 + c;
+  const int c = tid & 63, y = tid >> 6, col = id % blocks * 64 + c;   // (waves past the fourth only keep the barrier)
   int first = 0, runs = 0;
   if (!a.offsets) {
     runs = (int)((a.n + a.run_rows - 1) / a.run_rows);
@@ -184,25 +218,25 @@ __device__ __forceinline__ void bias_grad(const BiasGradArgs<T>& a, int id, floa
   }
   runs = min(runs, a.max_runs - first);   // (offsets that do not rise could count more runs than there are sums)
   float s = 0.f;
-  if (col < a.n_out)
+  if (col < a.n_out && y < 4)
     for (int r = y; r < runs; r += 4) s += a.sums[(int64_t)(first + r) * a.n_out + col];
-  lds[y * 64 + c] = s;
+  if (y < 4) lds[y * 64 + c] = s;
   __syncthreads();
   if (y == 0 && col < a.n_out) a.db[(int64_t)g * a.n_out + col] = (T)(s + lds[64 + c] + lds[128 + c] + lds[192 + c]);
 }
 
 // All three gradients in one launch: blocks below row_blocks form dx, the next
 // weight_blocks dW, the rest db.
-template <class T, bool ALX, bool ALW, class S>
+template <class T, bool AL, class S>
 __global__ void __launch_bounds__(S::NT)
 linear_grad_kernel(RowGradArgs<T> a, WeightGradArgs<T> b, BiasGradArgs<T> c, int row_blocks, int weight_blocks) {
   __shared__ __align__(16) unsigned short lds[tile_lds<T, S>];
   const int tid = threadIdx.x;
   int id = blockIdx.x;
   if (id < row_blocks) {
-    row_grad_tile<T, ALX, S>(a, xcd_order(id, row_blocks), lds, tid);
+    row_grad_tile<T, AL, S>(a, xcd_order(id, row_blocks), lds, tid);
   } else if ((id -= row_blocks) < weight_blocks) {
-    weight_grad_tile<T, ALW, S>(b, xcd_order(id, weight_blocks), lds, tid);
+    weight_grad_tile<T, AL, S>(b, xcd_order(id, weight_blocks), lds, tid);
   } else {
     bias_grad<T>(c, id - weight_blocks, reinterpret_cast<float*>(lds), tid);
   }
@@ -274,6 +308,7 @@ constexpr int kMaxLinearGroups = 1024;
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+bool near(int64_t ld) { return ld <= 1 << 20; }   // a tile's rows lie within 32-bit byte offsets
 size_t size_of(int dtype) { return dtype == MACE_TYPE_FP32 ? 4 : 2; }
 size_t round256(size_t b) { return (b + 255) & ~size_t(255); }
 
@@ -291,29 +326,59 @@ mace_status check(const mace_linear_desc* d) {
 int slope_run(int64_t n) { return (int)(std::max<int64_t>(1, ceil_div(n, 64 * 512)) * 64); }
 int64_t slope_runs(const mace_linear_desc& d) { return ceil_div(d.n_rows, slope_run(d.n_rows)) + d.n_groups; }
 
-// parts each group's rows are cut into for dW: enough blocks to fill the chip, at least 512 rows each
-int weight_splits(const mace_linear_desc& d, int bm, int bn) {
-  const int64_t tiles = ceil_div(d.n_in, bm) * ceil_div(d.n_out, bn) * d.n_groups;
-  const int64_t want = 512 / std::max<int64_t>(1, tiles), most = d.n_rows / d.n_groups / 512;
-  return (int)std::max<int64_t>(1, std::min({want, most, (int64_t)64}));
+constexpr int64_t kFillBlocks = 256, kLargeBlocks = 192;   // (256 CUs)
+
+// Large: launches of at least kLargeBlocks of its tiles; Mid: from kFillBlocks of its own
+template <class T, bool AL> struct Shapes {
+  using Large = TileShape<128, 128, 2, 2, 64, 2>;
+  using Mid = TileShape<128, 128, 2, 2, 64, 2>;
+  using Small = TileShape<64, 64, 2, 2, 64, 2>;
+};
+template <> struct Shapes<__bf16, true> {
+  using Large = TileShape<256, 256, 2, 4, 64, 2, true>;
+  using Mid = TileShape<128, 128, 2, 2, 64, 2, true>;
+  using Small = TileShape<64, 64, 2, 2, 64, 2, true>;
+};
+template <> struct Shapes<_Float16, true> : Shapes<__bf16, true> {};
+template <bool AL> struct Shapes<float, AL> {
+  using Large = TileShape<128, 128, 2, 2, 32, 1>;
+  using Mid = TileShape<128, 128, 2, 2, 32, 1>;
+  using Small = TileShape<64, 64, 2, 2, 32, 1>;
+};
+enum { kSmall, kMid, kLarge };
+int shape_of(int64_t rows, int64_t cols, int64_t batch = 1) {
+  if (ceil_div(rows, 256) * ceil_div(cols, 256) * batch >= kLargeBlocks) return kLarge;
+  return ceil_div(rows, 128) * ceil_div(cols, 128) * batch >= kFillBlocks ? kMid : kSmall;
+}
+// f(shape) for the kind of tile; shapes that are the same type are instantiated once
+template <class T, bool AL, class F>
+mace_status with_shape(int kind, F f) {
+  if (kind == kLarge) return f(typename Shapes<T, AL>::Large{});
+  if (kind == kMid) return f(typename Shapes<T, AL>::Mid{});
+  return f(typename Shapes<T, AL>::Small{});
 }
 
-constexpr int64_t kFillBlocks = 256;   // blocks from which the larger tile is taken (one per CU)
-
 struct BackwardPlan {
+  int weight_kind;
   int splits;
   int64_t lddz;
   size_t dz, sums, part, total;   // byte offsets
 };
 
-bool small_weight_tiles(const mace_linear_desc& d) {
-  return ceil_div(d.n_in, 128) * ceil_div(d.n_out, 128) * d.n_groups * std::max<int64_t>(1, d.n_rows / d.n_groups / 512) < kFillBlocks;
+// kind of tile of dW's blocks, and the parts each group's rows are cut into:
+// enough blocks to fill the chip, at least 512 rows each
+int weight_shape(const mace_linear_desc& d, int& splits) {
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(64, d.n_rows / d.n_groups / 512));
+  const int kind = shape_of(d.n_in, d.n_out, d.n_groups * most);
+  const int b = kind == kLarge ? 256 : (kind == kMid ? 128 : 64);
+  const int64_t tiles = ceil_div(d.n_in, b) * ceil_div(d.n_out, b) * d.n_groups;
+  splits = (int)std::max<int64_t>(1, std::min(most, (kind == kLarge ? 256 : 512) / tiles));
+  return kind;
 }
 
 BackwardPlan plan_backward(const mace_linear_desc& d, bool bias, bool weights) {
   BackwardPlan p{};
-  const int b = small_weight_tiles(d) ? 64 : 128;
-  p.splits = weight_splits(d, b, b);
+  p.weight_kind = weight_shape(d, p.splits);
   p.lddz = (d.n_out + 7) / 8 * 8;
   size_t o = 0;
   p.dz = o;
@@ -326,15 +391,6 @@ BackwardPlan plan_backward(const mace_linear_desc& d, bool bias, bool weights) {
   return p;
 }
 
-template <class T> struct Shapes {
-  using Mid = TileShape<128, 128, 2, 2, 64, 2>;
-  using Small = TileShape<64, 64, 2, 2, 64, 2>;
-};
-template <> struct Shapes<float> {
-  using Mid = TileShape<128, 128, 2, 2, 32, 1>;
-  using Small = TileShape<64, 64, 2, 2, 32, 1>;
-};
-
 mace_status launched() { return hipGetLastError() == hipSuccess ? MACE_OK : MACE_EHIP; }
 
 template <class T>
@@ -343,18 +399,19 @@ mace_status forward(const mace_linear_desc& d, const void* x, const void* w, con
   LinearArgs<T> a{(const T*)x, (const T*)w, (const T*)bias, (const T*)residual, (T*)y, (T*)z, offsets, d.n_rows,
                   d.ld_x, d.ld_y, d.ld_residual, d.ld_preact, d.n_in, d.n_out, d.n_groups, d.act};
   const bool al = aligned16(x) && aligned16(w) && aligned16(bias) && aligned16(residual) && aligned16(y) &&
-                  aligned16(z) && ((d.n_in | d.n_out | d.ld_x | d.ld_y | d.ld_residual | d.ld_preact) & 7) == 0;
-  auto go = [&](auto shape) -> mace_status {
-    using S = decltype(shape);
-    const int64_t blocks = (ceil_div(d.n_rows, S::BM) + (offsets ? d.n_groups : 0)) * ceil_div(d.n_out, S::BN);
-    if (blocks > INT32_MAX) return MACE_EUNSUPPORTED;
-    if (al) linear_fwd_kernel<T, true, S><<<(unsigned)blocks, S::NT, 0, s>>>(a);
-    else linear_fwd_kernel<T, false, S><<<(unsigned)blocks, S::NT, 0, s>>>(a);
-    return launched();
+                  aligned16(z) && ((d.n_in | d.n_out | d.ld_x | d.ld_y | d.ld_residual | d.ld_preact) & 7) == 0 &&
+                  near(d.ld_x);
+  auto go = [&](auto al_) {
+    constexpr bool AL = decltype(al_)::value;
+    return with_shape<T, AL>(shape_of(d.n_rows, d.n_out), [&](auto shape) -> mace_status {
+      using S = decltype(shape);
+      const int64_t blocks = (ceil_div(d.n_rows, S::BM) + (offsets ? d.n_groups : 0)) * ceil_div(d.n_out, S::BN);
+      if (blocks > INT32_MAX) return MACE_EUNSUPPORTED;
+      linear_fwd_kernel<T, AL, S><<<(unsigned)blocks, S::NT, 0, s>>>(a);
+      return launched();
+    });
   };
-  using Mid = typename Shapes<T>::Mid;
-  if (ceil_div(d.n_rows, Mid::BM) * ceil_div(d.n_out, Mid::BN) >= kFillBlocks) return go(Mid{});
-  return go(typename Shapes<T>::Small{});
+  return al ? go(Int<1>{}) : go(Int<0>{});
 }
 
 template <class T>
@@ -384,39 +441,38 @@ mace_status backward(const mace_linear_desc& d, const void* dy, int64_t lddy, co
     else go(linear_slope_kernel<T, false>);
     if ((st = launched()) != MACE_OK) return st;
   }
-  const bool al_z = aligned16(dz) && ((d.n_in | d.n_out | lddz) & 7) == 0;
-  const bool al_x = al_z && aligned16(w) && aligned16(dx) && (lddx & 7) == 0;
-  const bool al_w = al_z && aligned16(x) && aligned16(dw) && (d.ld_x & 7) == 0;
+  const bool al = aligned16(dz) && aligned16(w) && aligned16(dx) && aligned16(x) && aligned16(dw) && near(lddz) &&
+                  near(d.ld_x) && ((d.n_in | d.n_out | lddz | lddx | (dw ? d.ld_x : 0)) & 7) == 0;
   const RowGradArgs<T> ra{dz, (const T*)w, (T*)dx, offsets, d.n_rows, lddz, lddx, d.n_in, d.n_out, d.n_groups};
   const WeightGradArgs<T> wa{(const T*)x, dz, (T*)dw, p.splits > 1 ? reinterpret_cast<float*>(ws + p.part) : nullptr,
                              offsets, d.n_rows, d.ld_x, lddz, d.n_in, d.n_out, d.n_groups, p.splits};
   const BiasGradArgs<T> ba{sums, (T*)db, offsets, d.n_rows, d.n_out, slope_run(d.n_rows), (int)slope_runs(d)};
-  auto go = [&](auto shape, bool rows, bool weights, bool bias) -> mace_status {
-    using S = decltype(shape);
-    static_assert(S::NT == 256, "bias_grad's lanes");
-    const int64_t rb = rows ? (ceil_div(d.n_rows, S::BM) + (offsets ? d.n_groups : 0)) * ceil_div(d.n_in, S::BN) : 0;
-    const int64_t wb = weights ? ceil_div(d.n_in, S::BM) * ceil_div(d.n_out, S::BN) * d.n_groups * p.splits : 0;
-    const int64_t blocks = rb + wb + (bias ? ceil_div(d.n_out, 64) * d.n_groups : 0);
-    if (blocks > INT32_MAX) return MACE_EUNSUPPORTED;
-    if (blocks == 0) return MACE_OK;
-    auto f = al_x && al_w ? linear_grad_kernel<T, true, true, S>
-                          : (al_x ? linear_grad_kernel<T, true, false, S>
-                                  : (al_w ? linear_grad_kernel<T, false, true, S> : linear_grad_kernel<T, false, false, S>));
-    f<<<(unsigned)blocks, S::NT, 0, s>>>(ra, wa, ba, (int)rb, (int)wb);
-    return launched();
+  // one launch for all three where dx and dW take the same kind of tile
+  auto go = [&](auto al_, int kind, bool rows, bool weights, bool bias) {
+    constexpr bool AL = decltype(al_)::value;
+    return with_shape<T, AL>(kind, [&](auto shape) -> mace_status {
+      using S = decltype(shape);
+      const int64_t rb = rows ? (ceil_div(d.n_rows, S::BM) + (offsets ? d.n_groups : 0)) * ceil_div(d.n_in, S::BN) : 0;
+      const int64_t wb = weights ? ceil_div(d.n_in, S::BM) * ceil_div(d.n_out, S::BN) * d.n_groups * p.splits : 0;
+      const int64_t blocks = rb + wb + (bias ? ceil_div(d.n_out, 64) * d.n_groups : 0);
+      if (blocks > INT32_MAX) return MACE_EUNSUPPORTED;
+      if (blocks == 0) return MACE_OK;
+      linear_grad_kernel<T, AL, S><<<(unsigned)blocks, S::NT, 0, s>>>(ra, wa, ba, (int)rb, (int)wb);
+      return launched();
+    });
   };
-  using Mid = typename Shapes<T>::Mid;
-  using Small = typename Shapes<T>::Small;
+  auto grads = [&](int kind, bool rows, bool weights, bool bias) {
+    return al ? go(Int<1>{}, kind, rows, weights, bias) : go(Int<0>{}, kind, rows, weights, bias);
+  };
   const bool want_x = dx && d.n_rows > 0;
-  const bool small_x = ceil_div(d.n_rows, Mid::BM) * ceil_div(d.n_in, Mid::BN) < kFillBlocks;
-  const bool small_w = small_weight_tiles(d);
-  const bool x_big = want_x && !small_x, w_big = dw && !small_w;
-  if (x_big || w_big) {
-    if ((st = go(Mid{}, x_big, w_big, db != nullptr)) != MACE_OK) return st;
-    if ((st = go(Small{}, want_x && small_x, dw && small_w, false)) != MACE_OK) return st;
+  const int kind_x = shape_of(d.n_rows, d.n_in);
+  if (!want_x || !dw || kind_x == p.weight_kind) {
+    st = grads(dw ? p.weight_kind : kind_x, want_x, dw != nullptr, db != nullptr);
   } else {
-    if ((st = go(Small{}, want_x, dw != nullptr, db != nullptr)) != MACE_OK) return st;
+    if ((st = grads(kind_x, true, false, db != nullptr)) != MACE_OK) return st;
+    st = grads(p.weight_kind, false, true, false);
   }
+  if (st != MACE_OK) return st;
   if (dw && p.splits > 1) {
     const int64_t size = (int64_t)d.n_groups * d.n_in * d.n_out;
     linear_join_kernel<T><<<(unsigned)ceil_div(size, 1024), 256, 0, s>>>(wa.part, p.splits, size, (T*)dw);

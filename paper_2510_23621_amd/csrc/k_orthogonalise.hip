@@ -43,7 +43,7 @@ __device__ __forceinline__ void split_pair(f4 v, h4& hi, h4& lo) {
 }
 
 // ------------------------------------------------------------------ norm and packing
-constexpr int kNormBlocks = 64;   // most partial sums per matrix
+constexpr int kNormBlocks = 256;   // most partial sums per matrix
 
 template <class T>
 __global__ void __launch_bounds__(256) ns_norm_kernel(const T* __restrict__ g, int64_t stride, int64_t ld, int rows,
@@ -62,9 +62,11 @@ __global__ void __launch_bounds__(256) ns_norm_kernel(const T* __restrict__ g, i
   if (threadIdx.x == 0) part[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = red[0] + red[1] + red[2] + red[3];
 }
 
+// 1 / (|g| + eps) from the partial sums, by every wave alike
 __device__ __forceinline__ double ns_scale(const double* part, int n, double eps) {
   double s = 0.0;
-  for (int i = 0; i < n; ++i) s += part[i];
+  for (int i = threadIdx.x & 63; i < n; i += 64) s += part[i];
+  for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
   return 1.0 / (sqrt(s) + eps);
 }
 
@@ -114,8 +116,8 @@ __global__ void __launch_bounds__(256)
 ns_scale_kernel(const T* __restrict__ g, int64_t stride, int64_t ld, int rows, int cols, const double* __restrict__ part,
                 int parts, double eps, T* __restrict__ out, int64_t ostride, int64_t old) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= (int64_t)rows * cols) return;
   const double inv = ns_scale(part + (int64_t)blockIdx.y * parts, parts, eps);
+  if (i >= (int64_t)rows * cols) return;
   const int64_t r = i / cols, c = i % cols;
   out[blockIdx.y * ostride + r * old + c] = (T)(float)(to_f32(g[blockIdx.y * stride + r * ld + c]) * inv);
 }
@@ -450,7 +452,7 @@ __global__ void __launch_bounds__(S::NT) ns_symmetric_kernel(PairMat src, PairMa
   tile_gemm<T, S, true, true, true>(rs, cs, K, lds, tid, acc);
   _Float16* o = out.p + b * out.stride;
   const _Float16* a = src.p + b * src.stride;
-  for_results<S>(acc, min(S::BM, m - r0), min(S::BN, m - c0), tid, [&](int i, int j, f4 v, int k) {
+  for_results<S, false>(acc, min(S::BM, m - r0), min(S::BN, m - c0), tid, [&](int i, int j, f4 v, int k) {
     const int64_t at = (int64_t)(r0 + i) * out.ld + c0 + j;
     v *= cp;
     if constexpr (POLY) v += ca * read_pair(a + at, src.plane);   // (A and B have the same pitch)
@@ -495,7 +497,7 @@ ns_update_kernel(PairMat B, PairMat x, PairMat xo, int m, int n, float ca, float
   f4 acc[S::TN][S::TM];
   tile_gemm<T, S, true, false, true>(bs, xs, m, lds, tid, acc);
   const _Float16* xi = x.p + b * x.stride;
-  for_results<S>(acc, min(S::BM, m - r0), min(S::BN, x.ld - c0), tid, [&](int i, int j, f4 v, int k) {
+  for_results<S, true>(acc, min(S::BM, m - r0), min(S::BN, x.ld - c0), tid, [&](int i, int j, f4 v, int k) {
     const int64_t at = (int64_t)(r0 + i) * x.ld + c0 + j;   // (whole vectors: the pitch is a multiple of 8)
     v = cp * v + ca * read_pair(xi + at, x.plane);
     if (out) {
