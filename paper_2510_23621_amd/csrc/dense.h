@@ -234,20 +234,20 @@ __device__ __forceinline__ uint64_t uniform64(uint64_t v) {
 // fill 1024 consecutive bytes, so each lane reads the chunk that the tile's
 // layout wants at its place. Whole steps of BK only; the rest of a row
 // goes through TileSource, which fills with zeros.
-template <class T, int ROWS, int BK, bool KC, int NT>
+template <int ROWS, int BK, bool KC, int NT>
 struct DirectSource {
   static constexpr int NV = ROWS * BK / 8 / NT;
-  static_assert(ROWS * BK / 8 % NT == 0 && BK == 64 && sizeof(T) == 2, "whole vectors per thread");
+  static_assert(ROWS * BK / 8 % NT == 0, "whole vectors per thread");
   unsigned off[NV];   // bytes from the step's first element (the caller sees to it that they fit)
   uint64_t base, step;
-  __device__ __forceinline__ void init(const T* base_, int64_t ld, int rows, int tid) {
+  __device__ __forceinline__ void init(const void* base_, int64_t ld, int rows, int tid) {
     base = uniform64(reinterpret_cast<uint64_t>(base_));
     step = uniform64(2 * (KC ? (uint64_t)BK : BK * ld));
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
       const int f = tid + NT * u;
       if constexpr (KC) {
-        const int r = f / (BK / 8), c = f % (BK / 8) ^ (r & 7);
+        const int r = f / (BK / 8), c = f % (BK / 8) ^ (BK == 64 ? r & 7 : (r >> 1) & 3);
         off[u] = 2 * (unsigned)(min(r, rows - 1) * ld + 8 * c);
       } else {
         const int k = f / (ROWS / 8), c = f % (ROWS / 8) ^ ((k & 3) << 1);
@@ -259,17 +259,18 @@ struct DirectSource {
   // read, having no way to know that it reads the other buffer. They have no
   // register outputs; tile_gemm_direct waits for them (vmcnt) itself. The s_nop is
   // the wait state between writing M0 and an LDS copy.
-  __device__ __forceinline__ void issue(const unsigned short* t, int tid) {
+  // plane: bytes from the first plane to the one copied
+  __device__ __forceinline__ void issue(const unsigned short* t, int64_t plane, int tid) const {
     typedef __attribute__((address_space(3))) const unsigned short las;
     const unsigned at = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(las*)t + (tid & ~63) * 16);
 #pragma unroll
     for (int u = 0; u < NV; ++u)
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                    :
-                   : "s"(at + NT * u * 16), "v"(off[u]), "s"(base)
+                   : "s"(at + NT * u * 16), "v"(off[u]), "s"(base + plane)
                    : "memory", "m0");
-    base += step;
   }
+  __device__ __forceinline__ void next() { base += step; }
 };
 
 // The same for pairs of binary16 in two planes, 16-byte aligned rows of whole vectors.
@@ -419,12 +420,33 @@ __device__ __forceinline__ void for_results(const f4 (&acc)[S::TN][S::TM], int r
   }
 }
 
-// tile_gemm with both operands copied straight to LDS: two buffers, the next
-// step's copies in flight during this step's products.
+// One plane of T's elements, or the two planes of pairs.
+template <class T> struct Plane0 { using type = T; };
+template <> struct Plane0<HalfPair> { using type = _Float16; };
+
+// Waits until at most N copies to LDS are in flight and this wave's LDS reads
+// have returned, then meets the block's other waves.
+template <int N>
+__device__ __forceinline__ void copies_barrier() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "i"(N) : "memory");
+}
+
+// An operand of tile_gemm_direct: element (row, k) at p[row * ld + k] or
+// p[k * ld + row], `rows` in bounds; `plane` elements to a pair's second plane
+template <class T>
+struct Operand {
+  const typename Plane0<T>::type* p;
+  int64_t ld;
+  int rows;
+  int64_t plane;
+};
+
+// tile_gemm with both operands copied straight to LDS: a ring of STAGES buffers,
+// the copies of the next STAGES - 1 steps in flight during a step's products.
 template <class T, class S, bool KCR, bool KCC>
-__device__ __forceinline__ void tile_gemm_direct(const T* rb, int64_t rld, int rows, const T* cb, int64_t cld, int cols,
-                                                 int K, unsigned short* lds, int tid, f4 (&acc)[S::TN][S::TM]) {
-  constexpr int BUF = (S::BM + S::BN) * S::BK, CO = S::BM * S::BK;
+__device__ __forceinline__ void tile_gemm_direct(const Operand<T>& ro, const Operand<T>& co, int K, unsigned short* lds,
+                                                 int tid, f4 (&acc)[S::TN][S::TM]) {
+  constexpr int P = Planes<T>::n, CO = P * S::BM * S::BK, BUF = P * (S::BM + S::BN) * S::BK, ST = S::STAGES;
   const int lane = tid & 63, w = tid >> 6;
   const int m0 = (w / S::WN) * (S::BM / S::WM), n0 = (w % S::WN) * (S::BN / S::WN);
 #pragma unroll
@@ -433,40 +455,51 @@ __device__ __forceinline__ void tile_gemm_direct(const T* rb, int64_t rld, int r
     for (int i = 0; i < S::TM; ++i) acc[j][i] = f4{0.f, 0.f, 0.f, 0.f};
   if (K <= 0) return;
   const int whole = K / S::BK;
-  DirectSource<T, S::BM, S::BK, KCR, S::NT> r;
-  DirectSource<T, S::BN, S::BK, KCC, S::NT> c;
-  r.init(rb, rld, rows, tid);
-  c.init(cb, cld, cols, tid);
-  if (whole) {
-    r.issue(lds, tid);
-    c.issue(lds + CO, tid);
-    for (int i = 0; i < whole; ++i) {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __syncthreads();   // this step's tile is in LDS, the other buffer has been read
-      if (i + 1 < whole) {
-        r.issue(lds + (~i & 1) * BUF, tid);
-        c.issue(lds + (~i & 1) * BUF + CO, tid);
-      }
-      tile_products<T, S, KCR, KCC, 1>(lds + (i & 1) * BUF, lds + (i & 1) * BUF + CO, m0, n0, lane, acc);
+  using R = DirectSource<S::BM, S::BK, KCR, S::NT>;
+  using C = DirectSource<S::BN, S::BK, KCC, S::NT>;
+  constexpr int COPIES = P * (R::NV + C::NV);   // per step and wave
+  static_assert((ST - 2) * COPIES < 64, "the counter of copies in flight has six bits");
+  R r;
+  C c;
+  r.init(ro.p, ro.ld, ro.rows, tid);
+  c.init(co.p, co.ld, co.rows, tid);
+  auto copy = [&](int buffer) {
+    unsigned short* t = lds + buffer * BUF;
+#pragma unroll
+    for (int q = 0; q < P; ++q) {
+      r.issue(t + q * S::BM * S::BK, q ? 2 * ro.plane : 0, tid);
+      c.issue(t + CO + q * S::BN * S::BK, q ? 2 * co.plane : 0, tid);
     }
+    r.next();
+    c.next();
+  };
+#pragma unroll
+  for (int i = 0; i < ST - 1; ++i)
+    if (i < whole) copy(i);
+  int b = 0;   // buffer of step i
+  for (int i = 0; i < whole; ++i) {
+    // step i's copies have landed, and every wave has read the buffer of step i - 1
+    if (i + ST - 2 < whole) copies_barrier<(ST - 2) * COPIES>();
+    else copies_barrier<0>();
+    if (i + ST - 1 < whole) copy(b == 0 ? ST - 1 : b - 1);
+    const unsigned short* t = lds + b * BUF;
+    tile_products<T, S, KCR, KCC, P>(t, t + CO, m0, n0, lane, acc);
+    b = b + 1 == ST ? 0 : b + 1;
   }
   if (K % S::BK) {
-    const int64_t k = (int64_t)whole * S::BK;
-    unsigned short* t = lds + (whole & 1) * BUF;   // (read two steps ago, with a barrier since)
-    {
-      TileSource<T, S::BM, S::BK, KCR, true, S::NT> v;
-      v.init(rb + (KCR ? k : k * rld), rld, rows, tid);
-      v.load(K - (int)k, tid);
-      v.store(t, tid);
-    }
-    {
-      TileSource<T, S::BN, S::BK, KCC, true, S::NT> v;
-      v.init(cb + (KCC ? k : k * cld), cld, cols, tid);
-      v.load(K - (int)k, tid);
-      v.store(t + CO, tid);
-    }
+    const int k = whole * S::BK;
+    unsigned short* t = lds + b * BUF;   // (read ST steps ago, with a barrier since)
+    auto rest = [&](auto source, const Operand<T>& o, bool kc, unsigned short* d) {
+      const auto* p = o.p + (kc ? (int64_t)k : k * o.ld);
+      if constexpr (P == 2) source.init(p, o.plane, o.ld, o.rows, tid);
+      else source.init(p, o.ld, o.rows, tid);
+      source.load(K - k, tid);
+      source.store(d, tid);
+    };
+    rest(TileSource<T, S::BM, S::BK, KCR, true, S::NT>{}, ro, KCR, t);
+    rest(TileSource<T, S::BN, S::BK, KCC, true, S::NT>{}, co, KCC, t + CO);
     __syncthreads();
-    tile_products<T, S, KCR, KCC, 1>(t, t + CO, m0, n0, lane, acc);
+    tile_products<T, S, KCR, KCC, P>(t, t + CO, m0, n0, lane, acc);
   }
 }
 

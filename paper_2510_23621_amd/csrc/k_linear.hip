@@ -87,7 +87,7 @@ template <class T, class S, bool KCR, bool KCC, bool AL>
 __device__ __forceinline__ void product(const T* rb, int64_t rld, int rows, const T* cb, int64_t cld, int cols, int K,
                                         unsigned short* lds, int tid, f4 (&acc)[S::TN][S::TM]) {
   if constexpr (AL && S::DIRECT) {
-    tile_gemm_direct<T, S, KCR, KCC>(rb, rld, rows, cb, cld, cols, K, lds, tid, acc);
+    tile_gemm_direct<T, S, KCR, KCC>({rb, rld, rows, 0}, {cb, cld, cols, 0}, K, lds, tid, acc);
   } else {
     TileSource<T, S::BM, S::BK, KCR, AL, S::NT> r;
     TileSource<T, S::BN, S::BK, KCC, AL, S::NT> c;
@@ -122,18 +122,44 @@ __global__ void __launch_bounds__(S::NT) linear_fwd_kernel(LinearArgs<T> a) {
   f4 acc[S::TN][S::TM];
   product<T, S, true, false, AL>(a.x + run.row0 * a.ldx, a.ldx, run.rows, a.w + (int64_t)run.group * a.n_in * a.n_out + c0,
                                  a.n_out, a.n_out - c0, a.n_in, lds, tid, acc);
+  // epilogue: a tile row's residual is requested before the row above is stored
+  const int l = tid & 63, wv = tid >> 6;
+  const int m0 = (wv / S::WN) * (S::BM / S::WM) + (l & 15), n0 = (wv % S::WN) * (S::BN / S::WN) + 4 * (l >> 4);
   const T* bias = a.bias ? a.bias + (int64_t)run.group * a.n_out + c0 : nullptr;
   const T* res = a.residual ? a.residual + run.row0 * a.ldr + c0 : nullptr;
   auto finish = [&](auto act) {
-    for_results<S, AL>(acc, run.rows, cols, tid, [&](int m, int n, f4 v, int k) {
-      const bool vec = AL;
-      if (bias) v += read4(bias + n, k, vec);
-      if (z) store4(z + m * a.ldz + n, v, k, vec);
+    constexpr bool vec = AL;
+    f4 bj[S::TN], rj[2][S::TN];
+    auto count = [&](int j) { return AL ? 4 : min(4, cols - n0 - 16 * j); };
+    auto load_residual = [&](int i) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = activate<decltype(act)::value>(v[i]);
-      if (res) v += read4(res + m * a.ldr + n, k, vec);
-      store4(y + m * a.ldy + n, v, k, vec);
-    });
+      for (int j = 0; j < S::TN; ++j)
+        if (m0 + 16 * i < run.rows && n0 + 16 * j < cols)
+          rj[i & 1][j] = read4(res + (int64_t)(m0 + 16 * i) * a.ldr + n0 + 16 * j, count(j), vec);
+    };
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j) {
+      bj[j] = f4{0.f, 0.f, 0.f, 0.f};
+      if (bias && n0 + 16 * j < cols) bj[j] = read4(bias + n0 + 16 * j, count(j), vec);
+    }
+    if (res) load_residual(0);
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i) {
+      const int64_t m = m0 + 16 * i;
+      if (res && i + 1 < S::TM) load_residual(i + 1);
+      if (m >= run.rows) continue;
+#pragma unroll
+      for (int j = 0; j < S::TN; ++j) {
+        const int n = n0 + 16 * j;
+        if (n >= cols) continue;
+        f4 v = acc[j][i] + bj[j];
+        if (z) store4(z + m * a.ldz + n, v, count(j), vec);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = activate<decltype(act)::value>(v[q]);
+        if (res) v += rj[i & 1][j];
+        store4(y + m * a.ldy + n, v, count(j), vec);
+      }
+    }
   };
   if (a.act == MACE_ACT_SILU) finish(Int<MACE_ACT_SILU>{});
   else if (a.act == MACE_ACT_GELU) finish(Int<MACE_ACT_GELU>{});
@@ -337,7 +363,7 @@ template <class T, bool AL> struct Shapes {
 template <> struct Shapes<__bf16, true> {
   using Large = TileShape<256, 256, 2, 4, 64, 2, true>;
   using Mid = TileShape<128, 128, 2, 2, 64, 2, true>;
-  using Small = TileShape<64, 64, 2, 2, 64, 2, true>;
+  using Small = TileShape<64, 64, 2, 2, 64, 4, true>;
 };
 template <> struct Shapes<_Float16, true> : Shapes<__bf16, true> {};
 template <bool AL> struct Shapes<float, AL> {

@@ -417,11 +417,10 @@ ns_fit_kernel(const T* g, int64_t stride, int64_t ld, int m, int n, bool tall, d
 
 // ------------------------------------------------------------------ products
 
-// operand rows from row0 of a plane pair (T: binary16 reads the upper plane only)
-template <class T, class Src>
-__device__ __forceinline__ void source_of(Src& s, const PairMat& m, int b, int64_t at, int rows, int tid) {
-  if constexpr (__is_same(T, HalfPair)) s.init(m.p + b * m.stride + at, m.plane, m.ld, rows, tid);
-  else s.init(m.p + b * m.stride + at, m.ld, rows, tid);
+// operand of matrix b from element `at` (T: binary16 takes the upper plane only)
+template <class T>
+__device__ __forceinline__ Operand<T> operand(const PairMat& m, int b, int64_t at, int rows) {
+  return {m.p + b * m.stride + at, m.ld, rows, m.plane};
 }
 
 // Tile (tm, tn), tn <= tm, of a lower triangle of tiles
@@ -444,12 +443,9 @@ __global__ void __launch_bounds__(S::NT) ns_symmetric_kernel(PairMat src, PairMa
   triangle(id - b * tiles, tm, tn);
   const int r0 = tm * S::BM, c0 = tn * S::BN;
   static_assert(S::BM == S::BN, "square tiles");
-  TileSource<T, S::BM, S::BK, true, true, S::NT> rs;
-  TileSource<T, S::BN, S::BK, true, true, S::NT> cs;
-  source_of<T>(rs, src, b, (int64_t)r0 * src.ld, m - r0, tid);
-  source_of<T>(cs, src, b, (int64_t)c0 * src.ld, m - c0, tid);
   f4 acc[S::TN][S::TM];
-  tile_gemm<T, S, true, true, true>(rs, cs, K, lds, tid, acc);
+  tile_gemm_direct<T, S, true, true>(operand<T>(src, b, (int64_t)r0 * src.ld, m - r0),
+                                     operand<T>(src, b, (int64_t)c0 * src.ld, m - c0), K, lds, tid, acc);
   _Float16* o = out.p + b * out.stride;
   const _Float16* a = src.p + b * src.stride;
   for_results<S, false>(acc, min(S::BM, m - r0), min(S::BN, m - c0), tid, [&](int i, int j, f4 v, int k) {
@@ -490,12 +486,9 @@ ns_update_kernel(PairMat B, PairMat x, PairMat xo, int m, int n, float ca, float
   const int b = id / (tiles_n * tiles_m);
   id -= b * tiles_n * tiles_m;
   const int r0 = id / tiles_n * S::BM, c0 = id % tiles_n * S::BN;
-  TileSource<T, S::BM, S::BK, true, true, S::NT> bs;
-  TileSource<T, S::BN, S::BK, false, true, S::NT> xs;
-  source_of<T>(bs, B, b, (int64_t)r0 * B.ld, m - r0, tid);
-  source_of<T>(xs, x, b, c0, x.ld - c0, tid);
   f4 acc[S::TN][S::TM];
-  tile_gemm<T, S, true, false, true>(bs, xs, m, lds, tid, acc);
+  tile_gemm_direct<T, S, true, false>(operand<T>(B, b, (int64_t)r0 * B.ld, m - r0), operand<T>(x, b, c0, x.ld - c0), m,
+                                      lds, tid, acc);
   const _Float16* xi = x.p + b * x.stride;
   for_results<S, true>(acc, min(S::BM, m - r0), min(S::BN, x.ld - c0), tid, [&](int i, int j, f4 v, int k) {
     const int64_t at = (int64_t)(r0 + i) * x.ld + c0 + j;   // (whole vectors: the pitch is a multiple of 8)
@@ -592,12 +585,12 @@ NsPlan plan(const mace_orthogonalise_desc& d) {
 constexpr int64_t kFillBlocks = 256;   // blocks from which the larger tile is taken (one per CU)
 
 template <class T> struct Shapes {
-  using Mid = TileShape<128, 128, 2, 2, 64, 2>;
-  using Small = TileShape<64, 64, 2, 2, 64, 2>;
+  using Mid = TileShape<128, 128, 2, 2, 64, 2, true>;
+  using Small = TileShape<64, 64, 2, 2, 64, 4, true>;
 };
 template <> struct Shapes<HalfPair> {
-  using Mid = TileShape<128, 128, 2, 2, 32, 2>;
-  using Small = TileShape<64, 64, 2, 2, 32, 2>;
+  using Mid = TileShape<128, 128, 2, 2, 32, 2, true>;
+  using Small = TileShape<64, 64, 2, 2, 32, 4, true>;
 };
 
 template <class T, bool POLY>
