@@ -330,7 +330,7 @@ typedef struct mace_linear_desc {
  * 0, or NULL for one group of all rows; y (dev) [n_rows][n_out]; preact (dev)
  * [n_rows][n_out] or NULL: receives z, rounded to dtype, for the backward.
  * Rows behind group_offsets[n_groups] (a router's dropped slots) give zeros in
- * y and preact and are not read. */
+ * y and preact, whatever they hold. */
 mace_status mace_linear_forward(const mace_linear_desc* desc, const void* x, const void* weights, const void* bias,
                                 const void* residual, const int32_t* group_offsets, void* y, void* preact,
                                 void* stream);

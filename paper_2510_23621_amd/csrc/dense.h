@@ -8,6 +8,8 @@
 
 namespace mace {
 
+template <int I> struct Int { static constexpr int value = I; };
+
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
@@ -62,15 +64,15 @@ __device__ __forceinline__ Vec8<T> load8(const T* p) {
   else __builtin_memcpy(&r, p, sizeof(r));
   return r;
 }
-// p[0..n), zeros after it
+// p[0..7], zeros from `end` on (AL: there are none)
 template <class T, bool AL>
-__device__ __forceinline__ Vec8<T> load8_upto(const T* p, int n) {
-  if (n >= 8) return load8<T, AL>(p);
+__device__ __forceinline__ Vec8<T> load8_to(const T* p, const T* end) {
+  if (AL || p + 8 <= end) return load8<T, AL>(p);
   Vec8<T> r;
   r.zero();
 #pragma unroll
   for (int i = 0; i < 7; ++i)
-    if (i < n) r.set(i, p[i]);
+    if (p + i < end) r.set(i, p[i]);
   return r;
 }
 
@@ -94,17 +96,19 @@ __device__ __forceinline__ void to_planes(const Vec8<T>& x, us8 (&p)[Planes<T>::
   }
 }
 
-// n <= 4 consecutive elements from FP32 values, rounded once; vec: p is aligned
-// to four elements and n = 4
+// n <= 4 consecutive elements from FP32 values, rounded once; vec: n = 4 and p is
+// aligned to four elements. Whole vectors at other places go as unaligned ones.
 template <class T>
 __device__ __forceinline__ void store4(T* p, f4 v, int n, bool vec) {
   typedef T t4 __attribute__((ext_vector_type(4)));
   const t4 o = __builtin_convertvector(v, t4);
   if (vec) {
     *reinterpret_cast<t4*>(p) = o;
+  } else if (n >= 4) {
+    __builtin_memcpy(p, &o, sizeof(o));
   } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 3; ++i)
       if (i < n) p[i] = o[i];
   }
 }
@@ -112,11 +116,15 @@ template <class T>
 __device__ __forceinline__ f4 read4(const T* p, int n, bool vec) {
   typedef T t4 __attribute__((ext_vector_type(4)));
   if (vec) return __builtin_convertvector(*reinterpret_cast<const t4*>(p), f4);
-  f4 r = {0.f, 0.f, 0.f, 0.f};
+  t4 o = {(T)0.f, (T)0.f, (T)0.f, (T)0.f};
+  if (n >= 4) {
+    __builtin_memcpy(&o, p, sizeof(o));
+  } else {
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (i < n) r[i] = to_f32(p[i]);
-  return r;
+    for (int i = 0; i < 3; ++i)
+      if (i < n) o[i] = p[i];
+  }
+  return __builtin_convertvector(o, f4);
 }
 
 // ------------------------------------------------------------------ LDS tiles
@@ -158,18 +166,46 @@ __device__ __forceinline__ us8 tile_fragment(const unsigned short* t, int row0, 
   }
 }
 
+// FP32 tiles, copied as they are: KC [row][BK] with the 16-byte chunks of a row
+// XORed with the row, else [k][ROWS] with 64-byte pieces XORed with k / 8 (the
+// four lane groups of a fragment read different ones).
+template <int ROWS, int BK, bool KC>
+__device__ __forceinline__ int float_chunk(int row, int k) {   // offset of the 4-element chunk holding (row, k)
+  static_assert(BK == 32, "eight chunks per row");
+  if constexpr (KC) return row * BK + (((k >> 2) ^ (row & 7)) << 2);
+  else return k * ROWS + (((row >> 2) ^ ((k >> 3 & 3) << 2)) << 2);
+}
+// the fragment as tile_fragment's, split into its three bfloat16 parts
+template <int ROWS, int BK, bool KC>
+__device__ __forceinline__ void float_fragment(const float* t, int row0, int lane, us8 (&p)[3]) {
+  const int row = row0 + (lane & 15), k = 8 * (lane >> 4);
+  Vec8<float> v;
+  if constexpr (KC) {
+    v.v[0] = *reinterpret_cast<const f4*>(t + float_chunk<ROWS, BK, true>(row, k));
+    v.v[1] = *reinterpret_cast<const f4*>(t + float_chunk<ROWS, BK, true>(row, k + 4));
+  } else {
+    const float* q = t + float_chunk<ROWS, BK, false>(row, k) + (row & 3);   // (one chunk column for the eight k)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v.set(e, q[e * ROWS]);
+  }
+  to_planes<float>(v, p);
+}
+
 // Source of a tile in global memory: element (row, k) at base[row * ld + k] (KC)
-// or base[k * ld + row]. `rows` >= 1 of the tile's ROWS are in bounds: with AL
-// vectors past them repeat the last one (their results are not stored), else
-// they are cut. Every k past the end reads as zero.
-template <class T, int ROWS, int BK, bool KC, bool AL, int NT>
+// or base[k * ld + row]. `rows` >= 1 of the tile's ROWS are in bounds; what is
+// read in the places of the others is not used, and every k past the end reads as
+// zero. With AL vectors are aligned and whole, and those past the rows repeat the
+// last one. Otherwise a vector may run past its row, into the next one or the gap
+// before it, but not past `end`, the end of the whole tensor, where it is cut.
+// DEPTH sets of registers hold the tiles in flight.
+template <class T, int ROWS, int BK, bool KC, bool AL, int NT, int DEPTH = 1>
 struct TileSource {
   static constexpr int NV = ROWS * BK / 8 / NT;
   static constexpr int P = Planes<T>::n;
   static_assert(ROWS * BK / 8 % NT == 0, "whole vectors per thread");
   const T* p[NV];
-  int lim[NV];   // !AL: rows from the vector's first one to the end (row-contiguous)
-  Vec8<T> v[NV];
+  const T* end;
+  Vec8<T> v[DEPTH][NV];
   int64_t step;
   __device__ __forceinline__ static int row_of(int u, int tid) {
     const int f = tid + NT * u;
@@ -179,47 +215,63 @@ struct TileSource {
     const int f = tid + NT * u;
     return KC ? 8 * (f % (BK / 8)) : f / (ROWS / 8);
   }
-  __device__ __forceinline__ void init(const T* base, int64_t ld, int rows, int tid) {
+  __device__ __forceinline__ void init(const T* base, int64_t ld, int rows, int tid, const T* end_ = nullptr) {
     step = KC ? (int64_t)BK : BK * ld;
+    end = end_;
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
       const int r = row_of(u, tid), k = k_of(u, tid);
       if constexpr (KC) p[u] = base + (int64_t)min(r, rows - 1) * ld + k;
       else if constexpr (AL) p[u] = base + k * ld + min(r, rows - 8);   // (rows is a multiple of 8)
       else p[u] = base + k * ld + r;
-      lim[u] = rows - r;
     }
   }
-  // the tile at the current k; k_left: products' indices from it to the end
+  // the tile at the current k into register set D; k_left: products' indices from it to the end
+  template <int D = 0>
   __device__ __forceinline__ void load(int k_left, int tid) {
-    const bool cut = !AL && !KC;
-    if (k_left >= BK && !cut) {
 #pragma unroll
-      for (int u = 0; u < NV; ++u) v[u] = load8<T, AL>(p[u]);
-    } else {
+    for (int u = 0; u < NV; ++u) {
+      if constexpr (AL) {
+        if (k_left >= BK) {
+          v[D][u] = load8<T, true>(p[u]);
+        } else {
+          v[D][u].zero();
+          if (k_of(u, tid) < k_left) v[D][u] = load8<T, true>(p[u]);
+        }
+      } else {
+        v[D][u] = load8_to<T, false>(p[u], end);
+      }
+    }
+    if (!AL && k_left < BK) {
 #pragma unroll
       for (int u = 0; u < NV; ++u) {
-        const int k = k_of(u, tid);
-        const int n = KC ? k_left - k : (k < k_left ? (AL ? 8 : lim[u]) : 0);
-        if constexpr (AL) {
-          v[u].zero();
-          if (n > 0) v[u] = load8<T, AL>(p[u]);   // (contiguous extents are multiples of 8)
-        } else {
-          v[u] = load8_upto<T, AL>(p[u], n);
-        }
+        const int n = k_left - k_of(u, tid);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if ((KC ? i : 0) >= n) v[D][u].set(i, (T)0.f);
       }
     }
 #pragma unroll
     for (int u = 0; u < NV; ++u) p[u] += step;
   }
+  template <int D = 0>
   __device__ __forceinline__ void store(unsigned short* t, int tid) const {
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
       us8 q[P];
-      to_planes<T>(v[u], q);
+      to_planes<T>(v[D][u], q);
       const int o = tile_chunk<ROWS, BK, KC>(row_of(u, tid), k_of(u, tid));
 #pragma unroll
       for (int i = 0; i < P; ++i) *reinterpret_cast<us8*>(t + i * ROWS * BK + o) = q[i];
+    }
+  }
+  // FP32 as it is, in float_chunk's layout
+  __device__ __forceinline__ void store_floats(float* t, int tid) const {
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      const int r = row_of(u, tid), k = k_of(u, tid);
+      *reinterpret_cast<f4*>(t + float_chunk<ROWS, BK, KC>(r, k)) = v[0][u].v[0];
+      *reinterpret_cast<f4*>(t + float_chunk<ROWS, BK, KC>(KC ? r : r + 4, KC ? k + 4 : k)) = v[0][u].v[1];
     }
   }
 };
@@ -230,28 +282,31 @@ __device__ __forceinline__ uint64_t uniform64(uint64_t v) {
 }
 
 // The same tile copied from memory to LDS without passing through registers
-// (16-bit elements, 16-byte aligned rows of whole vectors): a wave's 64 lanes
+// (16-byte aligned rows of whole vectors): a wave's 64 lanes
 // fill 1024 consecutive bytes, so each lane reads the chunk that the tile's
-// layout wants at its place. Whole steps of BK only; the rest of a row
+// layout wants at its place. FP32 tiles are copied as they are (tile_floats). Whole steps of BK only; the rest of a row
 // goes through TileSource, which fills with zeros.
-template <int ROWS, int BK, bool KC, int NT>
+template <int ES, int ROWS, int BK, bool KC, int NT>
 struct DirectSource {
-  static constexpr int NV = ROWS * BK / 8 / NT;
-  static_assert(ROWS * BK / 8 % NT == 0, "whole vectors per thread");
+  static constexpr int VE = 16 / ES;   // elements of ES bytes per vector
+  static constexpr int NV = ROWS * BK / VE / NT;
+  static_assert(ROWS * BK / VE % NT == 0, "whole vectors per thread");
   unsigned off[NV];   // bytes from the step's first element (the caller sees to it that they fit)
   uint64_t base, step;
   __device__ __forceinline__ void init(const void* base_, int64_t ld, int rows, int tid) {
     base = uniform64(reinterpret_cast<uint64_t>(base_));
-    step = uniform64(2 * (KC ? (uint64_t)BK : BK * ld));
+    step = uniform64(ES * (KC ? (uint64_t)BK : BK * ld));
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
-      const int f = tid + NT * u;
+      const int f = tid + NT * u;   // the vector at this place of the tile
       if constexpr (KC) {
-        const int r = f / (BK / 8), c = f % (BK / 8) ^ (BK == 64 ? r & 7 : (r >> 1) & 3);
-        off[u] = 2 * (unsigned)(min(r, rows - 1) * ld + 8 * c);
+        constexpr int C = BK / VE;
+        const int r = f / C, c = f % C ^ (C == 8 ? r & 7 : (r >> 1) & 3);
+        off[u] = ES * (unsigned)(min(r, rows - 1) * ld + VE * c);
       } else {
-        const int k = f / (ROWS / 8), c = f % (ROWS / 8) ^ ((k & 3) << 1);
-        off[u] = 2 * (unsigned)(k * ld + min(8 * c, rows - 8));
+        constexpr int C = ROWS / VE;
+        const int k = f / C, c = f % C ^ (ES == 4 ? (k >> 3 & 3) << 2 : (k & 3) << 1);
+        off[u] = ES * (unsigned)(k * ld + min(VE * c, rows - VE));
       }
     }
   }
@@ -310,6 +365,7 @@ template <int BM_, int BN_, int WM_, int WN_, int BK_, int STAGES_, bool DIRECT_
 struct TileShape {
   static constexpr bool DIRECT = DIRECT_;   // operands straight to LDS where they are aligned
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, BK = BK_, STAGES = STAGES_;
+  static constexpr int DEPTH = STAGES == 1 ? 1 : 2;   // (of tile_gemm)
   static constexpr int NT = 64 * WM * WN;
   static constexpr int TM = BM / WM / 16, TN = BN / WN / 16;   // 16 x 16 tiles per wave
 };
@@ -354,12 +410,31 @@ __device__ __forceinline__ void tile_products(const unsigned short* tr, const un
   }
 }
 
-template <class T, class S> constexpr int tile_lds = S::STAGES * Planes<T>::n * (S::BM + S::BN) * S::BK;   // elements
+// the same for FP32 tiles, split as they are read
+template <class S, bool KCR, bool KCC>
+__device__ __forceinline__ void float_products(const float* tr, const float* tc, int m0, int n0, int lane,
+                                               f4 (&acc)[S::TN][S::TM]) {
+  us8 b[S::TM][3];
+#pragma unroll
+  for (int i = 0; i < S::TM; ++i) float_fragment<S::BM, S::BK, KCR>(tr, m0 + 16 * i, lane, b[i]);
+#pragma unroll
+  for (int j = 0; j < S::TN; ++j) {
+    us8 a[3];
+    float_fragment<S::BN, S::BK, KCC>(tc, n0 + 16 * j, lane, a);
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i) acc[j][i] = products<float, 3>(a, b[i], acc[j][i]);
+  }
+}
 
+// 16-bit units of LDS per operand element, and a block's total
+template <class T, class S> constexpr int tile_units = S::DIRECT && sizeof(T) == 4 ? 2 : Planes<T>::n;
+template <class T, class S> constexpr int tile_lds = S::STAGES * tile_units<T, S> * (S::BM + S::BN) * S::BK;
+
+// Staged through registers: two LDS buffers and S::DEPTH sets of registers, or one buffer.
 template <class T, class S, bool KCR, bool KCC, bool AL>
-__device__ __forceinline__ void tile_gemm(TileSource<T, S::BM, S::BK, KCR, AL, S::NT>& r,
-                                          TileSource<T, S::BN, S::BK, KCC, AL, S::NT>& c, int K, unsigned short* lds,
-                                          int tid, f4 (&acc)[S::TN][S::TM]) {
+__device__ __forceinline__ void tile_gemm(TileSource<T, S::BM, S::BK, KCR, AL, S::NT, S::DEPTH>& r,
+                                          TileSource<T, S::BN, S::BK, KCC, AL, S::NT, S::DEPTH>& c, int K,
+                                          unsigned short* lds, int tid, f4 (&acc)[S::TN][S::TM]) {
   constexpr int P = Planes<T>::n, BUF = P * (S::BM + S::BN) * S::BK, CO = P * S::BM * S::BK;
   const int lane = tid & 63, w = tid >> 6;
   const int m0 = (w / S::WN) * (S::BM / S::WM), n0 = (w % S::WN) * (S::BN / S::WN);
@@ -368,34 +443,45 @@ __device__ __forceinline__ void tile_gemm(TileSource<T, S::BM, S::BK, KCR, AL, S
 #pragma unroll
     for (int i = 0; i < S::TM; ++i) acc[j][i] = f4{0.f, 0.f, 0.f, 0.f};
   if (K <= 0) return;
-  r.load(K, tid);
-  c.load(K, tid);
+  r.template load<0>(K, tid);
+  c.template load<0>(K, tid);
   if constexpr (S::STAGES == 2) {
-    r.store(lds, tid);
-    c.store(lds + CO, tid);
+    static_assert(S::DEPTH == 2, "two register sets");
+    if (K > S::BK) {
+      r.template load<1>(K - S::BK, tid);
+      c.template load<1>(K - S::BK, tid);
+    }
+    r.template store<0>(lds, tid);
+    c.template store<0>(lds + CO, tid);
     __syncthreads();
-    for (int k = 0, s = 0; k < K; k += S::BK, s ^= 1) {
-      const bool more = k + S::BK < K;
-      if (more) {   // in flight during this step's products
-        r.load(K - k - S::BK, tid);
-        c.load(K - k - S::BK, tid);
+    // step at k out of buffer B: request the step after the next, store the next
+    auto step = [&](auto b_, int k) {
+      constexpr int B = decltype(b_)::value;
+      const int left = K - k;
+      if (left > 2 * S::BK) {
+        r.template load<B>(left - 2 * S::BK, tid);
+        c.template load<B>(left - 2 * S::BK, tid);
       }
-      tile_products<T, S, KCR, KCC, P>(lds + s * BUF, lds + s * BUF + CO, m0, n0, lane, acc);
-      if (more) {
-        r.store(lds + (s ^ 1) * BUF, tid);
-        c.store(lds + (s ^ 1) * BUF + CO, tid);
+      tile_products<T, S, KCR, KCC, P>(lds + B * BUF, lds + B * BUF + CO, m0, n0, lane, acc);
+      if (left > S::BK) {
+        r.template store<1 - B>(lds + (1 - B) * BUF, tid);
+        c.template store<1 - B>(lds + (1 - B) * BUF + CO, tid);
       }
       __syncthreads();
+    };
+    for (int k = 0; k < K; k += 2 * S::BK) {
+      step(Int<0>{}, k);
+      if (k + S::BK < K) step(Int<1>{}, k + S::BK);
     }
   } else {
     for (int k = 0; k < K; k += S::BK) {
       if (k) __syncthreads();   // the previous step's products have read the tile
-      r.store(lds, tid);
-      c.store(lds + CO, tid);
+      r.template store<0>(lds, tid);
+      c.template store<0>(lds + CO, tid);
       __syncthreads();
       if (k + S::BK < K) {
-        r.load(K - k - S::BK, tid);
-        c.load(K - k - S::BK, tid);
+        r.template load<0>(K - k - S::BK, tid);
+        c.template load<0>(K - k - S::BK, tid);
       }
       tile_products<T, S, KCR, KCC, P>(lds, lds + CO, m0, n0, lane, acc);
     }
@@ -439,6 +525,7 @@ struct Operand {
   int64_t ld;
   int rows;
   int64_t plane;
+  const typename Plane0<T>::type* end = nullptr;   // one past the tensor's last element, for unaligned operands
 };
 
 // tile_gemm with both operands copied straight to LDS: a ring of STAGES buffers,
@@ -446,7 +533,9 @@ struct Operand {
 template <class T, class S, bool KCR, bool KCC>
 __device__ __forceinline__ void tile_gemm_direct(const Operand<T>& ro, const Operand<T>& co, int K, unsigned short* lds,
                                                  int tid, f4 (&acc)[S::TN][S::TM]) {
-  constexpr int P = Planes<T>::n, CO = P * S::BM * S::BK, BUF = P * (S::BM + S::BN) * S::BK, ST = S::STAGES;
+  constexpr bool F = sizeof(T) == 4;
+  constexpr int Q = F ? 1 : Planes<T>::n;   // planes copied
+  constexpr int U = tile_units<T, S>, CO = U * S::BM * S::BK, BUF = U * (S::BM + S::BN) * S::BK, ST = S::STAGES;
   const int lane = tid & 63, w = tid >> 6;
   const int m0 = (w / S::WN) * (S::BM / S::WM), n0 = (w % S::WN) * (S::BN / S::WN);
 #pragma unroll
@@ -455,9 +544,9 @@ __device__ __forceinline__ void tile_gemm_direct(const Operand<T>& ro, const Ope
     for (int i = 0; i < S::TM; ++i) acc[j][i] = f4{0.f, 0.f, 0.f, 0.f};
   if (K <= 0) return;
   const int whole = K / S::BK;
-  using R = DirectSource<S::BM, S::BK, KCR, S::NT>;
-  using C = DirectSource<S::BN, S::BK, KCC, S::NT>;
-  constexpr int COPIES = P * (R::NV + C::NV);   // per step and wave
+  using R = DirectSource<F ? 4 : 2, S::BM, S::BK, KCR, S::NT>;
+  using C = DirectSource<F ? 4 : 2, S::BN, S::BK, KCC, S::NT>;
+  constexpr int COPIES = Q * (R::NV + C::NV);   // per step and wave
   static_assert((ST - 2) * COPIES < 64, "the counter of copies in flight has six bits");
   R r;
   C c;
@@ -466,12 +555,18 @@ __device__ __forceinline__ void tile_gemm_direct(const Operand<T>& ro, const Ope
   auto copy = [&](int buffer) {
     unsigned short* t = lds + buffer * BUF;
 #pragma unroll
-    for (int q = 0; q < P; ++q) {
+    for (int q = 0; q < Q; ++q) {
       r.issue(t + q * S::BM * S::BK, q ? 2 * ro.plane : 0, tid);
       c.issue(t + CO + q * S::BN * S::BK, q ? 2 * co.plane : 0, tid);
     }
     r.next();
     c.next();
+  };
+  auto multiply = [&](const unsigned short* t) {
+    if constexpr (F)
+      float_products<S, KCR, KCC>(reinterpret_cast<const float*>(t), reinterpret_cast<const float*>(t + CO), m0, n0, lane, acc);
+    else
+      tile_products<T, S, KCR, KCC, Q>(t, t + CO, m0, n0, lane, acc);
   };
 #pragma unroll
   for (int i = 0; i < ST - 1; ++i)
@@ -482,8 +577,7 @@ __device__ __forceinline__ void tile_gemm_direct(const Operand<T>& ro, const Ope
     if (i + ST - 2 < whole) copies_barrier<(ST - 2) * COPIES>();
     else copies_barrier<0>();
     if (i + ST - 1 < whole) copy(b == 0 ? ST - 1 : b - 1);
-    const unsigned short* t = lds + b * BUF;
-    tile_products<T, S, KCR, KCC, P>(t, t + CO, m0, n0, lane, acc);
+    multiply(lds + b * BUF);
     b = b + 1 == ST ? 0 : b + 1;
   }
   if (K % S::BK) {
@@ -491,15 +585,16 @@ __device__ __forceinline__ void tile_gemm_direct(const Operand<T>& ro, const Ope
     unsigned short* t = lds + b * BUF;   // (read ST steps ago, with a barrier since)
     auto rest = [&](auto source, const Operand<T>& o, bool kc, unsigned short* d) {
       const auto* p = o.p + (kc ? (int64_t)k : k * o.ld);
-      if constexpr (P == 2) source.init(p, o.plane, o.ld, o.rows, tid);
+      if constexpr (Q == 2) source.init(p, o.plane, o.ld, o.rows, tid);
       else source.init(p, o.ld, o.rows, tid);
       source.load(K - k, tid);
-      source.store(d, tid);
+      if constexpr (F) source.store_floats(reinterpret_cast<float*>(d), tid);
+      else source.store(d, tid);
     };
     rest(TileSource<T, S::BM, S::BK, KCR, true, S::NT>{}, ro, KCR, t);
     rest(TileSource<T, S::BN, S::BK, KCC, true, S::NT>{}, co, KCC, t + CO);
     __syncthreads();
-    tile_products<T, S, KCR, KCC, P>(t, t + CO, m0, n0, lane, acc);
+    multiply(t);
   }
 }
 

@@ -9,8 +9,6 @@
 namespace mace {
 namespace {
 
-template <int I> struct Int { static constexpr int value = I; };
-
 // ------------------------------------------------------------------ activations
 // Normal distribution: Phi(z), and exp(-z^2 / 2). erfc(x) = t q(t) exp(-x^2), t =
 // 1 / (1 + 0.36 x), with q a degree-9 polynomial fitted to a relative error of
@@ -84,16 +82,101 @@ struct BiasGradArgs {
 
 // The block's product, by the way its shape and operands allow
 template <class T, class S, bool KCR, bool KCC, bool AL>
-__device__ __forceinline__ void product(const T* rb, int64_t rld, int rows, const T* cb, int64_t cld, int cols, int K,
-                                        unsigned short* lds, int tid, f4 (&acc)[S::TN][S::TM]) {
+__device__ __forceinline__ void product(const Operand<T>& ro, const Operand<T>& co, int K, unsigned short* lds, int tid,
+                                        f4 (&acc)[S::TN][S::TM]) {
   if constexpr (AL && S::DIRECT) {
-    tile_gemm_direct<T, S, KCR, KCC>({rb, rld, rows, 0}, {cb, cld, cols, 0}, K, lds, tid, acc);
+    tile_gemm_direct<T, S, KCR, KCC>(ro, co, K, lds, tid, acc);
   } else {
-    TileSource<T, S::BM, S::BK, KCR, AL, S::NT> r;
-    TileSource<T, S::BN, S::BK, KCC, AL, S::NT> c;
-    r.init(rb, rld, rows, tid);
-    c.init(cb, cld, cols, tid);
+    TileSource<T, S::BM, S::BK, KCR, AL, S::NT, S::DEPTH> r;
+    TileSource<T, S::BN, S::BK, KCC, AL, S::NT, S::DEPTH> c;
+    r.init(ro.p, ro.ld, ro.rows, tid, ro.end);
+    c.init(co.p, co.ld, co.rows, tid, co.end);
     tile_gemm<T, S, KCR, KCC, AL>(r, c, K, lds, tid, acc);
+  }
+}
+
+// FP32 launches of few tiles: a block of four waves forms 16 RT x 16 CT results on
+// FP32 MFMA (v_mfma_f32_16x16x4: no splitting, and with few rows the weights' way
+// from memory bounds it, not the products), each wave every fourth run of 32 k;
+// the four partial sums are added through LDS. Lane l takes k + 8 (l/16) + 0..7 of
+// operand row l%16, straight from memory, a step ahead. f(row, column, values, count).
+template <int RT_, int CT_> struct ThinShape {
+  static constexpr int RT = RT_, CT = CT_, BM = 16 * RT, BN = 16 * CT, NT = 256;
+};
+template <class S, bool KCC, bool AL, class F>
+__device__ __forceinline__ void thin_product(const Operand<float>& ro, const Operand<float>& co, int K, float* lds, int tid,
+                                             F f) {
+  constexpr int RT = S::RT, CT = S::CT;
+  const int l = tid & 63, wv = tid >> 6, i = l & 15, g = l >> 4;
+  const float *x[RT], *w[CT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) x[r] = ro.p + min(16 * r + i, ro.rows - 1) * ro.ld + 8 * g;
+#pragma unroll
+  for (int c = 0; c < CT; ++c) {
+    const int64_t n = min(16 * c + i, co.rows - 1);
+    w[c] = co.p + (KCC ? n * co.ld + 8 * g : n + 8 * g * co.ld);
+  }
+  Vec8<float> xv[2][RT], wv8[2][CT];
+  auto load = [&](auto d_, int k) {
+    constexpr int D = decltype(d_)::value;
+    const int n = K - k - 8 * g;   // this lane's k in bounds
+    const bool whole = k + 32 <= K;
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      if (whole) {
+        xv[D][r] = load8<float, AL>(x[r] + k);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) xv[D][r].set(e, e < n ? x[r][k + e] : 0.f);
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+      if (KCC && whole) {
+        wv8[D][c] = load8<float, AL>(w[c] + k);
+      } else if (whole) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) wv8[D][c].set(e, w[c][(k + e) * co.ld]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) wv8[D][c].set(e, e < n ? w[c][KCC ? k + e : (k + e) * co.ld] : 0.f);
+      }
+    }
+  };
+  f4 acc[CT][RT];
+#pragma unroll
+  for (int c = 0; c < CT; ++c)
+#pragma unroll
+    for (int r = 0; r < RT; ++r) acc[c][r] = f4{0.f, 0.f, 0.f, 0.f};
+  auto multiply = [&](auto d_) {
+    constexpr int D = decltype(d_)::value;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+          acc[c][r] = __builtin_amdgcn_mfma_f32_16x16x4f32(wv8[D][c].get(e), xv[D][r].get(e), acc[c][r], 0, 0, 0);
+  };
+  int k = 32 * wv;
+  if (k < K) load(Int<0>{}, k);
+  for (; k < K; k += 256) {
+    if (k + 128 < K) load(Int<1>{}, k + 128);
+    multiply(Int<0>{});
+    if (k + 256 < K) load(Int<0>{}, k + 256);
+    if (k + 128 < K) multiply(Int<1>{});
+  }
+  f4* part = reinterpret_cast<f4*>(lds);   // [tile][wave][lane]
+#pragma unroll
+  for (int c = 0; c < CT; ++c)
+#pragma unroll
+    for (int r = 0; r < RT; ++r) part[((c * RT + r) * 4 + wv) * 64 + l] = acc[c][r];
+  __syncthreads();
+  if (wv < RT * CT) {   // a wave per tile
+    const f4* t = part + wv * 256 + l;
+    const f4 v = (t[0] + t[64]) + (t[128] + t[192]);
+    const int m = 16 * (wv % RT) + i, n = 16 * (wv / RT) + 4 * g;
+    if (m < ro.rows && n < co.rows) f(m, n, v, AL ? 4 : min(4, co.rows - n));
   }
 }
 
@@ -120,8 +203,11 @@ __global__ void __launch_bounds__(S::NT) linear_fwd_kernel(LinearArgs<T> a) {
     return;
   }
   f4 acc[S::TN][S::TM];
-  product<T, S, true, false, AL>(a.x + run.row0 * a.ldx, a.ldx, run.rows, a.w + (int64_t)run.group * a.n_in * a.n_out + c0,
-                                 a.n_out, a.n_out - c0, a.n_in, lds, tid, acc);
+  const T* x = a.x + run.row0 * a.ldx;
+  const T* w = a.w + (int64_t)run.group * a.n_in * a.n_out + c0;
+  product<T, S, true, false, AL>({x, a.ldx, run.rows, 0, a.x + (a.n - 1) * a.ldx + a.n_in},
+                                 {w, a.n_out, a.n_out - c0, 0, a.w + (int64_t)a.groups * a.n_in * a.n_out}, a.n_in, lds,
+                                 tid, acc);
   // epilogue: a tile row's residual is requested before the row above is stored
   const int l = tid & 63, wv = tid >> 6;
   const int m0 = (wv / S::WN) * (S::BM / S::WM) + (l & 15), n0 = (wv % S::WN) * (S::BN / S::WN) + 4 * (l >> 4);
@@ -166,6 +252,38 @@ __global__ void __launch_bounds__(S::NT) linear_fwd_kernel(LinearArgs<T> a) {
   else finish(Int<MACE_ACT_NONE>{});
 }
 
+template <bool AL, class S>
+__global__ void __launch_bounds__(S::NT) linear_fwd_thin_kernel(LinearArgs<float> a) {
+  __shared__ __align__(16) float lds[S::RT * S::CT * 1024];
+  const int tid = threadIdx.x;
+  const int tiles_n = (a.n_out + S::BN - 1) / S::BN;
+  const int id = blockIdx.x;
+  const int c0 = id % tiles_n * S::BN, cols = min(S::BN, a.n_out - c0);
+  RowRun run;
+  if (!find_run(a.offsets, a.groups, a.n, S::BM, id / tiles_n, run)) return;
+  float* y = a.y + run.row0 * a.ldy + c0;
+  float* z = a.z ? a.z + run.row0 * a.ldz + c0 : nullptr;
+  if (run.group >= a.groups) {
+    zero_rows(y, a.ldy, run.rows, cols, tid, S::NT);
+    if (z) zero_rows(z, a.ldz, run.rows, cols, tid, S::NT);
+    return;
+  }
+  const float* bias = a.bias ? a.bias + (int64_t)run.group * a.n_out + c0 : nullptr;
+  const float* res = a.residual ? a.residual + run.row0 * a.ldr + c0 : nullptr;
+  thin_product<S, false, AL>({a.x + run.row0 * a.ldx, a.ldx, run.rows, 0},
+                             {a.w + (int64_t)run.group * a.n_in * a.n_out + c0, a.n_out, cols, 0}, a.n_in, lds, tid,
+                             [&](int64_t m, int n, f4 v, int k) {
+    if (bias) v += read4(bias + n, k, AL);
+    if (z) store4(z + m * a.ldz + n, v, k, AL);
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      v[q] = a.act == MACE_ACT_SILU ? activate<MACE_ACT_SILU>(v[q])
+                                    : (a.act == MACE_ACT_GELU ? activate<MACE_ACT_GELU>(v[q]) : v[q]);
+    if (res) v += read4(res + m * a.ldr + n, k, AL);
+    store4(y + m * a.ldy + n, v, k, AL);
+  });
+}
+
 // dx = dz W_g^T: tile `id`
 template <class T, bool AL, class S>
 __device__ __forceinline__ void row_grad_tile(const RowGradArgs<T>& a, int id, unsigned short* lds, int tid) {
@@ -179,10 +297,28 @@ __device__ __forceinline__ void row_grad_tile(const RowGradArgs<T>& a, int id, u
     return;
   }
   f4 acc[S::TN][S::TM];
-  product<T, S, true, true, AL>(a.dz + run.row0 * a.lddz, a.lddz, run.rows,
-                                a.w + ((int64_t)run.group * a.n_in + c0) * a.n_out, a.n_out, cols, a.n_out, lds, tid, acc);
+  const T* dz = a.dz + run.row0 * a.lddz;
+  const T* w = a.w + ((int64_t)run.group * a.n_in + c0) * a.n_out;
+  product<T, S, true, true, AL>({dz, a.lddz, run.rows, 0, a.dz + (a.n - 1) * a.lddz + a.n_out},
+                                {w, a.n_out, cols, 0, a.w + (int64_t)a.groups * a.n_in * a.n_out}, a.n_out, lds, tid, acc);
   for_results<S, AL>(acc, run.rows, cols, tid,
                  [&](int m, int n, f4 v, int k) { store4(dx + m * a.lddx + n, v, k, AL); });
+}
+
+template <bool AL, class S>
+__device__ __forceinline__ void row_grad_thin(const RowGradArgs<float>& a, int id, float* lds, int tid) {
+  const int tiles_n = (a.n_in + S::BN - 1) / S::BN;
+  const int c0 = id % tiles_n * S::BN, cols = min(S::BN, a.n_in - c0);
+  RowRun run;
+  if (!find_run(a.offsets, a.groups, a.n, S::BM, id / tiles_n, run)) return;
+  float* dx = a.dx + run.row0 * a.lddx + c0;
+  if (run.group >= a.groups) {
+    zero_rows(dx, a.lddx, run.rows, cols, tid, S::NT);
+    return;
+  }
+  thin_product<S, true, AL>({a.dz + run.row0 * a.lddz, a.lddz, run.rows, 0},
+                            {a.w + ((int64_t)run.group * a.n_in + c0) * a.n_out, a.n_out, cols, 0}, a.n_out, lds, tid,
+                            [&](int64_t m, int n, f4 v, int k) { store4(dx + m * a.lddx + n, v, k, AL); });
 }
 
 // dW_g = x_g^T dz_g, the group's rows cut into `splits` parts: tile `id`
@@ -203,8 +339,9 @@ __device__ __forceinline__ void weight_grad_tile(const WeightGradArgs<T>& a, int
   const int64_t per = ((r1 - r0 + a.splits - 1) / a.splits + S::BK - 1) / S::BK * S::BK;
   const int64_t k0 = min(r1, r0 + split * per), k1 = min(r1, k0 + per);
   f4 acc[S::TN][S::TM];
-  product<T, S, false, false, AL>(a.x + k0 * a.ldx + m0, a.ldx, a.n_in - m0, a.dz + k0 * a.lddz + c0, a.lddz,
-                                  a.n_out - c0, (int)(k1 - k0), lds, tid, acc);
+  product<T, S, false, false, AL>({a.x + k0 * a.ldx + m0, a.ldx, a.n_in - m0, 0, a.x + (a.n - 1) * a.ldx + a.n_in},
+                                  {a.dz + k0 * a.lddz + c0, a.lddz, a.n_out - c0, 0, a.dz + (a.n - 1) * a.lddz + a.n_out},
+                                  (int)(k1 - k0), lds, tid, acc);
   const int64_t at = ((int64_t)g * a.n_in + m0) * a.n_out + c0;
   if (a.part) {
     float* o = a.part + (int64_t)split * a.groups * a.n_in * a.n_out + at;
@@ -253,14 +390,16 @@ __device__ __forceinline__ void bias_grad(const BiasGradArgs<T>& a, int id, floa
 
 // All three gradients in one launch: blocks below row_blocks form dx, the next
 // weight_blocks dW, the rest db.
-template <class T, bool AL, class S>
+// RS: the shape of dx's tiles, S or a thin one.
+template <class T, bool AL, class S, class RS>
 __global__ void __launch_bounds__(S::NT)
 linear_grad_kernel(RowGradArgs<T> a, WeightGradArgs<T> b, BiasGradArgs<T> c, int row_blocks, int weight_blocks) {
   __shared__ __align__(16) unsigned short lds[tile_lds<T, S>];
   const int tid = threadIdx.x;
   int id = blockIdx.x;
   if (id < row_blocks) {
-    row_grad_tile<T, AL, S>(a, xcd_order(id, row_blocks), lds, tid);
+    if constexpr (__is_same(S, RS)) row_grad_tile<T, AL, S>(a, xcd_order(id, row_blocks), lds, tid);
+    else row_grad_thin<AL, RS>(a, id, reinterpret_cast<float*>(lds), tid);
   } else if ((id -= row_blocks) < weight_blocks) {
     weight_grad_tile<T, AL, S>(b, xcd_order(id, weight_blocks), lds, tid);
   } else {
@@ -283,45 +422,54 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const float* __restric
 }
 
 // dz = dy act'(z) over a run of rows (where there is an activation), and the
-// run's column sums. A block takes 8 CX columns; its 256 / CX row lanes each sum
-// their rows, then are added in order.
+// run's column sums. A block takes 8 CX columns; its kSlopeThreads / CX row lanes
+// each sum their rows, then are added in order.
+constexpr int kSlopeThreads = 1024;
 template <class T, bool AL>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(kSlopeThreads)
 linear_slope_kernel(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ z, int64_t ldz, T* __restrict__ dz,
                     int64_t lddz, float* __restrict__ sums, const int* __restrict__ offsets, int groups, int64_t n,
                     int n_out, int act, int run_rows, int cx) {
-  __shared__ float red[256 * 8];
+  __shared__ float red[kSlopeThreads * 8];
   RowRun run;
   if (!find_run(offsets, groups, n, run_rows, blockIdx.x, run) || run.group >= groups) return;
-  const int tid = threadIdx.x, c = tid % cx, ry = tid / cx, R = 256 / cx;
+  const int tid = threadIdx.x, c = tid % cx, ry = tid / cx, R = kSlopeThreads / cx;
   const int col = 8 * (blockIdx.y * cx + c), k = n_out - col;
   float s[8] = {};
+  const T* dy_end = dy + (n - 1) * lddy + n_out;
+  const T* z_end = z ? z + (n - 1) * ldz + n_out : nullptr;
+  constexpr int U = 2;   // rows in flight
   if (k > 0)
-    for (int r = ry; r < run.rows; r += R) {
-      const int64_t row = run.row0 + r;
-      Vec8<T> g = load8_upto<T, AL>(dy + row * lddy + col, k);
-      if (dz) {
-        const Vec8<T> v = load8_upto<T, AL>(z + row * ldz + col, k);
-        float o[8];
+    for (int r0 = ry; r0 < run.rows; r0 += U * R) {
+      Vec8<T> g[U], v[U];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = g.get(i) * activation_slope(v.get(i), act);
+      for (int u = 0; u < U; ++u) {
+        const int64_t row = run.row0 + min(r0 + u * R, run.rows - 1);
+        g[u] = load8_to<T, AL>(dy + row * lddy + col, dy_end);
+        if (dz) v[u] = load8_to<T, AL>(z + row * ldz + col, z_end);
+      }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          s[i] += o[i];
-          g.set(i, (T)o[i]);
+      for (int u = 0; u < U; ++u) {
+        if (r0 + u * R >= run.rows) continue;
+        if (dz) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float o = g[u].get(i) * activation_slope(v[u].get(i), act);
+            s[i] += o;
+            g[u].set(i, (T)o);
+          }
+          *reinterpret_cast<Vec8<T>*>(dz + (run.row0 + r0 + u * R) * lddz + col) = g[u];   // (own buffer: rows padded to whole vectors)
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) s[i] += g[u].get(i);
         }
-        if (k >= 8) *reinterpret_cast<Vec8<T>*>(dz + row * lddz + col) = g;   // (own buffer: aligned rows)
-        else for (int i = 0; i < k; ++i) dz[row * lddz + col + i] = (T)o[i];
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s[i] += g.get(i);
       }
     }
   if (!sums) return;
 #pragma unroll
   for (int i = 0; i < 8; ++i) red[(ry * cx + c) * 8 + i] = s[i];
   __syncthreads();
-  for (int i = tid; i < 8 * cx; i += 256) {
+  for (int i = tid; i < 8 * cx; i += kSlopeThreads) {
     float t = 0.f;
     for (int r = 0; r < R; ++r) t += red[r * cx * 8 + i];
     const int o = 8 * blockIdx.y * cx + i;
@@ -355,9 +503,9 @@ int64_t slope_runs(const mace_linear_desc& d) { return ceil_div(d.n_rows, slope_
 constexpr int64_t kFillBlocks = 256, kLargeBlocks = 192;   // (256 CUs)
 
 // Large: launches of at least kLargeBlocks of its tiles; Mid: from kFillBlocks of its own
-template <class T, bool AL> struct Shapes {
-  using Large = TileShape<128, 128, 2, 2, 64, 2>;
-  using Mid = TileShape<128, 128, 2, 2, 64, 2>;
+template <class T, bool AL> struct Shapes {   // (16-bit, any alignment)
+  using Large = TileShape<128, 128, 2, 2, 64, 1>;
+  using Mid = TileShape<128, 128, 2, 2, 64, 1>;
   using Small = TileShape<64, 64, 2, 2, 64, 2>;
 };
 template <> struct Shapes<__bf16, true> {
@@ -366,11 +514,18 @@ template <> struct Shapes<__bf16, true> {
   using Small = TileShape<64, 64, 2, 2, 64, 4, true>;
 };
 template <> struct Shapes<_Float16, true> : Shapes<__bf16, true> {};
-template <bool AL> struct Shapes<float, AL> {
+template <> struct Shapes<float, false> {
   using Large = TileShape<128, 128, 2, 2, 32, 1>;
   using Mid = TileShape<128, 128, 2, 2, 32, 1>;
-  using Small = TileShape<64, 64, 2, 2, 32, 1>;
+  using Small = TileShape<64, 64, 2, 2, 32, 2>;
 };
+template <> struct Shapes<float, true> : Shapes<float, false> {};
+using Thin = ThinShape<1, 1>;
+using Thin2 = ThinShape<2, 2>;
+// FP32 launches of fewer than kThinBlocks 64 x 64 tiles; Thin2 from kFillBlocks of its own
+constexpr int64_t kThinBlocks = 192;
+bool thin(int64_t rows, int64_t cols) { return ceil_div(rows, 64) * ceil_div(cols, 64) < kThinBlocks; }
+bool thin2(int64_t rows, int64_t cols) { return ceil_div(rows, 32) * ceil_div(cols, 32) >= kFillBlocks; }
 enum { kSmall, kMid, kLarge };
 int shape_of(int64_t rows, int64_t cols, int64_t batch = 1) {
   if (ceil_div(rows, 256) * ceil_div(cols, 256) * batch >= kLargeBlocks) return kLarge;
@@ -427,8 +582,18 @@ mace_status forward(const mace_linear_desc& d, const void* x, const void* w, con
   const bool al = aligned16(x) && aligned16(w) && aligned16(bias) && aligned16(residual) && aligned16(y) &&
                   aligned16(z) && ((d.n_in | d.n_out | d.ld_x | d.ld_y | d.ld_residual | d.ld_preact) & 7) == 0 &&
                   near(d.ld_x);
-  auto go = [&](auto al_) {
+  auto go = [&](auto al_) -> mace_status {
     constexpr bool AL = decltype(al_)::value;
+    if constexpr (sizeof(T) == 4)
+      if (thin(d.n_rows, d.n_out)) {
+        auto run = [&](auto shape) {
+          using S = decltype(shape);
+          const int64_t blocks = (ceil_div(d.n_rows, S::BM) + (offsets ? d.n_groups : 0)) * ceil_div(d.n_out, S::BN);
+          linear_fwd_thin_kernel<AL, S><<<(unsigned)blocks, S::NT, 0, s>>>(a);
+          return launched();
+        };
+        return thin2(d.n_rows, d.n_out) ? run(Thin2{}) : run(Thin{});
+      }
     return with_shape<T, AL>(shape_of(d.n_rows, d.n_out), [&](auto shape) -> mace_status {
       using S = decltype(shape);
       const int64_t blocks = (ceil_div(d.n_rows, S::BM) + (offsets ? d.n_groups : 0)) * ceil_div(d.n_out, S::BN);
@@ -460,7 +625,7 @@ mace_status backward(const mace_linear_desc& d, const void* dy, int64_t lddy, co
     const dim3 grid((unsigned)slope_runs(d), (unsigned)ceil_div(vecs, cx));
     T* out = d.act != MACE_ACT_NONE ? const_cast<T*>(dz) : nullptr;
     auto go = [&](auto f) {
-      f<<<grid, 256, 0, s>>>((const T*)dy, lddy, (const T*)z, d.ld_preact, out, lddz, db ? sums : nullptr, offsets,
+      f<<<grid, kSlopeThreads, 0, s>>>((const T*)dy, lddy, (const T*)z, d.ld_preact, out, lddz, db ? sums : nullptr, offsets,
                              d.n_groups, d.n_rows, d.n_out, d.act, slope_run(d.n_rows), cx);
     };
     if (al) go(linear_slope_kernel<T, true>);
@@ -473,24 +638,32 @@ mace_status backward(const mace_linear_desc& d, const void* dy, int64_t lddy, co
   const WeightGradArgs<T> wa{(const T*)x, dz, (T*)dw, p.splits > 1 ? reinterpret_cast<float*>(ws + p.part) : nullptr,
                              offsets, d.n_rows, d.ld_x, lddz, d.n_in, d.n_out, d.n_groups, p.splits};
   const BiasGradArgs<T> ba{sums, (T*)db, offsets, d.n_rows, d.n_out, slope_run(d.n_rows), (int)slope_runs(d)};
-  // one launch for all three where dx and dW take the same kind of tile
+  const bool want_x = dx && d.n_rows > 0;
+  const bool thin_x = sizeof(T) == 4 && want_x && thin(d.n_rows, d.n_in);
+  // one launch for all three where dx and dW take the same kind of tile (thin
+  // tiles of dx go with small ones of dW)
   auto go = [&](auto al_, int kind, bool rows, bool weights, bool bias) {
     constexpr bool AL = decltype(al_)::value;
     return with_shape<T, AL>(kind, [&](auto shape) -> mace_status {
       using S = decltype(shape);
-      const int64_t rb = rows ? (ceil_div(d.n_rows, S::BM) + (offsets ? d.n_groups : 0)) * ceil_div(d.n_in, S::BN) : 0;
-      const int64_t wb = weights ? ceil_div(d.n_in, S::BM) * ceil_div(d.n_out, S::BN) * d.n_groups * p.splits : 0;
-      const int64_t blocks = rb + wb + (bias ? ceil_div(d.n_out, 64) * d.n_groups : 0);
-      if (blocks > INT32_MAX) return MACE_EUNSUPPORTED;
-      if (blocks == 0) return MACE_OK;
-      linear_grad_kernel<T, AL, S><<<(unsigned)blocks, S::NT, 0, s>>>(ra, wa, ba, (int)rb, (int)wb);
-      return launched();
+      auto run = [&](auto row_shape) -> mace_status {
+        using RS = decltype(row_shape);
+        const int64_t rb = rows ? (ceil_div(d.n_rows, RS::BM) + (offsets ? d.n_groups : 0)) * ceil_div(d.n_in, RS::BN) : 0;
+        const int64_t wb = weights ? ceil_div(d.n_in, S::BM) * ceil_div(d.n_out, S::BN) * d.n_groups * p.splits : 0;
+        const int64_t blocks = rb + wb + (bias ? ceil_div(d.n_out, 64) * d.n_groups : 0);
+        if (blocks > INT32_MAX) return MACE_EUNSUPPORTED;
+        if (blocks == 0) return MACE_OK;
+        linear_grad_kernel<T, AL, S, RS><<<(unsigned)blocks, S::NT, 0, s>>>(ra, wa, ba, (int)rb, (int)wb);
+        return launched();
+      };
+      if constexpr (sizeof(T) == 4 && S::BM == 64)
+        if (rows && thin_x) return thin2(d.n_rows, d.n_in) ? run(Thin2{}) : run(Thin{});
+      return run(S{});
     });
   };
   auto grads = [&](int kind, bool rows, bool weights, bool bias) {
     return al ? go(Int<1>{}, kind, rows, weights, bias) : go(Int<0>{}, kind, rows, weights, bias);
   };
-  const bool want_x = dx && d.n_rows > 0;
   const int kind_x = shape_of(d.n_rows, d.n_in);
   if (!want_x || !dw || kind_x == p.weight_kind) {
     st = grads(dw ? p.weight_kind : kind_x, want_x, dw != nullptr, db != nullptr);
