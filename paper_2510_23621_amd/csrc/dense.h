@@ -96,35 +96,42 @@ __device__ __forceinline__ void to_planes(const Vec8<T>& x, us8 (&p)[Planes<T>::
   }
 }
 
-// n <= 4 consecutive elements from FP32 values, rounded once; vec: n = 4 and p is
-// aligned to four elements. Whole vectors at other places go as unaligned ones.
-template <class T>
-__device__ __forceinline__ void store4(T* p, f4 v, int n, bool vec) {
-  typedef T t4 __attribute__((ext_vector_type(4)));
-  const t4 o = __builtin_convertvector(v, t4);
+typedef float f8 __attribute__((ext_vector_type(8)));
+template <int W> struct Floats { using type = f4; };
+template <> struct Floats<8> { using type = f8; };
+template <class V> constexpr int width_of = sizeof(V) / 4;
+
+// n <= W consecutive elements from FP32 values, rounded once; vec: n = W and p is
+// aligned to W elements. Whole vectors at other places go as unaligned ones.
+template <class T, class V>
+__device__ __forceinline__ void store_n(T* p, V v, int n, bool vec) {
+  constexpr int W = width_of<V>;
+  typedef T tw __attribute__((ext_vector_type(W)));
+  const tw o = __builtin_convertvector(v, tw);
   if (vec) {
-    *reinterpret_cast<t4*>(p) = o;
-  } else if (n >= 4) {
+    *reinterpret_cast<tw*>(p) = o;
+  } else if (n >= W) {
     __builtin_memcpy(p, &o, sizeof(o));
   } else {
 #pragma unroll
-    for (int i = 0; i < 3; ++i)
+    for (int i = 0; i < W - 1; ++i)
       if (i < n) p[i] = o[i];
   }
 }
-template <class T>
-__device__ __forceinline__ f4 read4(const T* p, int n, bool vec) {
-  typedef T t4 __attribute__((ext_vector_type(4)));
-  if (vec) return __builtin_convertvector(*reinterpret_cast<const t4*>(p), f4);
-  t4 o = {(T)0.f, (T)0.f, (T)0.f, (T)0.f};
-  if (n >= 4) {
+template <int W, class T>
+__device__ __forceinline__ typename Floats<W>::type read_n(const T* p, int n, bool vec) {
+  typedef T tw __attribute__((ext_vector_type(W)));
+  using V = typename Floats<W>::type;
+  if (vec) return __builtin_convertvector(*reinterpret_cast<const tw*>(p), V);
+  tw o = {};
+  if (n >= W) {
     __builtin_memcpy(&o, p, sizeof(o));
   } else {
 #pragma unroll
-    for (int i = 0; i < 3; ++i)
+    for (int i = 0; i < W - 1; ++i)
       if (i < n) o[i] = p[i];
   }
-  return __builtin_convertvector(o, f4);
+  return __builtin_convertvector(o, V);
 }
 
 // ------------------------------------------------------------------ LDS tiles
@@ -370,22 +377,21 @@ struct TileShape {
   static constexpr int TM = BM / WM / 16, TN = BN / WN / 16;   // 16 x 16 tiles per wave
 };
 
-template <class T, int P>
-__device__ __forceinline__ f4 products(const us8 (&a)[P], const us8 (&b)[P], f4 c) {
-  if constexpr (P == 1) {
-    return mfma32<T>(a[0], b[0], c);
-  } else if constexpr (P == 2) {
-    c = mfma32<T>(a[1], b[0], c);
-    c = mfma32<T>(a[0], b[1], c);
-    return mfma32<T>(a[0], b[0], c);
-  } else {
-    c = mfma32<T>(a[2], b[0], c);
-    c = mfma32<T>(a[1], b[1], c);
-    c = mfma32<T>(a[0], b[2], c);
-    c = mfma32<T>(a[1], b[0], c);
-    c = mfma32<T>(a[0], b[1], c);
-    return mfma32<T>(a[0], b[0], c);
-  }
+// The partial products kept, smallest first: parts of the first and the second factor
+template <int P> struct Partial;
+template <> struct Partial<1> { static constexpr int n = 1, a[1] = {0}, b[1] = {0}; };
+template <> struct Partial<2> { static constexpr int n = 3, a[3] = {1, 0, 0}, b[3] = {0, 1, 0}; };
+template <> struct Partial<3> { static constexpr int n = 6, a[6] = {2, 1, 0, 1, 0, 0}, b[6] = {0, 1, 2, 0, 1, 0}; };
+
+// acc[i] += a b[i], the partial products of one i in a row: an MFMA takes the sum
+// of the one before it without waiting (with the partial products outside the
+// time is the same to 2 %)
+template <class T, int P, int N>
+__device__ __forceinline__ void products(const us8 (&a)[P], const us8 (&b)[N][P], f4 (&acc)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int q = 0; q < Partial<P>::n; ++q) acc[i] = mfma32<T>(a[Partial<P>::a[q]], b[i][Partial<P>::b[q]], acc[i]);
 }
 
 // one BK step out of LDS: rows' planes at tr, columns' at tc
@@ -404,8 +410,7 @@ __device__ __forceinline__ void tile_products(const unsigned short* tr, const un
       us8 a[P];
 #pragma unroll
       for (int q = 0; q < P; ++q) a[q] = tile_fragment<S::BN, S::BK, KCC>(tc + q * S::BN * S::BK, n0 + 16 * j, k, lane);
-#pragma unroll
-      for (int i = 0; i < S::TM; ++i) acc[j][i] = products<T, P>(a, b[i], acc[j][i]);
+      products<T>(a, b, acc[j]);
     }
   }
 }
@@ -421,8 +426,7 @@ __device__ __forceinline__ void float_products(const float* tr, const float* tc,
   for (int j = 0; j < S::TN; ++j) {
     us8 a[3];
     float_fragment<S::BN, S::BK, KCC>(tc, n0 + 16 * j, lane, a);
-#pragma unroll
-    for (int i = 0; i < S::TM; ++i) acc[j][i] = products<float, 3>(a, b[i], acc[j][i]);
+    products<float>(a, b, acc[j]);
   }
 }
 
@@ -488,20 +492,51 @@ __device__ __forceinline__ void tile_gemm(TileSource<T, S::BM, S::BK, KCR, AL, S
   }
 }
 
-// This lane's four columns of the results of tile_gemm: f(row, column, values, count)
-// (AL: columns come in whole vectors)
-template <class S, bool AL, class F>
+// Two column tiles of a row tile as each lane gets them: four consecutive columns
+// 4 (l/16) of either. Exchanging the odd 16-lane rows of the one with the even rows
+// of the other leaves a lane with eight consecutive columns, 8 (l/32) of tile (l/16)
+// % 2: 16-byte accesses of 16-bit results, 64 bytes of a row together in place of
+// 32 (81920 x 64 -> 1280 bfloat16: 71 -> 41 us).
+__device__ __forceinline__ f8 join_tiles(f4 a, f4 b) {
+  f8 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    // (not bit casts: of a vector's element they take the vector's first)
+    const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(a[i]), __float_as_uint(b[i]), false, false);
+    r[i] = __uint_as_float(s[0]);
+    r[4 + i] = __uint_as_float(s[1]);
+  }
+  return r;
+}
+// vectors of columns per row tile, and the first column of vector j of lane l
+template <int TN, int W> constexpr int lane_vectors = TN * 4 / W;
+template <int W>
+__device__ __forceinline__ int lane_column(int j, int l) {
+  const int g = l >> 4;
+  return W == 4 ? 16 * j + 4 * g : 16 * (2 * j + (g & 1)) + 8 * (g >> 1);
+}
+template <int W, int TN, int TM>
+__device__ __forceinline__ typename Floats<W>::type lane_values(const f4 (&acc)[TN][TM], int j, int i) {
+  if constexpr (W == 4) return acc[j][i];
+  else return join_tiles(acc[2 * j][i], acc[2 * j + 1][i]);
+}
+// Consecutive columns a lane takes of results of type T
+template <class T> constexpr int lane_width = sizeof(T) == 2 ? 8 : 4;
+
+// This lane's results of a block's product, W consecutive columns at a time:
+// f(row, column, values, count) (AL: columns come in whole vectors)
+template <class S, int W, bool AL, class F>
 __device__ __forceinline__ void for_results(const f4 (&acc)[S::TN][S::TM], int rows, int cols, int tid, F f) {
   const int l = tid & 63, w = tid >> 6;
-  const int m0 = (w / S::WN) * (S::BM / S::WM) + (l & 15), n0 = (w % S::WN) * (S::BN / S::WN) + 4 * (l >> 4);
+  const int m0 = (w / S::WN) * (S::BM / S::WM) + (l & 15), n0 = (w % S::WN) * (S::BN / S::WN);
 #pragma unroll
   for (int i = 0; i < S::TM; ++i) {
     const int m = m0 + 16 * i;
-    if (m >= rows) continue;
 #pragma unroll
-    for (int j = 0; j < S::TN; ++j) {
-      const int n = n0 + 16 * j;
-      if (n < cols) f(m, n, acc[j][i], AL ? 4 : min(4, cols - n));
+    for (int j = 0; j < lane_vectors<S::TN, W>; ++j) {
+      const auto v = lane_values<W>(acc, j, i);   // (by every lane: the exchange reads across rows' lanes)
+      const int n = n0 + lane_column<W>(j, l);
+      if (m < rows && n < cols) f(m, n, v, AL ? W : min(W, cols - n));
     }
   }
 }

@@ -209,41 +209,42 @@ __global__ void __launch_bounds__(S::NT) linear_fwd_kernel(LinearArgs<T> a) {
                                  {w, a.n_out, a.n_out - c0, 0, a.w + (int64_t)a.groups * a.n_in * a.n_out}, a.n_in, lds,
                                  tid, acc);
   // epilogue: a tile row's residual is requested before the row above is stored
+  constexpr int W = lane_width<T>, NV = lane_vectors<S::TN, W>;
+  using V = typename Floats<W>::type;
   const int l = tid & 63, wv = tid >> 6;
-  const int m0 = (wv / S::WN) * (S::BM / S::WM) + (l & 15), n0 = (wv % S::WN) * (S::BN / S::WN) + 4 * (l >> 4);
+  const int m0 = (wv / S::WN) * (S::BM / S::WM) + (l & 15), n0 = (wv % S::WN) * (S::BN / S::WN);
   const T* bias = a.bias ? a.bias + (int64_t)run.group * a.n_out + c0 : nullptr;
   const T* res = a.residual ? a.residual + run.row0 * a.ldr + c0 : nullptr;
   auto finish = [&](auto act) {
-    constexpr bool vec = AL;
-    f4 bj[S::TN], rj[2][S::TN];
-    auto count = [&](int j) { return AL ? 4 : min(4, cols - n0 - 16 * j); };
+    V bj[NV], rj[2][NV];
+    auto column = [&](int j) { return n0 + lane_column<W>(j, l); };
+    auto count = [&](int j) { return AL ? W : min(W, cols - column(j)); };
     auto load_residual = [&](int i) {
 #pragma unroll
-      for (int j = 0; j < S::TN; ++j)
-        if (m0 + 16 * i < run.rows && n0 + 16 * j < cols)
-          rj[i & 1][j] = read4(res + (int64_t)(m0 + 16 * i) * a.ldr + n0 + 16 * j, count(j), vec);
+      for (int j = 0; j < NV; ++j)
+        if (m0 + 16 * i < run.rows && column(j) < cols)
+          rj[i & 1][j] = read_n<W>(res + (int64_t)(m0 + 16 * i) * a.ldr + column(j), count(j), AL);
     };
 #pragma unroll
-    for (int j = 0; j < S::TN; ++j) {
-      bj[j] = f4{0.f, 0.f, 0.f, 0.f};
-      if (bias && n0 + 16 * j < cols) bj[j] = read4(bias + n0 + 16 * j, count(j), vec);
+    for (int j = 0; j < NV; ++j) {
+      bj[j] = V{};
+      if (bias && column(j) < cols) bj[j] = read_n<W>(bias + column(j), count(j), AL);
     }
     if (res) load_residual(0);
 #pragma unroll
     for (int i = 0; i < S::TM; ++i) {
       const int64_t m = m0 + 16 * i;
       if (res && i + 1 < S::TM) load_residual(i + 1);
-      if (m >= run.rows) continue;
 #pragma unroll
-      for (int j = 0; j < S::TN; ++j) {
-        const int n = n0 + 16 * j;
-        if (n >= cols) continue;
-        f4 v = acc[j][i] + bj[j];
-        if (z) store4(z + m * a.ldz + n, v, count(j), vec);
+      for (int j = 0; j < NV; ++j) {
+        V v = lane_values<W>(acc, j, i) + bj[j];
+        const int n = column(j);
+        if (m >= run.rows || n >= cols) continue;
+        if (z) store_n(z + m * a.ldz + n, v, count(j), AL);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = activate<decltype(act)::value>(v[q]);
+        for (int q = 0; q < W; ++q) v[q] = activate<decltype(act)::value>(v[q]);
         if (res) v += rj[i & 1][j];
-        store4(y + m * a.ldy + n, v, count(j), vec);
+        store_n(y + m * a.ldy + n, v, count(j), AL);
       }
     }
   };
@@ -273,15 +274,160 @@ __global__ void __launch_bounds__(S::NT) linear_fwd_thin_kernel(LinearArgs<float
   thin_product<S, false, AL>({a.x + run.row0 * a.ldx, a.ldx, run.rows, 0},
                              {a.w + (int64_t)run.group * a.n_in * a.n_out + c0, a.n_out, cols, 0}, a.n_in, lds, tid,
                              [&](int64_t m, int n, f4 v, int k) {
-    if (bias) v += read4(bias + n, k, AL);
-    if (z) store4(z + m * a.ldz + n, v, k, AL);
+    if (bias) v += read_n<4>(bias + n, k, AL);
+    if (z) store_n(z + m * a.ldz + n, v, k, AL);
 #pragma unroll
     for (int q = 0; q < 4; ++q)
       v[q] = a.act == MACE_ACT_SILU ? activate<MACE_ACT_SILU>(v[q])
                                     : (a.act == MACE_ACT_GELU ? activate<MACE_ACT_GELU>(v[q]) : v[q]);
-    if (res) v += read4(res + m * a.ldr + n, k, AL);
-    store4(y + m * a.ldy + n, v, k, AL);
+    if (res) v += read_n<4>(res + m * a.ldr + n, k, AL);
+    store_n(y + m * a.ldy + n, v, k, AL);
   });
+}
+
+// Short sums (K up to 64 in FP32, 128 in 16 bits) over many rows: a wave keeps the
+// weights of 64 columns in registers, as MFMA operands, and the run's rows go past
+// them in chunks through LDS, where their parts lie split once for the block's four
+// waves. The next chunk's rows are requested before this chunk's results are
+// stored (memory operations complete in order: a later request would wait for
+// the stores). Bound by the results' way to memory: 81920 x 64 -> 1280 FP32 105 us
+// (4.0 TB/s written), bfloat16 41 us (5.1); as tiles 138 and 72 us.
+// KCC: the weights' rows are the columns of the result (dx).
+template <class T, int KS_> struct NarrowShape {   // K <= 32 KS
+  static constexpr int KS = KS_, BN = 256, NT = 256;
+  static constexpr int CHUNK = sizeof(T) == 4 ? 64 : 128, RUN = sizeof(T) == 4 ? 256 : 512;   // rows per chunk, per block
+  static constexpr int LDS = CHUNK * 32 * KS * Planes<T>::n;
+};
+template <class T, class S, bool KCC, bool AL, class F>
+__device__ __forceinline__ void narrow_rows(const Operand<T>& ro, const T* w, int64_t ldw, int cols, int K,
+                                            unsigned short* lds, int tid, F f) {
+  constexpr int P = Planes<T>::n, KS = S::KS, C = 4 * KS, NV = S::CHUNK * C / S::NT, W = lane_width<T>;
+  constexpr int PLANE = S::CHUNK * 32 * KS;
+  const int l = tid & 63, wv = tid >> 6, i = l & 15, g = l >> 4, c0 = 64 * wv;
+  // chunk rows of 4 KS vectors, XORed with the row (with the row pair at four vectors a row)
+  auto place = [](int r, int c) { return (r * C + (c ^ (C == 4 ? r >> 1 & 3 : r & 7))) << 3; };
+  Vec8<T> x[NV];
+  auto load = [&](int m0) {
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      const int e = tid + S::NT * u, k = 8 * (e % C), n = K - k;   // n: k in bounds
+      const T* p = ro.p + min(m0 + e / C, ro.rows - 1) * ro.ld + k;
+      if constexpr (AL) {
+        x[u].zero();
+        if (n > 0) x[u] = load8<T, true>(p);
+      } else {
+        x[u] = load8_to<T, false>(p, ro.end);
+        if (n < 8)
+#pragma unroll
+          for (int q = 0; q < 8; ++q)
+            if (q >= n) x[u].set(q, (T)0.f);
+      }
+    }
+  };
+  load(0);
+  us8 wr[4][KS][P];
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const int64_t n = min(c0 + 16 * j + i, cols - 1);
+      const int k = 32 * s + 8 * g;
+      Vec8<T> v;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v.set(e, k + e < K ? w[KCC ? n * ldw + k + e : (k + e) * ldw + n] : (T)0.f);
+      to_planes<T>(v, wr[j][s]);
+    }
+  for (int m0 = 0; m0 < ro.rows; m0 += S::CHUNK) {
+    if (m0) __syncthreads();   // the previous chunk has been read
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      const int e = tid + S::NT * u;
+      us8 q[P];
+      to_planes<T>(x[u], q);
+#pragma unroll
+      for (int p = 0; p < P; ++p) *reinterpret_cast<us8*>(lds + p * PLANE + place(e / C, e % C)) = q[p];
+    }
+    __syncthreads();
+    if (m0 + S::CHUNK < ro.rows) load(m0 + S::CHUNK);
+    const int top = min(S::CHUNK, ro.rows - m0);
+    for (int m = 0; m < top; m += 16) {
+      f4 acc[4][1];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[j][0] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        us8 xb[1][P];
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+          xb[0][p] = *reinterpret_cast<const us8*>(lds + p * PLANE + place(m + i, 4 * s + g));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) products<T>(wr[j][s], xb, acc[j]);
+      }
+#pragma unroll
+      for (int j = 0; j < lane_vectors<4, W>; ++j) {
+        const auto v = lane_values<W>(acc, j, 0);
+        const int n = c0 + lane_column<W>(j, l);
+        if (m + i < top && n < cols) f((int64_t)(m0 + m + i), n, v, AL ? W : min(W, cols - n));
+      }
+    }
+  }
+}
+
+template <class T, bool AL, class S>
+__global__ void __launch_bounds__(S::NT) __attribute__((amdgpu_waves_per_eu(2))) linear_fwd_narrow_kernel(LinearArgs<T> a) {
+  __shared__ __align__(16) unsigned short lds[S::LDS];
+  const int tid = threadIdx.x;
+  const int tiles_n = (a.n_out + S::BN - 1) / S::BN;
+  const int id = xcd_order(blockIdx.x, gridDim.x);
+  const int c0 = id % tiles_n * S::BN, cols = min(S::BN, a.n_out - c0);
+  RowRun run;
+  if (!find_run(a.offsets, a.groups, a.n, S::RUN, id / tiles_n, run)) return;
+  T* y = a.y + run.row0 * a.ldy + c0;
+  T* z = a.z ? a.z + run.row0 * a.ldz + c0 : nullptr;
+  if (run.group >= a.groups) {
+    zero_rows(y, a.ldy, run.rows, cols, tid, S::NT);
+    if (z) zero_rows(z, a.ldz, run.rows, cols, tid, S::NT);
+    return;
+  }
+  const T* bias = a.bias ? a.bias + (int64_t)run.group * a.n_out + c0 : nullptr;
+  const T* res = a.residual ? a.residual + run.row0 * a.ldr + c0 : nullptr;
+  auto finish = [&](auto act) {
+    narrow_rows<T, S, false, AL>({a.x + run.row0 * a.ldx, a.ldx, run.rows, 0, a.x + (a.n - 1) * a.ldx + a.n_in},
+                                 a.w + (int64_t)run.group * a.n_in * a.n_out + c0, a.n_out, cols, a.n_in, lds, tid,
+                                 [&](int64_t m, int n, auto v, int k) {
+      constexpr int W = width_of<decltype(v)>;
+      decltype(v) r = {};
+      if (res) r = read_n<W>(res + m * a.ldr + n, k, AL);
+      if (bias) v += read_n<W>(bias + n, k, AL);
+      if (z) store_n(z + m * a.ldz + n, v, k, AL);
+#pragma unroll
+      for (int q = 0; q < W; ++q) v[q] = activate<decltype(act)::value>(v[q]);
+      if (res) v += r;
+      store_n(y + m * a.ldy + n, v, k, AL);
+    });
+  };
+  if (a.act == MACE_ACT_SILU) finish(Int<MACE_ACT_SILU>{});
+  else if (a.act == MACE_ACT_GELU) finish(Int<MACE_ACT_GELU>{});
+  else finish(Int<MACE_ACT_NONE>{});
+}
+
+template <class T, bool AL, class S>
+__global__ void __launch_bounds__(S::NT) __attribute__((amdgpu_waves_per_eu(2))) linear_row_grad_narrow_kernel(RowGradArgs<T> a) {
+  __shared__ __align__(16) unsigned short lds[S::LDS];
+  const int tid = threadIdx.x;
+  const int tiles_n = (a.n_in + S::BN - 1) / S::BN;
+  const int id = xcd_order(blockIdx.x, gridDim.x);
+  const int c0 = id % tiles_n * S::BN, cols = min(S::BN, a.n_in - c0);
+  RowRun run;
+  if (!find_run(a.offsets, a.groups, a.n, S::RUN, id / tiles_n, run)) return;
+  T* dx = a.dx + run.row0 * a.lddx + c0;
+  if (run.group >= a.groups) {
+    zero_rows(dx, a.lddx, run.rows, cols, tid, S::NT);
+    return;
+  }
+  narrow_rows<T, S, true, AL>({a.dz + run.row0 * a.lddz, a.lddz, run.rows, 0, a.dz + (a.n - 1) * a.lddz + a.n_out},
+                              a.w + ((int64_t)run.group * a.n_in + c0) * a.n_out, a.n_out, cols, a.n_out, lds, tid,
+                              [&](int64_t m, int n, auto v, int k) { store_n(dx + m * a.lddx + n, v, k, AL); });
 }
 
 // dx = dz W_g^T: tile `id`
@@ -301,8 +447,8 @@ __device__ __forceinline__ void row_grad_tile(const RowGradArgs<T>& a, int id, u
   const T* w = a.w + ((int64_t)run.group * a.n_in + c0) * a.n_out;
   product<T, S, true, true, AL>({dz, a.lddz, run.rows, 0, a.dz + (a.n - 1) * a.lddz + a.n_out},
                                 {w, a.n_out, cols, 0, a.w + (int64_t)a.groups * a.n_in * a.n_out}, a.n_out, lds, tid, acc);
-  for_results<S, AL>(acc, run.rows, cols, tid,
-                 [&](int m, int n, f4 v, int k) { store4(dx + m * a.lddx + n, v, k, AL); });
+  for_results<S, lane_width<T>, AL>(acc, run.rows, cols, tid,
+                                    [&](int m, int n, auto v, int k) { store_n(dx + m * a.lddx + n, v, k, AL); });
 }
 
 template <bool AL, class S>
@@ -318,7 +464,7 @@ __device__ __forceinline__ void row_grad_thin(const RowGradArgs<float>& a, int i
   }
   thin_product<S, true, AL>({a.dz + run.row0 * a.lddz, a.lddz, run.rows, 0},
                             {a.w + ((int64_t)run.group * a.n_in + c0) * a.n_out, a.n_out, cols, 0}, a.n_out, lds, tid,
-                            [&](int64_t m, int n, f4 v, int k) { store4(dx + m * a.lddx + n, v, k, AL); });
+                            [&](int64_t m, int n, f4 v, int k) { store_n(dx + m * a.lddx + n, v, k, AL); });
 }
 
 // dW_g = x_g^T dz_g, the group's rows cut into `splits` parts: tile `id`
@@ -345,12 +491,12 @@ __device__ __forceinline__ void weight_grad_tile(const WeightGradArgs<T>& a, int
   const int64_t at = ((int64_t)g * a.n_in + m0) * a.n_out + c0;
   if (a.part) {
     float* o = a.part + (int64_t)split * a.groups * a.n_in * a.n_out + at;
-    for_results<S, AL>(acc, rows, cols, tid,
-                   [&](int m, int n, f4 v, int k) { store4(o + (int64_t)m * a.n_out + n, v, k, AL); });
+    for_results<S, 4, AL>(acc, rows, cols, tid,
+                          [&](int m, int n, f4 v, int k) { store_n(o + (int64_t)m * a.n_out + n, v, k, AL); });
   } else {
     T* o = a.dw + at;
-    for_results<S, AL>(acc, rows, cols, tid,
-                   [&](int m, int n, f4 v, int k) { store4(o + (int64_t)m * a.n_out + n, v, k, AL); });
+    for_results<S, lane_width<T>, AL>(acc, rows, cols, tid,
+                                      [&](int m, int n, auto v, int k) { store_n(o + (int64_t)m * a.n_out + n, v, k, AL); });
   }
 }
 
@@ -415,10 +561,10 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const float* __restric
   if (i >= size) return;
   const bool vec = size % 4 == 0;   // (part and out begin at multiples of 16 bytes, or vec is not taken)
   const int k = (int)min<int64_t>(4, size - i);
-  f4 s = read4(part + i, k, vec);
-  for (int p = 1; p < splits; ++p) s += read4(part + p * size + i, k, vec);
+  f4 s = read_n<4>(part + i, k, vec);
+  for (int p = 1; p < splits; ++p) s += read_n<4>(part + p * size + i, k, vec);
   const bool out_vec = vec && (reinterpret_cast<uintptr_t>(out) & (4 * sizeof(T) - 1)) == 0;
-  store4(out + i, s, k, out_vec);
+  store_n(out + i, s, k, out_vec);
 }
 
 // dz = dy act'(z) over a run of rows (where there is an activation), and the
@@ -526,6 +672,18 @@ using Thin2 = ThinShape<2, 2>;
 constexpr int64_t kThinBlocks = 192;
 bool thin(int64_t rows, int64_t cols) { return ceil_div(rows, 64) * ceil_div(cols, 64) < kThinBlocks; }
 bool thin2(int64_t rows, int64_t cols) { return ceil_div(rows, 32) * ceil_div(cols, 32) >= kFillBlocks; }
+// sums of K short enough for narrow_rows, and rows for at least kNarrowBlocks waves of 64 columns
+constexpr int64_t kNarrowBlocks = 1024;
+template <class T> bool narrow(int64_t rows, int64_t cols, int K) {
+  return K <= (sizeof(T) == 4 ? 64 : 128) && ceil_div(rows, 512) * ceil_div(cols, 64) >= kNarrowBlocks;
+}
+template <class T, class F>
+mace_status with_narrow(int K, F f) {
+  if (K <= 32) return f(NarrowShape<T, 1>{});
+  if constexpr (sizeof(T) == 2)
+    if (K > 64) return f(NarrowShape<T, 4>{});
+  return f(NarrowShape<T, 2>{});
+}
 enum { kSmall, kMid, kLarge };
 int shape_of(int64_t rows, int64_t cols, int64_t batch = 1) {
   if (ceil_div(rows, 256) * ceil_div(cols, 256) * batch >= kLargeBlocks) return kLarge;
@@ -584,6 +742,14 @@ mace_status forward(const mace_linear_desc& d, const void* x, const void* w, con
                   near(d.ld_x);
   auto go = [&](auto al_) -> mace_status {
     constexpr bool AL = decltype(al_)::value;
+    if (narrow<T>(d.n_rows, d.n_out, d.n_in))
+      return with_narrow<T>(d.n_in, [&](auto shape) -> mace_status {
+        using S = decltype(shape);
+        const int64_t blocks = (ceil_div(d.n_rows, S::RUN) + (offsets ? d.n_groups : 0)) * ceil_div(d.n_out, S::BN);
+        if (blocks > INT32_MAX) return MACE_EUNSUPPORTED;
+        linear_fwd_narrow_kernel<T, AL, S><<<(unsigned)blocks, S::NT, 0, s>>>(a);
+        return launched();
+      });
     if constexpr (sizeof(T) == 4)
       if (thin(d.n_rows, d.n_out)) {
         auto run = [&](auto shape) {
@@ -638,7 +804,21 @@ mace_status backward(const mace_linear_desc& d, const void* dy, int64_t lddy, co
   const WeightGradArgs<T> wa{(const T*)x, dz, (T*)dw, p.splits > 1 ? reinterpret_cast<float*>(ws + p.part) : nullptr,
                              offsets, d.n_rows, d.ld_x, lddz, d.n_in, d.n_out, d.n_groups, p.splits};
   const BiasGradArgs<T> ba{sums, (T*)db, offsets, d.n_rows, d.n_out, slope_run(d.n_rows), (int)slope_runs(d)};
-  const bool want_x = dx && d.n_rows > 0;
+  bool want_x = dx && d.n_rows > 0;
+  if (want_x && narrow<T>(d.n_rows, d.n_in, d.n_out)) {
+    auto run = [&](auto al_) {
+      constexpr bool AL = decltype(al_)::value;
+      return with_narrow<T>(d.n_out, [&](auto shape) -> mace_status {
+        using S = decltype(shape);
+        const int64_t blocks = (ceil_div(d.n_rows, S::RUN) + (offsets ? d.n_groups : 0)) * ceil_div(d.n_in, S::BN);
+        if (blocks > INT32_MAX) return MACE_EUNSUPPORTED;
+        linear_row_grad_narrow_kernel<T, AL, S><<<(unsigned)blocks, S::NT, 0, s>>>(ra);
+        return launched();
+      });
+    };
+    if ((st = al ? run(Int<1>{}) : run(Int<0>{})) != MACE_OK) return st;
+    want_x = false;
+  }
   const bool thin_x = sizeof(T) == 4 && want_x && thin(d.n_rows, d.n_in);
   // one launch for all three where dx and dW take the same kind of tile (thin
   // tiles of dx go with small ones of dW)

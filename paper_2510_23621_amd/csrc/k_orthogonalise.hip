@@ -33,13 +33,14 @@ struct PairMat {
 };
 
 typedef _Float16 h4 __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ f4 read_pair(const _Float16* p, int64_t plane) {
-  return __builtin_convertvector(*reinterpret_cast<const h4*>(p), f4) +
-         __builtin_convertvector(*reinterpret_cast<const h4*>(p + plane), f4);
+template <int W = 4>
+__device__ __forceinline__ typename Floats<W>::type read_pair(const _Float16* p, int64_t plane) {
+  return read_n<W>(p, W, true) + read_n<W>(p + plane, W, true);
 }
-__device__ __forceinline__ void split_pair(f4 v, h4& hi, h4& lo) {
-  hi = __builtin_convertvector(v, h4);
-  lo = __builtin_convertvector(v - __builtin_convertvector(hi, f4), h4);
+template <class V, class H>
+__device__ __forceinline__ void split_pair(V v, H& hi, H& lo) {
+  hi = __builtin_convertvector(v, H);
+  lo = __builtin_convertvector(v - __builtin_convertvector(hi, V), H);
 }
 
 // ------------------------------------------------------------------ norm and packing
@@ -253,33 +254,51 @@ template <int LD>
 __device__ __forceinline__ int fit_chunk(int i, int j) {
   return i * LD + (((j >> 3) ^ (((i & 3) << 1) | ((i >> 2) & 1))) << 3);
 }
+// (a fragment's chunk is (k / 8 + lane / 16) ^ swizzle with k a multiple of 32: one
+// XOR of k onto the lane's place at k = 0)
 template <int LD>
 __device__ __forceinline__ us8 fit_rows(const unsigned short* t, int row0, int k0, int lane) {
-  return *reinterpret_cast<const us8*>(t + fit_chunk<LD>(row0 + (lane & 15), k0 + 8 * (lane >> 4)));
+  return *reinterpret_cast<const us8*>(t + (fit_chunk<LD>(row0 + (lane & 15), 8 * (lane >> 4)) ^ k0));
 }
 template <int LD>
 __device__ __forceinline__ us8 fit_cols(const unsigned short* t, int col0, int k0, int lane) {
   typedef __attribute__((address_space(3))) s4 lds_s4;
   typedef short s8_ __attribute__((ext_vector_type(8)));
-  const int i = lane & 15, k = k0 + 8 * (lane >> 4) + (i >> 2), c = col0 + 4 * (i & 3);
-  const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(t + fit_chunk<LD>(k, c) + (c & 7)));
-  const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(t + fit_chunk<LD>(k + 4, c) + (c & 7)));
+  const int i = lane & 15, k = 8 * (lane >> 4) + (i >> 2), c = col0 + 4 * (i & 3);
+  const unsigned short* p = t + k0 * LD;   // (k0 does not change the swizzle)
+  const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(p + fit_chunk<LD>(k, c) + (c & 7)));
+  const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(p + fit_chunk<LD>(k + 4, c) + (c & 7)));
   const s8_ r = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   return __builtin_bit_cast(us8, r);
 }
 
-// D (R x C) = P Q over K on 8 waves as WR x WC parts; the lane's results in
+// D (R x C) = P Q over K on a 4 x 4 grid of waves; the lane's results in
 // acc[j][i]: row 16 i + l%16 and columns 16 j + 4 (l/16) + 0..3 of its wave's
-// part. QC: Q[k][c] is x itself, else Q = src^T and its columns are src's rows.
-template <int R, int C, int K, int LDP, int LDQ, bool QC, int WR, int WC>
+// part. QC: Q[k][c] is x itself, else Q = src^T and its columns are src's rows. SYM:
+// D is symmetric: the ten waves of the lower triangle of parts work, the others'
+// parts are mirrored by the caller.
+constexpr int kFitThreads = 1024;
+template <int R, int C, int K, int LDP, int LDQ, bool QC, bool SYM>
 struct FitProduct {
-  static constexpr int TI = R / WR / 16, TJ = C / WC / 16;
+  static constexpr int TI = R / 64, TJ = C / 64;
   f4 acc[TJ][TI];
   int r0, c0;
+  bool on;
+  __device__ __forceinline__ void place(int tid) {
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int wr = w >> 2, wc = w & 3;
+    on = true;
+    if constexpr (SYM) {
+      on = w < 10;
+      wr = w < 1 ? 0 : (w < 3 ? 1 : (w < 6 ? 2 : 3));
+      wc = w - wr * (wr + 1) / 2;
+    }
+    r0 = wr * (R / 4);
+    c0 = wc * (C / 4);
+  }
   __device__ __forceinline__ void run(const unsigned short* p, int plane_p, const unsigned short* q, int plane_q, int tid) {
-    const int lane = tid & 63, w = tid >> 6;
-    r0 = w / WC * (R / WR);
-    c0 = w % WC * (C / WC);
+    const int lane = tid & 63;
+    if (!on) return;
 #pragma unroll
     for (int j = 0; j < TJ; ++j)
 #pragma unroll
@@ -297,15 +316,15 @@ struct FitProduct {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
           a[h] = QC ? fit_cols<LDQ>(q + h * plane_q, c0 + 16 * j, k, lane) : fit_rows<LDQ>(q + h * plane_q, c0 + 16 * j, k, lane);
-#pragma unroll
-        for (int i = 0; i < TI; ++i) acc[j][i] = products<HalfPair, 2>(a, b[i], acc[j][i]);
+        products<HalfPair>(a, b, acc[j]);
       }
     }
   }
-  // f(row, column, values)
+  // f(row, column, values, number)
   template <class F>
   __device__ __forceinline__ void each(int tid, F f) const {
     const int lane = tid & 63;
+    if (!on) return;
 #pragma unroll
     for (int i = 0; i < TI; ++i)
 #pragma unroll
@@ -326,20 +345,35 @@ __device__ __forceinline__ void fit_write(unsigned short* t, int plane, int i, i
   *reinterpret_cast<h4*>(p + plane) = lo;
 }
 
+// the same at (i, j) .. (i, j + 3) and, where mirror, at the transposed places
+template <int LD>
+__device__ __forceinline__ void fit_write_symmetric(unsigned short* t, int plane, int i, int j, f4 v, bool mirror) {
+  fit_write<LD>(t, plane, i, j, v);
+  if (!mirror) return;
+  h4 hi, lo;
+  split_pair(v, hi, lo);
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    unsigned short* p = t + fit_chunk<LD>(j + c, i) + (i & 7);
+    p[0] = __builtin_bit_cast(unsigned short, (_Float16)hi[c]);
+    p[plane] = __builtin_bit_cast(unsigned short, (_Float16)lo[c]);
+  }
+}
+
 template <class T, int MM, int NN>
-__global__ void __launch_bounds__(512)
+__global__ void __launch_bounds__(kFitThreads)
 ns_fit_kernel(const T* g, int64_t stride, int64_t ld, int m, int n, bool tall, double eps, NsSteps steps, T* out,
               int64_t ostride, int64_t old) {
-  constexpr int PX = MM * NN, PA = MM * MM, QUADS = MM * NN / 4 / 512;
+  constexpr int PX = MM * NN, PA = MM * MM, QUADS = MM * NN / 4 / kFitThreads;
   extern __shared__ __align__(16) unsigned short fit_lds[];
   unsigned short *x = fit_lds, *A = fit_lds + 2 * PX;
-  __shared__ double red[8];
+  __shared__ double red[kFitThreads / 64];
   const int tid = threadIdx.x;
   const T* src = g + (int64_t)blockIdx.x * stride;
   T* dst = out + (int64_t)blockIdx.x * ostride;
   // quads of four columns; lanes run along g's contiguous axis
   auto place = [&](int u, int& i, int& j) {
-    const int q = tid + 512 * u;
+    const int q = tid + kFitThreads * u;
     i = tall ? q % MM : q / (NN / 4);
     j = 4 * (tall ? q / MM : q % (NN / 4));
   };
@@ -359,7 +393,7 @@ ns_fit_kernel(const T* g, int64_t stride, int64_t ld, int m, int n, bool tall, d
   if ((tid & 63) == 0) red[tid >> 6] = s;
   __syncthreads();
   s = 0.0;
-  for (int i = 0; i < 8; ++i) s += red[i];
+  for (int i = 0; i < kFitThreads / 64; ++i) s += red[i];
   const double inv = kScaleX / (sqrt(s) + eps);
 #pragma unroll
   for (int u = 0; u < QUADS; ++u) {
@@ -370,47 +404,59 @@ ns_fit_kernel(const T* g, int64_t stride, int64_t ld, int m, int n, bool tall, d
     fit_write<NN>(x, PX, i, j, v[u]);
   }
   __syncthreads();
-  constexpr int WC = MM == 64 ? 4 : 2, WR = 8 / WC;
+  // a wave's parts of x and A stay with it in FP32; LDS holds what the others multiply
+  using Gram = FitProduct<MM, MM, NN, NN, NN, false, true>;
+  using Square_ = FitProduct<MM, MM, MM, MM, MM, false, true>;
+  using Update = FitProduct<MM, NN, MM, MM, NN, true, false>;
+  f4 xr[Update::TI * Update::TJ];
+  {
+    Update p;
+    p.place(tid);
+    p.each(tid, [&](int i, int j, f4, int e) { xr[e] = fit_read<NN>(x, PX, i, j); });
+  }
   for (int st = 0; st < steps.n; ++st) {
     const float ca = (float)steps.c[st][0], cb = (float)steps.c[st][1] * (kScaleB / kScaleA),
                 cc = (float)steps.c[st][2] * (kScaleB / (kScaleA * kScaleA));
+    f4 ar[Gram::TI * Gram::TJ];
     {
-      FitProduct<MM, MM, NN, NN, NN, false, WR, WC> p;
+      Gram p;
+      p.place(tid);
       p.run(x, PX, x, PX, tid);
-      p.each(tid, [&](int i, int j, f4 r, int) { fit_write<MM>(A, PA, i, j, r * (kScaleA / (kScaleX * kScaleX))); });
+      p.each(tid, [&](int i, int j, f4 r, int e) {
+        ar[e] = r * (kScaleA / (kScaleX * kScaleX));
+        fit_write_symmetric<MM>(A, PA, i, j, ar[e], p.r0 != p.c0);
+      });
     }
     __syncthreads();
     {
-      FitProduct<MM, MM, MM, MM, MM, false, WR, WC> p;
+      Square_ p;
+      p.place(tid);
       p.run(A, PA, A, PA, tid);
-      f4 b[p.TI * p.TJ];
-      p.each(tid, [&](int i, int j, f4 r, int e) { b[e] = cc * r + cb * fit_read<MM>(A, PA, i, j); });
       __syncthreads();
-      p.each(tid, [&](int i, int j, f4, int e) { fit_write<MM>(A, PA, i, j, b[e]); });
+      p.each(tid, [&](int i, int j, f4 r, int e) {
+        fit_write_symmetric<MM>(A, PA, i, j, cc * r + cb * ar[e], p.r0 != p.c0);
+      });
     }
     __syncthreads();
-    {
-      FitProduct<MM, NN, MM, MM, NN, true, WR, WC> p;
-      p.run(A, PA, x, PX, tid);
-      const bool last = st + 1 == steps.n;
-      f4 b[p.TI * p.TJ];
-      p.each(tid, [&](int i, int j, f4 r, int e) { b[e] = (1.f / kScaleB) * r + ca * fit_read<NN>(x, PX, i, j); });
-      if (!last) {
-        __syncthreads();
-        p.each(tid, [&](int i, int j, f4, int e) { fit_write<NN>(x, PX, i, j, b[e]); });
-        __syncthreads();
-      } else {
-        p.each(tid, [&](int i, int j, f4, int e) {
-          if (i >= m) return;
+    Update p;
+    p.place(tid);
+    p.run(A, PA, x, PX, tid);
+    p.each(tid, [&](int i, int j, f4 r, int e) { xr[e] = (1.f / kScaleB) * r + ca * xr[e]; });
+    if (st + 1 < steps.n) {
+      __syncthreads();
+      p.each(tid, [&](int i, int j, f4, int e) { fit_write<NN>(x, PX, i, j, xr[e]); });
+      __syncthreads();
+    } else {
+      p.each(tid, [&](int i, int j, f4, int e) {
+        if (i >= m) return;
 #pragma unroll
-          for (int c = 0; c < 4; ++c)
-            if (j + c < n) {
-              const T r = (T)(b[e][c] * (1.f / kScaleX));
-              if (tall) dst[(int64_t)(j + c) * old + i] = r;
-              else dst[(int64_t)i * old + j + c] = r;
-            }
-        });
-      }
+        for (int c = 0; c < 4; ++c)
+          if (j + c < n) {
+            const T r = (T)(xr[e][c] * (1.f / kScaleX));
+            if (tall) dst[(int64_t)(j + c) * old + i] = r;
+            else dst[(int64_t)i * old + j + c] = r;
+          }
+      });
     }
   }
 }
@@ -448,15 +494,15 @@ __global__ void __launch_bounds__(S::NT) ns_symmetric_kernel(PairMat src, PairMa
                                      operand<T>(src, b, (int64_t)c0 * src.ld, m - c0), K, lds, tid, acc);
   _Float16* o = out.p + b * out.stride;
   const _Float16* a = src.p + b * src.stride;
-  for_results<S, false>(acc, min(S::BM, m - r0), min(S::BN, m - c0), tid, [&](int i, int j, f4 v, int k) {
+  for_results<S, 8, false>(acc, min(S::BM, m - r0), min(S::BN, m - c0), tid, [&](int i, int j, f8 v, int k) {
     const int64_t at = (int64_t)(r0 + i) * out.ld + c0 + j;
     v *= cp;
-    if constexpr (POLY) v += ca * read_pair(a + at, src.plane);   // (A and B have the same pitch)
-    h4 hi, lo;
+    if constexpr (POLY) v += ca * read_pair<8>(a + at, src.plane);   // (A and B have the same pitch)
+    h8 hi, lo;
     split_pair(v, hi, lo);
-    if (k == 4) {
-      *reinterpret_cast<h4*>(o + at) = hi;
-      *reinterpret_cast<h4*>(o + at + out.plane) = lo;
+    if (k == 8) {
+      *reinterpret_cast<h8*>(o + at) = hi;
+      *reinterpret_cast<h8*>(o + at + out.plane) = lo;
     } else {
       for (int q = 0; q < k; ++q) {
         o[at + q] = hi[q];
@@ -465,7 +511,7 @@ __global__ void __launch_bounds__(S::NT) ns_symmetric_kernel(PairMat src, PairMa
     }
     if (tm != tn)
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
+      for (int q = 0; q < 8; ++q)
         if (q < k) {
           const int64_t t = (int64_t)(c0 + j + q) * out.ld + r0 + i;
           o[t] = hi[q];
@@ -490,24 +536,25 @@ ns_update_kernel(PairMat B, PairMat x, PairMat xo, int m, int n, float ca, float
   tile_gemm_direct<T, S, true, false>(operand<T>(B, b, (int64_t)r0 * B.ld, m - r0), operand<T>(x, b, c0, x.ld - c0), m,
                                       lds, tid, acc);
   const _Float16* xi = x.p + b * x.stride;
-  for_results<S, true>(acc, min(S::BM, m - r0), min(S::BN, x.ld - c0), tid, [&](int i, int j, f4 v, int k) {
+  for_results<S, 8, true>(acc, min(S::BM, m - r0), min(S::BN, x.ld - c0), tid, [&](int i, int j, f8 v, int k) {
     const int64_t at = (int64_t)(r0 + i) * x.ld + c0 + j;   // (whole vectors: the pitch is a multiple of 8)
-    v = cp * v + ca * read_pair(xi + at, x.plane);
+    v = cp * v + ca * read_pair<8>(xi + at, x.plane);
     if (out) {
       v *= 1.f / kScaleX;
       O* o = out + b * ostride;
+      if (!tall) {
+        store_n(o + (int64_t)(r0 + i) * old + c0 + j, v, min(8, n - c0 - j), false);
+      } else {
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        if (c0 + j + q < n) {
-          if (tall) o[(int64_t)(c0 + j + q) * old + r0 + i] = (O)v[q];
-          else o[(int64_t)(r0 + i) * old + c0 + j + q] = (O)v[q];
-        }
+        for (int q = 0; q < 8; ++q)
+          if (c0 + j + q < n) o[(int64_t)(c0 + j + q) * old + r0 + i] = (O)v[q];
+      }
     } else {
-      h4 hi, lo;
+      h8 hi, lo;
       split_pair(v, hi, lo);
       _Float16* o = xo.p + b * xo.stride + at;
-      *reinterpret_cast<h4*>(o) = hi;
-      *reinterpret_cast<h4*>(o + xo.plane) = lo;
+      *reinterpret_cast<h8*>(o) = hi;
+      *reinterpret_cast<h8*>(o + xo.plane) = lo;
     }
   });
 }
@@ -528,19 +575,34 @@ mace_status check(const mace_orthogonalise_desc* d) {
   return MACE_OK;
 }
 
-// whether every step keeps its operands in range (mace.h)
-bool in_range(const double* c, int steps) {
+// whether every step keeps its operands in range (mace.h): the largest singular
+// value after each step and the largest b l + c l^2, l its square, at the ends of
+// the range and where their derivatives vanish
+bool in_range(const double* k, int steps) {
   double r = 1.0;   // largest singular value so far
-  for (int s = 0; s < steps; ++s, c += 3) {
-    if (!std::isfinite(c[0]) || !std::isfinite(c[1]) || !std::isfinite(c[2])) return false;
-    double next = 0.0;
-    for (int i = 0; i <= 2048; ++i) {
-      const double v = r * i / 2048.0, l = v * v, B = c[1] * l + c[2] * l * l;
-      if (!(std::fabs(B) <= kMaxB)) return false;
-      next = std::max(next, std::fabs((c[0] + B) * v));
+  for (int s = 0; s < steps; ++s, k += 3) {
+    const double a = k[0], b = k[1], c = k[2];
+    if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
+    double top = 0.0, next = 0.0;
+    auto at = [&](double l) {   // l clamped to the range: a point outside gives its end
+      l = std::min(std::max(l, 0.0), r * r);
+      const double B = b * l + c * l * l;
+      top = std::max(top, std::fabs(B));
+      next = std::max(next, std::fabs(a + B) * std::sqrt(l));
+    };
+    at(r * r);
+    if (c != 0.0) {
+      at(-b / (2.0 * c));
+      const double d = 9.0 * b * b - 20.0 * a * c;   // a + 3 b l + 5 c l^2 = 0
+      if (d >= 0.0) {
+        at((-3.0 * b + std::sqrt(d)) / (10.0 * c));
+        at((-3.0 * b - std::sqrt(d)) / (10.0 * c));
+      }
+    } else if (b != 0.0) {
+      at(-a / (3.0 * b));
     }
-    r = next * 1.001;   // (between the sample points, and rounding)
-    if (!(r <= kMaxSigma)) return false;
+    r = next * 1.001;   // (rounding)
+    if (!(top <= kMaxB) || !(r <= kMaxSigma)) return false;
   }
   return true;
 }
@@ -626,7 +688,7 @@ mace_status run_fit(const mace_orthogonalise_desc& d, const NsPlan& p, const NsS
   if (bytes > 65536 && hipFuncSetAttribute(reinterpret_cast<const void*>(f), hipFuncAttributeMaxDynamicSharedMemorySize,
                                            bytes) != hipSuccess)
     return MACE_EHIP;
-  f<<<(unsigned)d.batch, 512, bytes, s>>>(g, d.stride_g, d.ld_g, p.m, p.n, p.tall, d.eps, steps, out, d.stride_out,
+  f<<<(unsigned)d.batch, kFitThreads, bytes, s>>>(g, d.stride_g, d.ld_g, p.m, p.n, p.tall, d.eps, steps, out, d.stride_out,
                                           d.ld_out);
   return launched();
 }

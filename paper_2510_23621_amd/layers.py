@@ -237,6 +237,7 @@ def route_rows_backward(drows, plan: Route, *, stream=None):
 
 @lru_cache(maxsize=64)
 def _coefficients(steps: tuple) -> np.ndarray:
+    """float64 [n, 3] on the host; a training run has one or a few such schedules."""
     return np.ascontiguousarray(steps, dtype=np.float64).reshape(-1, 3)
 
 
@@ -247,7 +248,7 @@ def orthogonalise(g, coefficients=NEWTON_SCHULZ, *, eps: float = 1e-7):
     dtype = DTYPES.get(g.dtype)
     if dtype is None or g.dim() not in (2, 3) or not g.is_cuda:
         raise ValueError("g must be a [(batch,) rows, cols] GPU tensor of float32, bfloat16 or float16")
-    coef = _coefficients(tuple(tuple(float(v) for v in c) for c in coefficients))
+    coef = _coefficients(coefficients if type(coefficients) is tuple else tuple(map(tuple, coefficients)))
     if g.dim() == 3:
         (b, rows, cols), (sb, s0, s1) = g.shape, g.stride()
     else:

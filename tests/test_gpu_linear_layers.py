@@ -224,3 +224,17 @@ def test_other_stream_and_graph():
         torch.cuda.synchronize()
         for a, b in zip((y1, z1, *g1), (want, z, dx, dw, db)):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("n,n_in,n_out", [(30000, 64, 1280), (50011, 33, 1023), (40000, 20, 1000), (8209, 1100, 64),
+                                          (21000, 1600, 51), (25000, 120, 1400)])
+def test_short_sums_over_many_rows(n, n_in, n_out, dtype):
+    """Launches that keep the weights in registers, in the forward or for dx."""
+    case(n, n_in, n_out, dtype, "silu", seed=4, residual=False)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_short_sums_in_groups(dtype):
+    case(None, 48, 1500, dtype, "gelu", [0, 20000, 1, 513, 12000, 511], 600, seed=4)
+    case(None, 1500, 48, dtype, "none", [0, 20000, 1, 513, 12000, 511], 600, seed=4, residual=False)
