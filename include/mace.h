@@ -403,12 +403,13 @@ mace_status mace_route_combine_backward(const mace_route_desc* desc, const void*
  * singular values that can occur (0 to 1 at the start) no step may reach a
  * singular value beyond 3.4 or a b A + c A A beyond 200, else MACE_ERANGE
  * (the products' operands are pairs of binary16 with fixed scales).  Products
- * are as accurate as FP32's (in FP64 where the shorter side is at most 32); a
- * BF16 result of at least 128 rows and columns takes all but its last two steps
- * with binary16 operands, whose error stays below a third of the result's
- * rounding.  A matrix with a non-finite
- * element gives NaN, the others of the batch are not touched by it.  rows and
- * cols <= 2^15, batch * rows * cols <= 2^34, else MACE_EUNSUPPORTED.
+ * are as accurate as FP32's (in FP64 where the shorter side is at most 32, or at
+ * most 64 and the longer beyond 128); a BF16 result with both sides at least 128
+ * and one beyond takes all but its last two steps with binary16 operands, whose
+ * error stays below a third of the result's rounding.  A matrix with a
+ * non-finite element gives NaN, the others of the batch are not touched by it.
+ * rows and cols <= 2^15, batch <= 65535, batch * rows * cols <= 2^34, else
+ * MACE_EUNSUPPORTED.
  * workspace (dev) of at least mace_orthogonalise_workspace_bytes (0 on
  * invalid input). */
 typedef struct mace_orthogonalise_desc {

@@ -528,7 +528,14 @@ __device__ __forceinline__ void bias_grad(const BiasGradArgs<T>& a, int id, floa
   runs = min(runs, a.max_runs - first);   // (offsets that do not rise could count more runs than there are sums)
   float s = 0.f;
   if (col < a.n_out && y < 4)
-    for (int r = y; r < runs; r += 4) s += a.sums[(int64_t)(first + r) * a.n_out + col];
+    for (int r = y; r < runs; r += 32) {   // eight loads in flight, added in order
+      float v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v[u] = a.sums[(int64_t)(first + min(r + 4 * u, runs - 1)) * a.n_out + col];
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (r + 4 * u < runs) s += v[u];
+    }
   if (y < 4) lds[y * 64 + c] = s;
   __syncthreads();
   if (y == 0 && col < a.n_out) a.db[(int64_t)g * a.n_out + col] = (T)(s + lds[64 + c] + lds[128 + c] + lds[192 + c]);
@@ -561,8 +568,15 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const float* __restric
   if (i >= size) return;
   const bool vec = size % 4 == 0;   // (part and out begin at multiples of 16 bytes, or vec is not taken)
   const int k = (int)min<int64_t>(4, size - i);
-  f4 s = read_n<4>(part + i, k, vec);
-  for (int p = 1; p < splits; ++p) s += read_n<4>(part + p * size + i, k, vec);
+  f4 s = {0.f, 0.f, 0.f, 0.f};
+  for (int p = 0; p < splits; p += 8) {   // eight loads in flight, added in order
+    f4 v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] = read_n<4>(part + min(p + u, splits - 1) * size + i, k, vec);
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (p + u < splits) s += v[u];
+  }
   const bool out_vec = vec && (reinterpret_cast<uintptr_t>(out) & (4 * sizeof(T) - 1)) == 0;
   store_n(out + i, s, k, out_vec);
 }

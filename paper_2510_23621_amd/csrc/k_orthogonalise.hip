@@ -7,7 +7,7 @@
 // in place of six. Per step: A = x x^T and B = b A + c A A, both symmetric (one
 // half computed, the other mirrored), x <- a x + B x.
 //
-// With at most kGramMax rows the iteration runs on A alone, in FP64: every x is a
+// With few rows (kGramMax, kGramMaxLong) the iteration runs on A alone, in FP64: every x is a
 // polynomial of A_0 = x_0 x_0^T times x_0, so A <- P A P and Q <- P Q with
 // P = a + b A + c A A, and the result is Q x_0: two passes over the data instead of
 // two per step. FP64 because A holds the squares of the singular values and a
@@ -124,7 +124,9 @@ ns_scale_kernel(const T* __restrict__ g, int64_t stride, int64_t ld, int rows, i
 }
 
 // ------------------------------------------------------------------ few rows
-constexpr int kGramMax = 32, kGramChunk = 256;
+// FP64 up to 32 rows, and up to 64 of matrices too long for LDS
+constexpr int kGramMax = 32, kGramMaxLong = 64, kGramChunk = 256;
+constexpr int kFitMax = 128;   // longest side of a matrix iterated in LDS
 
 // element (i, j) of x's layout in g
 template <class T>
@@ -132,116 +134,184 @@ __device__ __forceinline__ float element(const T* g, int64_t ld, bool tall, int 
   return to_f32(tall ? g[(int64_t)j * ld + i] : g[(int64_t)i * ld + j]);
 }
 
-// A = g g^T over a chunk of columns; thread (ti, tj) sums a 2 x 2 block
-template <class T>
-__global__ void __launch_bounds__(256) ns_gram64_kernel(const T* __restrict__ g, int64_t stride, int64_t ld, int m, int n,
-                                                        bool tall, double* __restrict__ part) {
-  __shared__ float t[kGramMax][kGramChunk + 1];
-  const int tid = threadIdx.x, j0 = blockIdx.x * kGramChunk, w = min(kGramChunk, n - j0);
-  const T* src = g + (int64_t)blockIdx.y * stride;
-  const int m2 = (m + 1) & ~1;
-  for (int e = tid; e < m2 * kGramChunk; e += 256) {
-    const int i = tall ? e % m2 : e / kGramChunk, j = tall ? e / m2 : e % kGramChunk;
-    t[i][j] = i < m && j < w ? element(src, ld, tall, i, j0 + j) : 0.f;
-  }
-  __syncthreads();
-  const int ti = 2 * (tid >> 4), tj = 2 * (tid & 15);
-  if (ti >= m || tj >= m) return;
-  double s[2][2] = {};
-  for (int j = 0; j < w; ++j) {
-    const double a0 = t[ti][j], a1 = t[ti + 1][j], b0 = t[tj][j], b1 = t[tj + 1][j];
-    s[0][0] += a0 * b0;
-    s[0][1] += a0 * b1;
-    s[1][0] += a1 * b0;
-    s[1][1] += a1 * b1;
-  }
-  double* o = part + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * m * m;
-  for (int p = 0; p < 2; ++p)
-    for (int q = 0; q < 2; ++q)
-      if (ti + p < m && tj + q < m) o[(ti + p) * m + tj + q] = s[p][q];
+// Squares of R = 16, 32 or 64 rows, padded with zeros, on FP64 MFMA
+// (v_mfma_f64_16x16x4: lane l holds A[l%16][l/16] and B[l/16][l%16], register r of the
+// result is D[l/16 + 4 r][l%16]), a 16 x 16 tile per wave; R = 16 leaves three of four
+// waves idle.
+typedef double d4 __attribute__((ext_vector_type(4)));
+template <int R> constexpr int kThreads64 = R == 64 ? 1024 : 256;
+template <int R> struct Square { double v[R][R + 1]; };
+template <int R> struct Columns { float v[R][kGramChunk + 2]; };   // (a column of the four k groups per bank)
+
+template <int R, class F>
+__device__ __forceinline__ void each64(int tid, const d4& acc, F f) {   // f(row, column, value)
+  const int l = tid & 63, w = tid >> 6;
+  if (w >= (R / 16) * (R / 16)) return;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) f(16 * (w / (R / 16)) + (l >> 4) + 4 * q, 16 * (w % (R / 16)) + (l & 15), acc[q]);
+}
+// this wave's tile of A B over K, a(row, k) and b(k, column)
+template <int R, class FA, class FB>
+__device__ __forceinline__ d4 multiply64(int tid, int K, FA a, FB b) {
+  const int l = tid & 63, w = tid >> 6, i = l & 15, g = l >> 4;
+  d4 acc = {0.0, 0.0, 0.0, 0.0};
+  if (w >= (R / 16) * (R / 16)) return acc;
+  const int r = 16 * (w / (R / 16)) + i, c = 16 * (w % (R / 16)) + i;
+#pragma unroll 8
+  for (int k = 0; k < K; k += 4) acc = __builtin_amdgcn_mfma_f64_16x16x4f64(a(r, k + g), b(k + g, c), acc, 0, 0, 0);
+  return acc;
 }
 
+// columns j0 .. j0 + kGramChunk of x's layout, zeros outside it; all loads in flight at once
+template <int R, class T>
+__device__ __forceinline__ void load_columns(Columns<R>& t, const T* src, int64_t ld, int m, int n, int j0, bool tall, int tid) {
+  constexpr int NT = kThreads64<R>, U = R * kGramChunk / NT;
+  const int w = min(kGramChunk, n - j0);
+  auto place = [&](int u, int& i, int& j) {   // lanes along g's contiguous axis
+    const int e = tid + NT * u;
+    i = tall ? e % R : e / kGramChunk;
+    j = tall ? e / R : e % kGramChunk;
+  };
+  T v[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    int i, j;
+    place(u, i, j);
+    i = min(i, m - 1);
+    j = j0 + min(j, w - 1);
+    v[u] = tall ? src[(int64_t)j * ld + i] : src[(int64_t)i * ld + j];
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    int i, j;
+    place(u, i, j);
+    t.v[i][j] = i < m && j < w ? to_f32(v[u]) : 0.f;
+  }
+}
+// A = t t^T of the chunk's columns
+template <int R>
+__device__ __forceinline__ d4 gram64(const Columns<R>& t, int w, int tid) {
+  return multiply64<R>(tid, (w + 3) & ~3, [&](int r, int k) { return (double)t.v[r][k]; },
+                       [&](int k, int c) { return (double)t.v[c][k]; });
+}
+// the iteration on A = g g^T: Q <- Q / (|g| + eps), |g|^2 being the trace of A
 struct NsSteps {
   double c[64][3];
   int n;
 };
-
-typedef double Square[kGramMax][kGramMax + 1];
-__device__ __forceinline__ void multiply64(const Square& a, const Square& b, Square& c, int m, int tid) {   // c = a b
-  for (int e = tid; e < m * m; e += 256) {
-    const int i = e / m, j = e - i * m;
-    double s = 0.0;
-    for (int k = 0; k < m; ++k) s += a[i][k] * b[k][j];
-    c[i][j] = s;
-  }
-  __syncthreads();
-}
-
-// q = Q / (|g| + eps) of one matrix from the chunks' sums; |g|^2 is the trace
-__global__ void __launch_bounds__(256)
-ns_iterate64_kernel(const double* __restrict__ part, int chunks, int m, double eps, NsSteps steps, double* __restrict__ q) {
-  __shared__ Square A, P, Q, T;
-  __shared__ double s_inv;
-  const int tid = threadIdx.x;
-  const double* p = part + (int64_t)blockIdx.x * chunks * m * m;
-  for (int e = tid; e < m * m; e += 256) {
-    double s = 0.0;
-    for (int c = 0; c < chunks; ++c) s += p[(int64_t)c * m * m + e];
-    A[e / m][e % m] = s;
-    Q[e / m][e % m] = e / m == e % m ? 1.0 : 0.0;
-  }
-  __syncthreads();
-  if (tid == 0) {
-    double tr = 0.0;
-    for (int i = 0; i < m; ++i) tr += A[i][i];
-    s_inv = 1.0 / (sqrt(tr) + eps);
+template <int R>
+__device__ __forceinline__ void iterate64(Square<R>& A, Square<R>& P, Square<R>& Q, Square<R>& T, double& s_inv, double eps,
+                                          const NsSteps& steps, int tid) {
+  if (tid < 64) {
+    double tr = tid < R ? A.v[tid][tid] : 0.0;
+    for (int d = 32; d; d >>= 1) tr += __shfl_xor(tr, d);
+    if (tid == 0) s_inv = 1.0 / (sqrt(tr) + eps);
   }
   __syncthreads();
   const double inv = s_inv;
-  for (int e = tid; e < m * m; e += 256) A[e / m][e % m] = A[e / m][e % m] * inv * inv;
+  for (int e = tid; e < R * R; e += kThreads64<R>) {
+    A.v[e / R][e % R] *= inv * inv;
+    Q.v[e / R][e % R] = e / R == e % R ? 1.0 : 0.0;
+  }
   __syncthreads();
+  auto product = [&](const Square<R>& a, const Square<R>& b) {
+    return multiply64<R>(tid, R, [&](int r, int k) { return a.v[r][k]; }, [&](int k, int c) { return b.v[k][c]; });
+  };
   for (int st = 0; st < steps.n; ++st) {
     const double a = steps.c[st][0], b = steps.c[st][1], c = steps.c[st][2];
-    multiply64(A, A, T, m, tid);
-    for (int e = tid; e < m * m; e += 256) {
-      const int i = e / m, j = e % m;
-      P[i][j] = (i == j ? a : 0.0) + b * A[i][j] + c * T[i][j];
+    each64<R>(tid, product(A, A), [&](int i, int j, double v) { P.v[i][j] = (i == j ? a : 0.0) + b * A.v[i][j] + c * v; });
+    __syncthreads();
+    const bool more = st + 1 < steps.n;
+    const d4 q = product(P, Q), t = more ? product(P, A) : d4{};
+    __syncthreads();
+    each64<R>(tid, q, [&](int i, int j, double v) { Q.v[i][j] = v; });
+    if (more) {
+      each64<R>(tid, t, [&](int i, int j, double v) { T.v[i][j] = v; });
+      __syncthreads();
+      each64<R>(tid, product(T, P), [&](int i, int j, double v) { A.v[i][j] = v; });
     }
     __syncthreads();
-    multiply64(P, Q, T, m, tid);
-    for (int e = tid; e < m * m; e += 256) Q[e / m][e % m] = T[e / m][e % m];
-    __syncthreads();
-    if (st + 1 < steps.n) {
-      multiply64(P, A, T, m, tid);
-      multiply64(T, P, A, m, tid);
-    }
   }
-  for (int e = tid; e < m * m; e += 256) q[(int64_t)blockIdx.x * m * m + e] = Q[e / m][e % m] * inv;
+  for (int e = tid; e < R * R; e += kThreads64<R>) Q.v[e / R][e % R] *= inv;
+  __syncthreads();
+}
+// out = Q t for the chunk's columns: a wave per 16 columns at a time
+template <int R, class T>
+__device__ __forceinline__ void apply64(const Square<R>& Q, const Columns<R>& t, T* dst, int64_t old, int m, int w, int j0,
+                                        bool tall, int tid) {
+  const int l = tid & 63, wv = tid >> 6, i = l & 15, g = l >> 4;
+  for (int c = 16 * wv; c < w; c += kThreads64<R> / 4)
+#pragma unroll
+    for (int r = 0; r < R; r += 16) {
+      if (r >= m) break;
+      d4 acc = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+      for (int k = 0; k < R; k += 4)
+        acc = __builtin_amdgcn_mfma_f64_16x16x4f64(Q.v[r + i][k + g], (double)t.v[k + g][c + i], acc, 0, 0, 0);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int row = r + g + 4 * q, col = j0 + c + i;
+        if (row >= m || c + i >= w) continue;
+        const T v = (T)(float)acc[q];
+        if (tall) dst[(int64_t)col * old + row] = v;
+        else dst[(int64_t)row * old + col] = v;
+      }
+    }
 }
 
-// out = q g, one column of x per thread
-template <class T>
-__global__ void __launch_bounds__(256) ns_apply64_kernel(const T* g, int64_t stride, int64_t ld, int m, int n, bool tall,
-                                                         const double* __restrict__ q, T* out, int64_t ostride, int64_t old) {
-  __shared__ double sq[kGramMax * kGramMax];
-  for (int e = threadIdx.x; e < m * m; e += 256) sq[e] = q[(int64_t)blockIdx.y * m * m + e];
+// Matrices of at most kGramChunk columns: all of it in one launch, a block each
+template <class T, int R>
+__global__ void __launch_bounds__(kThreads64<R>)
+ns_small64_kernel(const T* g, int64_t stride, int64_t ld, int m, int n, bool tall, double eps, NsSteps steps, T* out,
+                  int64_t ostride, int64_t old) {
+  __shared__ Square<R> A, P, Q, S;
+  __shared__ Columns<R> t;
+  __shared__ double s_inv;
+  const int tid = threadIdx.x;
+  load_columns<R>(t, g + (int64_t)blockIdx.x * stride, ld, m, n, 0, tall, tid);
   __syncthreads();
-  const int j = blockIdx.x * 256 + threadIdx.x;
-  if (j >= n) return;
-  const T* src = g + (int64_t)blockIdx.y * stride;
-  T* o = out + (int64_t)blockIdx.y * ostride;
-  float x[kGramMax];
-#pragma unroll
-  for (int i = 0; i < kGramMax; ++i) x[i] = i < m ? element(src, ld, tall, i, j) : 0.f;
-  for (int r = 0; r < m; ++r) {
+  each64<R>(tid, gram64<R>(t, n, tid), [&](int i, int j, double v) { A.v[i][j] = v; });
+  __syncthreads();
+  iterate64<R>(A, P, Q, S, s_inv, eps, steps, tid);
+  apply64<R>(Q, t, out + (int64_t)blockIdx.x * ostride, old, m, n, 0, tall, tid);
+}
+// Longer ones: partial sums of A per chunk of columns, the iteration, the product per chunk
+template <class T, int R>
+__global__ void __launch_bounds__(kThreads64<R>) ns_gram64_kernel(const T* __restrict__ g, int64_t stride, int64_t ld, int m, int n,
+                                                        bool tall, double* __restrict__ part) {
+  __shared__ Columns<R> t;
+  const int tid = threadIdx.x, j0 = blockIdx.x * kGramChunk;
+  load_columns<R>(t, g + (int64_t)blockIdx.y * stride, ld, m, n, j0, tall, tid);
+  __syncthreads();
+  double* o = part + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * R * R;
+  each64<R>(tid, gram64<R>(t, min(kGramChunk, n - j0), tid), [&](int i, int j, double v) { o[i * R + j] = v; });
+}
+template <int R>
+__global__ void __launch_bounds__(kThreads64<R>)
+ns_iterate64_kernel(const double* __restrict__ part, int chunks, double eps, NsSteps steps, double* __restrict__ q) {
+  __shared__ Square<R> A, P, Q, S;
+  __shared__ double s_inv;
+  const int tid = threadIdx.x;
+  const double* p = part + (int64_t)blockIdx.x * chunks * R * R;
+  for (int e = tid; e < R * R; e += kThreads64<R>) {
     double s = 0.0;
-#pragma unroll
-    for (int i = 0; i < kGramMax; ++i)
-      if (i < m) s += sq[r * m + i] * (double)x[i];
-    const T v = (T)(float)s;
-    if (tall) o[(int64_t)j * old + r] = v;
-    else o[(int64_t)r * old + j] = v;
+    for (int c = 0; c < chunks; ++c) s += p[(int64_t)c * R * R + e];
+    A.v[e / R][e % R] = s;
   }
+  __syncthreads();
+  iterate64<R>(A, P, Q, S, s_inv, eps, steps, tid);
+  for (int e = tid; e < R * R; e += kThreads64<R>) q[(int64_t)blockIdx.x * R * R + e] = Q.v[e / R][e % R];
+}
+template <class T, int R>
+__global__ void __launch_bounds__(kThreads64<R>) ns_apply64_kernel(const T* g, int64_t stride, int64_t ld, int m, int n, bool tall,
+                                                         const double* __restrict__ q, T* out, int64_t ostride, int64_t old) {
+  __shared__ Square<R> Q;
+  __shared__ Columns<R> t;
+  const int tid = threadIdx.x, j0 = blockIdx.x * kGramChunk;
+  for (int e = tid; e < R * R; e += kThreads64<R>) Q.v[e / R][e % R] = q[(int64_t)blockIdx.y * R * R + e];
+  load_columns<R>(t, g + (int64_t)blockIdx.y * stride, ld, m, n, j0, tall, tid);
+  __syncthreads();
+  apply64<R>(Q, t, out + (int64_t)blockIdx.y * ostride, old, m, min(kGramChunk, n - j0), j0, tall, tid);
 }
 
 // ------------------------------------------------------------------ matrices that fit LDS
@@ -469,12 +539,14 @@ __device__ __forceinline__ Operand<T> operand(const PairMat& m, int b, int64_t a
   return {m.p + b * m.stride + at, m.ld, rows, m.plane};
 }
 
-// Tile (tm, tn), tn <= tm, of a lower triangle of tiles
+// Tile (tm, tn) of the lower triangle in tiles R times as high as wide: R (tm + 1)
+// tiles in row tm of tiles
+template <int R>
 __device__ __forceinline__ void triangle(int t, int& tm, int& tn) {
-  tm = (int)((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
-  while ((tm + 1) * (tm + 2) / 2 <= t) ++tm;
-  while (tm * (tm + 1) / 2 > t) --tm;
-  tn = t - tm * (tm + 1) / 2;
+  tm = (int)((sqrtf(8.f * (t / R) + 1.f) - 1.f) * 0.5f);
+  while (R * (tm + 1) * (tm + 2) / 2 <= t) ++tm;
+  while (R * tm * (tm + 1) / 2 > t) --tm;
+  tn = t - R * tm * (tm + 1) / 2;
 }
 
 // out = A = x x^T (POLY false, src = x), or out = B = b A + c A A (src = A), for the
@@ -486,9 +558,10 @@ __global__ void __launch_bounds__(S::NT) ns_symmetric_kernel(PairMat src, PairMa
   const int tid = threadIdx.x;
   const int id = xcd_order(blockIdx.x, gridDim.x), b = id / tiles;
   int tm, tn;
-  triangle(id - b * tiles, tm, tn);
+  constexpr int R = S::BM / S::BN;
+  triangle<R>(id - b * tiles, tm, tn);
   const int r0 = tm * S::BM, c0 = tn * S::BN;
-  static_assert(S::BM == S::BN, "square tiles");
+  if (c0 >= m) return;   // (the last row of tiles may be short)
   f4 acc[S::TN][S::TM];
   tile_gemm_direct<T, S, true, true>(operand<T>(src, b, (int64_t)r0 * src.ld, m - r0),
                                      operand<T>(src, b, (int64_t)c0 * src.ld, m - c0), K, lds, tid, acc);
@@ -509,7 +582,7 @@ __global__ void __launch_bounds__(S::NT) ns_symmetric_kernel(PairMat src, PairMa
         o[at + out.plane + q] = lo[q];
       }
     }
-    if (tm != tn)
+    if (tn < R * tm)   // below the diagonal blocks
 #pragma unroll
       for (int q = 0; q < 8; ++q)
         if (q < k) {
@@ -619,9 +692,9 @@ NsPlan plan(const mace_orthogonalise_desc& d) {
   p.n = std::max(d.rows, d.cols);
   p.mp = (p.m + 7) / 8 * 8;
   p.np = (p.n + 7) / 8 * 8;
-  p.gram = p.m <= kGramMax;
+  p.gram = p.m <= kGramMax || (p.m <= kGramMaxLong && p.n > kFitMax);
   p.parts = p.gram ? (int)ceil_div(p.n, kGramChunk) : (int)std::min<int64_t>(kNormBlocks, ceil_div(d.rows, 4));
-  p.fit = !p.gram && p.n <= 128;
+  p.fit = !p.gram && p.n <= kFitMax;
   size_t o = 0;
   auto take = [&](size_t bytes) {
     const size_t at = o;
@@ -629,8 +702,11 @@ NsPlan plan(const mace_orthogonalise_desc& d) {
     return at;
   };
   if (p.gram) {
-    p.part = take(sizeof(double) * d.batch * p.parts * p.m * p.m);
-    p.q = take(sizeof(double) * d.batch * p.m * p.m);
+    const int r = p.m <= 16 ? 16 : (p.m <= 32 ? 32 : 64);
+    if (p.parts > 1 || r == 64) {
+      p.part = take(sizeof(double) * d.batch * p.parts * r * r);
+      p.q = take(sizeof(double) * d.batch * r * r);
+    }
     p.total = o;
     return p;
   }
@@ -644,14 +720,20 @@ NsPlan plan(const mace_orthogonalise_desc& d) {
   return p;
 }
 
-constexpr int64_t kFillBlocks = 256;   // blocks from which the larger tile is taken (one per CU)
+constexpr int64_t kFillBlocks = 256;   // blocks of 128 x 128 from which those are taken (one per CU)
 
+// Sym: of the symmetric products of large matrices, whose lower triangles fill the
+// chip unevenly (two 2048 x 2048: 272 blocks of 128 x 128). Blocks half as wide
+// divide better and take 10 % less time with one plane; with two they are bound
+// by LDS and take 10 % more.
 template <class T> struct Shapes {
   using Mid = TileShape<128, 128, 2, 2, 64, 2, true>;
+  using Sym = TileShape<128, 64, 2, 2, 64, 2, true>;
   using Small = TileShape<64, 64, 2, 2, 64, 4, true>;
 };
 template <> struct Shapes<HalfPair> {
   using Mid = TileShape<128, 128, 2, 2, 32, 2, true>;
+  using Sym = Mid;
   using Small = TileShape<64, 64, 2, 2, 32, 4, true>;
 };
 
@@ -660,12 +742,12 @@ mace_status symmetric(const PairMat& src, const PairMat& out, int64_t batch, int
                       hipStream_t s) {
   auto go = [&](auto shape) {
     using S = decltype(shape);
-    const int64_t t = ceil_div(m, S::BM), tiles = t * (t + 1) / 2;
+    const int64_t t = ceil_div(m, S::BM), tiles = S::BM / S::BN * t * (t + 1) / 2;
     ns_symmetric_kernel<T, S, POLY><<<(unsigned)(tiles * batch), S::NT, 0, s>>>(src, out, m, K, (int)tiles, ca, cp);
     return launched();
   };
   const int64_t t = ceil_div(m, 128);
-  return t * (t + 1) / 2 * batch >= kFillBlocks ? go(typename Shapes<T>::Mid{}) : go(typename Shapes<T>::Small{});
+  return t * (t + 1) / 2 * batch >= kFillBlocks ? go(typename Shapes<T>::Sym{}) : go(typename Shapes<T>::Small{});
 }
 template <class T, class O>
 mace_status update(const PairMat& B, const PairMat& x, const PairMat& xo, int64_t batch, int m, int n, float ca, float cp,
@@ -707,14 +789,24 @@ mace_status run(const mace_orthogonalise_desc& d, const O* g, const double* coef
     return run_fit<O, 128, 128>(d, p, steps, g, out, s);
   }
   if (p.gram) {
-    double* q = reinterpret_cast<double*>(ws + p.q);
-    ns_gram64_kernel<O><<<dim3(p.parts, (unsigned)d.batch), 256, 0, s>>>(g, d.stride_g, d.ld_g, p.m, p.n, p.tall, part);
-    if ((st = launched()) != MACE_OK) return st;
-    ns_iterate64_kernel<<<(unsigned)d.batch, 256, 0, s>>>(part, p.parts, p.m, d.eps, steps, q);
-    if ((st = launched()) != MACE_OK) return st;
-    ns_apply64_kernel<O><<<dim3((unsigned)ceil_div(p.n, 256), (unsigned)d.batch), 256, 0, s>>>(
-        g, d.stride_g, d.ld_g, p.m, p.n, p.tall, q, out, d.stride_out, d.ld_out);
-    return launched();
+    auto go = [&](auto r_) -> mace_status {
+      constexpr int R = decltype(r_)::value;
+      if constexpr (R <= 32) if (p.parts == 1) {
+        ns_small64_kernel<O, R><<<(unsigned)d.batch, 256, 0, s>>>(g, d.stride_g, d.ld_g, p.m, p.n, p.tall, d.eps, steps,
+                                                                  out, d.stride_out, d.ld_out);
+        return launched();
+      }
+      double* q = reinterpret_cast<double*>(ws + p.q);
+      const dim3 grid(p.parts, (unsigned)d.batch);
+      constexpr int NT = kThreads64<R>;
+      ns_gram64_kernel<O, R><<<grid, NT, 0, s>>>(g, d.stride_g, d.ld_g, p.m, p.n, p.tall, part);
+      if ((st = launched()) != MACE_OK) return st;
+      ns_iterate64_kernel<R><<<(unsigned)d.batch, NT, 0, s>>>(part, p.parts, d.eps, steps, q);
+      if ((st = launched()) != MACE_OK) return st;
+      ns_apply64_kernel<O, R><<<grid, NT, 0, s>>>(g, d.stride_g, d.ld_g, p.m, p.n, p.tall, q, out, d.stride_out, d.ld_out);
+      return launched();
+    };
+    return p.m <= 16 ? go(Int<16>{}) : (p.m <= 32 ? go(Int<32>{}) : go(Int<64>{}));
   }
   ns_norm_kernel<O><<<dim3(p.parts, (unsigned)d.batch), 256, 0, s>>>(g, d.stride_g, d.ld_g, d.rows, d.cols, part);
   if ((st = launched()) != MACE_OK) return st;

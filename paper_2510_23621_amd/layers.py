@@ -42,20 +42,28 @@ def _current_stream(t) -> int:
     return torch._C._cuda_getCurrentRawStream(t.get_device())
 
 
-def _rows(t, n: int, c: int, like, name: str) -> int:
-    """Leading dimension of t, which has to be [n, c] with adjacent columns and of like's dtype and device."""
-    if t.shape != (n, c):
-        raise ValueError(f"{name} must be {(n, c)}, not {tuple(t.shape)}")
-    if t.dtype != like.dtype or t.get_device() != like.get_device():
-        raise ValueError(f"{name} must have the first tensor's dtype and device")
+def _leading(t, name: str) -> int:
+    """Leading dimension of a matrix, whose columns have to be adjacent."""
+    n, c = t.shape
+    if t.is_contiguous():
+        return c
     s0, s1 = t.stride()
     if (s1 != 1 and c > 1 and n > 0) or (s0 < c and n > 1):
         raise ValueError(f"{name}'s columns must be adjacent and its rows apart")
     return s0 if n > 1 else c
 
 
+def _rows(t, n: int, c: int, like, name: str) -> int:
+    """Leading dimension of t, which has to be [n, c] and of like's dtype and device."""
+    if t.shape != (n, c):
+        raise ValueError(f"{name} must be {(n, c)}, not {tuple(t.shape)}")
+    if t.dtype is not like.dtype or t.get_device() != like.get_device():
+        raise ValueError(f"{name} must have the first tensor's dtype and device")
+    return _leading(t, name)
+
+
 def _whole(t, shape, dtype, like, name: str):
-    if t.shape != shape or t.dtype != dtype or t.get_device() != like.get_device() or not t.is_contiguous():
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != like.get_device() or not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous {tuple(shape)} {dtype} on {like.device}")
 
 
@@ -79,16 +87,13 @@ def _linear_desc(x, w, offsets, act):
         groups, (k, n_out) = 1, shape
     else:
         raise ValueError("w must be [n_in, n_out] or [groups, n_in, n_out]")
-    if k != n_in or w.dtype != x.dtype or w.get_device() != x.get_device() or not w.is_contiguous():
+    if k != n_in or w.dtype is not x.dtype or w.get_device() != x.get_device() or not w.is_contiguous():
         raise ValueError(f"w must be contiguous with {n_in} input rows, of x's dtype and device")
     if offsets is not None:
         _whole(offsets, (groups + 1,), torch.int32, x, "offsets")
     elif groups != 1:
         raise ValueError("more than one group needs offsets")
-    s0, s1 = x.stride()
-    if (s1 != 1 and n_in > 1 and n > 0) or (s0 < n_in and n > 1):
-        raise ValueError("x's columns must be adjacent and its rows apart")
-    return B.mace_linear_desc(n, n_in, n_out, groups, dtype, a, s0 if n > 1 else n_in, n_out, n_out, n_out)
+    return B.mace_linear_desc(n, n_in, n_out, groups, dtype, a, _leading(x, "x"), n_out, n_out, n_out)
 
 
 @_streamed
@@ -155,18 +160,17 @@ class Route(NamedTuple):
 def route(expert, n_experts: int) -> Route:
     """The stable sort of the slots of expert (int32 [tokens, top_k]) by expert;
     slots with an index outside 0..n_experts-1 are dropped, behind the others."""
-    if expert.dim() != 2 or not expert.is_cuda or expert.dtype != torch.int32 or not expert.is_contiguous():
+    if expert.dim() != 2 or not expert.is_cuda or expert.dtype is not torch.int32 or not expert.is_contiguous():
         raise ValueError("expert must be a contiguous int32 [tokens, top_k] GPU tensor")
     n, k = expert.shape
     d = B.mace_route_desc(n, k, n_experts, 1, B.MACE_TYPE_FP32, 1, 1)
     lib = B.lib()
     s = n * k
-    buf = expert.new_empty(2 * s + max(n_experts, 0) + 1)   # one allocation
-    rows, slots, offsets = buf[:s].view(n, k), buf[s:2 * s], buf[2 * s:]
+    rows, slots = torch.empty_like(expert), expert.new_empty(s)
+    offsets = expert.new_empty(max(n_experts, 0) + 1)
     nbytes = lib.mace_route_workspace_bytes(d) if s > 4096 else 0
     ws = expert.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
-    at = buf.data_ptr()
-    B._check(lib.mace_route_build(d, expert.data_ptr(), at, at + 4 * s, at + 8 * s,
+    B._check(lib.mace_route_build(d, expert.data_ptr(), rows.data_ptr(), slots.data_ptr(), offsets.data_ptr(),
                                   None if ws is None else ws.data_ptr(), nbytes, _current_stream(expert)),
              "mace_route_build")
     return Route(rows, slots, offsets)
@@ -182,8 +186,10 @@ def route_rows(x, plan: Route):
     """[tokens * top_k, width] rows in expert order; zeros for dropped slots."""
     dtype = _gpu_matrix(x, "x")
     n, k = plan.row_of_slot.shape
-    width = x.shape[1]
-    ld = _rows(x, n, width, x, "x")
+    tokens, width = x.shape
+    if tokens != n:
+        raise ValueError(f"x must have {n} rows, not {tokens}")
+    ld = _leading(x, "x")
     d = B.mace_route_desc(n, k, plan.offsets.shape[0] - 1, width, dtype, ld, width)
     rows = x.new_empty((n * k, width))
     B._check(B.lib().mace_route_gather(d, x.data_ptr(), plan.row_of_slot.data_ptr(), plan.offsets.data_ptr(),
@@ -197,8 +203,10 @@ def combine_rows(rows, plan: Route, weights=None):
     [tokens, top_k], None: ones), summed."""
     dtype = _gpu_matrix(rows, "rows")
     n, k = plan.row_of_slot.shape
-    width = rows.shape[1]
-    ld = _rows(rows, n * k, width, rows, "rows")
+    slots, width = rows.shape
+    if slots != n * k:
+        raise ValueError(f"rows must have {n * k} rows, not {slots}")
+    ld = _leading(rows, "rows")
     _check_weights(weights, plan, rows)
     d = B.mace_route_desc(n, k, plan.offsets.shape[0] - 1, width, dtype, width, ld)
     out = rows.new_empty((n, width))
@@ -213,8 +221,10 @@ def combine_rows_backward(dout, rows, plan: Route, weights=None):
     """(drows, dweights) of `combine_rows`; dweights is None without weights."""
     dtype = _gpu_matrix(dout, "dout")
     n, k = plan.row_of_slot.shape
-    width = dout.shape[1]
-    ld = _rows(dout, n, width, dout, "dout")
+    tokens, width = dout.shape
+    if tokens != n:
+        raise ValueError(f"dout must have {n} rows, not {tokens}")
+    ld = _leading(dout, "dout")
     ld_rows = _rows(rows, n * k, width, dout, "rows")
     _check_weights(weights, plan, dout)
     d = B.mace_route_desc(n, k, plan.offsets.shape[0] - 1, width, dtype, ld, ld_rows)
