@@ -660,12 +660,20 @@ mace_status check(const mace_linear_desc* d) {
 int slope_run(int64_t n) { return (int)(std::max<int64_t>(1, ceil_div(n, 64 * 512)) * 64); }
 int64_t slope_runs(const mace_linear_desc& d) { return ceil_div(d.n_rows, slope_run(d.n_rows)) + d.n_groups; }
 
-constexpr int64_t kFillBlocks = 256, kLargeBlocks = 192;   // (256 CUs)
+// Which tile a launch takes, by the blocks it would give 256 CUs. Large from
+// kLargeBlocks of its own on: 8192 x 2048 x 2048 bfloat16 (256 of them) 70 us against
+// 79 as Mid, 8192 x 1024 x 1024 (128) 31 against 21. Mid from kFillBlocks on:
+// 8192 x 512 x 512 (256) 10.6 us against 12.3 as Small, 4096 x 512 x 512 (128) 9.4
+// against 8.5.
+constexpr int64_t kFillBlocks = 256, kLargeBlocks = 192;
 
-// Large: launches of at least kLargeBlocks of its tiles; Mid: from kFillBlocks of its own
+// 256 x 256 keeps the matrix pipes busiest (two waves per SIMD, 128 x 64 results
+// each); the others trade that for more blocks. FP32 is split as it is staged, so
+// its tiles hold three planes per operand; with eight waves a block's splitting
+// overlaps its products (4096 x 1024 x 1024: 57 us, four waves 67).
 template <class T, bool AL> struct Shapes {   // (16-bit, any alignment)
   using Large = TileShape<128, 128, 2, 2, 64, 1>;
-  using Mid = TileShape<128, 128, 2, 2, 64, 1>;
+  using Mid = TileShape<128, 128, 4, 2, 64, 1>;
   using Small = TileShape<64, 64, 2, 2, 64, 2>;
 };
 template <> struct Shapes<__bf16, true> {
@@ -676,17 +684,20 @@ template <> struct Shapes<__bf16, true> {
 template <> struct Shapes<_Float16, true> : Shapes<__bf16, true> {};
 template <> struct Shapes<float, false> {
   using Large = TileShape<128, 128, 2, 2, 32, 1>;
-  using Mid = TileShape<128, 128, 2, 2, 32, 1>;
+  using Mid = TileShape<128, 128, 4, 2, 32, 1>;
   using Small = TileShape<64, 64, 2, 2, 32, 2>;
 };
 template <> struct Shapes<float, true> : Shapes<float, false> {};
 using Thin = ThinShape<1, 1>;
 using Thin2 = ThinShape<2, 2>;
-// FP32 launches of fewer than kThinBlocks 64 x 64 tiles; Thin2 from kFillBlocks of its own
+// FP32 launches of fewer than kThinBlocks 64 x 64 tiles; Thin2 from kFillBlocks of
+// its own. 16 x 2048 x 2048 (32 tiles) 13 us against 49 as Small, 256 x 2048 x 2048
+// (128) 38 against 49, 1000 x 1031 x 777 (208) 43 against 33.
 constexpr int64_t kThinBlocks = 192;
 bool thin(int64_t rows, int64_t cols) { return ceil_div(rows, 64) * ceil_div(cols, 64) < kThinBlocks; }
 bool thin2(int64_t rows, int64_t cols) { return ceil_div(rows, 32) * ceil_div(cols, 32) >= kFillBlocks; }
-// sums of K short enough for narrow_rows, and rows for at least kNarrowBlocks waves of 64 columns
+// Sums of K short enough for narrow_rows, and rows for at least kNarrowBlocks waves of
+// 64 columns and 512 rows: four per SIMD, so that their weights' loads are hidden
 constexpr int64_t kNarrowBlocks = 1024;
 template <class T> bool narrow(int64_t rows, int64_t cols, int K) {
   return K <= (sizeof(T) == 4 ? 64 : 128) && ceil_div(rows, 512) * ceil_div(cols, 64) >= kNarrowBlocks;
@@ -699,8 +710,10 @@ mace_status with_narrow(int K, F f) {
   return f(NarrowShape<T, 2>{});
 }
 enum { kSmall, kMid, kLarge };
-int shape_of(int64_t rows, int64_t cols, int64_t batch = 1) {
-  if (ceil_div(rows, 256) * ceil_div(cols, 256) * batch >= kLargeBlocks) return kLarge;
+// runs: the groups that the rows are cut at; where they are short, a 256-row tile
+// would hold too few rows
+int shape_of(int64_t rows, int64_t cols, int64_t batch = 1, int64_t runs = 1) {
+  if ((runs == 1 || rows / runs >= 512) && ceil_div(rows, 256) * ceil_div(cols, 256) * batch >= kLargeBlocks) return kLarge;
   return ceil_div(rows, 128) * ceil_div(cols, 128) * batch >= kFillBlocks ? kMid : kSmall;
 }
 // f(shape) for the kind of tile; shapes that are the same type are instantiated once
@@ -774,7 +787,7 @@ mace_status forward(const mace_linear_desc& d, const void* x, const void* w, con
         };
         return thin2(d.n_rows, d.n_out) ? run(Thin2{}) : run(Thin{});
       }
-    return with_shape<T, AL>(shape_of(d.n_rows, d.n_out), [&](auto shape) -> mace_status {
+    return with_shape<T, AL>(shape_of(d.n_rows, d.n_out, 1, d.n_groups), [&](auto shape) -> mace_status {
       using S = decltype(shape);
       const int64_t blocks = (ceil_div(d.n_rows, S::BM) + (offsets ? d.n_groups : 0)) * ceil_div(d.n_out, S::BN);
       if (blocks > INT32_MAX) return MACE_EUNSUPPORTED;
@@ -858,7 +871,7 @@ mace_status backward(const mace_linear_desc& d, const void* dy, int64_t lddy, co
   auto grads = [&](int kind, bool rows, bool weights, bool bias) {
     return al ? go(Int<1>{}, kind, rows, weights, bias) : go(Int<0>{}, kind, rows, weights, bias);
   };
-  const int kind_x = shape_of(d.n_rows, d.n_in);
+  const int kind_x = shape_of(d.n_rows, d.n_in, 1, d.n_groups);
   if (!want_x || !dw || kind_x == p.weight_kind) {
     st = grads(dw ? p.weight_kind : kind_x, want_x, dw != nullptr, db != nullptr);
   } else {

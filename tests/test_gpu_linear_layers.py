@@ -238,3 +238,26 @@ def test_short_sums_over_many_rows(n, n_in, n_out, dtype):
 def test_short_sums_in_groups(dtype):
     case(None, 48, 1500, dtype, "gelu", [0, 20000, 1, 513, 12000, 511], 600, seed=4)
     case(None, 1500, 48, dtype, "none", [0, 20000, 1, 513, 12000, 511], 600, seed=4, residual=False)
+
+
+def test_offsets_beyond_32_bits():
+    """More than 2^31 elements of input: the last rows against the same rows alone.
+    The two calls take different tiles; both are within the bound of the exact one."""
+    n, k, m, last = (1 << 20) + 4133, 2048, 24, 300
+    gen = torch.Generator().manual_seed(7)
+    tail = randn(last, k, gen=gen, dtype="bf16")
+    w = randn(k, m, gen=gen, dtype="bf16", scale=k ** -0.5)
+    dy_tail = randn(last, m, gen=gen, dtype="bf16")
+    x = torch.zeros(n, k, dtype=torch.bfloat16, device="cuda")
+    x[-last:] = tail
+    dy = torch.zeros(n, m, dtype=torch.bfloat16, device="cuda")
+    dy[-last:] = dy_tail
+    wd = w.cuda()
+    y = L.linear(x, wd)
+    dx, dw, db = L.linear_backward(dy, x, wd)
+    X, W, DY = tail.double(), w.double(), dy_tail.double()
+    u = U["bf16"]
+    within(y[-last:], X @ W, product_error(X, W, k) + u * (X @ W).abs() * (1 + 2 * u), "y")
+    within(dx[-last:], DY @ W.t(), product_error(DY, W.t(), m) + u * (DY @ W.t()).abs() * (1 + 2 * u), "dx")
+    within(dw, X.t() @ DY, product_error(X.t(), DY, last) + u * (X.t() @ DY).abs() * (1 + 2 * u), "dw")
+    assert not y[:-last].any() and not dx[:-last].any()

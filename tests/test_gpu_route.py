@@ -176,3 +176,22 @@ def test_other_stream_and_graph():
         g.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+def test_offsets_beyond_32_bits():
+    """More than 2^31 elements of rows: copies are exact, sums of two equal halves too."""
+    n, k, width = (1 << 19) + 77, 2, 2112
+    e = torch.zeros(n, k, dtype=torch.int32, device="cuda")
+    e[:, 1] = 1
+    p = L.route(e, 2)
+    x = torch.zeros(n, width, dtype=torch.bfloat16, device="cuda")
+    x[-50:] = torch.randn(50, width, device="cuda").bfloat16()
+    rows = L.route_rows(x, p)
+    assert rows.numel() > 1 << 31
+    assert torch.equal(rows[-50:], x[-50:]) and torch.equal(rows[n - 50:n], x[-50:]) and not rows[:n - 50].any()
+    half = torch.full((n, k), 0.5, device="cuda")
+    assert torch.equal(L.combine_rows(rows, p, half), x)
+    drows, dw = L.combine_rows_backward(x, rows, p, half)
+    assert torch.equal(drows[-50:], (x[-50:].float() * 0.5).bfloat16()) and not drows[n:-50].any()
+    want = (x[-50:].double() ** 2).sum(1, keepdim=True).expand(50, 2).cpu()
+    within(dw[-50:], want, (width + 4) * U32 * want, "dweights")
