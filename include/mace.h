@@ -375,7 +375,7 @@ mace_status mace_route_build(const mace_route_desc* desc, const int32_t* expert,
                              void* stream);
 /* rows (dev) [n_tokens * top_k][width]: each kept slot's token, zeros for
  * dropped slots.  Its gradient is mace_route_combine without weights. */
-mace_status mace_route_gather(const mace_route_desc* desc, const void* tokens, const int32_t* row_of_slot,
+mace_status mace_route_gather(const mace_route_desc* desc, const void* tokens, const int32_t* slot_of_row,
                               const int32_t* offsets, void* rows, void* stream);
 /* out (dev) [n_tokens][width]: out_t = the sum over t's kept slots, in their
  * order, of weights[t][s] times the slot's row; weights (dev) [n_tokens][top_k]

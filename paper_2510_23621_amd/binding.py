@@ -455,8 +455,8 @@ def mace_route_build(desc: mace_route_desc, expert, row_of_slot, slot_of_row, of
                                   _ptr(workspace), workspace_bytes, _stream(stream)), "mace_route_build")
 
 
-def mace_route_gather(desc: mace_route_desc, tokens, row_of_slot, offsets, rows, stream=None):
-    _check(lib().mace_route_gather(desc, _ptr(tokens), _ptr(row_of_slot), _ptr(offsets), _ptr(rows),
+def mace_route_gather(desc: mace_route_desc, tokens, slot_of_row, offsets, rows, stream=None):
+    _check(lib().mace_route_gather(desc, _ptr(tokens), _ptr(slot_of_row), _ptr(offsets), _ptr(rows),
                                    _stream(stream)), "mace_route_gather")
 
 

@@ -922,8 +922,8 @@ extern "C" mace_status mace_linear_backward(const mace_linear_desc* desc, const 
   if (d.n_rows > 0 && (!dy || (dweights && !x) || (d.act != MACE_ACT_NONE && !preact))) return MACE_EINVAL;
   const BackwardPlan p = plan_backward(d, dbias != nullptr, dweights != nullptr);
   if (p.total > 0 && !workspace) return MACE_EINVAL;
+  if (p.total > 0 && workspace_bytes < p.total + 256) return MACE_ENOSPACE;
   char* ws = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(workspace) + 255) & ~uintptr_t(255));
-  if (p.total > 0 && size_t(ws - static_cast<char*>(workspace)) + p.total > workspace_bytes) return MACE_ENOSPACE;
   hipStream_t s = (hipStream_t)stream;
   if (d.dtype == MACE_TYPE_FP32)
     return backward<float>(d, dy, ld_dy, x, weights, preact, group_offsets, dx, ld_dx, dweights, dbias, ws, s);

@@ -869,8 +869,8 @@ extern "C" mace_status mace_orthogonalise(const mace_orthogonalise_desc* desc, c
   if (desc->batch == 0) return MACE_OK;
   if (!g || !out || !workspace) return MACE_EINVAL;
   if (!in_range(coefficients, desc->n_steps)) return MACE_ERANGE;
+  if (workspace_bytes < mace_orthogonalise_workspace_bytes(desc)) return MACE_ENOSPACE;
   char* ws = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(workspace) + 255) & ~uintptr_t(255));
-  if (size_t(ws - static_cast<char*>(workspace)) + plan(*desc).total > workspace_bytes) return MACE_ENOSPACE;
   hipStream_t s = (hipStream_t)stream;
   if (desc->dtype == MACE_TYPE_FP32)
     return run<float>(*desc, (const float*)g, coefficients, (float*)out, ws, s);

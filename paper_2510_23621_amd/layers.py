@@ -192,7 +192,7 @@ def route_rows(x, plan: Route):
     ld = _leading(x, "x")
     d = B.mace_route_desc(n, k, plan.offsets.shape[0] - 1, width, dtype, ld, width)
     rows = x.new_empty((n * k, width))
-    B._check(B.lib().mace_route_gather(d, x.data_ptr(), plan.row_of_slot.data_ptr(), plan.offsets.data_ptr(),
+    B._check(B.lib().mace_route_gather(d, x.data_ptr(), plan.slot_of_row.data_ptr(), plan.offsets.data_ptr(),
                                        rows.data_ptr(), _current_stream(x)), "mace_route_gather")
     return rows
 
