@@ -158,7 +158,7 @@ __device__ __forceinline__ void thin_product(const Operand<float>& ro, const Ope
         for (int r = 0; r < RT; ++r)
           acc[c][r] = __builtin_amdgcn_mfma_f32_16x16x4f32(wv8[D][c].get(e), xv[D][r].get(e), acc[c][r], 0, 0, 0);
   };
-  int k = 32 * wv;
+  int k = wv < 4 ? 32 * wv : K;   // (a larger block's other waves only keep the barrier)
   if (k < K) load(Int<0>{}, k);
   for (; k < K; k += 256) {
     if (k + 128 < K) load(Int<1>{}, k + 128);
@@ -170,7 +170,8 @@ __device__ __forceinline__ void thin_product(const Operand<float>& ro, const Ope
 #pragma unroll
   for (int c = 0; c < CT; ++c)
 #pragma unroll
-    for (int r = 0; r < RT; ++r) part[((c * RT + r) * 4 + wv) * 64 + l] = acc[c][r];
+    for (int r = 0; r < RT; ++r)
+      if (wv < 4) part[((c * RT + r) * 4 + wv) * 64 + l] = acc[c][r];
   __syncthreads();
   if (wv < RT * CT) {   // a wave per tile
     const f4* t = part + wv * 256 + l;
@@ -670,7 +671,8 @@ constexpr int64_t kFillBlocks = 256, kLargeBlocks = 192;
 // 256 x 256 keeps the matrix pipes busiest (two waves per SIMD, 128 x 64 results
 // each); the others trade that for more blocks. FP32 is split as it is staged, so
 // its tiles hold three planes per operand; with eight waves a block's splitting
-// overlaps its products (4096 x 1024 x 1024: 57 us, four waves 67).
+// overlaps its products (4096 x 1024 x 1024: 57 us, four waves 67; 4730 x 1978 -> 178:
+// 53 us, four waves 70).
 template <class T, bool AL> struct Shapes {   // (16-bit, any alignment)
   using Large = TileShape<128, 128, 2, 2, 64, 1>;
   using Mid = TileShape<128, 128, 4, 2, 64, 1>;
@@ -685,7 +687,7 @@ template <> struct Shapes<_Float16, true> : Shapes<__bf16, true> {};
 template <> struct Shapes<float, false> {
   using Large = TileShape<128, 128, 2, 2, 32, 1>;
   using Mid = TileShape<128, 128, 4, 2, 32, 1>;
-  using Small = TileShape<64, 64, 2, 2, 32, 2>;
+  using Small = TileShape<64, 64, 2, 4, 64, 1>;
 };
 template <> struct Shapes<float, true> : Shapes<float, false> {};
 using Thin = ThinShape<1, 1>;
