@@ -720,19 +720,22 @@ NsPlan plan(const mace_orthogonalise_desc& d) {
   return p;
 }
 
-constexpr int64_t kFillBlocks = 256;   // blocks of 128 x 128 from which those are taken (one per CU)
+constexpr int64_t kFillBlocks = 256;   // (one per CU)
 
-// Sym: of the symmetric products of large matrices, whose lower triangles fill the
-// chip unevenly (two 2048 x 2048: 272 blocks of 128 x 128). Blocks half as wide
-// divide better and take 10 % less time with one plane; with two they are bound
-// by LDS and take 10 % more.
+// Mid: 128 x 128, from one block per CU on. Half: the symmetric products' blocks, half
+// as wide, from one per CU on: there are few of them, one triangle's (two 1500 x 1500
+// BF16 552 us, with Small 611; four 1000 x 2000 564 against 619). Sym: the symmetric
+// products with a Mid block per CU; with two planes Half is bound by LDS there and
+// takes 10 % more than Mid, with one 10 % less.
 template <class T> struct Shapes {
   using Mid = TileShape<128, 128, 2, 2, 64, 2, true>;
-  using Sym = TileShape<128, 64, 2, 2, 64, 2, true>;
+  using Half = TileShape<128, 64, 2, 2, 64, 2, true>;
+  using Sym = Half;
   using Small = TileShape<64, 64, 2, 2, 64, 4, true>;
 };
 template <> struct Shapes<HalfPair> {
   using Mid = TileShape<128, 128, 2, 2, 32, 2, true>;
+  using Half = TileShape<128, 64, 2, 2, 32, 2, true>;
   using Sym = Mid;
   using Small = TileShape<64, 64, 2, 2, 32, 4, true>;
 };
@@ -747,7 +750,8 @@ mace_status symmetric(const PairMat& src, const PairMat& out, int64_t batch, int
     return launched();
   };
   const int64_t t = ceil_div(m, 128);
-  return t * (t + 1) / 2 * batch >= kFillBlocks ? go(typename Shapes<T>::Sym{}) : go(typename Shapes<T>::Small{});
+  if (t * (t + 1) / 2 * batch >= kFillBlocks) return go(typename Shapes<T>::Sym{});
+  return t * (t + 1) * batch >= kFillBlocks ? go(typename Shapes<T>::Half{}) : go(typename Shapes<T>::Small{});
 }
 template <class T, class O>
 mace_status update(const PairMat& B, const PairMat& x, const PairMat& xo, int64_t batch, int m, int n, float ca, float cp,
