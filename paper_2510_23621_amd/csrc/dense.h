@@ -496,7 +496,7 @@ __device__ __forceinline__ void tile_gemm(TileSource<T, S::BM, S::BK, KCR, AL, S
 // 4 (l/16) of either. Exchanging the odd 16-lane rows of the one with the even rows
 // of the other leaves a lane with eight consecutive columns, 8 (l/32) of tile (l/16)
 // % 2: 16-byte accesses of 16-bit results, 64 bytes of a row together in place of
-// 32 (81920 x 64 -> 1280 bfloat16: 71 -> 41 us).
+// 32 (81920 x 64 -> 1280 bfloat16: 75 -> 58 us).
 __device__ __forceinline__ f8 join_tiles(f4 a, f4 b) {
   f8 r;
 #pragma unroll

@@ -187,6 +187,11 @@ __device__ __forceinline__ void zero_rows(T* y, int64_t ld, int rows, int cols, 
   for (int i = tid; i < rows * cols; i += nt) y[(int64_t)(i / cols) * ld + i % cols] = (T)0.f;
 }
 
+// y = act(x W_g + b_g) + r: a tile of one group's rows per block, the epilogue on the
+// sums in registers, so that z and y go out and r comes in once. 36864 x 2048 x 2048
+// bfloat16 in eight groups, with z and r: 411 us; the products alone would take 300 at
+// the card's 1.03 PFLOP/s for a plain product of that size, and the 600 MB of x, z, r
+// and y 115 at a copy's rate, which only other blocks' products can hide.
 template <class T, bool AL, class S>
 __global__ void __launch_bounds__(S::NT) linear_fwd_kernel(LinearArgs<T> a) {
   __shared__ __align__(16) unsigned short lds[tile_lds<T, S>];
@@ -291,8 +296,10 @@ __global__ void __launch_bounds__(S::NT) linear_fwd_thin_kernel(LinearArgs<float
 // them in chunks through LDS, where their parts lie split once for the block's four
 // waves. The next chunk's rows are requested before this chunk's results are
 // stored (memory operations complete in order: a later request would wait for
-// the stores). Bound by the results' way to memory: 81920 x 64 -> 1280 FP32 105 us
-// (4.0 TB/s written), bfloat16 41 us (5.1); as tiles 138 and 72 us.
+// the stores). Bound by the results' way to memory, against which the products (73 us
+// at the matrix pipes' rate, FP32) are not wholly hidden: 81920 x 64 -> 1280 FP32 123
+// to 145 us from card to card (as tiles 172 where it takes 144), 524288 x 64 -> 64
+// bfloat16 38 us (3.5 TB/s; as tiles 53).
 // KCC: the weights' rows are the columns of the result (dx).
 template <class T, int KS_> struct NarrowShape {   // K <= 32 KS
   static constexpr int KS = KS_, BN = 256, NT = 256;
@@ -543,7 +550,9 @@ __device__ __forceinline__ void bias_grad(const BiasGradArgs<T>& a, int id, floa
 }
 
 // All three gradients in one launch: blocks below row_blocks form dx, the next
-// weight_blocks dW, the rest db.
+// weight_blocks dW, the rest db. A small layer's step is bound by its launches;
+// 36864 x 2048 x 2048 bfloat16 in eight groups 638 us, 0.97 PFLOP/s, bound by the
+// products.
 // RS: the shape of dx's tiles, S or a thin one.
 template <class T, bool AL, class S, class RS>
 __global__ void __launch_bounds__(S::NT)
@@ -584,7 +593,9 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const float* __restric
 
 // dz = dy act'(z) over a run of rows (where there is an activation), and the
 // run's column sums. A block takes 8 CX columns; its kSlopeThreads / CX row lanes
-// each sum their rows, then are added in order.
+// each sum their rows, then are added in order. One pass over dy and z (36864 x 2048
+// bfloat16: 101 us, 4.5 TB/s); both products read the rounded dz, so that the
+// activation is not evaluated again for every tile of columns.
 constexpr int kSlopeThreads = 1024;
 template <class T, bool AL>
 __global__ void __launch_bounds__(kSlopeThreads)
@@ -662,10 +673,10 @@ int slope_run(int64_t n) { return (int)(std::max<int64_t>(1, ceil_div(n, 64 * 51
 int64_t slope_runs(const mace_linear_desc& d) { return ceil_div(d.n_rows, slope_run(d.n_rows)) + d.n_groups; }
 
 // Which tile a launch takes, by the blocks it would give 256 CUs. Large from
-// kLargeBlocks of its own on: 8192 x 2048 x 2048 bfloat16 (256 of them) 70 us against
-// 79 as Mid, 8192 x 1024 x 1024 (128) 31 against 21. Mid from kFillBlocks on:
-// 8192 x 512 x 512 (256) 10.6 us against 12.3 as Small, 4096 x 512 x 512 (128) 9.4
-// against 8.5.
+// kLargeBlocks of its own on: 8192 x 2048 x 2048 bfloat16 (256 of them) 71 us against
+// 79 as Mid, 8192 x 1024 x 1024 (128) 34 against 24. Mid from kFillBlocks on:
+// 8192 x 512 x 512 (256) bfloat16 10.3 us against 12.1 as Small, FP32 34 against 39;
+// 4096 x 512 x 512 (128) 9.0 against 7.7, FP32 30 against 20.
 constexpr int64_t kFillBlocks = 256, kLargeBlocks = 192;
 
 // 256 x 256 keeps the matrix pipes busiest (two waves per SIMD, 128 x 64 results
@@ -693,15 +704,21 @@ template <> struct Shapes<float, true> : Shapes<float, false> {};
 using Thin = ThinShape<1, 1>;
 using Thin2 = ThinShape<2, 2>;
 // FP32 launches of fewer than kThinBlocks 64 x 64 tiles; Thin2 from kFillBlocks of
-// its own. 16 x 2048 x 2048 (32 tiles) 13 us against 49 as Small, 256 x 2048 x 2048
-// (128) 38 against 49, 1000 x 1031 x 777 (208) 43 against 33.
-constexpr int64_t kThinBlocks = 192;
+// its own. 16 x 2048 x 2048 (32 tiles) 12 us against 36 as Small, 256 x 1024 x 1024
+// (64) 11 against 20, 192 x 2048 x 2048 (96) 37 against 38, 320 x 256 x 1536 (120) 8.1
+// against 7.6, 640 x 1024 x 1024 (160) 31 against 24.
+constexpr int64_t kThinBlocks = 96;
 bool thin(int64_t rows, int64_t cols) { return ceil_div(rows, 64) * ceil_div(cols, 64) < kThinBlocks; }
 bool thin2(int64_t rows, int64_t cols) { return ceil_div(rows, 32) * ceil_div(cols, 32) >= kFillBlocks; }
 // Sums of K short enough for narrow_rows, and rows for at least kNarrowBlocks waves of
-// 64 columns and 512 rows: four per SIMD, so that their weights' loads are hidden
-constexpr int64_t kNarrowBlocks = 1024;
+// 64 columns and 512 rows: four per SIMD, so that their weights' loads are hidden.
+// FP32 sums of more than 32 products also need more than kNarrowColumns columns, as a
+// wave splits its rows for 64 columns at a time: 262144 x 64 -> 192 74 us against 94
+// as tiles, -> 128 74 against 62, 524288 x 64 -> 64 105 against 80 (32 -> 64: 55
+// against 61; bfloat16, 64 -> 64: 38 against 53).
+constexpr int64_t kNarrowBlocks = 1024, kNarrowColumns = 128;
 template <class T> bool narrow(int64_t rows, int64_t cols, int K) {
+  if (sizeof(T) == 4 && K > 32 && cols <= kNarrowColumns) return false;
   return K <= (sizeof(T) == 4 ? 64 : 128) && ceil_div(rows, 512) * ceil_div(cols, 64) >= kNarrowBlocks;
 }
 template <class T, class F>
