@@ -13,6 +13,11 @@
 // two per step. FP64 because A holds the squares of the singular values and a
 // small one's error grows with the square of the value: in 2^-24 arithmetic a
 // singular value of 0.003 would be off by a percent, in FP64 by 1e-11.
+// A zero singular value's place in A holds a rounding error, 2^-53, of either sign;
+// a step multiplies it by up to a^2, and a negative one has no plateau that would
+// stop it. Steps that could take it past 2^-13 (kGramGrowth; 10 of the default ones,
+// 33 of (1.5, -0.5, 0)) therefore go to the kernels that iterate x, where x x^T is new
+// in every step.
 #include <algorithm>
 #include <cmath>
 
@@ -126,6 +131,7 @@ ns_scale_kernel(const T* __restrict__ g, int64_t stride, int64_t ld, int rows, i
 // ------------------------------------------------------------------ few rows
 // FP64 up to 32 rows, and up to 64 of matrices too long for LDS
 constexpr int kGramMax = 32, kGramMaxLong = 64, kGramChunk = 256;
+constexpr double kGramGrowth = 0x1p40;
 constexpr int kFitMax = 128;   // longest side of a matrix iterated in LDS
 
 // element (i, j) of x's layout in g
@@ -654,24 +660,34 @@ mace_status check(const mace_orthogonalise_desc* d) {
   return MACE_OK;
 }
 
-// whether every step keeps its operands in range (mace.h): the largest singular
-// value after each step and the largest b l + c l^2, l its square, at the ends of
-// the range and where their derivatives vanish
-bool in_range(const double* k, int steps) {
+// Over the singular values that can occur, s with l = s^2, for x <- P(l) x per step,
+// P = a + b l + c l^2: whether every step keeps its operands in range (mace.h), and
+// how far a perturbation of A's eigenvalues can grow over the steps.
+struct StepRange {
+  bool ok;
+  double growth;
+};
+StepRange range_of(const double* k, int steps) {
   double r = 1.0;   // largest singular value so far
+  double growth = 1.0;
   for (int s = 0; s < steps; ++s, k += 3) {
     const double a = k[0], b = k[1], c = k[2];
-    if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
-    double top = 0.0, next = 0.0;
+    if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return {false, 0.0};
+    double top = 0.0, next = 0.0, p = 0.0, slope = 0.0;
     auto at = [&](double l) {   // l clamped to the range: a point outside gives its end
       l = std::min(std::max(l, 0.0), r * r);
       const double B = b * l + c * l * l;
       top = std::max(top, std::fabs(B));
       next = std::max(next, std::fabs(a + B) * std::sqrt(l));
+      p = std::max(p, std::fabs(a + B));
+      slope = std::max(slope, std::fabs(a + 3.0 * b * l + 5.0 * c * l * l));
     };
+    // the ends of the range, and where the derivatives vanish
+    at(0.0);
     at(r * r);
     if (c != 0.0) {
       at(-b / (2.0 * c));
+      at(-3.0 * b / (10.0 * c));
       const double d = 9.0 * b * b - 20.0 * a * c;   // a + 3 b l + 5 c l^2 = 0
       if (d >= 0.0) {
         at((-3.0 * b + std::sqrt(d)) / (10.0 * c));
@@ -681,9 +697,10 @@ bool in_range(const double* k, int steps) {
       at(-a / (3.0 * b));
     }
     r = next * 1.001;   // (rounding)
-    if (!(top <= kMaxB) || !(r <= kMaxSigma)) return false;
+    if (!(top <= kMaxB) || !(r <= kMaxSigma)) return {false, 0.0};
+    growth = growth * p * slope + 1.0;   // d(l P^2) / dl = P (P + 2 l P'); each step adds a rounding of its own
   }
-  return true;
+  return {true, growth};
 }
 
 struct NsPlan {
@@ -691,14 +708,14 @@ struct NsPlan {
   bool tall, gram, fit;   // which of the kernels above; neither: products by launches of tiles
   size_t part, q, x0, x1, A, B, total;
 };
-NsPlan plan(const mace_orthogonalise_desc& d) {
+NsPlan plan(const mace_orthogonalise_desc& d, double growth) {
   NsPlan p{};
   p.tall = d.rows > d.cols;
   p.m = std::min(d.rows, d.cols);
   p.n = std::max(d.rows, d.cols);
   p.mp = (p.m + 7) / 8 * 8;
   p.np = (p.n + 7) / 8 * 8;
-  p.gram = p.m <= kGramMax || (p.m <= kGramMaxLong && p.n > kFitMax);
+  p.gram = (p.m <= kGramMax || (p.m <= kGramMaxLong && p.n > kFitMax)) && growth <= kGramGrowth;
   p.parts = p.gram ? (int)ceil_div(p.n, kGramChunk) : (int)std::min<int64_t>(kNormBlocks, ceil_div(d.rows, 4));
   p.fit = !p.gram && p.n <= kFitMax;
   size_t o = 0;
@@ -786,8 +803,8 @@ mace_status run_fit(const mace_orthogonalise_desc& d, const NsPlan& p, const NsS
 }
 
 template <class O>
-mace_status run(const mace_orthogonalise_desc& d, const O* g, const double* coef, O* out, char* ws, hipStream_t s) {
-  const NsPlan p = plan(d);
+mace_status run(const mace_orthogonalise_desc& d, const NsPlan& p, const O* g, const double* coef, O* out, char* ws,
+                hipStream_t s) {
   double* part = reinterpret_cast<double*>(ws + p.part);
   mace_status st;
   NsSteps steps{};
@@ -868,7 +885,7 @@ using namespace mace;
 
 extern "C" size_t mace_orthogonalise_workspace_bytes(const mace_orthogonalise_desc* desc) {
   if (check(desc) != MACE_OK) return 0;
-  return plan(*desc).total + 256;
+  return std::max(plan(*desc, 1.0).total, plan(*desc, INFINITY).total) + 256;   // (whatever the coefficients)
 }
 
 extern "C" mace_status mace_orthogonalise(const mace_orthogonalise_desc* desc, const void* g, const double* coefficients,
@@ -878,13 +895,13 @@ extern "C" mace_status mace_orthogonalise(const mace_orthogonalise_desc* desc, c
   if (desc->n_steps > 0 && !coefficients) return MACE_EINVAL;
   if (desc->batch == 0) return MACE_OK;
   if (!g || !out || !workspace) return MACE_EINVAL;
-  if (!in_range(coefficients, desc->n_steps)) return MACE_ERANGE;
+  const StepRange range = range_of(coefficients, desc->n_steps);
+  if (!range.ok) return MACE_ERANGE;
   if (workspace_bytes < mace_orthogonalise_workspace_bytes(desc)) return MACE_ENOSPACE;
   char* ws = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(workspace) + 255) & ~uintptr_t(255));
+  const NsPlan p = plan(*desc, range.growth);
   hipStream_t s = (hipStream_t)stream;
-  if (desc->dtype == MACE_TYPE_FP32)
-    return run<float>(*desc, (const float*)g, coefficients, (float*)out, ws, s);
-  if (desc->dtype == MACE_TYPE_BF16)
-    return run<__bf16>(*desc, (const __bf16*)g, coefficients, (__bf16*)out, ws, s);
-  return run<_Float16>(*desc, (const _Float16*)g, coefficients, (_Float16*)out, ws, s);
+  if (desc->dtype == MACE_TYPE_FP32) return run<float>(*desc, p, (const float*)g, coefficients, (float*)out, ws, s);
+  if (desc->dtype == MACE_TYPE_BF16) return run<__bf16>(*desc, p, (const __bf16*)g, coefficients, (__bf16*)out, ws, s);
+  return run<_Float16>(*desc, p, (const _Float16*)g, coefficients, (_Float16*)out, ws, s);
 }
