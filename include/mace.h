@@ -405,10 +405,7 @@ mace_status mace_route_combine_backward(const mace_route_desc* desc, const void*
  * (the products' operands are pairs of binary16 with fixed scales).  Products
  * are as accurate as FP32's (in FP64 where the shorter side is at most 32, or at
  * most 64 and the longer beyond 128, over up to 10 of the default steps and as
- * many of others as multiply a rounding no more, 2^40 fold); a BF16 result with
- * both sides at least 128 and one beyond takes all but its last two steps with
- * binary16 operands, whose error stays below a third of the result's rounding.
- * A matrix with a
+ * many of others as multiply a rounding no more, 2^40 fold).  A matrix with a
  * non-finite element gives NaN, the others of the batch are not touched by it.
  * rows and cols <= 2^15, batch <= 65535, batch * rows * cols <= 2^34, else
  * MACE_EUNSUPPORTED.

@@ -541,9 +541,8 @@ ns_fit_kernel(const T* g, int64_t stride, int64_t ld, int m, int n, bool tall, d
 
 // ------------------------------------------------------------------ products
 
-// operand of matrix b from element `at` (T: binary16 takes the upper plane only)
-template <class T>
-__device__ __forceinline__ Operand<T> operand(const PairMat& m, int b, int64_t at, int rows) {
+// operand of matrix b from element `at`
+__device__ __forceinline__ Operand<HalfPair> operand(const PairMat& m, int b, int64_t at, int rows) {
   return {m.p + b * m.stride + at, m.ld, rows, m.plane};
 }
 
@@ -558,13 +557,12 @@ __device__ __forceinline__ void triangle(int t, int& tm, int& tn) {
 }
 
 // out = A = x x^T (POLY false, src = x), or out = B = b A + c A A (src = A), for the
-// lower triangle of tiles; the upper one is its mirror. Two 2048 x 2048: 87 and 90 us
-// with pairs, 36 and 40 with single planes, 0.6 and 0.45 PFLOP/s of the half that is
-// computed (272 blocks on 256 CUs, 544 half blocks with single planes).
-template <class T, class S, bool POLY>
+// lower triangle of tiles; the upper one is its mirror. Two 2048 x 2048: 87 and 90 us,
+// 0.6 PFLOP/s of the half that is computed (272 blocks on 256 CUs).
+template <class S, bool POLY>
 __global__ void __launch_bounds__(S::NT) ns_symmetric_kernel(PairMat src, PairMat out, int m, int K, int tiles,
                                                              float ca, float cp) {
-  __shared__ __align__(16) unsigned short lds[tile_lds<T, S>];
+  __shared__ __align__(16) unsigned short lds[tile_lds<HalfPair, S>];
   const int tid = threadIdx.x;
   const int id = xcd_order(blockIdx.x, gridDim.x), b = id / tiles;
   int tm, tn;
@@ -573,8 +571,8 @@ __global__ void __launch_bounds__(S::NT) ns_symmetric_kernel(PairMat src, PairMa
   const int r0 = tm * S::BM, c0 = tn * S::BN;
   if (c0 >= m) return;   // (the last row of tiles may be short)
   f4 acc[S::TN][S::TM];
-  tile_gemm_direct<T, S, true, true>(operand<T>(src, b, (int64_t)r0 * src.ld, m - r0),
-                                     operand<T>(src, b, (int64_t)c0 * src.ld, m - c0), K, lds, tid, acc);
+  tile_gemm_direct<HalfPair, S, true, true>(operand(src, b, (int64_t)r0 * src.ld, m - r0),
+                                            operand(src, b, (int64_t)c0 * src.ld, m - c0), K, lds, tid, acc);
   _Float16* o = out.p + b * out.stride;
   const _Float16* a = src.p + b * src.stride;
   for_results<S, 8, false>(acc, min(S::BM, m - r0), min(S::BN, m - c0), tid, [&](int i, int j, f8 v, int k) {
@@ -604,13 +602,13 @@ __global__ void __launch_bounds__(S::NT) ns_symmetric_kernel(PairMat src, PairMa
 }
 
 // x <- a x + B x, as pairs, or the last step's result in its own type and layout. Two
-// 2048 x 2048: 99 us with pairs (1.04 PFLOP/s), 43 with single planes (0.8), bound by
-// the products; 515 x 211 and smaller by a tile's own chain of loads and products.
-template <class T, class S, class O>
+// 2048 x 2048: 99 us (1.04 PFLOP/s), bound by the products; 515 x 211 and smaller by a
+// tile's own chain of loads and products.
+template <class S, class O>
 __global__ void __launch_bounds__(S::NT)
 ns_update_kernel(PairMat B, PairMat x, PairMat xo, int m, int n, float ca, float cp, O* out, int64_t ostride,
                  int64_t old, bool tall) {
-  __shared__ __align__(16) unsigned short lds[tile_lds<T, S>];
+  __shared__ __align__(16) unsigned short lds[tile_lds<HalfPair, S>];
   const int tid = threadIdx.x;
   const int tiles_n = (x.ld + S::BN - 1) / S::BN, tiles_m = (m + S::BM - 1) / S::BM;
   int id = xcd_order(blockIdx.x, gridDim.x);
@@ -618,8 +616,8 @@ ns_update_kernel(PairMat B, PairMat x, PairMat xo, int m, int n, float ca, float
   id -= b * tiles_n * tiles_m;
   const int r0 = id / tiles_n * S::BM, c0 = id % tiles_n * S::BN;
   f4 acc[S::TN][S::TM];
-  tile_gemm_direct<T, S, true, false>(operand<T>(B, b, (int64_t)r0 * B.ld, m - r0), operand<T>(x, b, c0, x.ld - c0), m,
-                                      lds, tid, acc);
+  tile_gemm_direct<HalfPair, S, true, false>(operand(B, b, (int64_t)r0 * B.ld, m - r0), operand(x, b, c0, x.ld - c0), m,
+                                             lds, tid, acc);
   const _Float16* xi = x.p + b * x.stride;
   for_results<S, 8, true>(acc, min(S::BM, m - r0), min(S::BN, x.ld - c0), tid, [&](int i, int j, f8 v, int k) {
     const int64_t at = (int64_t)(r0 + i) * x.ld + c0 + j;   // (whole vectors: the pitch is a multiple of 8)
@@ -746,47 +744,36 @@ NsPlan plan(const mace_orthogonalise_desc& d, double growth) {
 constexpr int64_t kFillBlocks = 256;   // (one per CU)
 
 // Mid: 128 x 128, from one block per CU on. Half: the symmetric products' blocks, half
-// as wide, from one per CU on: there are few of them, one triangle's (two 1500 x 1500
-// BF16 552 us, with Small 611; four 1000 x 2000 564 against 619). Sym: the symmetric
-// products with a Mid block per CU; with two planes Half is bound by LDS there and
-// takes 10 % more than Mid, with one 10 % less.
-template <class T> struct Shapes {
-  using Mid = TileShape<128, 128, 2, 2, 64, 2, true>;
-  using Half = TileShape<128, 64, 2, 2, 64, 2, true>;
-  using Sym = Half;
-  using Small = TileShape<64, 64, 2, 2, 64, 4, true>;
-};
-template <> struct Shapes<HalfPair> {
-  using Mid = TileShape<128, 128, 2, 2, 32, 2, true>;
-  using Half = TileShape<128, 64, 2, 2, 32, 2, true>;
-  using Sym = Mid;
-  using Small = TileShape<64, 64, 2, 2, 32, 4, true>;
-};
+// as wide, where Mid gives less than one per CU and Half that many: there are few of them,
+// one triangle's (two 1500 x 1500 BF16 552 us, with Small 611; four 1000 x 2000 564
+// against 619). With a Mid block per CU Half takes 10 % more, bound by LDS.
+using Mid = TileShape<128, 128, 2, 2, 32, 2, true>;
+using Half = TileShape<128, 64, 2, 2, 32, 2, true>;
+using Small = TileShape<64, 64, 2, 2, 32, 4, true>;
 
-template <class T, bool POLY>
+template <bool POLY>
 mace_status symmetric(const PairMat& src, const PairMat& out, int64_t batch, int m, int K, float ca, float cp,
                       hipStream_t s) {
   auto go = [&](auto shape) {
     using S = decltype(shape);
     const int64_t t = ceil_div(m, S::BM), tiles = S::BM / S::BN * t * (t + 1) / 2;
-    ns_symmetric_kernel<T, S, POLY><<<(unsigned)(tiles * batch), S::NT, 0, s>>>(src, out, m, K, (int)tiles, ca, cp);
+    ns_symmetric_kernel<S, POLY><<<(unsigned)(tiles * batch), S::NT, 0, s>>>(src, out, m, K, (int)tiles, ca, cp);
     return launched();
   };
   const int64_t t = ceil_div(m, 128);
-  if (t * (t + 1) / 2 * batch >= kFillBlocks) return go(typename Shapes<T>::Sym{});
-  return t * (t + 1) * batch >= kFillBlocks ? go(typename Shapes<T>::Half{}) : go(typename Shapes<T>::Small{});
+  if (t * (t + 1) / 2 * batch >= kFillBlocks) return go(Mid{});
+  return t * (t + 1) * batch >= kFillBlocks ? go(Half{}) : go(Small{});
 }
-template <class T, class O>
+template <class O>
 mace_status update(const PairMat& B, const PairMat& x, const PairMat& xo, int64_t batch, int m, int n, float ca, float cp,
                    O* out, int64_t ostride, int64_t old, bool tall, hipStream_t s) {
   auto go = [&](auto shape) {
     using S = decltype(shape);
     const int64_t blocks = ceil_div(m, S::BM) * ceil_div(x.ld, S::BN) * batch;
-    ns_update_kernel<T, S, O><<<(unsigned)blocks, S::NT, 0, s>>>(B, x, xo, m, n, ca, cp, out, ostride, old, tall);
+    ns_update_kernel<S, O><<<(unsigned)blocks, S::NT, 0, s>>>(B, x, xo, m, n, ca, cp, out, ostride, old, tall);
     return launched();
   };
-  return ceil_div(m, 128) * ceil_div(x.ld, 128) * batch >= kFillBlocks ? go(typename Shapes<T>::Mid{})
-                                                                        : go(typename Shapes<T>::Small{});
+  return ceil_div(m, 128) * ceil_div(x.ld, 128) * batch >= kFillBlocks ? go(Mid{}) : go(Small{});
 }
 
 template <class O, int MM, int NN>
@@ -851,28 +838,14 @@ mace_status run(const mace_orthogonalise_desc& d, const NsPlan& p, const O* g, c
   ns_pack_kernel<O><<<dim3((unsigned)ceil_div(p.np, 64), (unsigned)ceil_div(p.m, 64), (unsigned)d.batch), 256, 0, s>>>(
       g, d.stride_g, d.ld_g, p.m, p.n, p.tall, part, p.parts, d.eps, x, A, B);
   if ((st = launched()) != MACE_OK) return st;
-  // Steps from the end that take pairs. A BF16 result's earlier steps take the
-  // upper halves (2^-12 of the operands): what is left of that error after two
-  // steps of pairs is 2e-4 to 6e-4 of the result, against 1.7e-3 of its rounding
-  // (matrices of 128 to 1024 rows; with one step of pairs 5e-4 to 9e-4, with none
-  // 8e-4 to 2e-3). Below 128 rows too few directions average the error, and the
-  // products are not what takes the time.
-  const int exact_steps = d.dtype == MACE_TYPE_BF16 && p.m >= 128 ? 2 : d.n_steps;
   for (int i = 0; i < d.n_steps; ++i) {
-    const bool pairs = d.n_steps - i <= exact_steps, last = i == d.n_steps - 1;
     const float a = (float)coef[3 * i], b = (float)coef[3 * i + 1], c = (float)coef[3 * i + 2];
     const float g1 = kScaleA / (kScaleX * kScaleX), pb = b * (kScaleB / kScaleA),
                 pc = c * (kScaleB / (kScaleA * kScaleA)), u = 1.f / kScaleB;
-    O* o = last ? out : nullptr;
-    auto step = [&](auto t) -> mace_status {
-      using T = decltype(t);
-      mace_status e;
-      if ((e = symmetric<T, false>(x, A, d.batch, p.m, p.np, 0.f, g1, s)) != MACE_OK) return e;
-      if ((e = symmetric<T, true>(A, B, d.batch, p.m, p.m, pb, pc, s)) != MACE_OK) return e;
-      return update<T, O>(B, x, xo, d.batch, p.m, p.n, a, u, o, d.stride_out, d.ld_out, p.tall, s);
-    };
-    st = pairs ? step(HalfPair{}) : step((_Float16)0.f);
-    if (st != MACE_OK) return st;
+    O* o = i == d.n_steps - 1 ? out : nullptr;
+    if ((st = symmetric<false>(x, A, d.batch, p.m, p.np, 0.f, g1, s)) != MACE_OK) return st;
+    if ((st = symmetric<true>(A, B, d.batch, p.m, p.m, pb, pc, s)) != MACE_OK) return st;
+    if ((st = update<O>(B, x, xo, d.batch, p.m, p.n, a, u, o, d.stride_out, d.ld_out, p.tall, s)) != MACE_OK) return st;
     std::swap(x, xo);
   }
   return MACE_OK;
