@@ -28,7 +28,9 @@ __device__ __forceinline__ float normal_cdf(float z, float& e) {
 }
 template <int ACT>
 __device__ __forceinline__ float activate(float z) {
-  if constexpr (ACT == MACE_ACT_SILU) return silu(z);
+  // z / (1 + exp(-z)). exp_neg takes -88 at the least, and infinity not at all: above 88
+  // the quotient is z, below -88 (where it is under 2^-120) z 0, NaN at -infinity as GELU
+  if constexpr (ACT == MACE_ACT_SILU) return z * (z < -88.f ? 0.f : recip_ge1(1.f + exp_neg(fminf(z, 88.f))));
   if constexpr (ACT == MACE_ACT_GELU) {
     float e;
     return z * normal_cdf(z, e);
