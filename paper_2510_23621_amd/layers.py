@@ -3,9 +3,10 @@ expert and back, Newton-Schulz orthogonalisation, and the gradients of the
 first two.  torch allocates results and workspaces, the library's kernels do
 the work on ``stream`` (a torch.cuda.Stream; default: the current one).
 
-Tensors are float32, bfloat16 or float16 on one GPU; rows may be strided
-(any row stride, columns adjacent).  Tensors of another stream are the
-caller's to order, as with any torch operation.
+Tensors are float32, bfloat16 or float16 on one GPU, whichever is current, and
+``stream`` is one of that GPU's; rows may be strided (any row stride, columns
+adjacent).  Tensors of another stream are the caller's to order, as with any
+torch operation.
 
 The checks are written out in each function: a small layer's call is bound by
 the host, and one costs about as much as its kernel.
@@ -27,13 +28,22 @@ NEWTON_SCHULZ = ((3.4445, -4.7750, 2.0315),) * 5
 
 
 def _streamed(f):
-    """Runs f with `stream` as the current stream, so that what it allocates
-    belongs to the stream that uses it."""
+    """Runs f on the device of its first tensor, as the library launches on the
+    current device, and with `stream` as the current stream, so that what it
+    allocates belongs to the stream that uses it."""
+    first = f.__code__.co_varnames[0]
+
     @wraps(f)
     def on(*args, stream=None, **kw):
-        if stream is None:
+        device = (args[0] if args else kw[first]).get_device()   # (-1: a host tensor, which f refuses)
+        if stream is not None:
+            if stream.device.index != device:
+                raise ValueError(f"stream is of device {stream.device}, {first} of {device}")
+            with torch.cuda.stream(stream):   # (makes its device current, too)
+                return f(*args, **kw)
+        if device < 0 or device == torch._C._cuda_getDevice():
             return f(*args, **kw)
-        with torch.cuda.stream(stream):
+        with torch.cuda.device(device):
             return f(*args, **kw)
     return on
 
@@ -176,7 +186,13 @@ def route(expert, n_experts: int) -> Route:
     return Route(rows, slots, offsets)
 
 
-def _check_weights(weights, plan: Route, like):
+def _check_plan(plan: Route, like, weights=None):
+    device, slots = like.get_device(), plan.row_of_slot.numel()
+    for t in plan:
+        if t.get_device() != device or t.dtype is not torch.int32 or not t.is_contiguous():
+            raise ValueError(f"the plan's tensors must be contiguous int32 on {like.device}")
+    if plan.slot_of_row.numel() != slots:
+        raise ValueError(f"the plan's slot_of_row must have {slots} elements")
     if weights is not None:
         _whole(weights, plan.row_of_slot.shape, torch.float32, like, "weights")
 
@@ -189,6 +205,7 @@ def route_rows(x, plan: Route):
     tokens, width = x.shape
     if tokens != n:
         raise ValueError(f"x must have {n} rows, not {tokens}")
+    _check_plan(plan, x)
     ld = _leading(x, "x")
     d = B.mace_route_desc(n, k, plan.offsets.shape[0] - 1, width, dtype, ld, width)
     rows = x.new_empty((n * k, width))
@@ -207,7 +224,7 @@ def combine_rows(rows, plan: Route, weights=None):
     if slots != n * k:
         raise ValueError(f"rows must have {n * k} rows, not {slots}")
     ld = _leading(rows, "rows")
-    _check_weights(weights, plan, rows)
+    _check_plan(plan, rows, weights)
     d = B.mace_route_desc(n, k, plan.offsets.shape[0] - 1, width, dtype, width, ld)
     out = rows.new_empty((n, width))
     B._check(B.lib().mace_route_combine(d, rows.data_ptr(), None if weights is None else weights.data_ptr(),
@@ -226,7 +243,7 @@ def combine_rows_backward(dout, rows, plan: Route, weights=None):
         raise ValueError(f"dout must have {n} rows, not {tokens}")
     ld = _leading(dout, "dout")
     ld_rows = _rows(rows, n * k, width, dout, "rows")
-    _check_weights(weights, plan, dout)
+    _check_plan(plan, dout, weights)
     d = B.mace_route_desc(n, k, plan.offsets.shape[0] - 1, width, dtype, ld, ld_rows)
     drows = dout.new_empty((n * k, ld_rows))   # rows and their gradient share a leading dimension
     if ld_rows != width:
