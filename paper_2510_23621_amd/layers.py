@@ -6,7 +6,9 @@ the work on ``stream`` (a torch.cuda.Stream; default: the current one).
 Tensors are float32, bfloat16 or float16 on one GPU, whichever is current, and
 ``stream`` is one of that GPU's; rows may be strided (any row stride, columns
 adjacent).  Tensors of another stream are the caller's to order, as with any
-torch operation.
+torch operation.  Nothing here records a graph for autograd: the backward
+functions are called by the program, under torch.no_grad() or on detached
+tensors, and tensors that ask for a gradient are refused otherwise.
 
 The checks are written out in each function: a small layer's call is bound by
 the host, and one costs about as much as its kernel.
@@ -30,11 +32,17 @@ NEWTON_SCHULZ = ((3.4445, -4.7750, 2.0315),) * 5
 def _streamed(f):
     """Runs f on the device of its first tensor, as the library launches on the
     current device, and with `stream` as the current stream, so that what it
-    allocates belongs to the stream that uses it."""
+    allocates belongs to the stream that uses it.  Refuses tensors that ask for
+    a gradient: the result would have lost it without a word."""
     first = f.__code__.co_varnames[0]
 
     @wraps(f)
     def on(*args, stream=None, **kw):
+        if torch.is_grad_enabled():
+            for t in (*args, *kw.values()):
+                if getattr(t, "requires_grad", False):
+                    raise ValueError(f"{f.__name__} records no gradients: call it under torch.no_grad() or on "
+                                     "detached tensors")
         device = (args[0] if args else kw[first]).get_device()   # (-1: a host tensor, which f refuses)
         if stream is not None:
             if stream.device.index != device:
