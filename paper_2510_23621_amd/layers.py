@@ -5,10 +5,11 @@ the work on ``stream`` (a torch.cuda.Stream; default: the current one).
 
 Tensors are float32, bfloat16 or float16 on one GPU, whichever is current, and
 ``stream`` is one of that GPU's; rows may be strided (any row stride, columns
-adjacent).  Tensors of another stream are the caller's to order, as with any
-torch operation.  Nothing here records a graph for autograd: the backward
-functions are called by the program, under torch.no_grad() or on detached
-tensors, and tensors that ask for a gradient are refused otherwise.
+adjacent), and gradients handed to a backward function (dy, dout, drows) in any
+order, at the price of a copy.  Tensors of another stream are the caller's to
+order, as with any torch operation.  Nothing here records a graph for autograd:
+the backward functions are called by the program, under torch.no_grad() or on
+detached tensors, and tensors that ask for a gradient are refused otherwise.
 
 The checks are written out in each function: a small layer's call is bound by
 the host, and one costs about as much as its kernel.
@@ -69,6 +70,13 @@ def _leading(t, name: str) -> int:
     if (s1 != 1 and c > 1 and n > 0) or (s0 < c and n > 1):
         raise ValueError(f"{name}'s columns must be adjacent and its rows apart")
     return s0 if n > 1 else c
+
+
+def _gradient(t):
+    """t as the kernels can read it: autograd hands on expanded and transposed gradients."""
+    if t.is_contiguous() or t.dim() == 2 and t.stride(1) == 1 and t.stride(0) >= t.shape[1]:
+        return t
+    return t.contiguous()
 
 
 def _rows(t, n: int, c: int, like, name: str) -> int:
@@ -144,6 +152,7 @@ def linear_backward(dy, x, w, z=None, *, offsets=None, act: str = "none", bias: 
     in the others' places)."""
     d = _linear_desc(x, w, offsets, act)
     n, m = d.n_rows, d.n_out
+    dy = _gradient(dy)
     ld_dy = _rows(dy, n, m, x, "dy")
     if d.act:
         if z is None:
@@ -226,6 +235,10 @@ def route_rows(x, plan: Route):
 def combine_rows(rows, plan: Route, weights=None):
     """[tokens, width]: each token's kept rows times their weights (float32
     [tokens, top_k], None: ones), summed."""
+    return _combine(rows, plan, weights)
+
+
+def _combine(rows, plan: Route, weights=None):
     dtype = _gpu_matrix(rows, "rows")
     n, k = plan.row_of_slot.shape
     slots, width = rows.shape
@@ -244,6 +257,7 @@ def combine_rows(rows, plan: Route, weights=None):
 @_streamed
 def combine_rows_backward(dout, rows, plan: Route, weights=None):
     """(drows, dweights) of `combine_rows`; dweights is None without weights."""
+    dout = _gradient(dout)
     dtype = _gpu_matrix(dout, "dout")
     n, k = plan.row_of_slot.shape
     tokens, width = dout.shape
@@ -265,9 +279,10 @@ def combine_rows_backward(dout, rows, plan: Route, weights=None):
     return drows, dw
 
 
-def route_rows_backward(drows, plan: Route, *, stream=None):
+@_streamed
+def route_rows_backward(drows, plan: Route):
     """Gradient of `route_rows` with respect to x."""
-    return combine_rows(drows, plan, None, stream=stream)
+    return _combine(_gradient(drows), plan)
 
 
 @lru_cache(maxsize=64)
