@@ -266,16 +266,23 @@ def combine_rows_backward(dout, rows, plan: Route, weights=None):
     ld = _leading(dout, "dout")
     ld_rows = _rows(rows, n * k, width, dout, "rows")
     _check_plan(plan, dout, weights)
-    d = B.mace_route_desc(n, k, plan.offsets.shape[0] - 1, width, dtype, ld, ld_rows)
-    drows = dout.new_empty((n * k, ld_rows))   # rows and their gradient share a leading dimension
-    if ld_rows != width:
-        drows = drows[:, :width]
+    drows = dout.new_empty((n * k, width))
     dw = None if weights is None else torch.empty_like(weights)
-    B._check(B.lib().mace_route_combine_backward(d, dout.data_ptr(), rows.data_ptr(),
+    lib, stream = B.lib(), _current_stream(dout)
+
+    def call(ld_rows, drows, dw):   # (the library takes one leading dimension for rows and their gradient)
+        d = B.mace_route_desc(n, k, plan.offsets.shape[0] - 1, width, dtype, ld, ld_rows)
+        B._check(lib.mace_route_combine_backward(d, dout.data_ptr(), rows.data_ptr(),
                                                  None if weights is None else weights.data_ptr(),
-                                                 plan.row_of_slot.data_ptr(), plan.offsets.data_ptr(), drows.data_ptr(),
-                                                 None if dw is None else dw.data_ptr(), _current_stream(dout)),
-             "mace_route_combine_backward")
+                                                 plan.row_of_slot.data_ptr(), plan.offsets.data_ptr(),
+                                                 None if drows is None else drows.data_ptr(),
+                                                 None if dw is None else dw.data_ptr(), stream),
+                 "mace_route_combine_backward")
+    if ld_rows == width or dw is None:   # (without weights' gradients the rows are not read)
+        call(width, drows, dw)
+    else:
+        call(ld_rows, None, dw)
+        call(width, drows, None)
     return drows, dw
 
 
