@@ -16,7 +16,7 @@ the host, and one costs about as much as its kernel.
 """
 from __future__ import annotations
 
-from functools import lru_cache, wraps
+from functools import wraps
 from typing import NamedTuple
 
 import numpy as np
@@ -26,7 +26,8 @@ from . import binding as B
 
 DTYPES = {torch.float32: B.MACE_TYPE_FP32, torch.bfloat16: B.MACE_TYPE_BF16, torch.float16: B.MACE_TYPE_FP16}
 ACTIVATIONS = {"none": B.MACE_ACT_NONE, "silu": B.MACE_ACT_SILU, "gelu": B.MACE_ACT_GELU}
-# a, b, c of five steps that bring singular values from about 0.01..1 to about 0.7..1.2
+# a, b, c of five steps that bring singular values from about 0.01..1 to about 0.7..1.2: the
+# ones published with the Muon optimiser (K. Jordan and others, 2024)
 NEWTON_SCHULZ = ((3.4445, -4.7750, 2.0315),) * 5
 
 
@@ -292,10 +293,19 @@ def route_rows_backward(drows, plan: Route):
     return _combine(_gradient(drows), plan)
 
 
-@lru_cache(maxsize=64)
-def _coefficients(steps: tuple) -> np.ndarray:
-    """float64 [n, 3] on the host; a training run has one or a few such schedules."""
-    return np.ascontiguousarray(steps, dtype=np.float64).reshape(-1, 3)
+def _coefficients(steps) -> np.ndarray:
+    """float64 [n, 3] on the host."""
+    if not hasattr(steps, "__len__"):
+        steps = list(steps)
+    if len(steps) == 0:
+        return np.empty((0, 3))
+    try:
+        coef = np.array(steps, dtype=np.float64, order="C")
+    except ValueError:   # (of different lengths)
+        coef = None
+    if coef is None or coef.ndim != 2 or coef.shape[1] != 3:
+        raise ValueError("coefficients must be triples (a, b, c), one per step")
+    return coef
 
 
 @_streamed
@@ -305,7 +315,7 @@ def orthogonalise(g, coefficients=NEWTON_SCHULZ, *, eps: float = 1e-7):
     dtype = DTYPES.get(g.dtype)
     if dtype is None or g.dim() not in (2, 3) or not g.is_cuda:
         raise ValueError("g must be a [(batch,) rows, cols] GPU tensor of float32, bfloat16 or float16")
-    coef = _coefficients(coefficients if type(coefficients) is tuple else tuple(map(tuple, coefficients)))
+    coef = _coefficients(coefficients)
     if g.dim() == 3:
         (b, rows, cols), (sb, s0, s1) = g.shape, g.stride()
     else:
