@@ -94,11 +94,18 @@ def _whole(t, shape, dtype, like, name: str):
         raise ValueError(f"{name} must be contiguous {tuple(shape)} {dtype} on {like.device}")
 
 
+def _too_large(name: str):
+    # (the descriptors' fields have 32 bits and would wrap; what fits, the library itself takes or refuses)
+    raise ValueError(f"{name} has more than 2^31 - 1 columns, groups or choices")
+
+
 def _gpu_matrix(t, name: str) -> int:
     """The library's number of t's dtype; t has to be a matrix on a GPU."""
     dtype = DTYPES.get(t.dtype)
     if dtype is None or t.dim() != 2 or not t.is_cuda:
         raise ValueError(f"{name} must be a 2-d GPU tensor of float32, bfloat16 or float16")
+    if t.shape[1] >> 31:
+        _too_large(name)
     return dtype
 
 
@@ -116,6 +123,8 @@ def _linear_desc(x, w, offsets, act):
         raise ValueError("w must be [n_in, n_out] or [groups, n_in, n_out]")
     if k != n_in or w.dtype is not x.dtype or w.get_device() != x.get_device() or not w.is_contiguous():
         raise ValueError(f"w must be contiguous with {n_in} input rows, of x's dtype and device")
+    if (groups | n_out) >> 31:
+        _too_large("w")
     if offsets is not None:
         _whole(offsets, (groups + 1,), torch.int32, x, "offsets")
     elif groups != 1:
@@ -191,6 +200,8 @@ def route(expert, n_experts: int) -> Route:
     if expert.dim() != 2 or not expert.is_cuda or expert.dtype is not torch.int32 or not expert.is_contiguous():
         raise ValueError("expert must be a contiguous int32 [tokens, top_k] GPU tensor")
     n, k = expert.shape
+    if k >> 31 or not -1 << 31 <= n_experts < 1 << 31:
+        _too_large("expert")
     d = B.mace_route_desc(n, k, n_experts, 1, B.MACE_TYPE_FP32, 1, 1)
     lib = B.lib()
     s = n * k
@@ -322,6 +333,8 @@ def orthogonalise(g, coefficients=NEWTON_SCHULZ, *, eps: float = 1e-7):
         (rows, cols), (s0, s1), b, sb = g.shape, g.stride(), 1, 0
     if (s1 != 1 and cols > 1 or s0 < cols and rows > 1 or sb < 0) and g.numel():
         raise ValueError("g's columns must be adjacent and its rows apart")
+    if (rows | cols) >> 31:
+        _too_large("g")
     d = B.mace_orthogonalise_desc(b, rows, cols, dtype, len(coef), s0 if rows > 1 else cols, sb, cols, rows * cols, eps)
     out = g.new_empty(g.shape)
     lib = B.lib()
