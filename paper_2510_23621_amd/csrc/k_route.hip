@@ -11,57 +11,60 @@ namespace {
 constexpr int kMaxExperts = 512;   // (the sort's counters fit 64 KB of LDS)
 constexpr int kSortWaves = 16;
 constexpr int kSortThreads = 64 * kSortWaves;
-constexpr int kSortChunk = 4096;   // slots per block
+constexpr int kSortChunk = 4096;   // slots a block sorts at a time
+constexpr int kSortBlocks = 512;   // most blocks: each reads every block's counts
 
 __device__ __forceinline__ int bucket_of(int e, int E) { return e >= 0 && e < E ? e : E; }
 
-// slots per bucket of each chunk
-__global__ void __launch_bounds__(kSortThreads) route_count_kernel(const int* __restrict__ expert, int64_t slots, int E,
-                                                                   int* __restrict__ hist) {
+// slots per bucket of each block's span (consecutive chunks)
+__global__ void __launch_bounds__(kSortThreads) route_count_kernel(const int* __restrict__ expert, int64_t slots, int64_t span,
+                                                                   int E, int* __restrict__ hist) {
   __shared__ int cnt[kMaxExperts + 1];
   for (int i = threadIdx.x; i <= E; i += kSortThreads) cnt[i] = 0;
   __syncthreads();
-  const int64_t s0 = (int64_t)blockIdx.x * kSortChunk, s1 = min<int64_t>(slots, s0 + kSortChunk);
+  const int64_t s0 = blockIdx.x * span, s1 = min<int64_t>(slots, s0 + span);
   for (int64_t s = s0 + threadIdx.x; s < s1; s += kSortThreads) atomicAdd(&cnt[bucket_of(expert[s], E)], 1);
   __syncthreads();
   for (int i = threadIdx.x; i <= E; i += kSortThreads) hist[(size_t)blockIdx.x * (E + 1) + i] = cnt[i];
 }
 
-// The stable counting sort of one chunk. Bucket E holds the dropped slots, so
-// the result is a permutation of all slots. Each wave owns a contiguous part of
-// the chunk; its counters start behind every earlier slot of the same bucket
-// (earlier chunks from hist, earlier waves from their counts), and it ranks 64
+// The stable counting sort, a span of chunks per block. Bucket E holds the dropped
+// slots, so the result is a permutation of all slots. Each wave owns a contiguous part
+// of a chunk; its counters start behind every earlier slot of the same bucket
+// (earlier blocks from hist, earlier chunks and waves from their counts), and it ranks 64
 // slots at a time by matching buckets across its lanes. Integer counts only: the
 // order of the LDS additions does not matter. Up to one chunk the count is its own and
 // the sort one launch (96 slots 3.5 us, bound by the launch); 294,912 slots of 64
-// experts 14 us with the counting launch.
+// experts 14 us with the counting launch, 2^26 of 64 experts 470 us.
 __global__ void __launch_bounds__(kSortThreads)
-route_sort_kernel(const int* __restrict__ expert, int64_t slots, int E, int bits, const int* __restrict__ hist,
+route_sort_kernel(const int* __restrict__ expert, int64_t slots, int64_t span, int E, int bits, const int* __restrict__ hist,
                   int* __restrict__ row_of_slot, int* __restrict__ slot_of_row, int* __restrict__ offsets) {
   extern __shared__ int sm[];
   const int E1 = E + 1, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   int* cnt = sm;                       // [waves][E1]
-  int* base = cnt + kSortWaves * E1;   // [E1] slots of the bucket in earlier chunks
-  int* total = base + E1;              // [E1] slots of the bucket in all chunks, then its first row
+  int* next = cnt + kSortWaves * E1;   // [E1] slots of the bucket in earlier blocks, then its next row
+  int* total = next + E1;              // [E1] slots of the bucket in all blocks, then its first row
   for (int i = tid; i < (kSortWaves + 2) * E1; i += kSortThreads) sm[i] = 0;
   __syncthreads();
-  const int64_t c0 = (int64_t)blockIdx.x * kSortChunk;
+  const int64_t s0 = blockIdx.x * span, s1 = min<int64_t>(slots, s0 + span);
   constexpr int per = kSortChunk / kSortWaves;
-  const int64_t w0 = c0 + w * per, w1 = min<int64_t>(slots, w0 + per);
   int e[per / 64];
+  auto count = [&](int64_t c0) {   // the chunk's buckets, counted per wave
 #pragma unroll
-  for (int i = 0; i < per / 64; ++i) {
-    const int64_t s = w0 + 64 * i + lane;
-    e[i] = s < w1 ? bucket_of(expert[s], E) : -1;
-    if (e[i] >= 0) atomicAdd(&cnt[w * E1 + e[i]], 1);
-  }
+    for (int i = 0; i < per / 64; ++i) {
+      const int64_t s = c0 + w * per + 64 * i + lane;
+      e[i] = s < s1 ? bucket_of(expert[s], E) : -1;
+      if (e[i] >= 0) atomicAdd(&cnt[w * E1 + e[i]], 1);
+    }
+  };
+  count(s0);
   if (gridDim.x > 1) {
-    // groups of threads over (chunk, bucket): partial sums of the chunk counts
+    // groups of threads over (block, bucket): partial sums of the blocks' counts
     for (int i = tid; i < (int)gridDim.x * E1; i += kSortThreads) {
       const int b = i / E1, k = i - b * E1, h = hist[i];
       if (h) {
         atomicAdd(&total[k], h);
-        if (b < (int)blockIdx.x) atomicAdd(&base[k], h);
+        if (b < (int)blockIdx.x) atomicAdd(&next[k], h);
       }
     }
     __syncthreads();
@@ -93,34 +96,45 @@ route_sort_kernel(const int* __restrict__ expert, int64_t slots, int E, int bits
     }
   }
   __syncthreads();
-  for (int k = tid; k < E1; k += kSortThreads) {   // counters: the wave's first row per bucket
-    int at = total[k] + base[k];
-    for (int v = 0; v < kSortWaves; ++v) {
-      const int c = cnt[v * E1 + k];
-      cnt[v * E1 + k] = at;
-      at += c;
-    }
-  }
-  __syncthreads();
+  for (int k = tid; k < E1; k += kSortThreads) next[k] += total[k];   // (a thread keeps its buckets from here on)
   volatile int* mine = cnt + w * E1;
+  for (int64_t c0 = s0; c0 < s1; c0 += kSortChunk) {
+    if (c0 > s0) {
+      __syncthreads();   // every wave has ranked the chunk before
+      for (int i = tid; i < kSortWaves * E1; i += kSortThreads) cnt[i] = 0;
+      __syncthreads();
+      count(c0);
+      __syncthreads();
+    }
+    for (int k = tid; k < E1; k += kSortThreads) {   // counters: the wave's first row per bucket
+      int at = next[k];
+      for (int v = 0; v < kSortWaves; ++v) {
+        const int c = cnt[v * E1 + k];
+        cnt[v * E1 + k] = at;
+        at += c;
+      }
+      next[k] = at;
+    }
+    __syncthreads();
 #pragma unroll
-  for (int i = 0; i < per / 64; ++i) {
-    const int64_t s = w0 + 64 * i + lane;
-    const bool on = e[i] >= 0;
-    unsigned long long peers = __ballot(on);
-    for (int b = 0; b < bits; ++b) {
-      const unsigned long long m = __ballot(on && (e[i] >> b & 1));
-      peers &= (e[i] >> b & 1) ? m : ~m;
+    for (int i = 0; i < per / 64; ++i) {
+      const int64_t s = c0 + w * per + 64 * i + lane;
+      const bool on = e[i] >= 0;
+      unsigned long long peers = __ballot(on);
+      for (int b = 0; b < bits; ++b) {
+        const unsigned long long m = __ballot(on && (e[i] >> b & 1));
+        peers &= (e[i] >> b & 1) ? m : ~m;
+      }
+      if (on) {
+        const int rank = __popcll(peers & ((1ull << lane) - 1));
+        const int row = mine[e[i]] + rank;
+        row_of_slot[s] = row;
+        slot_of_row[row] = (int)s;
+      }
+      __builtin_amdgcn_wave_barrier();
+      if (on && lane == __ffsll(peers) - 1) mine[e[i]] = mine[e[i]] + __popcll(peers);
+      __builtin_amdgcn_wave_barrier();
     }
-    if (on) {
-      const int rank = __popcll(peers & ((1ull << lane) - 1));
-      const int row = mine[e[i]] + rank;
-      row_of_slot[s] = row;
-      slot_of_row[row] = (int)s;
-    }
-    __builtin_amdgcn_wave_barrier();
-    if (on && lane == __ffsll(peers) - 1) mine[e[i]] = mine[e[i]] + __popcll(peers);
-    __builtin_amdgcn_wave_barrier();
   }
 }
 
@@ -332,7 +346,7 @@ using namespace mace;
 
 extern "C" size_t mace_route_workspace_bytes(const mace_route_desc* desc) {
   if (check(desc) != MACE_OK) return 0;
-  return 256 + (size_t)chunks(*desc) * (desc->n_experts + 1) * sizeof(int);
+  return 256 + (size_t)std::min<int64_t>(chunks(*desc), kSortBlocks) * (desc->n_experts + 1) * sizeof(int);
 }
 
 extern "C" mace_status mace_route_build(const mace_route_desc* desc, const int32_t* expert, int32_t* row_of_slot,
@@ -343,7 +357,8 @@ extern "C" mace_status mace_route_build(const mace_route_desc* desc, const int32
   const int64_t slots = desc->n_tokens * desc->top_k;
   if (!offsets || (slots > 0 && (!expert || !row_of_slot || !slot_of_row))) return MACE_EINVAL;
   const int E = desc->n_experts;
-  const int64_t blocks = std::max<int64_t>(1, chunks(*desc));
+  const int64_t each = std::max<int64_t>(1, (chunks(*desc) + kSortBlocks - 1) / kSortBlocks);   // chunks per block
+  const int64_t blocks = std::max<int64_t>(1, (chunks(*desc) + each - 1) / each), span = each * kSortChunk;
   int* hist = reinterpret_cast<int*>((reinterpret_cast<uintptr_t>(workspace) + 3) & ~uintptr_t(3));
   if (blocks > 1) {
     if (!workspace) return MACE_EINVAL;
@@ -353,11 +368,11 @@ extern "C" mace_status mace_route_build(const mace_route_desc* desc, const int32
   int bits = 1;
   while ((1 << bits) <= E) ++bits;
   if (blocks > 1) {
-    route_count_kernel<<<(unsigned)blocks, kSortThreads, 0, s>>>(expert, slots, E, hist);
+    route_count_kernel<<<(unsigned)blocks, kSortThreads, 0, s>>>(expert, slots, span, E, hist);
     if ((st = launched()) != MACE_OK) return st;
   }
   route_sort_kernel<<<(unsigned)blocks, kSortThreads, (kSortWaves + 2) * (E + 1) * sizeof(int), s>>>(
-      expert, slots, E, bits, hist, row_of_slot, slot_of_row, offsets);
+      expert, slots, span, E, bits, hist, row_of_slot, slot_of_row, offsets);
   return launched();
 }
 
