@@ -633,6 +633,18 @@ __device__ __forceinline__ void tile_gemm_direct(const Operand<T>& ro, const Ope
   }
 }
 
+// Blocks of a launch, numbered along x and then along y. An axis takes fewer than 2^32
+// threads: a longer one wraps, without an error. grid_of puts at most 2^21 blocks on x
+// (of 1024 threads at most) and fills the last row of y: a kernel's blocks past its work
+// return.
+constexpr int64_t kGridRow = 1 << 21, kGridMost = 1 << 30;
+inline bool fits_grid(int64_t blocks) { return blocks <= kGridMost; }
+inline dim3 grid_of(int64_t blocks) {
+  return dim3((unsigned)(blocks < kGridRow ? blocks : kGridRow), (unsigned)((blocks + kGridRow - 1) / kGridRow));
+}
+__device__ __forceinline__ int block_id() { return blockIdx.y * gridDim.x + blockIdx.x; }
+__device__ __forceinline__ int block_count() { return gridDim.x * gridDim.y; }
+
 // Work items 0..n-1 in the order blocks take them: consecutive block numbers go
 // to different XCDs, so each XCD gets a contiguous run of items (neighbours
 // share operand rows in its L2).

@@ -79,7 +79,7 @@ struct BiasGradArgs {
   T* db;
   const int* offsets;
   int64_t n;
-  int n_out, run_rows, max_runs;
+  int n_out, groups, run_rows, max_runs;
 };
 
 // The block's product, by the way its shape and operands allow
@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(S::NT) linear_fwd_kernel(LinearArgs<T> a) {
   __shared__ __align__(16) unsigned short lds[tile_lds<T, S>];
   const int tid = threadIdx.x;
   const int tiles_n = (a.n_out + S::BN - 1) / S::BN;
-  const int id = xcd_order(blockIdx.x, gridDim.x);
+  const int id = xcd_order(block_id(), block_count());
   const int c0 = id % tiles_n * S::BN, cols = min(S::BN, a.n_out - c0);
   RowRun run;
   if (!find_run(a.offsets, a.groups, a.n, S::BM, id / tiles_n, run)) return;
@@ -266,7 +266,7 @@ __global__ void __launch_bounds__(S::NT) linear_fwd_thin_kernel(LinearArgs<float
   __shared__ __align__(16) float lds[S::RT * S::CT * 1024];
   const int tid = threadIdx.x;
   const int tiles_n = (a.n_out + S::BN - 1) / S::BN;
-  const int id = blockIdx.x;
+  const int id = block_id();
   const int c0 = id % tiles_n * S::BN, cols = min(S::BN, a.n_out - c0);
   RowRun run;
   if (!find_run(a.offsets, a.groups, a.n, S::BM, id / tiles_n, run)) return;
@@ -388,7 +388,7 @@ __global__ void __launch_bounds__(S::NT) __attribute__((amdgpu_waves_per_eu(2)))
   __shared__ __align__(16) unsigned short lds[S::LDS];
   const int tid = threadIdx.x;
   const int tiles_n = (a.n_out + S::BN - 1) / S::BN;
-  const int id = xcd_order(blockIdx.x, gridDim.x);
+  const int id = xcd_order(block_id(), block_count());
   const int c0 = id % tiles_n * S::BN, cols = min(S::BN, a.n_out - c0);
   RowRun run;
   if (!find_run(a.offsets, a.groups, a.n, S::RUN, id / tiles_n, run)) return;
@@ -426,7 +426,7 @@ __global__ void __launch_bounds__(S::NT) __attribute__((amdgpu_waves_per_eu(2)))
   __shared__ __align__(16) unsigned short lds[S::LDS];
   const int tid = threadIdx.x;
   const int tiles_n = (a.n_in + S::BN - 1) / S::BN;
-  const int id = xcd_order(blockIdx.x, gridDim.x);
+  const int id = xcd_order(block_id(), block_count());
   const int c0 = id % tiles_n * S::BN, cols = min(S::BN, a.n_in - c0);
   RowRun run;
   if (!find_run(a.offsets, a.groups, a.n, S::RUN, id / tiles_n, run)) return;
@@ -515,6 +515,7 @@ __device__ __forceinline__ void weight_grad_tile(const WeightGradArgs<T>& a, int
 template <class T>
 __device__ __forceinline__ void bias_grad(const BiasGradArgs<T>& a, int id, float* lds, int tid) {
   const int blocks = (a.n_out + 63) / 64, g = id / blocks;
+  if (g >= a.groups) return;   // (a grid's last row is full)
   const int c = tid & 63, y = tid >> 6, col = id % blocks * 64 + c;   // (waves past the fourth only keep the barrier)
   int first = 0, runs = 0;
   if (!a.offsets) {
@@ -561,7 +562,7 @@ __global__ void __launch_bounds__(S::NT)
 linear_grad_kernel(RowGradArgs<T> a, WeightGradArgs<T> b, BiasGradArgs<T> c, int row_blocks, int weight_blocks) {
   __shared__ __align__(16) unsigned short lds[tile_lds<T, S>];
   const int tid = threadIdx.x;
-  int id = blockIdx.x;
+  int id = block_id();
   if (id < row_blocks) {
     if constexpr (__is_same(S, RS)) row_grad_tile<T, AL, S>(a, xcd_order(id, row_blocks), lds, tid);
     else row_grad_thin<AL, RS>(a, id, reinterpret_cast<float*>(lds), tid);
@@ -794,8 +795,8 @@ mace_status forward(const mace_linear_desc& d, const void* x, const void* w, con
       return with_narrow<T>(d.n_in, [&](auto shape) -> mace_status {
         using S = decltype(shape);
         const int64_t blocks = (ceil_div(d.n_rows, S::RUN) + (offsets ? d.n_groups : 0)) * ceil_div(d.n_out, S::BN);
-        if (blocks > INT32_MAX) return MACE_EUNSUPPORTED;
-        linear_fwd_narrow_kernel<T, AL, S><<<(unsigned)blocks, S::NT, 0, s>>>(a);
+        if (!fits_grid(blocks)) return MACE_EUNSUPPORTED;
+        linear_fwd_narrow_kernel<T, AL, S><<<grid_of(blocks), S::NT, 0, s>>>(a);
         return launched();
       });
     if constexpr (sizeof(T) == 4)
@@ -803,7 +804,7 @@ mace_status forward(const mace_linear_desc& d, const void* x, const void* w, con
         auto run = [&](auto shape) {
           using S = decltype(shape);
           const int64_t blocks = (ceil_div(d.n_rows, S::BM) + (offsets ? d.n_groups : 0)) * ceil_div(d.n_out, S::BN);
-          linear_fwd_thin_kernel<AL, S><<<(unsigned)blocks, S::NT, 0, s>>>(a);
+          linear_fwd_thin_kernel<AL, S><<<grid_of(blocks), S::NT, 0, s>>>(a);
           return launched();
         };
         return thin2(d.n_rows, d.n_out) ? run(Thin2{}) : run(Thin{});
@@ -811,8 +812,8 @@ mace_status forward(const mace_linear_desc& d, const void* x, const void* w, con
     return with_shape<T, AL>(shape_of(d.n_rows, d.n_out, 1, d.n_groups), [&](auto shape) -> mace_status {
       using S = decltype(shape);
       const int64_t blocks = (ceil_div(d.n_rows, S::BM) + (offsets ? d.n_groups : 0)) * ceil_div(d.n_out, S::BN);
-      if (blocks > INT32_MAX) return MACE_EUNSUPPORTED;
-      linear_fwd_kernel<T, AL, S><<<(unsigned)blocks, S::NT, 0, s>>>(a);
+      if (!fits_grid(blocks)) return MACE_EUNSUPPORTED;
+      linear_fwd_kernel<T, AL, S><<<grid_of(blocks), S::NT, 0, s>>>(a);
       return launched();
     });
   };
@@ -851,7 +852,7 @@ mace_status backward(const mace_linear_desc& d, const void* dy, int64_t lddy, co
   const RowGradArgs<T> ra{dz, (const T*)w, (T*)dx, offsets, d.n_rows, lddz, lddx, d.n_in, d.n_out, d.n_groups};
   const WeightGradArgs<T> wa{(const T*)x, dz, (T*)dw, p.splits > 1 ? reinterpret_cast<float*>(ws + p.part) : nullptr,
                              offsets, d.n_rows, d.ld_x, lddz, d.n_in, d.n_out, d.n_groups, p.splits};
-  const BiasGradArgs<T> ba{sums, (T*)db, offsets, d.n_rows, d.n_out, slope_run(d.n_rows), (int)slope_runs(d)};
+  const BiasGradArgs<T> ba{sums, (T*)db, offsets, d.n_rows, d.n_out, db ? d.n_groups : 0, slope_run(d.n_rows), (int)slope_runs(d)};
   bool want_x = dx && d.n_rows > 0;
   if (want_x && narrow<T>(d.n_rows, d.n_in, d.n_out)) {
     auto run = [&](auto al_) {
@@ -859,8 +860,8 @@ mace_status backward(const mace_linear_desc& d, const void* dy, int64_t lddy, co
       return with_narrow<T>(d.n_out, [&](auto shape) -> mace_status {
         using S = decltype(shape);
         const int64_t blocks = (ceil_div(d.n_rows, S::RUN) + (offsets ? d.n_groups : 0)) * ceil_div(d.n_in, S::BN);
-        if (blocks > INT32_MAX) return MACE_EUNSUPPORTED;
-        linear_row_grad_narrow_kernel<T, AL, S><<<(unsigned)blocks, S::NT, 0, s>>>(ra);
+        if (!fits_grid(blocks)) return MACE_EUNSUPPORTED;
+        linear_row_grad_narrow_kernel<T, AL, S><<<grid_of(blocks), S::NT, 0, s>>>(ra);
         return launched();
       });
     };
@@ -879,9 +880,9 @@ mace_status backward(const mace_linear_desc& d, const void* dy, int64_t lddy, co
         const int64_t rb = rows ? (ceil_div(d.n_rows, RS::BM) + (offsets ? d.n_groups : 0)) * ceil_div(d.n_in, RS::BN) : 0;
         const int64_t wb = weights ? ceil_div(d.n_in, S::BM) * ceil_div(d.n_out, S::BN) * d.n_groups * p.splits : 0;
         const int64_t blocks = rb + wb + (bias ? ceil_div(d.n_out, 64) * d.n_groups : 0);
-        if (blocks > INT32_MAX) return MACE_EUNSUPPORTED;
+        if (!fits_grid(blocks)) return MACE_EUNSUPPORTED;
         if (blocks == 0) return MACE_OK;
-        linear_grad_kernel<T, AL, S, RS><<<(unsigned)blocks, S::NT, 0, s>>>(ra, wa, ba, (int)rb, (int)wb);
+        linear_grad_kernel<T, AL, S, RS><<<grid_of(blocks), S::NT, 0, s>>>(ra, wa, ba, (int)rb, (int)wb);
         return launched();
       };
       if constexpr (sizeof(T) == 4 && S::BM == 64)

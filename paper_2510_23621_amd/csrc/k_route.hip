@@ -177,10 +177,10 @@ struct RouteArgs {
   const int *row_of_slot, *offsets;
 };
 
-// Item blockIdx.x * 256 + threadIdx.x as (row, vector) of rows of nv vectors, with
+// Item block_id() * 256 + threadIdx.x as (row, vector) of rows of nv vectors, with
 // one division of 64 bits per block.
 __device__ __forceinline__ int64_t item_row(int nv, int& vec) {
-  const uint64_t i0 = (uint64_t)blockIdx.x * 256;
+  const uint64_t i0 = (uint64_t)block_id() * 256;
   const uint64_t q0 = i0 >> 32 ? i0 / (unsigned)nv : (unsigned)i0 / (unsigned)nv;
   const unsigned j = (unsigned)(i0 - q0 * (unsigned)nv) + threadIdx.x, q = j / (unsigned)nv;
   vec = (int)(j - q * (unsigned)nv);
@@ -256,7 +256,7 @@ route_combine_bwd_kernel(RouteArgs a, int lg, const T* __restrict__ dout, const 
                          const float* __restrict__ weights, T* __restrict__ drows, float* __restrict__ dweights) {
   constexpr int VE = kVecElems<T>;
   const int lane = threadIdx.x & (lg - 1);
-  const int64_t t = ((int64_t)blockIdx.x * 256 + threadIdx.x) / lg;
+  const int64_t t = ((int64_t)block_id() * 256 + threadIdx.x) / lg;
   if (t >= a.n) return;   // (whole groups of lanes)
   const int live = a.offsets[a.E];
   for (int s0 = 0; s0 < a.k; s0 += U) {
@@ -386,9 +386,9 @@ extern "C" mace_status mace_route_gather(const mace_route_desc* desc, const void
     using T = decltype(zero);
     const RouteArgs a = args_of<T>(*desc, nullptr, offsets);
     const int64_t blocks = (a.n * a.k * a.nv + 255) / 256;
-    if (blocks > INT32_MAX) return MACE_EUNSUPPORTED;
+    if (!fits_grid(blocks)) return MACE_EUNSUPPORTED;
     auto f = aligned<T>(*desc, tokens, rows) ? route_gather_kernel<T, true> : route_gather_kernel<T, false>;
-    f<<<(unsigned)blocks, 256, 0, (hipStream_t)stream>>>(a, slot_of_row, (const T*)tokens, (T*)rows);
+    f<<<grid_of(blocks), 256, 0, (hipStream_t)stream>>>(a, slot_of_row, (const T*)tokens, (T*)rows);
     return launched();
   });
 }
@@ -403,11 +403,11 @@ extern "C" mace_status mace_route_combine(const mace_route_desc* desc, const voi
     using T = decltype(zero);
     const RouteArgs a = args_of<T>(*desc, row_of_slot, offsets);
     const int64_t blocks = (a.n * a.nv + 255) / 256;
-    if (blocks > INT32_MAX) return MACE_EUNSUPPORTED;
+    if (!fits_grid(blocks)) return MACE_EUNSUPPORTED;
     return by_slots(a.k, [&](auto u) {
       constexpr int U = decltype(u)::value;
       auto f = aligned<T>(*desc, rows, out) ? route_combine_kernel<T, true, U> : route_combine_kernel<T, false, U>;
-      f<<<(unsigned)blocks, 256, 0, (hipStream_t)stream>>>(a, (const T*)rows, weights, (T*)out);
+      f<<<grid_of(blocks), 256, 0, (hipStream_t)stream>>>(a, (const T*)rows, weights, (T*)out);
       return launched();
     });
   });
@@ -426,11 +426,11 @@ extern "C" mace_status mace_route_combine_backward(const mace_route_desc* desc, 
     int lg = 1;
     while (lg < 64 && lg < a.nv) lg *= 2;
     const int64_t blocks = (a.n * lg + 255) / 256;
-    if (blocks > INT32_MAX) return MACE_EUNSUPPORTED;
+    if (!fits_grid(blocks)) return MACE_EUNSUPPORTED;
     return by_slots(a.k, [&](auto u) {
       constexpr int U = decltype(u)::value;
       auto f = aligned<T>(*desc, dout, rows, drows) ? route_combine_bwd_kernel<T, true, U> : route_combine_bwd_kernel<T, false, U>;
-      f<<<(unsigned)blocks, 256, 0, (hipStream_t)stream>>>(a, lg, (const T*)dout, (const T*)rows, weights, (T*)drows, dweights);
+      f<<<grid_of(blocks), 256, 0, (hipStream_t)stream>>>(a, lg, (const T*)dout, (const T*)rows, weights, (T*)drows, dweights);
       return launched();
     });
   });
