@@ -173,31 +173,6 @@ __device__ __forceinline__ us8 tile_fragment(const unsigned short* t, int row0, 
   }
 }
 
-// FP32 tiles, copied as they are: KC [row][BK] with the 16-byte chunks of a row
-// XORed with the row, else [k][ROWS] with 64-byte pieces XORed with k / 8 (the
-// four lane groups of a fragment read different ones).
-template <int ROWS, int BK, bool KC>
-__device__ __forceinline__ int float_chunk(int row, int k) {   // offset of the 4-element chunk holding (row, k)
-  static_assert(BK == 32, "eight chunks per row");
-  if constexpr (KC) return row * BK + (((k >> 2) ^ (row & 7)) << 2);
-  else return k * ROWS + (((row >> 2) ^ ((k >> 3 & 3) << 2)) << 2);
-}
-// the fragment as tile_fragment's, split into its three bfloat16 parts
-template <int ROWS, int BK, bool KC>
-__device__ __forceinline__ void float_fragment(const float* t, int row0, int lane, us8 (&p)[3]) {
-  const int row = row0 + (lane & 15), k = 8 * (lane >> 4);
-  Vec8<float> v;
-  if constexpr (KC) {
-    v.v[0] = *reinterpret_cast<const f4*>(t + float_chunk<ROWS, BK, true>(row, k));
-    v.v[1] = *reinterpret_cast<const f4*>(t + float_chunk<ROWS, BK, true>(row, k + 4));
-  } else {
-    const float* q = t + float_chunk<ROWS, BK, false>(row, k) + (row & 3);   // (one chunk column for the eight k)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v.set(e, q[e * ROWS]);
-  }
-  to_planes<float>(v, p);
-}
-
 // Source of a tile in global memory: element (row, k) at base[row * ld + k] (KC)
 // or base[k * ld + row]. `rows` >= 1 of the tile's ROWS are in bounds; what is
 // read in the places of the others is not used, and every k past the end reads as
@@ -272,15 +247,6 @@ struct TileSource {
       for (int i = 0; i < P; ++i) *reinterpret_cast<us8*>(t + i * ROWS * BK + o) = q[i];
     }
   }
-  // FP32 as it is, in float_chunk's layout
-  __device__ __forceinline__ void store_floats(float* t, int tid) const {
-#pragma unroll
-    for (int u = 0; u < NV; ++u) {
-      const int r = row_of(u, tid), k = k_of(u, tid);
-      *reinterpret_cast<f4*>(t + float_chunk<ROWS, BK, KC>(r, k)) = v[0][u].v[0];
-      *reinterpret_cast<f4*>(t + float_chunk<ROWS, BK, KC>(KC ? r : r + 4, KC ? k + 4 : k)) = v[0][u].v[1];
-    }
-  }
 };
 
 __device__ __forceinline__ uint64_t uniform64(uint64_t v) {
@@ -288,32 +254,31 @@ __device__ __forceinline__ uint64_t uniform64(uint64_t v) {
          (unsigned)__builtin_amdgcn_readfirstlane((int)v);
 }
 
-// The same tile copied from memory to LDS without passing through registers
-// (16-byte aligned rows of whole vectors): a wave's 64 lanes
-// fill 1024 consecutive bytes, so each lane reads the chunk that the tile's
-// layout wants at its place. FP32 tiles are copied as they are (tile_floats). Whole steps of BK only; the rest of a row
-// goes through TileSource, which fills with zeros.
-template <int ES, int ROWS, int BK, bool KC, int NT>
+// The same tile of 16-bit elements copied from memory to LDS without passing through
+// registers (16-byte aligned rows of whole vectors): a wave's 64 lanes fill 1024
+// consecutive bytes, so each lane reads the chunk that the tile's layout wants at its
+// place. Whole steps of BK only; the rest of a row goes through TileSource, which
+// fills with zeros.
+template <int ROWS, int BK, bool KC, int NT>
 struct DirectSource {
-  static constexpr int VE = 16 / ES;   // elements of ES bytes per vector
-  static constexpr int NV = ROWS * BK / VE / NT;
-  static_assert(ROWS * BK / VE % NT == 0, "whole vectors per thread");
+  static constexpr int NV = ROWS * BK / 8 / NT;
+  static_assert(ROWS * BK / 8 % NT == 0, "whole vectors per thread");
   unsigned off[NV];   // bytes from the step's first element (the caller sees to it that they fit)
   uint64_t base, step;
   __device__ __forceinline__ void init(const void* base_, int64_t ld, int rows, int tid) {
     base = uniform64(reinterpret_cast<uint64_t>(base_));
-    step = uniform64(ES * (KC ? (uint64_t)BK : BK * ld));
+    step = uniform64(2 * (KC ? (uint64_t)BK : BK * ld));
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
       const int f = tid + NT * u;   // the vector at this place of the tile
       if constexpr (KC) {
-        constexpr int C = BK / VE;
+        constexpr int C = BK / 8;
         const int r = f / C, c = f % C ^ (C == 8 ? r & 7 : (r >> 1) & 3);
-        off[u] = ES * (unsigned)(min(r, rows - 1) * ld + VE * c);
+        off[u] = 2 * (unsigned)(min(r, rows - 1) * ld + 8 * c);
       } else {
-        constexpr int C = ROWS / VE;
-        const int k = f / C, c = f % C ^ (ES == 4 ? (k >> 3 & 3) << 2 : (k & 3) << 1);
-        off[u] = ES * (unsigned)(k * ld + min(VE * c, rows - VE));
+        constexpr int C = ROWS / 8;
+        const int k = f / C, c = f % C ^ (k & 3) << 1;
+        off[u] = 2 * (unsigned)(k * ld + min(8 * c, rows - 8));
       }
     }
   }
@@ -415,24 +380,8 @@ __device__ __forceinline__ void tile_products(const unsigned short* tr, const un
   }
 }
 
-// the same for FP32 tiles, split as they are read
-template <class S, bool KCR, bool KCC>
-__device__ __forceinline__ void float_products(const float* tr, const float* tc, int m0, int n0, int lane,
-                                               f4 (&acc)[S::TN][S::TM]) {
-  us8 b[S::TM][3];
-#pragma unroll
-  for (int i = 0; i < S::TM; ++i) float_fragment<S::BM, S::BK, KCR>(tr, m0 + 16 * i, lane, b[i]);
-#pragma unroll
-  for (int j = 0; j < S::TN; ++j) {
-    us8 a[3];
-    float_fragment<S::BN, S::BK, KCC>(tc, n0 + 16 * j, lane, a);
-    products<float>(a, b, acc[j]);
-  }
-}
-
-// 16-bit units of LDS per operand element, and a block's total
-template <class T, class S> constexpr int tile_units = S::DIRECT && sizeof(T) == 4 ? 2 : Planes<T>::n;
-template <class T, class S> constexpr int tile_lds = S::STAGES * tile_units<T, S> * (S::BM + S::BN) * S::BK;
+// 16-bit units of LDS of a block
+template <class T, class S> constexpr int tile_lds = S::STAGES * Planes<T>::n * (S::BM + S::BN) * S::BK;
 
 // Staged through registers: two LDS buffers and S::DEPTH sets of registers, or one buffer.
 template <class T, class S, bool KCR, bool KCC, bool AL>
@@ -568,9 +517,8 @@ struct Operand {
 template <class T, class S, bool KCR, bool KCC>
 __device__ __forceinline__ void tile_gemm_direct(const Operand<T>& ro, const Operand<T>& co, int K, unsigned short* lds,
                                                  int tid, f4 (&acc)[S::TN][S::TM]) {
-  constexpr bool F = sizeof(T) == 4;
-  constexpr int Q = F ? 1 : Planes<T>::n;   // planes copied
-  constexpr int U = tile_units<T, S>, CO = U * S::BM * S::BK, BUF = U * (S::BM + S::BN) * S::BK, ST = S::STAGES;
+  static_assert(sizeof(T) != 4, "FP32 is split on its way through registers");
+  constexpr int P = Planes<T>::n, CO = P * S::BM * S::BK, BUF = P * (S::BM + S::BN) * S::BK, ST = S::STAGES;
   const int lane = tid & 63, w = tid >> 6;
   const int m0 = (w / S::WN) * (S::BM / S::WM), n0 = (w % S::WN) * (S::BN / S::WN);
 #pragma unroll
@@ -579,9 +527,9 @@ __device__ __forceinline__ void tile_gemm_direct(const Operand<T>& ro, const Ope
     for (int i = 0; i < S::TM; ++i) acc[j][i] = f4{0.f, 0.f, 0.f, 0.f};
   if (K <= 0) return;
   const int whole = K / S::BK;
-  using R = DirectSource<F ? 4 : 2, S::BM, S::BK, KCR, S::NT>;
-  using C = DirectSource<F ? 4 : 2, S::BN, S::BK, KCC, S::NT>;
-  constexpr int COPIES = Q * (R::NV + C::NV);   // per step and wave
+  using R = DirectSource<S::BM, S::BK, KCR, S::NT>;
+  using C = DirectSource<S::BN, S::BK, KCC, S::NT>;
+  constexpr int COPIES = P * (R::NV + C::NV);   // per step and wave
   static_assert((ST - 2) * COPIES < 64, "the counter of copies in flight has six bits");
   R r;
   C c;
@@ -590,19 +538,14 @@ __device__ __forceinline__ void tile_gemm_direct(const Operand<T>& ro, const Ope
   auto copy = [&](int buffer) {
     unsigned short* t = lds + buffer * BUF;
 #pragma unroll
-    for (int q = 0; q < Q; ++q) {
+    for (int q = 0; q < P; ++q) {
       r.issue(t + q * S::BM * S::BK, q ? 2 * ro.plane : 0, tid);
       c.issue(t + CO + q * S::BN * S::BK, q ? 2 * co.plane : 0, tid);
     }
     r.next();
     c.next();
   };
-  auto multiply = [&](const unsigned short* t) {
-    if constexpr (F)
-      float_products<S, KCR, KCC>(reinterpret_cast<const float*>(t), reinterpret_cast<const float*>(t + CO), m0, n0, lane, acc);
-    else
-      tile_products<T, S, KCR, KCC, Q>(t, t + CO, m0, n0, lane, acc);
-  };
+  auto multiply = [&](const unsigned short* t) { tile_products<T, S, KCR, KCC, P>(t, t + CO, m0, n0, lane, acc); };
 #pragma unroll
   for (int i = 0; i < ST - 1; ++i)
     if (i < whole) copy(i);
@@ -620,11 +563,10 @@ __device__ __forceinline__ void tile_gemm_direct(const Operand<T>& ro, const Ope
     unsigned short* t = lds + b * BUF;   // (read ST steps ago, with a barrier since)
     auto rest = [&](auto source, const Operand<T>& o, bool kc, unsigned short* d) {
       const auto* p = o.p + (kc ? (int64_t)k : k * o.ld);
-      if constexpr (Q == 2) source.init(p, o.plane, o.ld, o.rows, tid);
+      if constexpr (P == 2) source.init(p, o.plane, o.ld, o.rows, tid);
       else source.init(p, o.ld, o.rows, tid);
       source.load(K - k, tid);
-      if constexpr (F) source.store_floats(reinterpret_cast<float*>(d), tid);
-      else source.store(d, tid);
+      source.store(d, tid);
     };
     rest(TileSource<T, S::BM, S::BK, KCR, true, S::NT>{}, ro, KCR, t);
     rest(TileSource<T, S::BN, S::BK, KCC, true, S::NT>{}, co, KCC, t + CO);
