@@ -686,10 +686,13 @@ constexpr int64_t kFillBlocks = 256, kLargeBlocks = 192;
 // each); the others trade that for more blocks. FP32 is split as it is staged, so
 // its tiles hold three planes per operand; with eight waves a block's splitting
 // overlaps its products (4096 x 1024 x 1024: 57 us, four waves 67; 4730 x 1978 -> 178:
-// 53 us, four waves 70).
+// 53 us, four waves 70). Where several such blocks share a CU they overlap each other, and
+// four waves take 36864 x 2048 x 2048 in 1529 us against 1546, 36864 x 1023 x 1023 in 425
+// against 458, but their dx in 1500 against 1462 and 410 against 405. 16-bit operands at
+// any alignment stay with eight (36864 x 1023 x 1023: 135 us, four waves 144).
 template <class T, bool AL> struct Shapes {   // (16-bit, any alignment)
-  using Large = TileShape<128, 128, 2, 2, 64, 1>;
   using Mid = TileShape<128, 128, 4, 2, 64, 1>;
+  using Large = Mid;
   using Small = TileShape<64, 64, 2, 2, 64, 2>;
 };
 template <> struct Shapes<__bf16, true> {
@@ -754,13 +757,16 @@ struct BackwardPlan {
 };
 
 // kind of tile of dW's blocks, and the parts each group's rows are cut into:
-// enough blocks to fill the chip, at least 512 rows each
+// enough blocks to fill the chip, at least 512 rows each (of a group of mean size). Only
+// aligned 16-bit rows have 256-wide tiles (20000 x 512 x 2048 FP32 222 us with the 8 parts
+// that fill it, 231 with 16)
 int weight_shape(const mace_linear_desc& d, int& splits) {
   const int64_t most = std::max<int64_t>(1, std::min<int64_t>(64, d.n_rows / d.n_groups / 512));
   const int kind = shape_of(d.n_in, d.n_out, d.n_groups * most);
-  const int b = kind == kLarge ? 256 : (kind == kMid ? 128 : 64);
+  const bool wide = kind == kLarge && d.dtype != MACE_TYPE_FP32 && ((d.n_in | d.n_out) & 7) == 0;
+  const int b = wide ? 256 : (kind == kSmall ? 64 : 128);
   const int64_t tiles = ceil_div(d.n_in, b) * ceil_div(d.n_out, b) * d.n_groups;
-  splits = (int)std::max<int64_t>(1, std::min(most, (kind == kLarge ? 256 : 512) / tiles));
+  splits = (int)std::max<int64_t>(1, std::min(most, (wide ? 256 : 512) / tiles));
   return kind;
 }
 
