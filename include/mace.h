@@ -402,7 +402,7 @@ mace_status mace_route_combine_backward(const mace_route_desc* desc, const void*
  * [n_steps][3], 0 <= n_steps <= 64.  They are checked on the host: over the
  * singular values that can occur (0 to 1 at the start) no step may reach a
  * singular value beyond 3.4 or a b A + c A A beyond 200, else MACE_ERANGE
- * (the products' operands are pairs of binary16 with fixed scales).  Products
+ * (the products' operands are pairs of binary16, scaled to that range).  Products
  * are as accurate as FP32's (in FP64 where the shorter side is at most 32, or at
  * most 64 and the longer beyond 128, over up to 10 of the default steps and as
  * many of others as multiply a rounding no more, 2^40 fold).  A matrix with a

@@ -27,8 +27,18 @@
 namespace mace {
 namespace {
 
+// Scales of the operands where the largest singular value is at least one half and b A +
+// c A A at least one; where steps leave less, x, A and B are scaled up by powers of two
+// (range_of), so that a pair's smallest digits are never what counts. A's scale is the
+// square of x's over kScaleX in all cases.
 constexpr float kScaleX = 4096.f, kScaleA = 4096.f, kScaleB = 256.f;
 constexpr double kMaxSigma = 3.4, kMaxB = 200.0;   // 3.4^2 kScaleA and 200 kScaleB fit binary16
+constexpr int kMaxSteps = 64;
+// A step on scaled operands, B <- b A + c (A A) and x <- a x + u (B x)
+struct ScaledSteps {
+  float a[kMaxSteps], u[kMaxSteps], b[kMaxSteps], c[kMaxSteps];
+  int n;
+};
 
 // one matrix's planes: hi [rows][ld], then lo
 struct PairMat {
@@ -202,7 +212,7 @@ __device__ __forceinline__ d4 gram64(const Columns<R>& t, int w, int tid) {
 }
 // the iteration on A = g g^T: Q <- Q / (|g| + eps), |g|^2 being the trace of A
 struct NsSteps {
-  double c[64][3];
+  double c[kMaxSteps][3];
   int n;
 };
 template <int R>
@@ -440,7 +450,7 @@ __device__ __forceinline__ void fit_write_symmetric(unsigned short* t, int plane
 
 template <class T, int MM, int NN>
 __global__ void __launch_bounds__(kFitThreads)
-ns_fit_kernel(const T* g, int64_t stride, int64_t ld, int m, int n, bool tall, double eps, NsSteps steps, T* out,
+ns_fit_kernel(const T* g, int64_t stride, int64_t ld, int m, int n, bool tall, double eps, ScaledSteps steps, T* out,
               int64_t ostride, int64_t old) {
   constexpr int PX = MM * NN, PA = MM * MM, QUADS = MM * NN / 4 / kFitThreads;
   extern __shared__ __align__(16) unsigned short fit_lds[];
@@ -493,8 +503,7 @@ ns_fit_kernel(const T* g, int64_t stride, int64_t ld, int m, int n, bool tall, d
     p.each(tid, [&](int i, int j, f4, int e) { xr[e] = fit_read<NN>(x, PX, i, j); });
   }
   for (int st = 0; st < steps.n; ++st) {
-    const float ca = (float)steps.c[st][0], cb = (float)steps.c[st][1] * (kScaleB / kScaleA),
-                cc = (float)steps.c[st][2] * (kScaleB / (kScaleA * kScaleA));
+    const float ca = steps.a[st], cu = steps.u[st], cb = steps.b[st], cc = steps.c[st];
     f4 ar[Gram::TI * Gram::TJ];
     {
       Gram p;
@@ -519,7 +528,7 @@ ns_fit_kernel(const T* g, int64_t stride, int64_t ld, int m, int n, bool tall, d
     Update p;
     p.place(tid);
     p.run(A, PA, x, PX, tid);
-    p.each(tid, [&](int i, int j, f4 r, int e) { xr[e] = (1.f / kScaleB) * r + ca * xr[e]; });
+    p.each(tid, [&](int i, int j, f4 r, int e) { xr[e] = cu * r + ca * xr[e]; });
     if (st + 1 < steps.n) {
       __syncthreads();
       p.each(tid, [&](int i, int j, f4, int e) { fit_write<NN>(x, PX, i, j, xr[e]); });
@@ -647,7 +656,7 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 mace_status launched() { return hipGetLastError() == hipSuccess ? MACE_OK : MACE_EHIP; }
 
 mace_status check(const mace_orthogonalise_desc* d) {
-  if (!d || d->batch < 0 || d->rows < 1 || d->cols < 1 || d->n_steps < 0 || d->n_steps > 64 || !(d->eps >= 0))
+  if (!d || d->batch < 0 || d->rows < 1 || d->cols < 1 || d->n_steps < 0 || d->n_steps > kMaxSteps || !(d->eps >= 0))
     return MACE_EINVAL;
   if (d->dtype < MACE_TYPE_FP32 || d->dtype > MACE_TYPE_FP16) return MACE_EINVAL;
   if (d->ld_g < d->cols || d->ld_out < d->cols || d->stride_g < 0 || d->stride_out < 0) return MACE_EINVAL;
@@ -659,18 +668,28 @@ mace_status check(const mace_orthogonalise_desc* d) {
 }
 
 // Over the singular values that can occur, s with l = s^2, for x <- P(l) x per step,
-// P = a + b l + c l^2: whether every step keeps its operands in range (mace.h), and
-// how far a perturbation of A's eigenvalues can grow over the steps.
+// P = a + b l + c l^2: whether every step keeps its operands in range (mace.h), the steps
+// on operands scaled to that range, and how far a rounding error of A, relative to A's
+// largest eigenvalue, can grow over the steps.
 struct StepRange {
   bool ok;
   double growth;
+  ScaledSteps scaled;
 };
+// the power of two, at most 2^60, that takes a value below 1 to 1/2 .. 1
+int raise_of(double v) {
+  int e;
+  std::frexp(v, &e);
+  return std::min(60, std::max(0, -e));
+}
 StepRange range_of(const double* k, int steps) {
   double r = 1.0;   // largest singular value so far
-  double growth = 1.0;
+  int up = 0;       // x is scaled by kScaleX 2^up
+  StepRange out{true, 1.0, {}};
+  out.scaled.n = steps;   // (steps after one that leaves zeros: zeros)
   for (int s = 0; s < steps; ++s, k += 3) {
     const double a = k[0], b = k[1], c = k[2];
-    if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return {false, 0.0};
+    if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return {};
     double top = 0.0, next = 0.0, p = 0.0, slope = 0.0;
     auto at = [&](double l) {   // l clamped to the range: a point outside gives its end
       l = std::min(std::max(l, 0.0), r * r);
@@ -694,11 +713,22 @@ StepRange range_of(const double* k, int steps) {
     } else if (b != 0.0) {
       at(-a / (3.0 * b));
     }
+    const double before = r;
     r = next * 1.001;   // (rounding)
-    if (!(top <= kMaxB) || !(r <= kMaxSigma)) return {false, 0.0};
-    growth = growth * p * slope + 1.0;   // d(l P^2) / dl = P (P + 2 l P'); each step adds a rounding of its own
+    if (!(top <= kMaxB) || !(r <= kMaxSigma)) return {};
+    if (r == 0.0) break;   // zeros from here on
+    // d(l P^2) / dl = P (P + 2 l P'); each step adds a rounding of its own
+    out.growth = out.growth * p * slope * (before / r) * (before / r) + 1.0;
+    // (the last step's result leaves at kScaleX, in FP32)
+    const int up_next = s + 1 < steps ? raise_of(r) : 0, up_b = top > 0.0 ? raise_of(top) : 0;
+    const double sa = std::ldexp(kScaleA, 2 * up), sb = std::ldexp(kScaleB, up_b);
+    out.scaled.a[s] = (float)std::ldexp(a, up_next - up);
+    out.scaled.u[s] = (float)std::ldexp(1.0 / sb, up_next - up);
+    out.scaled.b[s] = (float)(b * (sb / sa));
+    out.scaled.c[s] = (float)(c * (sb / sa) / sa);
+    up = up_next;
   }
-  return {true, growth};
+  return out;
 }
 
 struct NsPlan {
@@ -777,7 +807,7 @@ mace_status update(const PairMat& B, const PairMat& x, const PairMat& xo, int64_
 }
 
 template <class O, int MM, int NN>
-mace_status run_fit(const mace_orthogonalise_desc& d, const NsPlan& p, const NsSteps& steps, const O* g, O* out,
+mace_status run_fit(const mace_orthogonalise_desc& d, const NsPlan& p, const ScaledSteps& steps, const O* g, O* out,
                     hipStream_t s) {
   constexpr int bytes = 2 * 2 * (MM * NN + MM * MM);
   auto f = ns_fit_kernel<O, MM, NN>;
@@ -790,19 +820,19 @@ mace_status run_fit(const mace_orthogonalise_desc& d, const NsPlan& p, const NsS
 }
 
 template <class O>
-mace_status run(const mace_orthogonalise_desc& d, const NsPlan& p, const O* g, const double* coef, O* out, char* ws,
-                hipStream_t s) {
+mace_status run(const mace_orthogonalise_desc& d, const NsPlan& p, const ScaledSteps& scaled, const O* g,
+                const double* coef, O* out, char* ws, hipStream_t s) {
   double* part = reinterpret_cast<double*>(ws + p.part);
   mace_status st;
-  NsSteps steps{};
-  steps.n = d.n_steps;
-  for (int i = 0; i < 3 * d.n_steps; ++i) steps.c[i / 3][i % 3] = coef[i];
   if (p.fit && d.n_steps > 0) {
-    if (p.n <= 64) return run_fit<O, 64, 64>(d, p, steps, g, out, s);
-    if (p.m <= 64) return run_fit<O, 64, 128>(d, p, steps, g, out, s);
-    return run_fit<O, 128, 128>(d, p, steps, g, out, s);
+    if (p.n <= 64) return run_fit<O, 64, 64>(d, p, scaled, g, out, s);
+    if (p.m <= 64) return run_fit<O, 64, 128>(d, p, scaled, g, out, s);
+    return run_fit<O, 128, 128>(d, p, scaled, g, out, s);
   }
   if (p.gram) {
+    NsSteps steps{};
+    steps.n = d.n_steps;
+    for (int i = 0; i < 3 * d.n_steps; ++i) steps.c[i / 3][i % 3] = coef[i];
     auto go = [&](auto r_) -> mace_status {
       constexpr int R = decltype(r_)::value;
       if constexpr (R <= 32) if (p.parts == 1) {
@@ -839,13 +869,13 @@ mace_status run(const mace_orthogonalise_desc& d, const NsPlan& p, const O* g, c
       g, d.stride_g, d.ld_g, p.m, p.n, p.tall, part, p.parts, d.eps, x, A, B);
   if ((st = launched()) != MACE_OK) return st;
   for (int i = 0; i < d.n_steps; ++i) {
-    const float a = (float)coef[3 * i], b = (float)coef[3 * i + 1], c = (float)coef[3 * i + 2];
-    const float g1 = kScaleA / (kScaleX * kScaleX), pb = b * (kScaleB / kScaleA),
-                pc = c * (kScaleB / (kScaleA * kScaleA)), u = 1.f / kScaleB;
+    constexpr float g = kScaleA / (kScaleX * kScaleX);
     O* o = i == d.n_steps - 1 ? out : nullptr;
-    if ((st = symmetric<false>(x, A, d.batch, p.m, p.np, 0.f, g1, s)) != MACE_OK) return st;
-    if ((st = symmetric<true>(A, B, d.batch, p.m, p.m, pb, pc, s)) != MACE_OK) return st;
-    if ((st = update<O>(B, x, xo, d.batch, p.m, p.n, a, u, o, d.stride_out, d.ld_out, p.tall, s)) != MACE_OK) return st;
+    if ((st = symmetric<false>(x, A, d.batch, p.m, p.np, 0.f, g, s)) != MACE_OK) return st;
+    if ((st = symmetric<true>(A, B, d.batch, p.m, p.m, scaled.b[i], scaled.c[i], s)) != MACE_OK) return st;
+    if ((st = update<O>(B, x, xo, d.batch, p.m, p.n, scaled.a[i], scaled.u[i], o, d.stride_out, d.ld_out, p.tall, s)) !=
+        MACE_OK)
+      return st;
     std::swap(x, xo);
   }
   return MACE_OK;
@@ -874,7 +904,8 @@ extern "C" mace_status mace_orthogonalise(const mace_orthogonalise_desc* desc, c
   char* ws = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(workspace) + 255) & ~uintptr_t(255));
   const NsPlan p = plan(*desc, range.growth);
   hipStream_t s = (hipStream_t)stream;
-  if (desc->dtype == MACE_TYPE_FP32) return run<float>(*desc, p, (const float*)g, coefficients, (float*)out, ws, s);
-  if (desc->dtype == MACE_TYPE_BF16) return run<__bf16>(*desc, p, (const __bf16*)g, coefficients, (__bf16*)out, ws, s);
-  return run<_Float16>(*desc, p, (const _Float16*)g, coefficients, (_Float16*)out, ws, s);
+  if (desc->dtype == MACE_TYPE_FP32) return run<float>(*desc, p, range.scaled, (const float*)g, coefficients, (float*)out, ws, s);
+  if (desc->dtype == MACE_TYPE_BF16)
+    return run<__bf16>(*desc, p, range.scaled, (const __bf16*)g, coefficients, (__bf16*)out, ws, s);
+  return run<_Float16>(*desc, p, range.scaled, (const _Float16*)g, coefficients, (_Float16*)out, ws, s);
 }
