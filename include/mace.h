@@ -296,7 +296,9 @@ mace_status mace_graph_check(mace_graph* g, int32_t* device_flags, void* stream)
  * handle.  All matrices are row-major, as in the weight blob; `dtype` is the
  * type of every operand and result unless said otherwise, sums are FP32 and
  * each result is rounded once, to nearest even.  FP32 products are split-BF16
- * ones (as MACE_PRODUCTS_SPLIT_BF16, with the same range).  Leading dimensions
+ * ones (as MACE_PRODUCTS_SPLIT_BF16, with the same range: an infinite operand
+ * gives NaN), but a linear layer's y and dx of fewer than 96 blocks of 64 x 64
+ * come from FP32 matrix instructions, which keep infinities.  Leading dimensions
  * are in elements and at least the row length; any alignment of rows to an
  * element runs, 16-byte aligned rows of a multiple of 8 elements run fastest.
  * No entry point synchronises, allocates or records a memset: all can be
@@ -336,8 +338,10 @@ mace_status mace_linear_forward(const mace_linear_desc* desc, const void* x, con
                                 void* stream);
 
 /* Gradients of mace_linear_forward from dy (dev) [n_rows][n_out]:
- * dz = dy act'(z) (rounded to dtype where there is an activation: it is the
- * products' operand), dx = dz W_g^T, dweights_g = x_g^T dz_g, dbias_g = the
+ * dz = dy act'(z) (taken at the z that was saved, and rounded to dtype where
+ * there is an activation, as it is the products' operand: 2.4e-3 relative error
+ * of BF16 gradients where rounding them alone gives 1.7e-3, 3.0e-4 of FP16 ones
+ * where it gives 2.1e-4), dx = dz W_g^T, dweights_g = x_g^T dz_g, dbias_g = the
  * column sums of dz_g before that rounding; the residual's gradient is dy.
  * preact: the forward's z (MACE_ACT_NONE: not read, may be NULL).  dx (dev)
  * [n_rows][n_in], dweights (dev) [n_groups][n_in][n_out], dbias (dev)

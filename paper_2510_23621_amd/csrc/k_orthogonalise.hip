@@ -336,8 +336,8 @@ __global__ void __launch_bounds__(kThreads64<R>) ns_apply64_kernel(const T* g, i
 // [i][j]: rows by ds_read_b128, columns by ds_read_b64_tr_b16; the 16-byte chunks
 // of row i are XORed with its three low bits rotated, which keeps eight rows' chunks
 // (b128) and four rows' pairs of chunks (transposed) apart. One launch in place of 17:
-// 64 x 64 15 us, 128 x 128 53 us for one matrix or for thirty; a step of 128 x 128
-// takes 7.7 us, of which LDS is busy for 60%.
+// 64 x 64 15 us, 128 x 128 53 us for one matrix or for thirty: LDS is busy for 54 % of
+// that (half of it bank conflicts), the matrix pipes for 28 %.
 template <int LD>
 __device__ __forceinline__ int fit_chunk(int i, int j) {
   return i * LD + (((j >> 3) ^ (((i & 3) << 1) | ((i >> 2) & 1))) << 3);
@@ -775,8 +775,10 @@ constexpr int64_t kFillBlocks = 256;   // (one per CU)
 
 // Mid: 128 x 128, from one block per CU on. Half: the symmetric products' blocks, half
 // as wide, where Mid gives less than one per CU and Half that many: there are few of them,
-// one triangle's (two 1500 x 1500 BF16 552 us, with Small 611; four 1000 x 2000 564
-// against 619). With a Mid block per CU Half takes 10 % more, bound by LDS.
+// one triangle's (two 1500 x 1500 752 us, with Small 820; four 1000 x 2000 750 against 817;
+// but thirty 300 x 515, whose last tiles are mostly empty, 305 against 278). With a Mid
+// block per CU Half takes 9 to 13 % more, as it reads more LDS per product (two 2048 x 2048
+// 1440 us against 1315, one 2900 x 2905 2700 against 2400).
 using Mid = TileShape<128, 128, 2, 2, 32, 2, true>;
 using Half = TileShape<128, 64, 2, 2, 32, 2, true>;
 using Small = TileShape<64, 64, 2, 2, 32, 4, true>;

@@ -188,9 +188,9 @@ __device__ __forceinline__ int64_t item_row(int nv, int& vec) {
 }
 
 // rows[r] = x[slot_of_row[r] / k], zeros from the first dropped row on. In the rows'
-// order: they are written one after the other, and a token's k reads after the first
-// come from the caches (36,864 tokens to 8 experts, 1024 bfloat16 wide: 183 us; in the
-// tokens' order, read once and written k times, 199).
+// order: they are written one after the other, and a token is read k times, each time
+// past the L2s (36,864 tokens to 8 experts, 1024 bfloat16 wide: 183 us, 606 MB read and
+// as many written, 6.5 TB/s; in the tokens' order, read once and written k times, 199).
 template <class T, bool AL>
 __global__ void __launch_bounds__(256) route_gather_kernel(RouteArgs a, const int* __restrict__ slot_of_row,
                                                            const T* __restrict__ x, T* __restrict__ rows) {
@@ -212,7 +212,7 @@ __global__ void __launch_bounds__(256) route_gather_kernel(RouteArgs a, const in
 // out[t] = sum_s weight[t, s] rows[row_of_slot[t, s]] over the kept slots, in
 // the slots' order, in FP32, rounded once. Dropped slots' rows are not used,
 // whatever they hold. One thread per 16 bytes of a token. 36,864 x 8 rows of 1024
-// bfloat16: 160 us, 4.2 TB/s, bound by HBM.
+// bfloat16: 160 us, 4.2 TB/s where a large copy reaches 5.2; nearly all of it are reads.
 template <class T, bool AL, int U>
 __global__ void __launch_bounds__(256)
 route_combine_kernel(RouteArgs a, const T* __restrict__ rows, const float* __restrict__ weights, T* __restrict__ out) {
@@ -249,7 +249,8 @@ route_combine_kernel(RouteArgs a, const T* __restrict__ rows, const float* __res
 
 // drows[row] = weight dout[t] and dweights[t, s] = <rows[row], dout[t]>, zeros
 // for dropped slots. LG lanes (a power of two) per token, U slots at a time, dout read
-// once for U rows. 36,864 x 8 rows of 1024 bfloat16: 244 us, 5.3 TB/s, bound by HBM.
+// once for U rows. 36,864 x 8 rows of 1024 bfloat16: 244 us, 5.6 TB/s of memory
+// traffic (rows and dout read, gradients written): a large copy's rate.
 template <class T, bool AL, int U>
 __global__ void __launch_bounds__(256)
 route_combine_bwd_kernel(RouteArgs a, int lg, const T* __restrict__ dout, const T* __restrict__ rows,
