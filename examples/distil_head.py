@@ -4,8 +4,10 @@ The teacher is the library's own model on periodic water; the student sees
 radial sums over an atom's neighbours and runs on the dense operators: a
 trunk layer, a router that sends each atom to two of four experts, the experts'
 two layers as grouped linears, and a linear readout.  Every gradient is one of
-the library's backward calls (the router's softmax is differentiated here), and
-the weight matrices are updated with orthogonalised momenta.
+the library's backward calls, and the weight matrices are updated with
+orthogonalised momenta.  With `keep8` the experts' input and pre-activation wait
+for the backward as 8-bit rows; `serve` and `predict` run the trained student on
+8-bit weights.
 
     python examples/distil_head.py [steps]
 """
@@ -65,15 +67,16 @@ def init(n_in):
             "down.b": z(EXPERTS, WIDTH), "read.w": w(WIDTH, 1), "read.b": z(1)}
 
 
-def step(p, x, y):
+def step(p, x, y, keep8=False):
     """The loss and its gradients."""
     h, zh = L.linear(x, p["trunk.w"], p["trunk.b"], act="silu", save=True)
     logits = L.linear(h, p["router.w"])
-    top, expert = torch.topk(logits, TOP_K, dim=1)
-    weights = torch.softmax(top, 1)
-    plan = L.route(expert.int(), EXPERTS)
+    expert, weights = L.choose_experts(logits, TOP_K)
+    plan = L.route(expert, EXPERTS)
     rows = L.route_rows(h, plan)
     a, za = L.linear(rows, p["up.w"], p["up.b"], offsets=plan.offsets, act="silu", save=True)
+    if keep8:
+        rows, za = L.pack_rows(rows), L.pack_rows(za)
     b = L.linear(a, p["down.w"], p["down.b"], offsets=plan.offsets)
     mixed = L.combine_rows(b, plan, weights)
     mixed += h
@@ -83,23 +86,38 @@ def step(p, x, y):
     dmixed, g["read.w"], g["read.b"] = L.linear_backward(err * (2 / len(y)), mixed, p["read.w"])
     db, dweights = L.combine_rows_backward(dmixed, b, plan, weights)
     da, g["down.w"], g["down.b"] = L.linear_backward(db, a, p["down.w"], offsets=plan.offsets)
-    drows, g["up.w"], g["up.b"] = L.linear_backward(da, rows, p["up.w"], za, offsets=plan.offsets, act="silu")
-    dtop = weights * (dweights - (weights * dweights).sum(1, keepdim=True))
-    dlogits = torch.zeros_like(logits).scatter_(1, expert, dtop)
+    up_backward = L.linear_backward8 if keep8 else L.linear_backward
+    drows, g["up.w"], g["up.b"] = up_backward(da, rows, p["up.w"], za, offsets=plan.offsets, act="silu")
+    dlogits = L.choose_experts_backward(dweights, logits, expert)
     dh, g["router.w"], _ = L.linear_backward(dlogits, h, p["router.w"], bias=False)
     dh += L.route_rows_backward(drows, plan) + dmixed
     _, g["trunk.w"], g["trunk.b"] = L.linear_backward(dh, x, p["trunk.w"], zh, act="silu", need_dx=False)
     return (err * err).mean(), g
 
 
-def train(steps=200, rate=0.03, momentum=0.9, log=print):
+def serve(p):
+    """The parameters with the layers' weights in 8 bits (the router, which decides, and the readout as they are)."""
+    return {k: L.pack_weights(t) if k in ("trunk.w", "up.w", "down.w") else t for k, t in p.items()}
+
+
+def predict(s, x):
+    """Energies [atoms, 1] of the student that `serve` gives."""
+    h = L.linear8(x, s["trunk.w"], s["trunk.b"], act="silu")
+    expert, weights = L.choose_experts(L.linear(h, s["router.w"]), TOP_K)
+    plan = L.route(expert, EXPERTS)
+    a = L.linear8(L.route_rows(h, plan), s["up.w"], s["up.b"], offsets=plan.offsets, act="silu")
+    b = L.linear8(a, s["down.w"], s["down.b"], offsets=plan.offsets)
+    return L.linear(L.combine_rows(b, plan, weights) + h, s["read.w"], s["read.b"])
+
+
+def train(steps=200, rate=0.03, momentum=0.9, log=print, keep8=False):
     """First and last loss."""
     x, y = teacher_data()
     p = init(x.shape[1])
     v = {k: torch.zeros_like(t) for k, t in p.items()}
     losses = []
     for i in range(steps):
-        loss, g = step(p, x, y)
+        loss, g = step(p, x, y, keep8)
         decay = rate * (1 - i / steps)
         for k, t in p.items():
             v[k].mul_(momentum).add_(g[k])
@@ -111,6 +129,7 @@ def train(steps=200, rate=0.03, momentum=0.9, log=print):
         if i % 20 == 0 or i == steps - 1:
             losses.append(loss.item())
             log(f"step {i:4d}  loss {losses[-1]:.4f}  (variance of the energies 1)", flush=True)
+    log(f"served in 8 bits: loss {(predict(serve(p), x) - y).square().mean().item():.4f}", flush=True)
     return losses[0], losses[-1]
 
 

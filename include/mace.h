@@ -396,6 +396,117 @@ mace_status mace_route_combine_backward(const mace_route_desc* desc, const void*
                                         const float* weights, const int32_t* row_of_slot, const int32_t* offsets,
                                         void* drows, float* dweights, void* stream);
 
+/* Embedding: out_t = scale table[ids_t], rounded once; an id outside 0 ..
+ * n_rows - 1 (-1, say: padding) gives zeros.  table (dev) [n_rows][width], ids
+ * (dev) [n_ids], out (dev) [n_ids][width].  width <= 2^20, n_ids <= 2^30, n_rows
+ * <= 2^30, else MACE_EUNSUPPORTED; scale finite. */
+typedef struct mace_embed_desc {
+  int64_t n_ids, n_rows;
+  int32_t width, dtype;      /* mace_dtype of table, out and their gradients */
+  int64_t ld_table, ld_out;  /* of [n_rows][width] and [n_ids][width] tensors */
+  double scale;
+} mace_embed_desc;
+mace_status mace_embed_forward(const mace_embed_desc* desc, const void* table, const int32_t* ids, void* out,
+                               void* stream);
+/* Gradient of the table from dout (dev) [n_ids][width] (leading dimension
+ * ld_out): dtable (dev) [n_rows][width] (leading dimension ld_table), row v
+ * being scale times the FP32 sum of dout_t over the t with ids_t = v, in a
+ * fixed order; zeros for a row that does not occur.  Every row is written, the
+ * gaps between them are not.  workspace (dev) of at least
+ * mace_embed_backward_workspace_bytes (0 on invalid input). */
+size_t mace_embed_backward_workspace_bytes(const mace_embed_desc* desc);
+mace_status mace_embed_backward(const mace_embed_desc* desc, const void* dout, const int32_t* ids, void* dtable,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
+/* Choice of experts.  The scores of a token are s = softmax(logits) or
+ * 1 / (1 + exp(-logits)); a logit of -infinity or of its type's lowest value is
+ * masked: its expert has the score 0 and is never chosen, nor is one with a bias
+ * of -infinity.  Experts are compared by s + bias (without a bias by the logits
+ * themselves, which order them the same way).  With n_groups > 1 the experts
+ * are n_groups runs of n_experts / n_groups; a group counts for the sum of its
+ * two largest s + bias (one, if only one can be chosen), and the top_groups
+ * best take part.  Of their experts the top_k best are chosen, best first; equal
+ * ones go by the lower index, and values are compared as in FP64, so that the
+ * choice does not depend on roundings of the scores.  expert (dev)
+ * [n_tokens][top_k], -1 where fewer are left (mace_route_build drops such
+ * slots); weights (dev) [n_tokens][top_k] FP32: scale s_j, with `normalise`
+ * scale s_j / the sum of the chosen s, 0 where there is no expert.  A token with
+ * a NaN logit (softmax: or an infinite one; either: or a NaN in s + bias) has no
+ * order: it gets the experts 0 .. top_k - 1 and NaN weights.
+ * logits (dev) [n_tokens][n_experts] of dtype, bias (dev) [n_experts] FP32 or
+ * NULL.  n_experts <= 512, n_groups <= 64, top_k <= 64, n_tokens * top_k <= 2^30,
+ * else MACE_EUNSUPPORTED. */
+typedef enum { MACE_SCORES_SOFTMAX = 0, MACE_SCORES_SIGMOID = 1 } mace_scores;
+typedef struct mace_choose_desc {
+  int64_t n_tokens;
+  int32_t n_experts, top_k;
+  int32_t n_groups, top_groups; /* n_groups divides n_experts; top_k <= top_groups * n_experts / n_groups */
+  int32_t dtype;                /* mace_dtype of logits and their gradient */
+  int32_t scores;               /* mace_scores */
+  int32_t normalise;            /* 0 or 1 */
+  int64_t ld_logits;
+  double scale;                 /* finite */
+} mace_choose_desc;
+mace_status mace_choose_forward(const mace_choose_desc* desc, const void* logits, const float* bias, int32_t* expert,
+                                float* weights, void* stream);
+/* Gradient of the logits through the weights from dweights (dev)
+ * [n_tokens][top_k] FP32 and the experts that mace_choose_forward chose
+ * (entries outside 0 .. n_experts - 1 take no part; the choice itself and the
+ * bias have no gradient): dlogits (dev) [n_tokens][n_experts] of dtype, every
+ * element written, zeros for masked experts. */
+mace_status mace_choose_backward(const mace_choose_desc* desc, const float* dweights, const void* logits,
+                                 const int32_t* expert, void* dlogits, int64_t ld_dlogits, void* stream);
+
+/* Rows of 8-bit integers: x_ij stands as q_ij s_i with s_i = max_j |x_ij| / 127
+ * rounded to FP32 (at least 2^-126) and q_ij the integer nearest to x_ij / s_i
+ * (the exact quotient; halves to the even one), -127 .. 127.  A row with a
+ * non-finite element gets the scale NaN and zeros.  values (dev) int8
+ * [n_rows][ld_values]: 16-byte aligned, ld_values a multiple of 16 and at least
+ * n_cols, with zeros in the columns from n_cols to the next multiple of 16;
+ * scales (dev) FP32 [n_rows].
+ * mace_unpack_rows gives q s in FP32, rounded once to dtype.  n_rows <= 2^30,
+ * n_cols <= 131072 (so that sums of products fit 32 bits) and ld_values <= 2^20,
+ * else MACE_EUNSUPPORTED. */
+typedef struct mace_rows8_desc {
+  int64_t n_rows;
+  int32_t n_cols, dtype;    /* mace_dtype of x */
+  int64_t ld_x, ld_values;
+} mace_rows8_desc;
+mace_status mace_pack_rows(const mace_rows8_desc* desc, const void* x, void* values, float* scales, void* stream);
+mace_status mace_unpack_rows(const mace_rows8_desc* desc, const void* values, const float* scales, void* x,
+                             void* stream);
+/* The same for the output columns of weights (dev) [n_groups][n_in][n_out]
+ * contiguous: values (dev) int8 [n_groups][n_out][ld_values] and scales (dev)
+ * FP32 [n_groups][n_out], one scale for each group's column. */
+mace_status mace_pack_weights(int32_t n_groups, int32_t n_in, int32_t n_out, int32_t dtype, const void* weights,
+                              void* values, int64_t ld_values, float* scales, void* stream);
+
+/* mace_linear_forward on 8-bit rows and weights: y_i = act(sx_i sw_gn (sum_k
+ * qx_ik qw_gnk) + b_g) + r_i with exact 32-bit integer sums; desc->dtype is the type
+ * of bias, residual and y, desc->n_in <= 131072.  x8 (dev) with leading dimension
+ * desc->ld_x and x_scales as mace_pack_rows gives them, w8 with leading
+ * dimension ld_w and w_scales as mace_pack_weights does.  Alternatively x_scales
+ * is NULL and x8 (dev) [n_rows][n_in] of dtype, rounded to 8-bit rows on the way
+ * in workspace (dev), of at least mace_linear8_workspace_bytes (0 on invalid
+ * input; not used with x_scales). */
+size_t mace_linear8_workspace_bytes(const mace_linear_desc* desc);
+mace_status mace_linear8_forward(const mace_linear_desc* desc, const void* x8, const float* x_scales, const void* w8,
+                                 int64_t ld_w, const float* w_scales, const void* bias, const void* residual,
+                                 const int32_t* group_offsets, void* y, void* workspace, size_t workspace_bytes,
+                                 void* stream);
+
+/* mace_linear_backward from an input and a pre-activation kept as 8-bit rows
+ * between the passes (mace_pack_rows of x and of z; desc->ld_x and
+ * desc->ld_preact are their leading dimensions, multiples of 16): the gradients
+ * at x = q s rounded to dtype, as it is the products' operand, and at z = q s.
+ * Weights, dy and the gradients are of dtype as there; z8 and z_scales are not
+ * read and may be NULL without an activation, x8 and x_scales without dweights. */
+size_t mace_linear_backward8_workspace_bytes(const mace_linear_desc* desc, int32_t want_bias, int32_t want_weights);
+mace_status mace_linear_backward8(const mace_linear_desc* desc, const void* dy, int64_t ld_dy, const void* x8,
+                                  const float* x_scales, const void* weights, const void* z8, const float* z_scales,
+                                  const int32_t* group_offsets, void* dx, int64_t ld_dx, void* dweights, void* dbias,
+                                  void* workspace, size_t workspace_bytes, void* stream);
+
 /* Newton-Schulz orthogonalisation of a batch of matrices (gradients or their
  * momenta, before an optimiser applies them): x = g / (|g|_F + eps), then per
  * step (a, b, c) of coefficients x <- a x + (b A + c A A) x with A = x x^T;

@@ -34,6 +34,8 @@ MACE_TYPE_FP16 = 2
 MACE_ACT_NONE = 0
 MACE_ACT_SILU = 1
 MACE_ACT_GELU = 2
+MACE_SCORES_SOFTMAX = 0
+MACE_SCORES_SIGMOID = 1
 MACE_NEIGHBOR_SCRATCH_BYTES = 80 << 20
 MAX_LAYERS = 8   # MACE_MAX_LAYERS
 STATUS = {0: "MACE_OK", -1: "MACE_EINVAL", -2: "MACE_ERANGE", -3: "MACE_ENOSPACE", -4: "MACE_EHIP",
@@ -48,7 +50,10 @@ EXPORTED = ["mace_weight_layout", "mace_workspace_bytes", "mace_neighbor_list", 
             "mace_debug_fused_linears", "mace_linear_forward", "mace_linear_backward",
             "mace_linear_backward_workspace_bytes", "mace_route_workspace_bytes", "mace_route_build",
             "mace_route_gather", "mace_route_combine", "mace_route_combine_backward",
-            "mace_orthogonalise_workspace_bytes", "mace_orthogonalise"]
+            "mace_orthogonalise_workspace_bytes", "mace_orthogonalise", "mace_embed_forward",
+            "mace_embed_backward_workspace_bytes", "mace_embed_backward", "mace_choose_forward", "mace_choose_backward",
+            "mace_pack_rows", "mace_unpack_rows", "mace_pack_weights", "mace_linear8_workspace_bytes",
+            "mace_linear8_forward", "mace_linear_backward8_workspace_bytes", "mace_linear_backward8"]
 
 
 class MaceError(RuntimeError):
@@ -83,6 +88,24 @@ class mace_orthogonalise_desc(ctypes.Structure):
                 ("dtype", ctypes.c_int32), ("n_steps", ctypes.c_int32), ("ld_g", ctypes.c_int64),
                 ("stride_g", ctypes.c_int64), ("ld_out", ctypes.c_int64), ("stride_out", ctypes.c_int64),
                 ("eps", ctypes.c_double)]
+
+
+class mace_embed_desc(ctypes.Structure):
+    _fields_ = [("n_ids", ctypes.c_int64), ("n_rows", ctypes.c_int64), ("width", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("ld_table", ctypes.c_int64), ("ld_out", ctypes.c_int64),
+                ("scale", ctypes.c_double)]
+
+
+class mace_choose_desc(ctypes.Structure):
+    _fields_ = [("n_tokens", ctypes.c_int64), ("n_experts", ctypes.c_int32), ("top_k", ctypes.c_int32),
+                ("n_groups", ctypes.c_int32), ("top_groups", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("scores", ctypes.c_int32), ("normalise", ctypes.c_int32), ("ld_logits", ctypes.c_int64),
+                ("scale", ctypes.c_double)]
+
+
+class mace_rows8_desc(ctypes.Structure):
+    _fields_ = [("n_rows", ctypes.c_int64), ("n_cols", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("ld_x", ctypes.c_int64), ("ld_values", ctypes.c_int64)]
 
 
 def make_desc(n_species, K, hidden_lmax, r_cut, c_norm, n_layers=2, sh_lmax=3, correlation=3, n_bessel=8,
@@ -156,6 +179,23 @@ def lib() -> ctypes.CDLL:
         L.mace_orthogonalise_workspace_bytes.argtypes = [op]
         L.mace_orthogonalise_workspace_bytes.restype = Z
         L.mace_orthogonalise.argtypes = [op, P, P, P, P, Z, P]
+        ep, cp = ctypes.POINTER(mace_embed_desc), ctypes.POINTER(mace_choose_desc)
+        qp = ctypes.POINTER(mace_rows8_desc)
+        L.mace_embed_forward.argtypes = [ep, P, P, P, P]
+        L.mace_embed_backward_workspace_bytes.argtypes = [ep]
+        L.mace_embed_backward_workspace_bytes.restype = Z
+        L.mace_embed_backward.argtypes = [ep, P, P, P, P, Z, P]
+        L.mace_choose_forward.argtypes = [cp, P, P, P, P, P]
+        L.mace_choose_backward.argtypes = [cp, P, P, P, P, I64, P]
+        L.mace_pack_rows.argtypes = [qp, P, P, P, P]
+        L.mace_unpack_rows.argtypes = [qp, P, P, P, P]
+        L.mace_pack_weights.argtypes = [I32, I32, I32, I32, P, P, I64, P, P]
+        L.mace_linear8_workspace_bytes.argtypes = [lp]
+        L.mace_linear8_workspace_bytes.restype = Z
+        L.mace_linear8_forward.argtypes = [lp, P, P, P, I64, P, P, P, P, P, P, Z, P]
+        L.mace_linear_backward8_workspace_bytes.argtypes = [lp, I32, I32]
+        L.mace_linear_backward8_workspace_bytes.restype = Z
+        L.mace_linear_backward8.argtypes = [lp, P, I64, P, P, P, P, P, P, P, I64, P, P, P, Z, P]
         for name in EXPORTED:
             f = getattr(L, name)
             if f.restype is ctypes.c_int:
@@ -490,3 +530,62 @@ def kernel_ids() -> dict:
             return out
         out[name] = k
         k += 1
+
+
+def mace_embed_forward(desc: mace_embed_desc, table, ids, out, stream=None):
+    _check(lib().mace_embed_forward(desc, _ptr(table), _ptr(ids), _ptr(out), _stream(stream)), "mace_embed_forward")
+
+
+def mace_embed_backward_workspace_bytes(desc: mace_embed_desc) -> int:
+    return lib().mace_embed_backward_workspace_bytes(desc)
+
+
+def mace_embed_backward(desc: mace_embed_desc, dout, ids, dtable, workspace, workspace_bytes, stream=None):
+    _check(lib().mace_embed_backward(desc, _ptr(dout), _ptr(ids), _ptr(dtable), _ptr(workspace), workspace_bytes,
+                                     _stream(stream)), "mace_embed_backward")
+
+
+def mace_choose_forward(desc: mace_choose_desc, logits, bias, expert, weights, stream=None):
+    _check(lib().mace_choose_forward(desc, _ptr(logits), _ptr(bias), _ptr(expert), _ptr(weights), _stream(stream)),
+           "mace_choose_forward")
+
+
+def mace_choose_backward(desc: mace_choose_desc, dweights, logits, expert, dlogits, ld_dlogits, stream=None):
+    _check(lib().mace_choose_backward(desc, _ptr(dweights), _ptr(logits), _ptr(expert), _ptr(dlogits), ld_dlogits,
+                                      _stream(stream)), "mace_choose_backward")
+
+
+def mace_pack_rows(desc: mace_rows8_desc, x, values, scales, stream=None):
+    _check(lib().mace_pack_rows(desc, _ptr(x), _ptr(values), _ptr(scales), _stream(stream)), "mace_pack_rows")
+
+
+def mace_unpack_rows(desc: mace_rows8_desc, values, scales, x, stream=None):
+    _check(lib().mace_unpack_rows(desc, _ptr(values), _ptr(scales), _ptr(x), _stream(stream)), "mace_unpack_rows")
+
+
+def mace_pack_weights(n_groups, n_in, n_out, dtype, weights, values, ld_values, scales, stream=None):
+    _check(lib().mace_pack_weights(n_groups, n_in, n_out, dtype, _ptr(weights), _ptr(values), ld_values, _ptr(scales),
+                                   _stream(stream)), "mace_pack_weights")
+
+
+def mace_linear8_workspace_bytes(desc: mace_linear_desc) -> int:
+    return lib().mace_linear8_workspace_bytes(desc)
+
+
+def mace_linear8_forward(desc: mace_linear_desc, x8, x_scales, w8, ld_w, w_scales, bias, residual, group_offsets, y,
+                         workspace, workspace_bytes, stream=None):
+    _check(lib().mace_linear8_forward(desc, _ptr(x8), _ptr(x_scales), _ptr(w8), ld_w, _ptr(w_scales), _ptr(bias),
+                                      _ptr(residual), _ptr(group_offsets), _ptr(y), _ptr(workspace), workspace_bytes,
+                                      _stream(stream)), "mace_linear8_forward")
+
+
+def mace_linear_backward8_workspace_bytes(desc: mace_linear_desc, want_bias: bool, want_weights: bool) -> int:
+    return lib().mace_linear_backward8_workspace_bytes(desc, want_bias, want_weights)
+
+
+def mace_linear_backward8(desc: mace_linear_desc, dy, ld_dy, x8, x_scales, weights, z8, z_scales, group_offsets, dx,
+                          ld_dx, dweights, dbias, workspace, workspace_bytes, stream=None):
+    _check(lib().mace_linear_backward8(desc, _ptr(dy), ld_dy, _ptr(x8), _ptr(x_scales), _ptr(weights), _ptr(z8),
+                                       _ptr(z_scales), _ptr(group_offsets), _ptr(dx), ld_dx, _ptr(dweights),
+                                       _ptr(dbias), _ptr(workspace), workspace_bytes, _stream(stream)),
+           "mace_linear_backward8")

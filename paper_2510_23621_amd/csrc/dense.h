@@ -20,6 +20,11 @@ typedef short s4 __attribute__((ext_vector_type(4)));
 // significand bits, for operands whose range is known.
 struct HalfPair {};
 
+// Two 8-bit integers, consecutive in k: products of integers go through the tiles as 16-bit
+// units of K / 2, a fragment of 8 units being 16 integers.
+struct IntPair { unsigned short pair; };
+typedef int i4 __attribute__((ext_vector_type(4)));
+
 // Planes an operand is carried as: FP32 as three bfloat16 (x0 + x1 + x2 = x
 // exactly, the six partial products down to 2^-18 relative kept, so products
 // are as accurate as FP32's), 16-bit types as themselves, pairs as two (three
@@ -30,7 +35,10 @@ template <> struct Planes<HalfPair> { static constexpr int n = 2; };
 
 template <class T>
 __device__ __forceinline__ f4 mfma32(us8 a, us8 b, f4 c) {
-  if constexpr (sizeof(T) == 4 || __is_same(T, __bf16))
+  if constexpr (__is_same(T, IntPair))   // (32-bit integer sums in the accumulator's registers)
+    return __builtin_bit_cast(f4, __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i4, a), __builtin_bit_cast(i4, b),
+                                                                        __builtin_bit_cast(i4, c), 0, 0, 0));
+  else if constexpr (sizeof(T) == 4 || __is_same(T, __bf16))
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), c, 0, 0, 0);
   else
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
@@ -230,7 +238,7 @@ struct TileSource {
         const int n = k_left - k_of(u, tid);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          if ((KC ? i : 0) >= n) v[D][u].set(i, (T)0.f);
+          if ((KC ? i : 0) >= n) v[D][u].set(i, T{});
       }
     }
 #pragma unroll

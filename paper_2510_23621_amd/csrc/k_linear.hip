@@ -1,61 +1,15 @@
 // Grouped dense layer y = act(x W_g + b_g) + r and its backward pass:
-// mace_linear_forward, mace_linear_backward.
+// mace_linear_forward, mace_linear_backward, mace_linear_backward8.
 #include <algorithm>
 #include <cmath>
 
-#include "../../include/mace.h"
-#include "dense.h"
+#include "linear.h"
+#include "rows8.h"
 
 namespace mace {
 namespace {
 
-// ------------------------------------------------------------------ activations
-// Normal distribution: Phi(z), and exp(-z^2 / 2). erfc(x) = t q(t) exp(-x^2), t =
-// 1 / (1 + 0.36 x), with q a degree-9 polynomial fitted to a relative error of
-// 1.6e-7 (evaluated in FP32) over x >= 0: no cancellation in either tail.
-__device__ __forceinline__ float normal_cdf(float z, float& e) {
-  const float x = fminf(fabsf(z), 30.f);
-  const float t = recip_ge1(__builtin_fmaf(x, 0.36f * 0.70710678118654752f, 1.f));
-  e = exp_neg(0.5f * x * x);
-  constexpr float q[10] = {0.20310825109481812f, 0.20310771465301514f, 0.1899440586566925f,  0.16391651332378387f,
-                           0.12292544543743134f, 0.10651545226573944f, -0.02863478660583496f, 0.14342354238033295f,
-                           -0.14196832478046417f, 0.03766215592622757f};
-  float p = q[9];
-#pragma unroll
-  for (int i = 8; i >= 0; --i) p = __builtin_fmaf(p, t, q[i]);
-  const float h = 0.5f * t * p * e;   // Phi(-|z|)
-  return z > 0.f ? 1.f - h : h;
-}
-template <int ACT>
-__device__ __forceinline__ float activate(float z) {
-  // z / (1 + exp(-z)). exp_neg takes -88 at the least, and infinity not at all: above 88
-  // the quotient is z, below -88 (where it is under 2^-120) z 0, NaN at -infinity as GELU
-  if constexpr (ACT == MACE_ACT_SILU) return z * (z < -88.f ? 0.f : recip_ge1(1.f + exp_neg(fminf(z, 88.f))));
-  if constexpr (ACT == MACE_ACT_GELU) {
-    float e;
-    return z * normal_cdf(z, e);
-  }
-  return z;
-}
-// act'(z); beyond |z| = 88 the slopes are 0 and 1 to FP32, and z (1 - s) would
-// be inf 0 at an infinite z
-__device__ __forceinline__ float activation_slope(float z, int act) {
-  z = z > 88.f ? 88.f : (z < -88.f ? -88.f : z);   // (keeps NaN)
-  if (act == MACE_ACT_SILU) return silu_grad(z);
-  float e;
-  const float c = normal_cdf(z, e);
-  return __builtin_fmaf(0.39894228040143268f * z, e, c);
-}
-
 // ------------------------------------------------------------------ arguments
-template <class T>
-struct LinearArgs {
-  const T *x, *w, *bias, *residual;
-  T *y, *z;
-  const int* offsets;
-  int64_t n, ldx, ldy, ldr, ldz;
-  int n_in, n_out, groups, act;
-};
 template <class T>
 struct RowGradArgs {
   const T *dz, *w;
@@ -183,12 +137,6 @@ __device__ __forceinline__ void thin_product(const Operand<float>& ro, const Ope
   }
 }
 
-// rows behind the last group: zeros
-template <class T>
-__device__ __forceinline__ void zero_rows(T* y, int64_t ld, int rows, int cols, int tid, int nt) {
-  for (int i = tid; i < rows * cols; i += nt) y[(int64_t)(i / cols) * ld + i % cols] = (T)0.f;
-}
-
 // y = act(x W_g + b_g) + r: a tile of one group's rows per block, the epilogue on the
 // sums in registers, so that z and y go out and r comes in once. 36864 x 2048 x 2048
 // bfloat16 in eight groups, with z and r: 411 us; the products alone would take 300 at
@@ -216,49 +164,7 @@ __global__ void __launch_bounds__(S::NT) linear_fwd_kernel(LinearArgs<T> a) {
   product<T, S, true, false, AL>({x, a.ldx, run.rows, 0, a.x + (a.n - 1) * a.ldx + a.n_in},
                                  {w, a.n_out, a.n_out - c0, 0, a.w + (int64_t)a.groups * a.n_in * a.n_out}, a.n_in, lds,
                                  tid, acc);
-  // epilogue: a tile row's residual is requested before the row above is stored
-  constexpr int W = lane_width<T>, NV = lane_vectors<S::TN, W>;
-  using V = typename Floats<W>::type;
-  const int l = tid & 63, wv = tid >> 6;
-  const int m0 = (wv / S::WN) * (S::BM / S::WM) + (l & 15), n0 = (wv % S::WN) * (S::BN / S::WN);
-  const T* bias = a.bias ? a.bias + (int64_t)run.group * a.n_out + c0 : nullptr;
-  const T* res = a.residual ? a.residual + run.row0 * a.ldr + c0 : nullptr;
-  auto finish = [&](auto act) {
-    V bj[NV], rj[2][NV];
-    auto column = [&](int j) { return n0 + lane_column<W>(j, l); };
-    auto count = [&](int j) { return AL ? W : min(W, cols - column(j)); };
-    auto load_residual = [&](int i) {
-#pragma unroll
-      for (int j = 0; j < NV; ++j)
-        if (m0 + 16 * i < run.rows && column(j) < cols)
-          rj[i & 1][j] = read_n<W>(res + (int64_t)(m0 + 16 * i) * a.ldr + column(j), count(j), AL);
-    };
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      bj[j] = V{};
-      if (bias && column(j) < cols) bj[j] = read_n<W>(bias + column(j), count(j), AL);
-    }
-    if (res) load_residual(0);
-#pragma unroll
-    for (int i = 0; i < S::TM; ++i) {
-      const int64_t m = m0 + 16 * i;
-      if (res && i + 1 < S::TM) load_residual(i + 1);
-#pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        V v = lane_values<W>(acc, j, i) + bj[j];
-        const int n = column(j);
-        if (m >= run.rows || n >= cols) continue;
-        if (z) store_n(z + m * a.ldz + n, v, count(j), AL);
-#pragma unroll
-        for (int q = 0; q < W; ++q) v[q] = activate<decltype(act)::value>(v[q]);
-        if (res) v += rj[i & 1][j];
-        store_n(y + m * a.ldy + n, v, count(j), AL);
-      }
-    }
-  };
-  if (a.act == MACE_ACT_SILU) finish(Int<MACE_ACT_SILU>{});
-  else if (a.act == MACE_ACT_GELU) finish(Int<MACE_ACT_GELU>{});
-  else finish(Int<MACE_ACT_NONE>{});
+  linear_epilogue<T, AL, S>(a, run, c0, cols, y, z, tid, [&](int j, int i) { return lane_values<lane_width<T>>(acc, j, i); });
 }
 
 template <bool AL, class S>
@@ -594,15 +500,35 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const float* __restric
   store_n(out + i, s, k, out_vec);
 }
 
+// eight z of a row
+template <class Z, bool AL>
+struct SlopeValues {
+  Vec8<Z> v;
+  __device__ __forceinline__ void load(const Z* p, const Z* end, const float*, int64_t) { v = load8_to<Z, AL>(p, end); }
+  __device__ __forceinline__ float get(int i) const { return v.get(i); }
+};
+template <bool AL>
+struct SlopeValues<int8_t, AL> {   // (8-bit rows are padded to whole vectors)
+  uint2 q;
+  float s;
+  __device__ __forceinline__ void load(const int8_t* p, const int8_t*, const float* zs, int64_t row) {
+    q = *reinterpret_cast<const uint2*>(p);
+    s = zs[row];
+  }
+  __device__ __forceinline__ float get(int i) const { return s * (float)(int8_t)((i < 4 ? q.x : q.y) >> 8 * (i & 3)); }
+};
+
 // dz = dy act'(z) over a run of rows (where there is an activation), and the
 // run's column sums. A block takes 8 CX columns; its kSlopeThreads / CX row lanes
 // each sum their rows, then are added in order. One pass over dy and z (36864 x 2048
 // bfloat16: 101 to 115 us from card to card, 4.5 to 3.9 TB/s); both products read the rounded dz, so that the
 // activation is not evaluated again for every tile of columns.
+// Z: T, or int8_t with a scale for each row (z stands as q s, in FP32).
 constexpr int kSlopeThreads = 1024;
-template <class T, bool AL>
+template <class T, bool AL, class Z>
 __global__ void __launch_bounds__(kSlopeThreads)
-linear_slope_kernel(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ z, int64_t ldz, T* __restrict__ dz,
+linear_slope_kernel(const T* __restrict__ dy, int64_t lddy, const Z* __restrict__ z, int64_t ldz,
+                    const float* __restrict__ zs, T* __restrict__ dz,
                     int64_t lddz, float* __restrict__ sums, const int* __restrict__ offsets, int groups, int64_t n,
                     int n_out, int act, int run_rows, int cx) {
   __shared__ float red[kSlopeThreads * 8];
@@ -612,16 +538,17 @@ linear_slope_kernel(const T* __restrict__ dy, int64_t lddy, const T* __restrict_
   const int col = 8 * (blockIdx.y * cx + c), k = n_out - col;
   float s[8] = {};
   const T* dy_end = dy + (n - 1) * lddy + n_out;
-  const T* z_end = z ? z + (n - 1) * ldz + n_out : nullptr;
+  const Z* z_end = z ? z + (n - 1) * ldz + n_out : nullptr;
   constexpr int U = 2;   // rows in flight
   if (k > 0)
     for (int r0 = ry; r0 < run.rows; r0 += U * R) {
-      Vec8<T> g[U], v[U];
+      Vec8<T> g[U];
+      SlopeValues<Z, AL> v[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int64_t row = run.row0 + min(r0 + u * R, run.rows - 1);
         g[u] = load8_to<T, AL>(dy + row * lddy + col, dy_end);
-        if (dz) v[u] = load8_to<T, AL>(z + row * ldz + col, z_end);
+        if (dz) v[u].load(z + row * ldz + col, z_end, zs, row);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -655,7 +582,6 @@ linear_slope_kernel(const T* __restrict__ dy, int64_t lddy, const T* __restrict_
 // ------------------------------------------------------------------ host
 constexpr int kMaxLinearGroups = 1024;
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 bool near(int64_t ld) { return ld <= 1 << 20; }   // a tile's rows lie within 32-bit byte offsets
 size_t size_of(int dtype) { return dtype == MACE_TYPE_FP32 ? 4 : 2; }
@@ -785,8 +711,6 @@ BackwardPlan plan_backward(const mace_linear_desc& d, bool bias, bool weights) {
   return p;
 }
 
-mace_status launched() { return hipGetLastError() == hipSuccess ? MACE_OK : MACE_EHIP; }
-
 template <class T>
 mace_status forward(const mace_linear_desc& d, const void* x, const void* w, const void* bias, const void* residual,
                     const int* offsets, void* y, void* z, hipStream_t s) {
@@ -826,9 +750,9 @@ mace_status forward(const mace_linear_desc& d, const void* x, const void* w, con
   return al ? go(Int<1>{}) : go(Int<0>{});
 }
 
-template <class T>
+template <class T, class Z = T>
 mace_status backward(const mace_linear_desc& d, const void* dy, int64_t lddy, const void* x, const void* w, const void* z,
-                     const int* offsets, void* dx, int64_t lddx, void* dw, void* db, char* ws, hipStream_t s) {
+                     const float* zs, const int* offsets, void* dx, int64_t lddx, void* dw, void* db, char* ws, hipStream_t s) {
   const BackwardPlan p = plan_backward(d, db != nullptr, dw != nullptr);
   const T* dz = (const T*)dy;
   int64_t lddz = lddy;
@@ -842,15 +766,15 @@ mace_status backward(const mace_linear_desc& d, const void* dy, int64_t lddy, co
     const int vecs = (d.n_out + 7) / 8;
     int cx = 1;
     while (cx < 64 && cx < vecs) cx *= 2;
-    const bool al = aligned16(dy) && aligned16(z) && ((d.n_out | lddy | d.ld_preact) & 7) == 0;
+    const bool al = aligned16(dy) && (__is_same(Z, int8_t) || aligned16(z)) && ((d.n_out | lddy | d.ld_preact) & 7) == 0;
     const dim3 grid((unsigned)slope_runs(d), (unsigned)ceil_div(vecs, cx));
     T* out = d.act != MACE_ACT_NONE ? const_cast<T*>(dz) : nullptr;
     auto go = [&](auto f) {
-      f<<<grid, kSlopeThreads, 0, s>>>((const T*)dy, lddy, (const T*)z, d.ld_preact, out, lddz, db ? sums : nullptr, offsets,
+      f<<<grid, kSlopeThreads, 0, s>>>((const T*)dy, lddy, (const Z*)z, d.ld_preact, zs, out, lddz, db ? sums : nullptr, offsets,
                              d.n_groups, d.n_rows, d.n_out, d.act, slope_run(d.n_rows), cx);
     };
-    if (al) go(linear_slope_kernel<T, true>);
-    else go(linear_slope_kernel<T, false>);
+    if (al) go(linear_slope_kernel<T, true, Z>);
+    else go(linear_slope_kernel<T, false, Z>);
     if ((st = launched()) != MACE_OK) return st;
   }
   const bool al = aligned16(dz) && aligned16(w) && aligned16(dx) && aligned16(x) && aligned16(dw) && near(lddz) &&
@@ -954,8 +878,62 @@ extern "C" mace_status mace_linear_backward(const mace_linear_desc* desc, const 
   char* ws = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(workspace) + 255) & ~uintptr_t(255));
   hipStream_t s = (hipStream_t)stream;
   if (d.dtype == MACE_TYPE_FP32)
-    return backward<float>(d, dy, ld_dy, x, weights, preact, group_offsets, dx, ld_dx, dweights, dbias, ws, s);
+    return backward<float>(d, dy, ld_dy, x, weights, preact, nullptr, group_offsets, dx, ld_dx, dweights, dbias, ws, s);
   if (d.dtype == MACE_TYPE_BF16)
-    return backward<__bf16>(d, dy, ld_dy, x, weights, preact, group_offsets, dx, ld_dx, dweights, dbias, ws, s);
-  return backward<_Float16>(d, dy, ld_dy, x, weights, preact, group_offsets, dx, ld_dx, dweights, dbias, ws, s);
+    return backward<__bf16>(d, dy, ld_dy, x, weights, preact, nullptr, group_offsets, dx, ld_dx, dweights, dbias, ws, s);
+  return backward<_Float16>(d, dy, ld_dy, x, weights, preact, nullptr, group_offsets, dx, ld_dx, dweights, dbias, ws, s);
+}
+
+// The input's 8-bit rows are written out in dtype first, as the products' operand
+namespace {
+int64_t ld_input8(const mace_linear_desc& d) { return (d.n_in + 7) / 8 * 8; }
+size_t input8_bytes(const mace_linear_desc& d, bool weights) {
+  return weights ? round256(size_t(d.n_rows) * ld_input8(d) * size_of(d.dtype)) : 0;
+}
+mace_status check8(const mace_linear_desc* d) {
+  const mace_status st = check(d);
+  if (st != MACE_OK) return st;
+  if (d->ld_x % 16 || (d->act != MACE_ACT_NONE && d->ld_preact % 16)) return MACE_EINVAL;
+  const bool wide = d->act != MACE_ACT_NONE && (d->n_out > kMaxColumns8 || d->ld_preact > kMaxPitch8);
+  return wide || d->n_in > kMaxColumns8 || d->ld_x > kMaxPitch8 ? MACE_EUNSUPPORTED : MACE_OK;
+}
+}  // namespace
+
+extern "C" size_t mace_linear_backward8_workspace_bytes(const mace_linear_desc* desc, int32_t want_bias, int32_t want_weights) {
+  if (check8(desc) != MACE_OK) return 0;
+  return input8_bytes(*desc, want_weights != 0) + plan_backward(*desc, want_bias != 0, want_weights != 0).total + 256;
+}
+
+extern "C" mace_status mace_linear_backward8(const mace_linear_desc* desc, const void* dy, int64_t ld_dy, const void* x8,
+                                             const float* x_scales, const void* weights, const void* z8,
+                                             const float* z_scales, const int32_t* group_offsets, void* dx, int64_t ld_dx,
+                                             void* dweights, void* dbias, void* workspace, size_t workspace_bytes,
+                                             void* stream) {
+  mace_status st = check8(desc);
+  if (st != MACE_OK) return st;
+  mace_linear_desc d = *desc;
+  if (!weights || (d.n_groups > 1 && !group_offsets) || ld_dy < d.n_out || (dx && ld_dx < d.n_in)) return MACE_EINVAL;
+  if (d.n_rows > 0) {
+    if (!dy || (dweights && (!x8 || !x_scales || !aligned16(x8)))) return MACE_EINVAL;
+    if (d.act != MACE_ACT_NONE && (!z8 || !z_scales || !aligned16(z8))) return MACE_EINVAL;
+  }
+  const size_t need = mace_linear_backward8_workspace_bytes(desc, dbias != nullptr, dweights != nullptr);
+  if (need > 256 && !workspace) return MACE_EINVAL;
+  if (need > 256 && workspace_bytes < need) return MACE_ENOSPACE;
+  char* ws = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(workspace) + 255) & ~uintptr_t(255));
+  hipStream_t s = (hipStream_t)stream;
+  const void* x = nullptr;
+  if (dweights && d.n_rows > 0) {
+    const mace_rows8_desc r{d.n_rows, d.n_in, d.dtype, ld_input8(d), d.ld_x};
+    if ((st = mace_unpack_rows(&r, x8, x_scales, ws, stream)) != MACE_OK) return st;
+    x = ws;
+  }
+  ws += input8_bytes(d, dweights != nullptr);
+  d.ld_x = ld_input8(d);
+  return by_type(d.dtype, [&](auto zero) {
+    using T = decltype(zero);
+    if (d.act != MACE_ACT_NONE)
+      return backward<T, int8_t>(d, dy, ld_dy, x, weights, z8, z_scales, group_offsets, dx, ld_dx, dweights, dbias, ws, s);
+    return backward<T>(d, dy, ld_dy, x, weights, nullptr, nullptr, group_offsets, dx, ld_dx, dweights, dbias, ws, s);
+  });
 }

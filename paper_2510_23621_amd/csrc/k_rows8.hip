@@ -1,0 +1,192 @@
+// Rows and weights as 8-bit integers with scales: mace_pack_rows, mace_unpack_rows,
+// mace_pack_weights.
+#include <algorithm>
+
+#include "rows8.h"
+
+namespace mace {
+namespace {
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+struct Rows8Args {
+  int64_t n, ld_x, ld_values;
+  int cols, chunks;   // chunks: of 16 columns, the zeros behind the last column among them
+  int lg;             // lanes per row
+};
+
+// NaN wins, whatever the order
+__device__ __forceinline__ float larger(float a, float b) { return a > b || a != a ? a : b; }
+
+// lg lanes (a power of two up to a block) a row: its largest magnitude, then its integers, 16 a lane.
+template <class T, bool AL>
+__global__ void __launch_bounds__(256) pack_rows_kernel(Rows8Args a, const T* __restrict__ x, int8_t* __restrict__ values,
+                                                        float* __restrict__ scales) {
+  __shared__ float red[4];
+  const int tid = threadIdx.x, lane = tid & (a.lg - 1);
+  const int64_t row = ((int64_t)block_id() * 256 + tid) / a.lg;
+  const bool on = row < a.n;
+  const T* p = x + (on ? row : 0) * a.ld_x;
+  auto load = [&](int c) {   // columns 16 c .. 16 c + 15, zeros past the last
+    Vec8<T> v[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) v[h] = load8_to<T, AL>(p + 16 * c + 8 * h, p + a.cols);
+    struct R { Vec8<T> v[2]; } r;
+    r.v[0] = v[0], r.v[1] = v[1];
+    return r;
+  };
+  float m = 0.f;
+  if (on)
+    for (int c = lane; c < a.chunks; c += a.lg) {
+      const auto r = load(c);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) m = larger(m, fabsf(r.v[i >> 3].get(i & 7)));
+    }
+  for (int d = 1; d < min(a.lg, 64); d <<= 1) m = larger(m, __shfl_xor(m, d));
+  if (a.lg == 256) {   // (of every thread or none)
+    if ((tid & 63) == 0) red[tid >> 6] = m;
+    __syncthreads();
+    m = larger(larger(red[0], red[1]), larger(red[2], red[3]));
+  }
+  if (!on) return;
+  const float s = scale8(m), inv = inverse8(s);
+  if (lane == 0) scales[row] = s;
+  for (int c = lane; c < a.chunks; c += a.lg) {
+    const auto r = load(c);
+    uint4 o;
+    unsigned* w = &o.x;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      unsigned b = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int e = 4 * j + i;
+        const int q = s == s ? round8(r.v[e >> 3].get(e & 7), s, inv) : 0;
+        b |= (unsigned)(q & 255) << 8 * i;
+      }
+      w[j] = b;
+    }
+    *reinterpret_cast<uint4*>(values + row * a.ld_values + 16 * c) = o;
+  }
+}
+
+// x = q s, 8 columns a thread
+template <class T, bool AL>
+__global__ void __launch_bounds__(256) unpack_rows_kernel(Rows8Args a, const int8_t* __restrict__ values,
+                                                          const float* __restrict__ scales, T* __restrict__ x) {
+  int vec;
+  const int64_t row = item_row((a.cols + 7) / 8, vec);
+  if (row >= a.n) return;
+  const int c = 8 * vec;
+  const uint2 q = *reinterpret_cast<const uint2*>(values + row * a.ld_values + c);
+  const float s = scales[row];
+  f8 v;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = s * (float)(int8_t)((i < 4 ? q.x : q.y) >> 8 * (i & 3));
+  store_n(x + row * a.ld_x + c, v, min(8, a.cols - c), AL);
+}
+
+// Weights: a block takes 64 output columns of a group, one a lane, its waves' rows
+// 16 at a time; the column's largest magnitude over all rows first.
+template <class T>
+__global__ void __launch_bounds__(256) pack_weights_kernel(const T* __restrict__ w, int n_in, int n_out, int64_t ld,
+                                                           int8_t* __restrict__ values, float* __restrict__ scales) {
+  __shared__ float red[4][64];
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, tiles = (n_out + 63) / 64;
+  const int64_t g = block_id() / tiles;
+  const int col = block_id() % tiles * 64 + lane;
+  const bool on = col < n_out;
+  w += g * n_in * n_out + (on ? col : 0);
+  float m = 0.f;
+  if (on)
+    for (int k = wv; k < n_in; k += 4) m = larger(m, fabsf(to_f32(w[(int64_t)k * n_out])));
+  red[wv][lane] = m;
+  __syncthreads();
+  m = larger(larger(red[0][lane], red[1][lane]), larger(red[2][lane], red[3][lane]));
+  if (!on) return;
+  const float s = scale8(m), inv = inverse8(s);
+  if (wv == 0) scales[g * n_out + col] = s;
+  values += (g * n_out + col) * ld;
+  for (int64_t k0 = 16 * wv; k0 < n_in; k0 += 64) {
+    uint4 o;
+    unsigned* b = &o.x;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      b[j] = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int64_t k = k0 + 4 * j + i;
+        const int q = k < n_in && s == s ? round8(to_f32(w[k * n_out]), s, inv) : 0;
+        b[j] |= (unsigned)(q & 255) << 8 * i;
+      }
+    }
+    *reinterpret_cast<uint4*>(values + k0) = o;
+  }
+}
+
+// ------------------------------------------------------------------ host
+mace_status check(const mace_rows8_desc* d) {
+  if (!d || d->n_rows < 0 || d->n_cols < 1 || d->dtype < MACE_TYPE_FP32 || d->dtype > MACE_TYPE_FP16) return MACE_EINVAL;
+  if (d->ld_x < d->n_cols || d->ld_values < d->n_cols || d->ld_values % 16) return MACE_EINVAL;
+  if (d->n_rows > (1 << 30) || d->n_cols > kMaxColumns8 || d->ld_values > kMaxPitch8) return MACE_EUNSUPPORTED;
+  return MACE_OK;
+}
+
+}  // namespace
+}  // namespace mace
+
+using namespace mace;
+
+extern "C" mace_status mace_pack_rows(const mace_rows8_desc* desc, const void* x, void* values, float* scales, void* stream) {
+  const mace_status st = check(desc);
+  if (st != MACE_OK) return st;
+  if (desc->n_rows == 0) return MACE_OK;
+  if (!x || !values || !scales || !aligned16(values)) return MACE_EINVAL;
+  return by_type(desc->dtype, [&](auto zero) -> mace_status {
+    using T = decltype(zero);
+    const mace_rows8_desc& d = *desc;
+    Rows8Args a{d.n_rows, d.ld_x, d.ld_values, d.n_cols, (int)ceil_div(d.n_cols, 16), 1};
+    while (a.lg < a.chunks && a.lg < 64) a.lg *= 2;
+    if (a.chunks > 128) a.lg = 256;
+    const int64_t blocks = ceil_div(d.n_rows, 256 / a.lg);
+    if (!fits_grid(blocks)) return MACE_EUNSUPPORTED;
+    const bool al = aligned16(x) && ((d.n_cols | d.ld_x) & 15) == 0;
+    auto f = al ? pack_rows_kernel<T, true> : pack_rows_kernel<T, false>;
+    f<<<grid_of(blocks), 256, 0, (hipStream_t)stream>>>(a, (const T*)x, (int8_t*)values, scales);
+    return launched();
+  });
+}
+
+extern "C" mace_status mace_unpack_rows(const mace_rows8_desc* desc, const void* values, const float* scales, void* x,
+                                        void* stream) {
+  const mace_status st = check(desc);
+  if (st != MACE_OK) return st;
+  if (desc->n_rows == 0) return MACE_OK;
+  if (!x || !values || !scales || !aligned16(values)) return MACE_EINVAL;
+  return by_type(desc->dtype, [&](auto zero) -> mace_status {
+    using T = decltype(zero);
+    const mace_rows8_desc& d = *desc;
+    const Rows8Args a{d.n_rows, d.ld_x, d.ld_values, d.n_cols, (int)ceil_div(d.n_cols, 16), 1};
+    const int64_t blocks = ceil_div(d.n_rows * ceil_div(d.n_cols, 8), 256);
+    if (!fits_grid(blocks)) return MACE_EUNSUPPORTED;
+    const bool al = aligned16(x) && ((d.n_cols | d.ld_x) & 7) == 0;
+    auto f = al ? unpack_rows_kernel<T, true> : unpack_rows_kernel<T, false>;
+    f<<<grid_of(blocks), 256, 0, (hipStream_t)stream>>>(a, (const int8_t*)values, scales, (T*)x);
+    return launched();
+  });
+}
+
+extern "C" mace_status mace_pack_weights(int32_t n_groups, int32_t n_in, int32_t n_out, int32_t dtype, const void* weights,
+                                         void* values, int64_t ld_values, float* scales, void* stream) {
+  if (n_groups < 1 || n_in < 1 || n_out < 1 || dtype < MACE_TYPE_FP32 || dtype > MACE_TYPE_FP16) return MACE_EINVAL;
+  if (!weights || !values || !scales || !aligned16(values) || ld_values < n_in || ld_values % 16) return MACE_EINVAL;
+  if (n_groups > 1024 || n_in > kMaxColumns8 || n_out > (1 << 20) || ld_values > kMaxPitch8) return MACE_EUNSUPPORTED;
+  return by_type(dtype, [&](auto zero) -> mace_status {
+    using T = decltype(zero);
+    const int64_t blocks = n_groups * ceil_div(n_out, 64);
+    if (!fits_grid(blocks)) return MACE_EUNSUPPORTED;
+    pack_weights_kernel<T><<<grid_of(blocks), 256, 0, (hipStream_t)stream>>>((const T*)weights, n_in, n_out, ld_values,
+                                                                            (int8_t*)values, scales);
+    return launched();
+  });
+}

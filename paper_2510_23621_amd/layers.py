@@ -1,11 +1,13 @@
-"""Dense operators on torch tensors: grouped linear layers, rows sorted by
-expert and back, Newton-Schulz orthogonalisation, and the gradients of the
-first two.  torch allocates results and workspaces, the library's kernels do
-the work on ``stream`` (a torch.cuda.Stream; default: the current one).
+"""Dense operators on torch tensors: grouped linear layers, embeddings, the
+choice of experts, rows sorted by expert and back, Newton-Schulz
+orthogonalisation, and the gradients of all but the last; linear layers served
+in 8 bits, and their gradients from activations kept in 8 bits.  torch allocates
+results and workspaces, the library's kernels do the work on ``stream`` (a
+torch.cuda.Stream; default: the current one).
 
 Tensors are float32, bfloat16 or float16 on one GPU, whichever is current, and
 ``stream`` is one of that GPU's; rows may be strided (any row stride, columns
-adjacent), and gradients handed to a backward function (dy, dout, drows) in any
+adjacent), and gradients handed to a backward function (dy, dout, drows, dweights) in any
 order, at the price of a copy.  Tensors of another stream are the caller's to
 order, as with any torch operation.  Nothing here records a graph for autograd:
 the backward functions are called by the program, under torch.no_grad() or on
@@ -25,6 +27,7 @@ import torch
 from . import binding as B
 
 DTYPES = {torch.float32: B.MACE_TYPE_FP32, torch.bfloat16: B.MACE_TYPE_BF16, torch.float16: B.MACE_TYPE_FP16}
+SCORES = {"softmax": B.MACE_SCORES_SOFTMAX, "sigmoid": B.MACE_SCORES_SIGMOID}
 ACTIVATIONS = {"none": B.MACE_ACT_NONE, "silu": B.MACE_ACT_SILU, "gelu": B.MACE_ACT_GELU}
 # a, b, c of five steps that bring singular values from about 0.01..1 to about 0.7..1.2: the
 # ones published with the Muon optimiser (K. Jordan and others, 2024)
@@ -42,10 +45,14 @@ def _streamed(f):
     def on(*args, stream=None, **kw):
         if torch.is_grad_enabled():
             for t in (*args, *kw.values()):
-                if getattr(t, "requires_grad", False):
+                if getattr(t, "requires_grad", False) or isinstance(t, tuple) and any(getattr(u, "requires_grad", False)
+                                                                                      for u in t):
                     raise ValueError(f"{f.__name__} records no gradients: call it under torch.no_grad() or on "
                                      "detached tensors")
-        device = (args[0] if args else kw[first]).get_device()   # (-1: a host tensor, which f refuses)
+        t = args[0] if args else kw[first]
+        if isinstance(t, tuple):   # (Rows8: the device of its values)
+            t = t[0]
+        device = t.get_device()   # (-1: a host tensor, which f refuses)
         if stream is not None:
             if stream.device.index != device:
                 raise ValueError(f"stream is of device {stream.device}, {first} of {device}")
@@ -302,6 +309,279 @@ def combine_rows_backward(dout, rows, plan: Route, weights=None):
 def route_rows_backward(drows, plan: Route):
     """Gradient of `route_rows` with respect to x."""
     return _combine(_gradient(drows), plan)
+
+
+class Choice(NamedTuple):
+    """The experts of each token, best first, and their weights (`choose_experts`)."""
+    expert: torch.Tensor    # int32 [tokens, top_k], -1 where fewer are left
+    weights: torch.Tensor   # float32 [tokens, top_k]
+
+
+def _choose_desc(logits, top_k, groups, top_groups, scores, normalise, scale):
+    dtype, kind = _gpu_matrix(logits, "logits"), SCORES.get(scores)
+    if kind is None:
+        raise ValueError(f"scores must be one of {sorted(SCORES)}")
+    n, e = logits.shape
+    for v in (top_k, groups, top_groups):
+        if not 0 < v < 1 << 31:
+            raise ValueError("top_k, groups and top_groups must be positive 32-bit integers")
+    return B.mace_choose_desc(n, e, top_k, groups, top_groups, dtype, kind, bool(normalise), _leading(logits, "logits"), scale)
+
+
+@_streamed
+def choose_experts(logits, top_k: int, *, bias=None, scores: str = "softmax", groups: int = 1, top_groups: int | None = None,
+                   normalise: bool = True, scale: float = 1.0) -> Choice:
+    """The top_k experts of each token by score + bias and their weights, scale
+    times the scores (softmax or sigmoid of logits [tokens, experts]), divided by
+    the chosen ones' sum if `normalise`.  bias (float32 [experts]) sways the
+    choice only.  groups: runs of experts of which the top_groups (default: all)
+    with the largest sums of their two best take part.  Equal ones go by the
+    lower index.  A logit of -infinity or the type's lowest value masks its
+    expert; where fewer than top_k are left the expert is -1, which `route`
+    drops, and the weight 0.  A token with a NaN gets NaN weights."""
+    d = _choose_desc(logits, top_k, groups, groups if top_groups is None else top_groups, scores, normalise, scale)
+    if bias is not None:
+        _whole(bias, (d.n_experts,), torch.float32, logits, "bias")
+    expert = logits.new_empty((d.n_tokens, top_k), dtype=torch.int32)
+    weights = logits.new_empty((d.n_tokens, top_k), dtype=torch.float32)
+    B._check(B.lib().mace_choose_forward(d, logits.data_ptr(), None if bias is None else bias.data_ptr(),
+                                         expert.data_ptr(), weights.data_ptr(), _current_stream(logits)),
+             "mace_choose_forward")
+    return Choice(expert, weights)
+
+
+@_streamed
+def choose_experts_backward(dweights, logits, expert, *, scores: str = "softmax", normalise: bool = True,
+                            scale: float = 1.0):
+    """Gradient of the logits from dweights (float32 [tokens, top_k]) and the
+    experts that `choose_experts` chose, which themselves have no gradient."""
+    if expert.dim() != 2:
+        raise ValueError("expert must be [tokens, top_k]")
+    n, k = expert.shape
+    if dweights.dim() != 2 or not dweights.is_cuda:
+        raise ValueError(f"dweights must be a float32 {(n, k)} GPU tensor")
+    d = _choose_desc(logits, k, 1, 1, scores, normalise, scale)
+    if not dweights.is_contiguous():
+        dweights = dweights.contiguous()
+    _whole(expert, (d.n_tokens, k), torch.int32, logits, "expert")
+    _whole(dweights, (d.n_tokens, k), torch.float32, logits, "dweights")
+    dlogits = logits.new_empty(logits.shape)
+    B._check(B.lib().mace_choose_backward(d, dweights.data_ptr(), logits.data_ptr(), expert.data_ptr(),
+                                          dlogits.data_ptr(), d.n_experts, _current_stream(logits)),
+             "mace_choose_backward")
+    return dlogits
+
+
+def _ids(ids):
+    if ids.dtype is not torch.int32 or not ids.is_cuda or not ids.is_contiguous():
+        raise ValueError("ids must be a contiguous int32 GPU tensor")
+
+
+@_streamed
+def embed(ids, table, *, scale: float = 1.0):
+    """scale table[ids] for int32 ids of any shape: [*ids.shape, width], zeros
+    for ids outside the table (-1, say, in a padded batch)."""
+    _ids(ids)
+    dtype = _gpu_matrix(table, "table")
+    v, width = table.shape
+    if table.get_device() != ids.get_device():
+        raise ValueError("table must be on ids' device")
+    d = B.mace_embed_desc(ids.numel(), v, width, dtype, _leading(table, "table"), width, scale)
+    out = table.new_empty((*ids.shape, width))
+    B._check(B.lib().mace_embed_forward(d, table.data_ptr(), ids.data_ptr(), out.data_ptr(), _current_stream(ids)),
+             "mace_embed_forward")
+    return out
+
+
+@_streamed
+def embed_backward(dout, ids, n_rows: int, *, scale: float = 1.0):
+    """Gradient [n_rows, width] of the table of `embed`, in dout's dtype."""
+    _ids(ids)
+    if dout.dim() < 1 or dout.shape[:-1] != ids.shape or dout.get_device() != ids.get_device():
+        raise ValueError(f"dout must be {(*ids.shape, 'width')} on ids' device")
+    if not 0 < n_rows < 1 << 31:
+        raise ValueError("n_rows must be a positive 32-bit integer")
+    width = dout.shape[-1]
+    dout = _gradient(dout if dout.dim() == 2 else dout.reshape(ids.numel(), width))
+    d = B.mace_embed_desc(ids.numel(), n_rows, width, _gpu_matrix(dout, "dout"), width, _leading(dout, "dout"), scale)
+    dtable = dout.new_empty((n_rows, width))
+    lib = B.lib()
+    # (0 for sizes the library does not take: the call itself says which error)
+    nbytes = lib.mace_embed_backward_workspace_bytes(d) or 1
+    ws = dout.new_empty(nbytes, dtype=torch.uint8)
+    B._check(lib.mace_embed_backward(d, dout.data_ptr(), ids.data_ptr(), dtable.data_ptr(), ws.data_ptr(), nbytes,
+                                     _current_stream(dout)), "mace_embed_backward")
+    return dtable
+
+
+class Rows8(NamedTuple):
+    """Rows of 8-bit integers with a scale each (`pack_rows`): values[i, :columns] * scales[i]."""
+    values: torch.Tensor   # int8 [n, columns rounded up to a multiple of 16]
+    scales: torch.Tensor   # float32 [n]
+    columns: int
+
+
+class Weights8(NamedTuple):
+    """Weights of 8-bit integers with a scale for each output column (`pack_weights`)."""
+    values: torch.Tensor   # int8 [groups, n_out, n_in rounded up to a multiple of 16]
+    scales: torch.Tensor   # float32 [groups, n_out]
+    n_in: int
+
+
+def _check_rows8(r: Rows8, name: str):
+    v, s, c = r
+    if v.dim() != 2 or v.dtype is not torch.int8 or not v.is_cuda or not v.is_contiguous() or not 0 < c <= v.shape[1]:
+        raise ValueError(f"{name}'s values must be contiguous int8 [n, columns, padded] on a GPU")
+    _whole(s, (v.shape[0],), torch.float32, v, f"{name}'s scales")
+
+
+@_streamed
+def pack_rows(x) -> Rows8:
+    """x's rows as the nearest 8-bit integers in -127..127 and a float32 scale,
+    the row's largest magnitude / 127, each: half the size of a 16-bit activation
+    kept for the backward (`linear_backward8`), and an operand of `linear8`.  A
+    row with a non-finite element gets the scale NaN."""
+    dtype = _gpu_matrix(x, "x")
+    n, c = x.shape
+    ld = (c + 15) // 16 * 16
+    d = B.mace_rows8_desc(n, c, dtype, _leading(x, "x"), ld)
+    values, scales = x.new_empty((n, ld), dtype=torch.int8), x.new_empty(n, dtype=torch.float32)
+    B._check(B.lib().mace_pack_rows(d, x.data_ptr(), values.data_ptr(), scales.data_ptr(), _current_stream(x)),
+             "mace_pack_rows")
+    return Rows8(values, scales, c)
+
+
+@_streamed
+def unpack_rows(rows: Rows8, dtype: torch.dtype = torch.float32):
+    """[n, columns] values that rows stand for, rounded once to dtype."""
+    _check_rows8(rows, "rows")
+    if dtype not in DTYPES:
+        raise ValueError("dtype must be float32, bfloat16 or float16")
+    values, scales, c = rows
+    d = B.mace_rows8_desc(values.shape[0], c, DTYPES[dtype], c, values.shape[1])
+    x = values.new_empty((values.shape[0], c), dtype=dtype)
+    B._check(B.lib().mace_unpack_rows(d, values.data_ptr(), scales.data_ptr(), x.data_ptr(), _current_stream(values)),
+             "mace_unpack_rows")
+    return x
+
+
+@_streamed
+def pack_weights(w) -> Weights8:
+    """w [n_in, n_out] or [groups, n_in, n_out] for `linear8`: 8-bit integers and
+    a float32 scale for each output column of each group."""
+    dtype = DTYPES.get(w.dtype)
+    if dtype is None or w.dim() not in (2, 3) or not w.is_cuda or not w.is_contiguous():
+        raise ValueError("w must be a contiguous [(groups,) n_in, n_out] GPU tensor of float32, bfloat16 or float16")
+    g, k, m = w.shape if w.dim() == 3 else (1, *w.shape)
+    if (g | k | m) >> 31:
+        _too_large("w")
+    ld = (k + 15) // 16 * 16
+    values, scales = w.new_empty((g, m, ld), dtype=torch.int8), w.new_empty((g, m), dtype=torch.float32)
+    B._check(B.lib().mace_pack_weights(g, k, m, dtype, w.data_ptr(), values.data_ptr(), ld, scales.data_ptr(),
+                                       _current_stream(w)), "mace_pack_weights")
+    return Weights8(values, scales, k)
+
+
+@_streamed
+def linear8(x, w: Weights8, bias=None, residual=None, *, offsets=None, act: str = "none", dtype: torch.dtype | None = None):
+    """`linear` in 8 bits: y = act(x W_g + b_g) + residual with x's rows rounded as
+    `pack_rows` does and weights of `pack_weights`; the products' sums are exact.
+    x: [n, n_in] of float32, bfloat16 or float16, or Rows8; dtype (for Rows8 only;
+    default float32) is that of bias, residual and y."""
+    values, w_scales, n_in = w
+    if values.dim() != 3 or values.dtype is not torch.int8 or not values.is_contiguous() or not 0 < n_in <= values.shape[2]:
+        raise ValueError("w must be Weights8 as pack_weights gives them")
+    groups, m, ld_w = values.shape
+    a = ACTIVATIONS.get(act)
+    if a is None:
+        raise ValueError(f"act must be one of {sorted(ACTIVATIONS)}")
+    if isinstance(x, tuple):
+        _check_rows8(x, "x")
+        x, x_scales, c = x
+        dtype = torch.float32 if dtype is None else dtype
+        if dtype not in DTYPES:
+            raise ValueError("dtype must be float32, bfloat16 or float16")
+        like, ld_x = x.new_empty(0, dtype=dtype), x.shape[1]
+    else:
+        _gpu_matrix(x, "x")
+        if dtype is not None and dtype is not x.dtype:
+            raise ValueError("dtype is x's, but for Rows8")
+        x_scales, c, like, ld_x = None, x.shape[1], x, _leading(x, "x")
+    n = x.shape[0]
+    if c != n_in or values.get_device() != x.get_device():
+        raise ValueError(f"w must have {c} input rows and be on x's device")
+    _whole(w_scales, (groups, m), torch.float32, x, "w's scales")
+    if offsets is not None:
+        _whole(offsets, (groups + 1,), torch.int32, x, "offsets")
+    elif groups != 1:
+        raise ValueError("more than one group needs offsets")
+    d = B.mace_linear_desc(n, n_in, m, groups, DTYPES[like.dtype], a, ld_x, m, m, m)
+    if bias is not None:
+        if bias.shape != (groups, m) and (groups != 1 or bias.shape != (m,)):
+            raise ValueError(f"bias must be {(groups, m)}")
+        _whole(bias, bias.shape, like.dtype, x, "bias")
+    if residual is not None:
+        d.ld_residual = _rows(residual, n, m, like, "residual")
+    y = like.new_empty((n, m))
+    lib = B.lib()
+    nbytes = 0 if x_scales is not None else lib.mace_linear8_workspace_bytes(d) or 1
+    ws = x.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
+    B._check(lib.mace_linear8_forward(d, x.data_ptr(), None if x_scales is None else x_scales.data_ptr(),
+                                      values.data_ptr(), ld_w, w_scales.data_ptr(),
+                                      None if bias is None else bias.data_ptr(),
+                                      None if residual is None else residual.data_ptr(),
+                                      None if offsets is None else offsets.data_ptr(), y.data_ptr(),
+                                      None if ws is None else ws.data_ptr(), nbytes, _current_stream(x)),
+             "mace_linear8_forward")
+    return y
+
+
+@_streamed
+def linear_backward8(dy, x: Rows8, w, z: Rows8 | None = None, *, offsets=None, act: str = "none", bias: bool = True,
+                     need_dx: bool = True, need_dw: bool = True):
+    """(dx, dw, db) of `linear` from dy, with x and z (what `linear` saved) kept as
+    8-bit rows of `pack_rows` since the forward: the gradients at the values that
+    they stand for."""
+    dy = _gradient(dy)
+    dtype, a = _gpu_matrix(dy, "dy"), ACTIVATIONS.get(act)
+    if a is None:
+        raise ValueError(f"act must be one of {sorted(ACTIVATIONS)}")
+    _check_rows8(x, "x")
+    n, m = dy.shape
+    groups, k, n_out = w.shape if w.dim() == 3 else (1, *w.shape) if w.dim() == 2 else (0, 0, 0)
+    if groups == 0 or n_out != m or w.dtype is not dy.dtype or w.get_device() != dy.get_device() or not w.is_contiguous():
+        raise ValueError(f"w must be contiguous [(groups,) n_in, {m}], of dy's dtype and device")
+    if (groups | k) >> 31:
+        _too_large("w")
+    if x.values.shape[0] != n or x.columns != k or x.values.get_device() != dy.get_device():
+        raise ValueError(f"x must stand for {(n, k)} on dy's device")
+    if offsets is not None:
+        _whole(offsets, (groups + 1,), torch.int32, dy, "offsets")
+    elif groups != 1:
+        raise ValueError("more than one group needs offsets")
+    ld_z = m
+    if a:
+        if z is None:
+            raise ValueError("an activation's gradient needs z")
+        _check_rows8(z, "z")
+        if z.values.shape[0] != n or z.columns != m or z.values.get_device() != dy.get_device():
+            raise ValueError(f"z must stand for {(n, m)} on dy's device")
+        ld_z = z.values.shape[1]
+    d = B.mace_linear_desc(n, k, m, groups, dtype, a, x.values.shape[1], m, m, ld_z)
+    dx = dy.new_empty((n, k)) if need_dx else None
+    dw = torch.empty_like(w) if need_dw else None
+    db = dy.new_empty((*w.shape[:-2], m)) if bias else None
+    lib = B.lib()
+    nbytes = lib.mace_linear_backward8_workspace_bytes(d, bias, need_dw) or 1
+    ws = dy.new_empty(nbytes, dtype=torch.uint8)
+    B._check(lib.mace_linear_backward8(d, dy.data_ptr(), _leading(dy, "dy"), x.values.data_ptr(), x.scales.data_ptr(),
+                                       w.data_ptr(), z.values.data_ptr() if a else None,
+                                       z.scales.data_ptr() if a else None,
+                                       None if offsets is None else offsets.data_ptr(),
+                                       None if dx is None else dx.data_ptr(), k,
+                                       None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr(),
+                                       ws.data_ptr(), nbytes, _current_stream(dy)), "mace_linear_backward8")
+    return dx, dw, db
 
 
 def _coefficients(steps) -> np.ndarray:

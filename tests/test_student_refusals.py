@@ -1,0 +1,171 @@
+"""Argument errors of embeddings, the choice of experts, 8-bit rows and the layers on
+them: the documented status before any device work, on the CPU."""
+import os
+
+import numpy as np
+import pytest
+
+B = pytest.importorskip("paper_2510_23621_amd.binding")
+pytestmark = pytest.mark.skipif(not os.path.exists(B.LIB_PATH), reason="libmace_amd.so not built")
+
+EINVAL, ENOSPACE, EUNSUPPORTED = -1, -3, -7
+_BUF = np.zeros(4096 + 2, np.float64)
+A = _BUF[(-_BUF.ctypes.data // 8) % 2:][:4096]   # 16-byte aligned; stands for every tensor: refused calls do not touch it
+ODD = A.ctypes.data + 8
+
+
+def code(f, *a):
+    return getattr(B.lib(), f)(*[x.ctypes.data if isinstance(x, np.ndarray) else x for x in a])
+
+
+def each_missing(f, ok, places, want=EINVAL):
+    for i in places:
+        bad = list(ok)
+        bad[i] = None
+        assert code(f, *bad) == want, i
+
+
+def embed(**kw):
+    return B.mace_embed_desc(**{**dict(n_ids=10, n_rows=5, width=8, dtype=0, ld_table=8, ld_out=8, scale=1.0), **kw})
+
+
+@pytest.mark.parametrize("change,want", [
+    (dict(n_ids=-1), EINVAL), (dict(n_rows=0), EINVAL), (dict(width=0), EINVAL), (dict(dtype=3), EINVAL), (dict(dtype=-1), EINVAL),
+    (dict(ld_table=7), EINVAL), (dict(ld_out=7), EINVAL), (dict(scale=float("nan")), EINVAL), (dict(scale=float("inf")), EINVAL),
+    (dict(scale=1e39), EINVAL), (dict(n_ids=(1 << 30) + 1), EUNSUPPORTED), (dict(n_rows=(1 << 30) + 1), EUNSUPPORTED),
+    (dict(width=(1 << 20) + 1, ld_table=1 << 21, ld_out=1 << 21), EUNSUPPORTED)])
+def test_embed_descriptor(change, want):
+    d = embed(**change)
+    assert code("mace_embed_forward", d, A, A, A, None) == want
+    assert code("mace_embed_backward_workspace_bytes", d) == 0
+    assert code("mace_embed_backward", d, A, A, A, A, 1 << 40, None) == want
+
+
+def test_embed_arguments():
+    assert code("mace_embed_forward", None, A, A, A, None) == EINVAL
+    each_missing("mace_embed_forward", [embed(), A, A, A, None], (1, 2, 3))
+    each_missing("mace_embed_backward", [embed(), A, A, A, A, 1 << 40, None], (1, 2, 3, 4))
+    assert code("mace_embed_backward", embed(), A, A, A, A, 64, None) == ENOSPACE
+    assert code("mace_embed_forward", embed(n_ids=0), None, None, None, None) == 0
+    assert B.mace_embed_backward_workspace_bytes(embed()) > 0
+
+
+def choose(**kw):
+    return B.mace_choose_desc(**{**dict(n_tokens=10, n_experts=12, top_k=2, n_groups=3, top_groups=2, dtype=0, scores=0,
+                                        normalise=1, ld_logits=12, scale=1.0), **kw})
+
+
+@pytest.mark.parametrize("change,want", [
+    (dict(n_tokens=-1), EINVAL), (dict(n_experts=0), EINVAL), (dict(top_k=0), EINVAL), (dict(n_groups=0), EINVAL),
+    (dict(top_groups=0), EINVAL), (dict(top_groups=4), EINVAL), (dict(n_groups=5), EINVAL), (dict(top_k=9), EINVAL),
+    (dict(top_k=5, top_groups=1), EINVAL), (dict(dtype=3), EINVAL), (dict(dtype=-1), EINVAL), (dict(scores=2), EINVAL),
+    (dict(normalise=2), EINVAL), (dict(ld_logits=11), EINVAL), (dict(scale=float("nan")), EINVAL), (dict(scale=1e39), EINVAL),
+    (dict(n_experts=513, ld_logits=513), EUNSUPPORTED), (dict(n_experts=130, n_groups=65, ld_logits=130), EUNSUPPORTED),
+    (dict(n_experts=100, n_groups=1, top_groups=1, top_k=65, ld_logits=100), EUNSUPPORTED),
+    (dict(n_tokens=(1 << 30) + 1, top_k=1), EUNSUPPORTED), (dict(n_tokens=(1 << 29) + 1), EUNSUPPORTED)])
+def test_choose_descriptor(change, want):
+    d = choose(**change)
+    assert code("mace_choose_forward", d, A, A, A, A, None) == want
+    assert code("mace_choose_backward", d, A, A, A, A, 600, None) == want
+
+
+def test_choose_arguments():
+    assert code("mace_choose_forward", None, A, A, A, A, None) == EINVAL
+    each_missing("mace_choose_forward", [choose(), A, A, A, A, None], (1, 3, 4))   # (a bias is not needed)
+    each_missing("mace_choose_backward", [choose(), A, A, A, A, 12, None], (1, 2, 3, 4))
+    assert code("mace_choose_backward", choose(), A, A, A, A, 11, None) == EINVAL
+    assert code("mace_choose_forward", choose(n_tokens=0), None, None, None, None, None) == 0
+    assert code("mace_choose_backward", choose(n_tokens=0), None, None, None, None, 12, None) == 0
+
+
+def rows8(**kw):
+    return B.mace_rows8_desc(**{**dict(n_rows=10, n_cols=20, dtype=0, ld_x=20, ld_values=32), **kw})
+
+
+@pytest.mark.parametrize("change,want", [
+    (dict(n_rows=-1), EINVAL), (dict(n_cols=0), EINVAL), (dict(dtype=3), EINVAL), (dict(dtype=-1), EINVAL), (dict(ld_x=19), EINVAL),
+    (dict(ld_values=16), EINVAL), (dict(ld_values=40), EINVAL), (dict(n_rows=(1 << 30) + 1), EUNSUPPORTED),
+    (dict(n_cols=131073, ld_x=131073, ld_values=131088), EUNSUPPORTED), (dict(ld_values=(1 << 20) + 16), EUNSUPPORTED)])
+def test_rows8_descriptor(change, want):
+    d = rows8(**change)
+    assert code("mace_pack_rows", d, A, A, A, None) == want
+    assert code("mace_unpack_rows", d, A, A, A, None) == want
+
+
+def test_rows8_arguments():
+    for f in ("mace_pack_rows", "mace_unpack_rows"):
+        assert code(f, None, A, A, A, None) == EINVAL
+        each_missing(f, [rows8(), A, A, A, None], (1, 2, 3))
+        assert code(f, rows8(n_rows=0), None, None, None, None) == 0
+    assert code("mace_pack_rows", rows8(), A, ODD, A, None) == EINVAL
+    assert code("mace_unpack_rows", rows8(), ODD, A, A, None) == EINVAL
+
+
+def test_pack_weights_arguments():
+    ok = [2, 20, 8, 0, A, A, 32, A, None]
+    for i, v in ((0, 0), (1, 0), (2, 0), (3, 3), (3, -1), (4, None), (5, None), (5, ODD), (6, 16), (6, 40), (7, None)):
+        bad = list(ok)
+        bad[i] = v
+        assert code("mace_pack_weights", *bad) == EINVAL, (i, v)
+    for i, v, ld in ((0, 1025, 32), (1, 131073, 131088), (2, (1 << 20) + 1, 32), (0, 2, (1 << 20) + 16)):
+        bad = list(ok)
+        bad[i], bad[6] = v, ld
+        assert code("mace_pack_weights", *bad) == EUNSUPPORTED, (i, v)
+
+
+def linear(**kw):
+    return B.mace_linear_desc(**{**dict(n_rows=10, n_in=20, n_out=24, n_groups=2, dtype=0, act=1, ld_x=32, ld_y=24, ld_residual=24,
+                                        ld_preact=32), **kw})
+
+
+LINEAR = [(dict(n_rows=-1), EINVAL), (dict(n_in=0), EINVAL), (dict(n_out=0), EINVAL), (dict(n_groups=0), EINVAL), (dict(dtype=3), EINVAL),
+          (dict(act=3), EINVAL), (dict(act=-1), EINVAL), (dict(ld_x=16), EINVAL), (dict(ld_y=23), EINVAL), (dict(ld_residual=23), EINVAL),
+          (dict(n_groups=1025), EUNSUPPORTED), (dict(n_rows=(1 << 30) + 1), EUNSUPPORTED),
+          (dict(n_in=131073, ld_x=131088), EUNSUPPORTED)]
+
+
+@pytest.mark.parametrize("change,want", LINEAR + [(dict(n_out=(1 << 20) + 1, ld_y=1 << 21, ld_residual=1 << 21), EUNSUPPORTED)])
+def test_linear8_descriptor(change, want):
+    d = linear(**change)
+    assert code("mace_linear8_workspace_bytes", d) == 0
+    assert code("mace_linear8_forward", d, A, A, A, 131088, A, A, A, A, A, A, 1 << 40, None) == want
+    assert code("mace_linear8_forward", d, A, None, A, 131088, A, A, A, A, A, A, 1 << 40, None) == want
+
+
+def test_linear8_arguments():
+    ok = [linear(), A, A, A, 32, A, A, A, A, A, None, 0, None]
+    assert code("mace_linear8_forward", None, *ok[1:]) == EINVAL
+    each_missing("mace_linear8_forward", ok, (1, 3, 5, 8, 9))   # x, weights and their scales, offsets of two groups, y
+    for i, v in ((1, ODD), (3, ODD), (4, 16), (4, 40), (0, linear(ld_x=40))):
+        bad = list(ok)
+        bad[i] = v
+        assert code("mace_linear8_forward", *bad) == EINVAL, i
+    for i, v in ((4, (1 << 20) + 16), (0, linear(ld_x=(1 << 20) + 16))):
+        bad = list(ok)
+        bad[i] = v
+        assert code("mace_linear8_forward", *bad) == EUNSUPPORTED, i
+    ok[2] = None   # rows of dtype need the workspace
+    assert code("mace_linear8_forward", *ok) == EINVAL
+    ok[10], ok[11] = A, 16
+    assert code("mace_linear8_forward", *ok) == ENOSPACE
+    assert code("mace_linear8_forward", linear(n_rows=0), None, None, A, 32, A, None, None, A, None, None, 0, None) == 0
+
+
+@pytest.mark.parametrize("change,want", LINEAR + [
+    (dict(ld_preact=23), EINVAL), (dict(ld_x=40), EINVAL), (dict(ld_preact=40), EINVAL), (dict(ld_x=(1 << 20) + 16), EUNSUPPORTED),
+    (dict(ld_preact=(1 << 20) + 16), EUNSUPPORTED), (dict(n_out=131073, ld_y=1 << 18, ld_residual=1 << 18, ld_preact=1 << 18), EUNSUPPORTED)])
+def test_linear_backward8_descriptor(change, want):
+    d = linear(**change)
+    assert code("mace_linear_backward8_workspace_bytes", d, 1, 1) == 0
+    assert code("mace_linear_backward8", d, A, 1 << 18, A, A, A, A, A, A, A, 1 << 18, A, A, A, 1 << 40, None) == want
+
+
+def test_linear_backward8_arguments():
+    ok = [linear(), A, 24, A, A, A, A, A, A, A, 20, A, A, A, 1 << 40, None]
+    assert code("mace_linear_backward8", None, *ok[1:]) == EINVAL
+    each_missing("mace_linear_backward8", ok, (1, 3, 4, 5, 6, 7, 8, 13))
+    for i, v in ((2, 23), (10, 19), (3, ODD), (6, ODD)):
+        bad = list(ok)
+        bad[i] = v
+        assert code("mace_linear_backward8", *bad) == EINVAL, i
+    assert code("mace_linear_backward8", *ok[:14], 16, None) == ENOSPACE
