@@ -8,11 +8,12 @@ namespace mace {
 namespace {
 
 constexpr int kMaxChoices = 64, kMaxExpertGroups = 64, kMaxScored = 512;
-constexpr int kPerLane = kMaxScored / 64;
 
 struct ChooseArgs {
   int64_t n, ld;
   int E, k, groups, top_groups, per;   // per: experts of a group
+  int per_inverse;                     // 2^20 / per, rounded up: n per_inverse >> 20 is n / per for n < 512
+  int group_lanes;                     // lanes of a group where it is whole lanes, a power of two of them; or 0
   int sigmoid, normalise;
   float scale;
 };
@@ -22,206 +23,533 @@ template <> __device__ __forceinline__ float lowest<float>() { return -3.4028234
 template <> __device__ __forceinline__ float lowest<__bf16>() { return -3.3895313892515355e38f; }
 template <> __device__ __forceinline__ float lowest<_Float16>() { return -65504.f; }
 
-__device__ __forceinline__ double shfl_xor(double v, int m) { return __shfl_xor(v, m); }
-
-// Largest (value, lowest index) over the wave, in every lane; NaN does not occur
-__device__ __forceinline__ void wave_best(double& v, int& i) {
+// ------------------------------------------------------------------ lanes of a row
+// LPR consecutive lanes hold a token's row. Their sums, maxima and minima go
+// through the vector units' own exchanges (DPP, and swaps of half rows), without LDS.
+template <int CTRL>
+__device__ __forceinline__ int dpp(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, true); }
+// the two values that a step of distance S joins, in some order: v's and its partner's
+template <int S, class X>
+__device__ __forceinline__ void exchange(X v, X& a, X& b) {
+  constexpr int W = sizeof(X) / 4;
+  int in[W], x[W], y[W];
+  __builtin_memcpy(in, &v, sizeof(X));
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const double ov = __shfl_xor(v, d);
-    const int oi = __shfl_xor(i, d);
-    if (ov > v || (ov == v && oi < i)) v = ov, i = oi;
+  for (int i = 0; i < W; ++i) {
+    x[i] = in[i];
+    if constexpr (S == 1) y[i] = dpp<0xb1>(in[i]);         // quads as 1 0 3 2
+    else if constexpr (S == 2) y[i] = dpp<0x4e>(in[i]);    // quads as 2 3 0 1
+    else if constexpr (S == 4) y[i] = dpp<0x141>(in[i]);   // eight lanes mirrored (quads are alike by now)
+    else if constexpr (S == 8) y[i] = dpp<0x140>(in[i]);   // sixteen mirrored
+    else {
+      const auto r = S == 16 ? __builtin_amdgcn_permlane16_swap(in[i], in[i], false, false)
+                             : __builtin_amdgcn_permlane32_swap(in[i], in[i], false, false);
+      x[i] = r[0], y[i] = r[1];
+    }
+  }
+  __builtin_memcpy(&a, x, sizeof(X));
+  __builtin_memcpy(&b, y, sizeof(X));
+}
+// f over the row's values, in every lane of it (f symmetric in its arguments)
+template <int LPR, class X, class F>
+__device__ __forceinline__ X over_row(X v, F f) {
+  X a, b;
+  if constexpr (LPR > 1) exchange<1>(v, a, b), v = f(a, b);
+  if constexpr (LPR > 2) exchange<2>(v, a, b), v = f(a, b);
+  if constexpr (LPR > 4) exchange<4>(v, a, b), v = f(a, b);
+  if constexpr (LPR > 8) exchange<8>(v, a, b), v = f(a, b);
+  if constexpr (LPR > 16) exchange<16>(v, a, b), v = f(a, b);
+  if constexpr (LPR > 32) exchange<32>(v, a, b), v = f(a, b);
+  return v;
+}
+__device__ __forceinline__ int max_of(int a, int b) { return max(a, b); }
+__device__ __forceinline__ float max_of(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ double max_of(double a, double b) { return fmax(a, b); }
+__device__ __forceinline__ int min_of(int a, int b) { return min(a, b); }
+__device__ __forceinline__ double min_of(double a, double b) { return fmin(a, b); }
+template <int LPR, class X>
+__device__ __forceinline__ X row_max(X v) { return over_row<LPR>(v, [](X a, X b) { return max_of(a, b); }); }
+template <int LPR, class X>
+__device__ __forceinline__ X row_sum(X v) { return over_row<LPR>(v, [](X a, X b) { return a + b; }); }
+template <int LPR>
+__device__ __forceinline__ int row_min(int v) { return over_row<LPR>(v, [](int a, int b) { return min(a, b); }); }
+template <int LPR>
+__device__ __forceinline__ bool row_any(bool v) { return over_row<LPR>((int)v, [](int a, int b) { return a | b; }); }
+
+// Keys are compared as integers in FP32 (the same order, and maxima that need not quiet a NaN
+// first: they fold into the exchange) and as they are in FP64.
+constexpr int kNoKey = (int)0xff800000 ^ 0x7fffffff;   // of -infinity
+__device__ __forceinline__ int key_of(float v) {   // (of zeros: +0 only)
+  const int i = __float_as_int(v);
+  return i ^ ((i >> 31) & 0x7fffffff);
+}
+__device__ __forceinline__ float value_of(int k) { return __int_as_float(k ^ ((k >> 31) & 0x7fffffff)); }
+__device__ __forceinline__ double value_of(double k) { return k; }
+__device__ __forceinline__ int no_key(int) { return kNoKey; }
+__device__ __forceinline__ double no_key(double) { return -__builtin_inff(); }
+
+// exp(-d) and 1 / (1 + exp(-x)) in either precision; NaN goes through
+__device__ __forceinline__ float exp_minus(float d) { return d == d ? exp_neg(fminf(d, 200.f)) : d; }
+__device__ __forceinline__ double exp_minus(double d) { return exp(-d); }
+__device__ __forceinline__ float sigmoid_of(float x) { return x == x ? recip_ge1(1.f + exp_neg(fminf(x, 200.f))) : x; }
+__device__ __forceinline__ double sigmoid_of(double x) { return 1 / (1 + exp(-x)); }
+// A chosen expert's score over exp(m), m the largest chosen logit (of a sigmoid: at most 0), for
+// renormalised weights: no 0 / 0 where all scores underflow
+template <class R>
+__device__ __forceinline__ R relative_score(R x, R m, bool sigmoid) {
+  if (!sigmoid) return exp_minus(m - x);
+  return exp_minus(m - (x > 0 ? 0 : x)) / (1 + exp_minus(x > 0 ? x : -x));
+}
+
+// V consecutive values of a row, `fill` from `end` on
+template <int V, class T>
+__device__ __forceinline__ void load_row(const T* p, int first, int end, float fill, float (&x)[V]) {
+  if (first + V <= end) {
+    typedef T tv __attribute__((ext_vector_type(V)));
+    tv t;
+    __builtin_memcpy(&t, p + first, sizeof(t));
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = to_f32(t[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = first + i < end ? to_f32(p[first + i]) : fill;
   }
 }
 
-// log of 1 / (1 + exp(-l))
-__device__ __forceinline__ double log_sigmoid(double l) { return (l < 0 ? l : 0.) - log1p(exp(-fabs(l))); }
+// ------------------------------------------------------------------ choice
+template <int LPR, int V>
+struct ChooseShape {
+  static constexpr int ROWS = 256 / LPR;                      // tokens per block
+  static constexpr int K = LPR * V < kMaxChoices ? LPR * V : kMaxChoices;
+  static constexpr int G = LPR * V < kMaxExpertGroups ? LPR * V : kMaxExpertGroups;
+};
+template <int LPR, int V>
+struct ChooseLds {
+  using S = ChooseShape<LPR, V>;
+  union {
+    struct {
+      int key[(V + 1) * 256];     // each lane's keys, largest first, and none behind them
+      int index[(V + 1) * 256];   // their experts
+    } sorted;
+    double key[S::ROWS][LPR * V];   // (or integers)
+  };
+  double total[S::ROWS][S::G];   // (or floats)
+  int taken[S::ROWS][S::G];
+  int index[S::ROWS][S::K];   // the choice
+};
 
-// A wave per token, lane l holding experts l, l + 64, ...; all in FP64, so that the order
-// of nearly equal scores is that of the scores and not of their roundings.
-template <class T>
+// Of a token's keys those outside its top_groups best groups become no_key. True: two
+// groups' totals differ by at most tol and a few units of themselves.
+template <class Key, int LPR, int V>
+__device__ __forceinline__ bool take_groups(const ChooseArgs& a, Key (&key)[V], float tol, int lane, int row, ChooseLds<LPR, V>& sm) {
+  using R = decltype(value_of(Key{}));
+  const Key none = no_key(Key{});
+  const R empty = -__builtin_inff();   // (total of a group without experts)
+  const int first = lane * V;
+  R* total = reinterpret_cast<R*>(sm.total[row]);
+  bool near_tie = false;
+  auto total_of = [&](Key c1, Key c2) {
+    const R t = value_of(c1);
+    return c2 > none ? t + value_of(c2) : (c1 > none ? t : empty);
+  };
+  // is the group's total among the top_groups largest
+  auto decide = [&](int g) {
+    const R mine = total[g];
+    int better = 0;
+    for (int h = 0; h < a.groups; ++h) {
+      const R o = total[h];
+      better += o > mine || (o == mine && h < g);
+      near_tie |= h != g && fabsf((float)(o - mine)) <= __builtin_fmaf(fabsf((float)mine), 4.7683716e-7f, tol);
+    }
+    return better < a.top_groups;
+  };
+  if (a.group_lanes) {   // whole lanes: their two best, joined over the group's lanes
+    Key c1 = none, c2 = none;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      c2 = max_of(c2, min_of(c1, key[i]));
+      c1 = max_of(c1, key[i]);
+    }
+    auto join = [&](auto step) {
+      if constexpr (decltype(step)::value < LPR) {
+        Key a1, b1, a2, b2;
+        exchange<decltype(step)::value>(c1, a1, b1);
+        exchange<decltype(step)::value>(c2, a2, b2);
+        c1 = max_of(a1, b1);
+        c2 = max_of(min_of(a1, b1), max_of(a2, b2));
+      }
+    };
+    if (a.group_lanes > 1) join(Int<1>{});
+    if (a.group_lanes > 2) join(Int<2>{});
+    if (a.group_lanes > 4) join(Int<4>{});
+    if (a.group_lanes > 8) join(Int<8>{});
+    if (a.group_lanes > 16) join(Int<16>{});
+    const int g = min(first * a.per_inverse >> 20, a.groups - 1);
+    if (first == g * a.per) total[g] = total_of(c1, c2);
+    __builtin_amdgcn_wave_barrier();
+    const bool taken = decide(g);
+#pragma unroll
+    for (int i = 0; i < V; ++i) key[i] = taken ? key[i] : none;
+  } else {
+    Key* keys = reinterpret_cast<Key*>(sm.key[row]);
+#pragma unroll
+    for (int i = 0; i < V; ++i) keys[first + i] = key[i];
+    __builtin_amdgcn_wave_barrier();
+    for (int g = lane; g < a.groups; g += LPR) {
+      Key c1 = none, c2 = none;
+      for (int j = 0; j < a.per; ++j) {
+        const Key c = keys[g * a.per + j];
+        c2 = max_of(c2, min_of(c1, c));
+        c1 = max_of(c1, c);
+      }
+      total[g] = total_of(c1, c2);
+    }
+    __builtin_amdgcn_wave_barrier();
+    for (int g = lane; g < a.groups; g += LPR) sm.taken[row][g] = decide(g);
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int g = min((first + i) * a.per_inverse >> 20, a.groups - 1);
+      key[i] = sm.taken[row][g] ? key[i] : none;
+    }
+  }
+  __builtin_amdgcn_wave_barrier();
+  return near_tie;
+}
+
+// The choice in FP64, for rows that FP32 cannot decide: k rounds of the largest key with the
+// lowest index, stored if `store`.
+template <class T, int LPR, int V>
+__device__ __noinline__ void choose_exact(ChooseArgs a, const T* logits, const float* bias, double top, int lane, int row,
+                                          bool store, ChooseLds<LPR, V>& sm) {
+  const double none = -__builtin_inff();
+  const int first = lane * V;
+  float x[V], b[V];   // (read again: the way here is rare, and the registers of the usual one its own)
+  load_row<V>(logits, first, a.E, -__builtin_inff(), x);
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    b[i] = 0.f;
+    if (!(x[i] > lowest<T>())) x[i] = -__builtin_inff();
+  }
+  if (bias) load_row<V>(bias, first, a.E, 0.f, b);
+  double key[V], sum = 0;
+  if (!a.sigmoid) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) sum += x[i] > none ? exp(x[i] - top) : 0.;
+    sum = row_sum<LPR>(sum);
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+    key[i] = x[i] > none ? (a.sigmoid ? 1 / (1 + exp(-(double)x[i])) : exp(x[i] - top) / sum) + b[i] : none;
+  if (a.groups > 1) take_groups<double, LPR, V>(a, key, 0.f, lane, row, sm);
+  if (!bias)   // the logits decide
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (key[i] > none) key[i] = x[i];
+  if (store)
+    for (int j = lane; j < a.k; j += LPR) sm.index[row][j] = -1;
+  __builtin_amdgcn_wave_barrier();
+  for (int j = 0; j < a.k; ++j) {
+    double best = key[0];
+#pragma unroll
+    for (int i = 1; i < V; ++i) best = fmax(best, key[i]);
+    best = row_max<LPR>(best);
+    const bool on = best > none;
+    if (!__any(on)) break;
+    int e = 1 << 20;
+#pragma unroll
+    for (int i = V - 1; i >= 0; --i)
+      if (key[i] == best) e = first + i;
+    e = row_min<LPR>(e);
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (first + i == e) key[i] = none;
+    if (on && store && lane == 0) sm.index[row][j] = e;
+  }
+  __builtin_amdgcn_wave_barrier();
+}
+
+// The choice in FP32. Each lane sorts its keys; a round takes the largest head of the row's
+// lanes, of equal ones the first lane's, which holds the lower indices. True: a decision was
+// nearer than its error.
+//
+// Error of a score: the exponential is off by its argument's rounding, 2^-24 of |x - top| or
+// |x|, and a few units, the sum over experts by V + 6 more: ((D + 40) M) 2^-24 with D the row's
+// largest such argument and M = 1 / sum (or 1) the largest score there can be; s + b adds half a unit
+// of itself. Two keys may differ by twice that, two groups' totals by four times.
+template <int LPR, int V>
+__device__ __forceinline__ bool choose_fast(const ChooseArgs& a, const float (&x)[V], const float (&b)[V], bool biased, float top,
+                                            int lane, int row, bool& bad, ChooseLds<LPR, V>& sm) {
+  const float none = -__builtin_inff();
+  constexpr float kLog2e = 1.44269502162933349609375f;
+  int key[V];
+  float tol = 0.f;
+  bool near_tie = false;
+  if (!biased)
+#pragma unroll
+    for (int i = 0; i < V; ++i) key[i] = key_of(x[i] + 0.f);
+  if (biased || a.groups > 1) {   // (otherwise the logits decide, exactly)
+    float s[V], sum = 0.f;
+    int arg = 0;   // of values that are not negative, in the order of their bits
+#pragma unroll
+    for (int i = 0; i < V; ++i) {   // (masked: the argument is infinite, s 0)
+      const float d = a.sigmoid ? -x[i] : x[i] - top;
+      const float e = __builtin_amdgcn_exp2f(d * kLog2e);
+      s[i] = a.sigmoid ? __builtin_amdgcn_rcpf(1.f + e) : e;
+      sum += s[i];
+      arg = max(arg, __float_as_int(fabsf(d)));
+    }
+    float unit = 1.f;
+    if (!a.sigmoid) unit = __builtin_amdgcn_rcpf(row_sum<LPR>(sum));
+    int scored[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const float c = __builtin_fmaf(s[i], unit, b[i]);
+      const bool on = x[i] > none;
+      bad |= on && c != c;
+      scored[i] = key_of(on ? c : none);
+    }
+    tol = (fminf(__int_as_float(row_max<LPR>(arg)), 100.f) + 40.f) * unit * 1.1920929e-7f + 1e-36f;
+    if (a.groups > 1) near_tie = take_groups<int, LPR, V>(a, scored, 2 * tol, lane, row, sm);
+#pragma unroll
+    for (int i = 0; i < V; ++i)   // (without a bias the logits decide within the groups)
+      key[i] = biased ? scored[i] : (scored[i] > kNoKey ? key[i] : kNoKey);
+  }
+  int index[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) index[i] = lane * V + i;
+#pragma unroll
+  for (int i = 0; i < V; ++i)   // neighbours change places only if the second is larger: equal ones keep their order
+#pragma unroll
+    for (int j = i & 1; j + 1 < V; j += 2) {
+      const int k0 = key[j], k1 = key[j + 1], i0 = index[j], i1 = index[j + 1];
+      const bool swap = k1 > k0;
+      key[j] = max(k0, k1), key[j + 1] = min(k0, k1);
+      index[j] = swap ? i1 : i0, index[j + 1] = swap ? i0 : i1;
+    }
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    sm.sorted.key[256 * i + threadIdx.x] = key[i];
+    sm.sorted.index[256 * i + threadIdx.x] = index[i];
+  }
+  sm.sorted.key[256 * V + threadIdx.x] = kNoKey;
+  for (int j = lane; j < a.k; j += LPR) sm.index[row][j] = -1;
+  __builtin_amdgcn_wave_barrier();
+  int head = key[0], expert = index[0], at = threadIdx.x;
+  float before = __builtin_inff();
+  // the row's lanes below this one
+  const unsigned long long below = ((1ull << lane) - 1) << (threadIdx.x & 63 & ~(LPR - 1));
+  const int rounds = biased ? a.k + 1 : a.k;   // (one more, to see how near the next one came)
+  for (int j = 0; j < rounds; ++j) {
+    const int best = row_max<LPR>(head);
+    const bool has = head == best && best > kNoKey;
+    const unsigned long long m = __ballot(has);
+    if (!m) break;
+    if (biased) {
+      const float v = value_of(best);
+      near_tie |= best > kNoKey && before - v <= __builtin_fmaf(fabsf(v), 2.3841858e-7f, tol);
+      before = v;
+    }
+    if (has && !(m & below)) {
+      if (j < a.k) sm.index[row][j] = expert;
+      at += 256;
+      head = sm.sorted.key[at];
+      expert = sm.sorted.index[at];
+    }
+  }
+  __builtin_amdgcn_wave_barrier();
+  return row_any<LPR>(near_tie);
+}
+
+// LPR lanes per token, V consecutive experts each. Scores in FP32; the few rows where a
+// decision lies within their error are decided again in FP64.
+template <class T, int LPR, int V>
 __global__ void __launch_bounds__(256)
 choose_kernel(ChooseArgs a, const T* __restrict__ logits, const float* __restrict__ bias, int* __restrict__ expert,
               float* __restrict__ weights) {
-  __shared__ double sm[4][kMaxScored];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int64_t t = (int64_t)block_id() * 4 + w;
-  if (t >= a.n) return;
-  const double none = -__builtin_inf();
-  double l[kPerLane], key[kPerLane];
-  double top = none, sum = 0;
+  using S = ChooseShape<LPR, V>;
+  __shared__ ChooseLds<LPR, V> sm;
+  const int lane = threadIdx.x % LPR, row = threadIdx.x / LPR;
+  const int64_t t = (int64_t)block_id() * S::ROWS + row;
+  if (t - row >= a.n) return;   // (a grid's last row of blocks is full)
+  const bool live = t < a.n;   // (a wave's other rows go on)
+  const int64_t at = live ? t : 0;
+  const float none = -__builtin_inff();
+  float x[V], b[V];
+  load_row<V>(logits + at * a.ld, lane * V, a.E, none, x);
+#pragma unroll
+  for (int i = 0; i < V; ++i) b[i] = 0.f;
+  if (bias) load_row<V>(bias, lane * V, a.E, 0.f, b);
   bool bad = false;
+  const float largest = a.sigmoid ? __builtin_inff() : 3.4028234663852886e38f;
 #pragma unroll
-  for (int i = 0; i < kPerLane; ++i) {
-    const int e = lane + 64 * i;
-    l[i] = none;
-    if (e < a.E) {
-      const float x = to_f32(logits[t * a.ld + e]);
-      bad |= x != x || (!a.sigmoid && x == __builtin_inff());
-      if (x > lowest<T>()) l[i] = x;
-    }
-    top = fmax(top, l[i]);
+  for (int i = 0; i < V; ++i) {
+    bad |= !(x[i] <= largest);
+    x[i] = x[i] > lowest<T>() ? x[i] : none;
   }
+  float top = none;
+  if (!a.sigmoid) {
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) top = fmax(top, __shfl_xor(top, d));
-  double norm = 0;   // log of the softmax's denominator
-  if (!a.sigmoid && top > none) {
-#pragma unroll
-    for (int i = 0; i < kPerLane; ++i) sum += l[i] > none ? exp(l[i] - top) : 0.;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
-    norm = top + log(sum);
+    for (int i = 0; i < V; ++i) top = fmaxf(top, x[i]);
+    top = row_max<LPR>(top);
   }
-  // scores
+  const bool again = choose_fast<LPR, V>(a, x, b, bias != nullptr, top, lane, row, bad, sm);
+  if (__any(again)) choose_exact<T, LPR, V>(a, logits + at * a.ld, bias, top, lane, row, again, sm);
+  bad = row_any<LPR>(bad);
+  float norm = 0.f;   // sum of exp(x - top) of the softmax
+  if (!a.sigmoid && !a.normalise) {
 #pragma unroll
-  for (int i = 0; i < kPerLane; ++i) {
-    const int e = lane + 64 * i;
-    double c = none;
-    if (l[i] > none) {
-      const double s = a.sigmoid ? 1 / (1 + exp(-l[i])) : exp(l[i] - top) / sum;
-      c = s + (bias ? (double)bias[e] : 0.);
-      bad |= c != c;
-    }
-    key[i] = c;
-    if (e < a.E) sm[w][e] = c;
+    for (int i = 0; i < V; ++i) norm += x[i] > none ? exp_minus(top - x[i]) : 0.f;
+    norm = row_sum<LPR>(norm);
   }
-  __builtin_amdgcn_wave_barrier();
-  const bool no_order = __any(bad);
-  if (a.groups > 1) {
-    double total = none;   // lane g: group g
-    if (lane < a.groups) {
-      double c1 = none, c2 = none;
-      for (int j = 0; j < a.per; ++j) {
-        const double c = sm[w][lane * a.per + j];
-        if (c > c1) c2 = c1, c1 = c;
-        else if (c > c2) c2 = c;
-      }
-      total = c2 > none ? c1 + c2 : c1;
-    }
-    unsigned long long taken = 0;
-    for (int j = 0; j < a.top_groups; ++j) {
-      double v = total;
-      int g = lane;
-      wave_best(v, g);
-      if (!(v > none)) break;
-      taken |= 1ull << g;
-      if (lane == g) total = none;
-    }
+  constexpr int P = (S::K + LPR - 1) / LPR;
+  float v[P], most = none, total = 0.f;
 #pragma unroll
-    for (int i = 0; i < kPerLane; ++i)
-      if (!(taken >> ((lane + 64 * i) / a.per) & 1)) key[i] = none;
+  for (int p = 0; p < P; ++p) {
+    if (p * LPR >= a.k) break;
+    const int j = lane + p * LPR, e = j < a.k ? sm.index[row][j] : -1;
+    v[p] = none;
+    if (e >= 0) v[p] = to_f32(logits[at * a.ld + e]);
+    most = fmaxf(most, v[p]);
   }
-  if (!bias) {
+  most = row_max<LPR>(most);
+  if (a.sigmoid) most = fminf(most, 0.f);
 #pragma unroll
-    for (int i = 0; i < kPerLane; ++i)
-      if (key[i] > none) key[i] = l[i];
+  for (int p = 0; p < P; ++p) {
+    if (p * LPR >= a.k) break;
+    if (!(v[p] > none)) v[p] = 0.f;
+    else if (a.normalise) v[p] = relative_score(v[p], most, a.sigmoid);
+    else v[p] = a.sigmoid ? sigmoid_of(v[p]) : exp_minus(top - v[p]) / norm;
+    total += v[p];
   }
-  // lane j keeps choice j
-  int chosen = -1;
-  double log_score = none;
-  for (int j = 0; j < a.k; ++j) {
-    double v = none;
-    int e = 1 << 20;
+  total = a.normalise ? row_sum<LPR>(total) : 1.f;
+  if (!live) return;
 #pragma unroll
-    for (int i = 0; i < kPerLane; ++i)
-      if (key[i] > v) v = key[i], e = lane + 64 * i;
-    wave_best(v, e);
-    if (!(v > none)) break;
-    double mine = 0;
-#pragma unroll
-    for (int i = 0; i < kPerLane; ++i)
-      if (e == lane + 64 * i) key[i] = none, mine = l[i];
-    mine = __shfl(mine, e & 63);
-    if (lane == j) {
-      chosen = e;
-      log_score = a.sigmoid ? log_sigmoid(mine) : mine - norm;
-    }
-  }
-  double value = chosen >= 0 ? exp(log_score) : 0.;
-  if (a.normalise) {
-    double m = log_score;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) m = fmax(m, __shfl_xor(m, d));
-    value = chosen >= 0 ? exp(log_score - m) : 0.;
-    double total = value;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) total += __shfl_xor(total, d);
-    if (chosen >= 0) value /= total;
-  }
-  if (lane < a.k) {
-    expert[t * a.k + lane] = no_order ? lane : chosen;
-    weights[t * a.k + lane] = no_order ? __builtin_nanf("") : (float)(a.scale * value);
+  for (int p = 0; p < P; ++p) {
+    const int j = lane + p * LPR;
+    if (j >= a.k) break;
+    const int e = sm.index[row][j];
+    expert[t * a.k + j] = bad ? j : e;
+    weights[t * a.k + j] = bad ? __builtin_nanf("") : (e >= 0 ? a.scale * (v[p] / total) : 0.f);
   }
 }
 
-// A wave per token. v_j are the (renormalised) scores, g_j the weights' gradients:
-// renormalised dlogit_j = scale v_j (g_j - sum g v), times 1 - s_j for a sigmoid;
-// otherwise scale s_j g_j, times 1 - s_j or less scale s_e sum g s for every expert e.
-template <class T>
+// ------------------------------------------------------------------ gradient
+template <int LPR, int V>
+struct ChooseGradLds {
+  using S = ChooseShape<LPR, V>;
+  float d[S::ROWS][LPR * V];
+  int place[S::ROWS][LPR * V];
+};
+
+// v_j are the (renormalised) scores, g_j the weights' gradients: renormalised
+// dlogit_j = scale v_j (g_j - sum g v), times 1 - s_j for a sigmoid; otherwise scale s_j
+// g_j, times 1 - s_j or less scale s_e sum g s for every expert e. The chosen experts' values are
+// scattered through LDS; only a softmax that is not renormalised reads all logits.
+template <class T, int LPR, int V>
 __global__ void __launch_bounds__(256)
 choose_bwd_kernel(ChooseArgs a, const float* __restrict__ dweights, const T* __restrict__ logits,
                   const int* __restrict__ expert, T* __restrict__ dlogits, int64_t ld_d) {
-  const int lane = threadIdx.x & 63;
-  const int64_t t = (int64_t)block_id() * 4 + (threadIdx.x >> 6);
-  if (t >= a.n) return;
+  using S = ChooseShape<LPR, V>;
+  __shared__ ChooseGradLds<LPR, V> sm;
+  const int lane = threadIdx.x % LPR, row = threadIdx.x / LPR, first = lane * V;
+  const int64_t t = (int64_t)block_id() * S::ROWS + row;
+  if (t - row >= a.n) return;   // (a grid's last row of blocks is full)
+  const bool live = t < a.n;
+  const int64_t at = live ? t : 0;
   const float none = -__builtin_inff();
-  float l[kPerLane], top = none, sum = 0.f;
   const bool dense = !a.sigmoid && !a.normalise;
+  float x[V], top = none, norm = 0.f;
+  if (dense) {
+    load_row<V>(logits + at * a.ld, first, a.E, none, x);
 #pragma unroll
-  for (int i = 0; i < kPerLane; ++i) {
-    const int e = lane + 64 * i;
-    l[i] = e < a.E ? to_f32(logits[t * a.ld + e]) : none;
-    if (l[i] <= lowest<T>()) l[i] = none;
-    top = fmaxf(top, l[i]);
-  }
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-  if (!(top > none)) top = 0.f;
-#pragma unroll
-  for (int i = 0; i < kPerLane; ++i) sum += expf(l[i] - top);   // (-infinity: 0; NaN goes on)
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
-  // lane j: choice j
-  int e = -1;
-  float x = none, g = 0.f;
-  if (lane < a.k) {
-    e = expert[t * a.k + lane];
-    if (e < 0 || e >= a.E) e = -1;
-    if (e >= 0) {
-      x = to_f32(logits[t * a.ld + e]);
-      g = dweights[t * a.k + lane];
+    for (int i = 0; i < V; ++i) {
+      if (x[i] <= lowest<T>()) x[i] = none;   // (NaN stays)
+      top = fmaxf(top, x[i]);
     }
+    top = row_max<LPR>(top);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      x[i] = x[i] == none ? 0.f : exp_minus(top - x[i]);
+      norm += x[i];
+    }
+    norm = row_sum<LPR>(norm);
   }
-  float s = e < 0 ? 0.f : (a.sigmoid ? 1.f / (1.f + expf(-x)) : expf(x - top) / sum), v = s;
-  if (a.normalise) {
-    const float ls = e < 0 ? none : (a.sigmoid ? fminf(x, 0.f) - log1pf(expf(-fabsf(x))) : x);
-    float m = ls;
+  constexpr int P = (S::K + LPR - 1) / LPR;
+  int e[P];
+  float g[P], v[P], l[P], most = none, total = 0.f, inner = 0.f;
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
-    v = e < 0 ? 0.f : expf(ls - m);
-    float total = v;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) total += __shfl_xor(total, d);
-    if (e >= 0) v /= total;
+  for (int p = 0; p < P; ++p) {
+    const int j = lane + p * LPR;
+    e[p] = j < a.k ? expert[at * a.k + j] : -1;
+    if (e[p] >= a.E) e[p] = -1;
+    g[p] = e[p] >= 0 ? dweights[at * a.k + j] : 0.f;
+    l[p] = e[p] >= 0 ? to_f32(logits[at * a.ld + e[p]]) : none;
+    most = fmaxf(most, l[p]);
   }
-  float inner = g * v;
+  most = row_max<LPR>(most);
+  if (a.sigmoid) most = fminf(most, 0.f);
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) inner += __shfl_xor(inner, d);
-  float mine = a.normalise ? v * (g - inner) : v * g;
-  if (a.sigmoid) mine *= 1.f / (1.f + expf(x));
-  if (e < 0) mine = 0.f;
-  float out[kPerLane] = {};
-  for (int j = 0; j < a.k; ++j) {
-    const int ej = __shfl(e, j);
-    const float dj = __shfl(mine, j);
-#pragma unroll
-    for (int i = 0; i < kPerLane; ++i)
-      if (ej == lane + 64 * i) out[i] += dj;
+  for (int p = 0; p < P; ++p) {
+    v[p] = 0.f;
+    if (p * LPR >= a.k) continue;
+    if (e[p] >= 0) {
+      if (a.normalise) v[p] = relative_score(l[p], most, a.sigmoid);
+      else v[p] = a.sigmoid ? sigmoid_of(l[p]) : (l[p] <= lowest<T>() ? 0.f : exp_minus(top - l[p]) / norm);
+    }
+    total += v[p];
   }
+  total = a.normalise ? row_sum<LPR>(total) : 1.f;
 #pragma unroll
-  for (int i = 0; i < kPerLane; ++i) {
-    if (dense && l[i] > none) out[i] -= expf(l[i] - top) / sum * inner;
-    if (lane + 64 * i < a.E) dlogits[t * ld_d + lane + 64 * i] = (T)(a.scale * out[i]);
+  for (int p = 0; p < P; ++p) {
+    if (e[p] >= 0) v[p] /= total;
+    inner += g[p] * v[p];
+  }
+  inner = row_sum<LPR>(inner);
+#pragma unroll
+  for (int i = 0; i < V; ++i) sm.d[row][first + i] = 0.f;
+  __builtin_amdgcn_wave_barrier();
+  // an expert named twice gets both terms, in their order: seen by whose mark stayed
+  bool twice = false;
+#pragma unroll
+  for (int p = 0; p < P; ++p)
+    if (e[p] >= 0) sm.place[row][e[p]] = lane + p * LPR;
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    if (e[p] >= 0) twice |= sm.place[row][e[p]] != lane + p * LPR;
+    v[p] *= a.normalise ? g[p] - inner : g[p];
+    if (a.sigmoid && e[p] >= 0) v[p] *= sigmoid_of(-l[p]);
+  }
+  if (!__any(twice)) {
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+      if (e[p] >= 0) sm.d[row][e[p]] = v[p];
+  } else {
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+      for (int j = 0; j < LPR; ++j) {
+        if (lane == j && e[p] >= 0) sm.d[row][e[p]] += v[p];
+        __builtin_amdgcn_wave_barrier();
+      }
+  }
+  __builtin_amdgcn_wave_barrier();
+  if (!live || first >= a.E) return;
+  typedef T tv __attribute__((ext_vector_type(V)));
+  tv out;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    float d = sm.d[row][first + i];
+    if (dense && x[i] != 0.f) d -= x[i] / norm * inner;
+    out[i] = (T)(a.scale * d);
+  }
+  T* q = dlogits + t * ld_d + first;
+  if (first + V <= a.E) {
+    __builtin_memcpy(q, &out, sizeof(out));
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (first + i < a.E) q[i] = out[i];
   }
 }
 
@@ -236,9 +564,19 @@ mace_status check(const mace_choose_desc* d) {
   if (d->n_tokens > (1 << 30) || d->n_tokens * d->top_k > (1 << 30)) return MACE_EUNSUPPORTED;
   return MACE_OK;
 }
-ChooseArgs args_of(const mace_choose_desc& d) {
-  return {d.n_tokens, d.ld_logits, d.n_experts, d.top_k, d.n_groups, d.top_groups, d.n_experts / d.n_groups,
-          d.scores == MACE_SCORES_SIGMOID, d.normalise, (float)d.scale};
+// lanes per token and experts per lane
+template <class F>
+mace_status with_row(int E, F f) {
+  if (E <= 16) return f(Int<4>{}, Int<4>{});
+  if (E <= 64) return f(Int<16>{}, Int<4>{});
+  if (E <= 128) return f(Int<16>{}, Int<8>{});
+  if (E <= 256) return f(Int<32>{}, Int<8>{});
+  return f(Int<64>{}, Int<8>{});
+}
+ChooseArgs args_of(const mace_choose_desc& d, int v) {
+  const int per = d.n_experts / d.n_groups, lanes = per % v ? 0 : per / v;
+  return {d.n_tokens, d.ld_logits, d.n_experts, d.top_k, d.n_groups, d.top_groups, per, ((1 << 20) + per - 1) / per,
+          lanes & (lanes - 1) ? 0 : lanes, d.scores == MACE_SCORES_SIGMOID, d.normalise, (float)d.scale};
 }
 
 }  // namespace
@@ -254,9 +592,13 @@ extern "C" mace_status mace_choose_forward(const mace_choose_desc* desc, const v
   if (!logits || !expert || !weights) return MACE_EINVAL;
   return by_type(desc->dtype, [&](auto zero) -> mace_status {
     using T = decltype(zero);
-    const ChooseArgs a = args_of(*desc);
-    choose_kernel<T><<<grid_of((a.n + 3) / 4), 256, 0, (hipStream_t)stream>>>(a, (const T*)logits, bias, expert, weights);
-    return launched();
+    return with_row(desc->n_experts, [&](auto lpr, auto v) {
+      constexpr int LPR = decltype(lpr)::value, V = decltype(v)::value, rows = ChooseShape<LPR, V>::ROWS;
+      const ChooseArgs a = args_of(*desc, V);
+      choose_kernel<T, LPR, V><<<grid_of((a.n + rows - 1) / rows), 256, 0, (hipStream_t)stream>>>(a, (const T*)logits, bias,
+                                                                                                 expert, weights);
+      return launched();
+    });
   });
 }
 
@@ -269,9 +611,12 @@ extern "C" mace_status mace_choose_backward(const mace_choose_desc* desc, const 
   if (!dweights || !logits || !expert || !dlogits) return MACE_EINVAL;
   return by_type(desc->dtype, [&](auto zero) -> mace_status {
     using T = decltype(zero);
-    const ChooseArgs a = args_of(*desc);
-    choose_bwd_kernel<T><<<grid_of((a.n + 3) / 4), 256, 0, (hipStream_t)stream>>>(a, dweights, (const T*)logits, expert,
-                                                                                 (T*)dlogits, ld_dlogits);
-    return launched();
+    return with_row(desc->n_experts, [&](auto lpr, auto v) {
+      constexpr int LPR = decltype(lpr)::value, V = decltype(v)::value, rows = ChooseShape<LPR, V>::ROWS;
+      const ChooseArgs a = args_of(*desc, V);
+      choose_bwd_kernel<T, LPR, V><<<grid_of((a.n + rows - 1) / rows), 256, 0, (hipStream_t)stream>>>(
+          a, dweights, (const T*)logits, expert, (T*)dlogits, ld_dlogits);
+      return launched();
+    });
   });
 }
