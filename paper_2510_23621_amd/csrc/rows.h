@@ -37,15 +37,16 @@ __device__ __forceinline__ void store_vec(T* p, const RowVec<T>& r, int n) {
   }
 }
 
-// Item block_id() * 256 + threadIdx.x as (row, vector) of rows of nv vectors, with
+// Item block * 256 + threadIdx.x as (row, vector) of rows of nv vectors, with
 // one division of 64 bits per block.
-__device__ __forceinline__ int64_t item_row(int nv, int& vec) {
-  const uint64_t i0 = (uint64_t)block_id() * 256;
+__device__ __forceinline__ int64_t item_row(int nv, int& vec, int block) {
+  const uint64_t i0 = (uint64_t)block * 256;
   const uint64_t q0 = i0 >> 32 ? i0 / (unsigned)nv : (unsigned)i0 / (unsigned)nv;
   const unsigned j = (unsigned)(i0 - q0 * (unsigned)nv) + threadIdx.x, q = j / (unsigned)nv;
   vec = (int)(j - q * (unsigned)nv);
   return (int64_t)(q0 + q);
 }
+__device__ __forceinline__ int64_t item_row(int nv, int& vec) { return item_row(nv, vec, block_id()); }
 
 inline mace_status launched() { return hipGetLastError() == hipSuccess ? MACE_OK : MACE_EHIP; }
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }

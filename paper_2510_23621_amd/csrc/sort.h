@@ -11,7 +11,7 @@ namespace mace {
 constexpr int kSortBuckets = 512;   // besides the one behind them (the counters fit 64 KB of LDS)
 constexpr int kSortWaves = 16;
 constexpr int kSortThreads = 64 * kSortWaves;
-constexpr int kSortChunk = 4096;   // slots a block sorts at a time
+constexpr int kSortChunkMost = 4096;   // slots a block sorts at a time, at most
 constexpr int kSortBlocks = 512;   // most blocks: each reads every block's counts
 
 // What is sorted: bucket(s) of slot s, 0 .. E, and place(s, row), which stores that
@@ -38,7 +38,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(Slots sl, int6
 // the sort one launch (96 slots 3.5 us, bound by the launch); 294,912 slots of 64
 // experts 14 us with the counting launch, 2^26 of 64 experts 470 us.
 // offsets [E + 1], or NULL: the first row of each bucket.
-template <class Slots>
+template <class Slots, int kSortChunk>
 __global__ void __launch_bounds__(kSortThreads)
 sort_kernel(Slots sl, int64_t slots, int64_t span, int E, int bits, const int* __restrict__ hist, int* __restrict__ offsets) {
   extern __shared__ int sm[];
@@ -139,22 +139,25 @@ sort_kernel(Slots sl, int64_t slots, int64_t span, int E, int bits, const int* _
 }
 
 // The launches. hist: sort_blocks(slots) * (E + 1) ints where that is more than one block.
-inline int64_t sort_chunks(int64_t slots) { return (slots + kSortChunk - 1) / kSortChunk; }
-inline int64_t sort_blocks(int64_t slots) {
-  const int64_t each = std::max<int64_t>(1, (sort_chunks(slots) + kSortBlocks - 1) / kSortBlocks);   // chunks per block
-  return std::max<int64_t>(1, (sort_chunks(slots) + each - 1) / each);
+template <int kSortChunk = kSortChunkMost>
+int64_t sort_chunks(int64_t slots) { return (slots + kSortChunk - 1) / kSortChunk; }
+template <int kSortChunk = kSortChunkMost>
+int64_t sort_blocks(int64_t slots) {
+  const int64_t chunks = sort_chunks<kSortChunk>(slots);
+  const int64_t each = std::max<int64_t>(1, (chunks + kSortBlocks - 1) / kSortBlocks);   // chunks per block
+  return std::max<int64_t>(1, (chunks + each - 1) / each);
 }
-template <class Slots>
+template <int kSortChunk = kSortChunkMost, class Slots>
 mace_status sort_slots(const Slots& sl, int64_t slots, int E, int* hist, int* offsets, hipStream_t s) {
-  const int64_t each = std::max<int64_t>(1, (sort_chunks(slots) + kSortBlocks - 1) / kSortBlocks);
-  const int64_t blocks = sort_blocks(slots), span = each * kSortChunk;
+  const int64_t each = std::max<int64_t>(1, (sort_chunks<kSortChunk>(slots) + kSortBlocks - 1) / kSortBlocks);
+  const int64_t blocks = sort_blocks<kSortChunk>(slots), span = each * kSortChunk;
   int bits = 1;
   while ((1 << bits) <= E) ++bits;
   if (blocks > 1) {
     sort_count_kernel<<<(unsigned)blocks, kSortThreads, 0, s>>>(sl, slots, span, E, hist);
     if (hipGetLastError() != hipSuccess) return MACE_EHIP;
   }
-  sort_kernel<<<(unsigned)blocks, kSortThreads, (kSortWaves + 2) * (E + 1) * sizeof(int), s>>>(sl, slots, span, E, bits, hist,
+  sort_kernel<Slots, kSortChunk><<<(unsigned)blocks, kSortThreads, (kSortWaves + 2) * (E + 1) * sizeof(int), s>>>(sl, slots, span, E, bits, hist,
                                                                                               offsets);
   return hipGetLastError() == hipSuccess ? MACE_OK : MACE_EHIP;
 }
