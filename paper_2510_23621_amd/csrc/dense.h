@@ -127,10 +127,9 @@ __device__ __forceinline__ void store_n(T* p, V v, int n, bool vec) {
   }
 }
 template <int W, class T>
-__device__ __forceinline__ typename Floats<W>::type read_n(const T* p, int n, bool vec) {
+__device__ __forceinline__ auto read_raw(const T* p, int n, bool vec) {   // as the elements are
   typedef T tw __attribute__((ext_vector_type(W)));
-  using V = typename Floats<W>::type;
-  if (vec) return __builtin_convertvector(*reinterpret_cast<const tw*>(p), V);
+  if (vec) return *reinterpret_cast<const tw*>(p);
   tw o = {};
   if (n >= W) {
     __builtin_memcpy(&o, p, sizeof(o));
@@ -139,7 +138,11 @@ __device__ __forceinline__ typename Floats<W>::type read_n(const T* p, int n, bo
     for (int i = 0; i < W - 1; ++i)
       if (i < n) o[i] = p[i];
   }
-  return __builtin_convertvector(o, V);
+  return o;
+}
+template <int W, class T>
+__device__ __forceinline__ typename Floats<W>::type read_n(const T* p, int n, bool vec) {
+  return __builtin_convertvector(read_raw<W>(p, n, vec), typename Floats<W>::type);
 }
 
 // ------------------------------------------------------------------ LDS tiles

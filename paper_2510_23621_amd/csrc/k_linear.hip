@@ -164,7 +164,7 @@ __global__ void __launch_bounds__(S::NT) linear_fwd_kernel(LinearArgs<T> a) {
   product<T, S, true, false, AL>({x, a.ldx, run.rows, 0, a.x + (a.n - 1) * a.ldx + a.n_in},
                                  {w, a.n_out, a.n_out - c0, 0, a.w + (int64_t)a.groups * a.n_in * a.n_out}, a.n_in, lds,
                                  tid, acc);
-  linear_epilogue<T, AL, S>(a, run, c0, cols, y, z, tid, [&](int j, int i) { return lane_values<lane_width<T>>(acc, j, i); });
+  linear_epilogue<T, AL, S>(a, run, c0, cols, y, z, tid, [&](int j, int i, auto b) { return lane_values<lane_width<T>>(acc, j, i) + b; });
 }
 
 template <bool AL, class S>

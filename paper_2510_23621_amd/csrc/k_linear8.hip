@@ -50,12 +50,146 @@ __global__ void __launch_bounds__(S::NT) linear8_kernel(Linear8Args<T> p) {
     ws[j] = V{};
     if (n < cols) ws[j] = read_n<W>(p.ws + w_row + n, min(W, cols - n), false);
   }
-  linear_epilogue<T, AL, S>(a, run, c0, cols, y, (T*)nullptr, tid, [&](int j, int i) {
+  linear_epilogue<T, AL, S, sizeof(T) == 2 ? 4 : 2, sizeof(T) == 2>(a, run, c0, cols, y, (T*)nullptr, tid, [&](int j, int i, V b) {
     V v = lane_values<W>(acc, j, i);
 #pragma unroll
-    for (int q = 0; q < W; ++q) v[q] = (float)__float_as_int(v[q]) * xs[i] * ws[j][q];
+    for (int q = 0; q < W; ++q) v[q] = __builtin_fmaf((float)__float_as_int(v[q]) * xs[i], ws[j][q], b[q]);
     return v;
   });
+}
+
+// Few rows: a block of four waves forms 16 x 16 results, each wave a quarter of K, added through LDS.
+// The rows lie in LDS as integers over all of K; where they come as T the block rounds them itself
+// (no launch and no way through memory for them). The weights go straight to the matrix
+// instructions, requested before the rows. One row of 2048 bfloat16 on 2048 x 2048: 6.9 us, of
+// which the weights' 4 MB take 0.8 at a copy's rate; the rest is the launch and three dependent trips to memory.
+constexpr int kThinRows = 16, kThinCols = 16, kThinLds = 56 << 10;
+// bytes from row to row: 16 more than a multiple of 128, so that eight rows' 16 bytes lie in all banks
+int thin_pitch(int n_in) { return (n_in + 127) / 128 * 128 + 16; }
+int thin_lds(int n_in) { return kThinRows * thin_pitch(n_in); }
+
+template <class T, bool AL, bool PACKED>
+__global__ void __launch_bounds__(256) linear8_thin_kernel(Linear8Args<T> p, int n_in, int pitch) {
+  extern __shared__ __align__(16) int8_t rows8[];
+  __shared__ float scale[kThinRows];
+  __shared__ unsigned red[4];
+  __shared__ i4 part[4 * 64];
+  const LinearArgs<T>& a = p.a;
+  const int tid = threadIdx.x, l = tid & 63, wv = tid >> 6, i = l & 15, g = l >> 4;
+  const int tiles_n = (a.n_out + kThinCols - 1) / kThinCols;
+  const int id = block_id();
+  const int c0 = id % tiles_n * kThinCols, cols = min(kThinCols, a.n_out - c0);
+  RowRun run;
+  if (!find_run(a.offsets, a.groups, a.n, kThinRows, id / tiles_n, run)) return;
+  T* y = a.y + run.row0 * a.ldy + c0;
+  if (run.group >= a.groups) {
+    zero_rows(y, a.ldy, run.rows, cols, tid, 256);
+    return;
+  }
+  const int k16 = (n_in + 15) / 16 * 16;
+  const int64_t w_row = (int64_t)run.group * a.n_out + c0;
+  const int8_t* w = reinterpret_cast<const int8_t*>(a.w) + (w_row + min(i, cols - 1)) * 2 * p.ldw + 16 * g;
+  constexpr int U = 8;   // steps of 64 products' indices in flight
+  i4 wr[U];
+  auto load_weights = [&](int k) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int at = k + 256 * u;
+      wr[u] = i4{0, 0, 0, 0};
+      if (at + 16 * g < k16) wr[u] = *reinterpret_cast<const i4*>(w + at);
+    }
+  };
+  load_weights(64 * wv);
+  // what the epilogue adds, requested before the rows too
+  const int n = 4 * g, count = min(4, cols - n);
+  typedef T t4 __attribute__((ext_vector_type(4)));
+  t4 res = {};
+  f4 ws = {0.f, 0.f, 0.f, 0.f}, bias = ws;
+  if (wv == 0 && count > 0) {
+    ws = read_n<4>(p.ws + w_row + n, count, false);
+    if (a.bias) bias = read_n<4>(a.bias + w_row + n, count, false);
+    if (a.residual && i < run.rows) res = read_raw<4>(a.residual + (run.row0 + i) * a.ldr + c0 + n, count, false);
+  }
+  // rows: tpr threads (a power of two) each, 16 columns at a time, zeros from k16 on
+  int tpr = 256 / kThinRows;
+  while (tpr < 256 && 256 / (2 * tpr) >= run.rows) tpr *= 2;
+  const int row = tid / tpr, t = tid & (tpr - 1), chunks = pitch / 16 - 1;
+  const int64_t r = run.row0 + min(row, run.rows - 1);
+  int8_t* mine = rows8 + row * pitch;
+  if constexpr (PACKED) {
+    const int8_t* x = reinterpret_cast<const int8_t*>(a.x) + r * 2 * a.ldx;
+    for (int c = t; c < chunks; c += tpr) {
+      i4 q = {0, 0, 0, 0};
+      if (16 * c < k16) q = *reinterpret_cast<const i4*>(x + 16 * c);
+      *reinterpret_cast<i4*>(mine + 16 * c) = q;
+    }
+    if (t == 0) scale[row] = p.xs[r];
+  } else {
+    const T* x = a.x + r * a.ldx;
+    constexpr int H = sizeof(T) == 2 ? 8 : 4;   // chunks requested at a time; the first ones stay in registers
+    Cols16<T> v[H];
+    auto load = [&](int c) {
+#pragma unroll
+      for (int h = 0; h < H; ++h)
+        if (16 * (c + h * tpr) < n_in) v[h] = load_cols16<T, AL>(x, c + h * tpr, n_in);
+    };
+    Magnitude<T> most;
+    for (int c = t + H * tpr * ((chunks - 1 - t) / (H * tpr)); c >= 0; c -= H * tpr) {   // (the first ones last)
+      load(c);
+#pragma unroll
+      for (int h = 0; h < H; ++h)
+        if (16 * (c + h * tpr) < n_in) most.add(v[h]);
+    }
+    unsigned m = most.bits();
+    for (int d = 1; d < min(tpr, 64); d <<= 1) m = max(m, (unsigned)__shfl_xor((int)m, d));
+    if (tpr > 64) {   // (of every thread or none)
+      if (l == 0) red[wv] = m;
+      __syncthreads();
+      for (int q = 0; q < tpr / 64; ++q) m = max(m, red[row * (tpr / 64) + q]);
+    }
+    const float s = scale8(Magnitude<T>::value(m)), inv = inverse8(s);
+    bool again = false;
+    for (int c = t; c < chunks; c += H * tpr) {
+      if (c > t) load(c);
+#pragma unroll
+      for (int h = 0; h < H; ++h)
+        if (c + h * tpr < chunks) {
+          i4 q = {0, 0, 0, 0};
+          if (16 * (c + h * tpr) < n_in) q = round_most16(v[h], s, inv, again);
+          *reinterpret_cast<i4*>(mine + 16 * (c + h * tpr)) = q;
+        }
+    }
+    if (again)   // (apart, and one chunk at a time: a block runs through this code once, and waits for its instructions)
+#pragma unroll 1
+      for (int c = t; 16 * c < n_in; c += tpr)
+        *reinterpret_cast<i4*>(mine + 16 * c) = round_cols16(load_cols16<T, AL>(x, c, n_in), s, inv);
+    if (t == 0) scale[row] = s;
+  }
+  __syncthreads();
+  // (rows past the run's are as LDS held them: integers, whose results are not stored)
+  i4 acc = {0, 0, 0, 0};
+  for (int k = 64 * wv; k < k16; k += 256 * U) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int at = k + 256 * u;
+      if (at < k16)
+        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(wr[u], *reinterpret_cast<const i4*>(rows8 + i * pitch + at + 16 * g), acc, 0, 0, 0);
+    }
+    if (k + 256 * U < k16) load_weights(k + 256 * U);
+  }
+  part[tid] = acc;
+  __syncthreads();
+  if (wv || count <= 0 || i >= run.rows) return;
+  acc = (part[l] + part[64 + l]) + (part[128 + l] + part[192 + l]);
+  f4 v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    v[e] = __builtin_fmaf((float)acc[e] * scale[i], ws[e], bias[e]);
+    v[e] = a.act == MACE_ACT_SILU ? activate_as<MACE_ACT_SILU, sizeof(T) == 2>(v[e])
+                                  : (a.act == MACE_ACT_GELU ? activate<MACE_ACT_GELU>(v[e]) : v[e]);
+  }
+  if (a.residual) v += __builtin_convertvector(res, f4);
+  store_n(y + i * a.ldy + n, v, count, false);
 }
 
 // ------------------------------------------------------------------ host
@@ -84,12 +218,32 @@ mace_status with_shape(int64_t rows, int64_t cols, int64_t groups, F f) {
   return f(Small{});
 }
 
+// The thin kernel up to two blocks per CU, where K fits LDS: rounding a block's rows again for every
+// 16 columns costs it more on larger launches. With rows in bfloat16 (the other way rounds them in a
+// launch of its own): 1 x 2048 x 2048 (128 blocks) 6.7 us against 11.4, 256 x 97 x 211 (224) 6.7
+// against 9.8, 64 x 512 x 2048 (512) 7.4 against 8.9, 128 x 512 x 2048 (1024) 13.2 against 8.9.
+constexpr int kThinBlocks = 512;
+bool thin(const mace_linear_desc& d) {
+  return thin_lds(d.n_in) <= kThinLds && ceil_div(d.n_rows, kThinRows) * ceil_div(d.n_out, kThinCols) <= kThinBlocks;
+}
+template <class T>
+mace_status forward_thin(const mace_linear_desc& d, const Linear8Args<T>& p, bool packed, hipStream_t s) {
+  const int64_t blocks = (ceil_div(d.n_rows, kThinRows) + (p.a.offsets ? d.n_groups : 0)) * ceil_div(d.n_out, kThinCols);
+  if (!fits_grid(blocks)) return MACE_EUNSUPPORTED;
+  const bool al = aligned16(p.a.x) && ((d.n_in | d.ld_x) & 15) == 0;
+  auto f = packed ? linear8_thin_kernel<T, true, true>
+                  : (al ? linear8_thin_kernel<T, true, false> : linear8_thin_kernel<T, false, false>);
+  f<<<grid_of(blocks), 256, thin_lds(d.n_in), s>>>(p, d.n_in, thin_pitch(d.n_in));
+  return launched();
+}
+
 template <class T>
 mace_status forward(const mace_linear_desc& d, const void* x8, int64_t ld_x8, const float* xs, const void* w8, int64_t ld_w,
                     const float* ws, const void* bias, const void* residual, const int* offsets, void* y, hipStream_t s) {
   const Linear8Args<T> p{{(const T*)x8, (const T*)w8, (const T*)bias, (const T*)residual, (T*)y, nullptr, offsets, d.n_rows,
-                          ld_x8 / 2, d.ld_y, d.ld_residual, d.ld_y, (int)padded(d.n_in) / 2, d.n_out, d.n_groups, d.act},
+                          xs ? ld_x8 / 2 : ld_x8, d.ld_y, d.ld_residual, d.ld_y, (int)padded(d.n_in) / 2, d.n_out, d.n_groups, d.act},
                          xs, ws, ld_w / 2};
+  if (thin(d)) return forward_thin<T>(d, p, xs != nullptr, s);
   const bool al = aligned16(bias) && aligned16(residual) && aligned16(y) &&
                   ((d.n_out | d.ld_y | (residual ? d.ld_residual : 0)) & 7) == 0;
   return with_shape(d.n_rows, d.n_out, d.n_groups, [&](auto shape) -> mace_status {
@@ -109,6 +263,7 @@ using namespace mace;
 
 extern "C" size_t mace_linear8_workspace_bytes(const mace_linear_desc* desc) {
   if (check(desc) != MACE_OK) return 0;
+  if (thin(*desc)) return 256;
   return 256 + round256(size_t(desc->n_rows) * padded(desc->n_in)) + round256(size_t(desc->n_rows) * sizeof(float));
 }
 
@@ -125,7 +280,7 @@ extern "C" mace_status mace_linear8_forward(const mace_linear_desc* desc, const 
   if (ld_w > kMaxPitch8 || (x_scales && d.ld_x > kMaxPitch8)) return MACE_EUNSUPPORTED;
   if (d.n_rows == 0) return MACE_OK;
   int64_t ld = d.ld_x;
-  if (!x_scales) {
+  if (!x_scales && !thin(d)) {
     if (!workspace) return MACE_EINVAL;
     if (workspace_bytes < mace_linear8_workspace_bytes(desc)) return MACE_ENOSPACE;
     char* ws = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(workspace) + 255) & ~uintptr_t(255));

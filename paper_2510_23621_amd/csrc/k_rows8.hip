@@ -15,58 +15,50 @@ struct Rows8Args {
   int lg;             // lanes per row
 };
 
-// NaN wins, whatever the order
-__device__ __forceinline__ float larger(float a, float b) { return a > b || a != a ? a : b; }
-
-// lg lanes (a power of two up to a block) a row: its largest magnitude, then its integers, 16 a lane.
-template <class T, bool AL>
+// lg lanes (a power of two up to a block) a row, 16 columns at a time: its largest magnitude, then its
+// integers. CH: chunks of columns that a lane holds between the two, 0: any number, read twice.
+template <class T, bool AL, int CH>
 __global__ void __launch_bounds__(256) pack_rows_kernel(Rows8Args a, const T* __restrict__ x, int8_t* __restrict__ values,
                                                         float* __restrict__ scales) {
-  __shared__ float red[4];
+  __shared__ unsigned red[4];
   const int tid = threadIdx.x, lane = tid & (a.lg - 1);
   const int64_t row = ((int64_t)block_id() * 256 + tid) / a.lg;
   const bool on = row < a.n;
   const T* p = x + (on ? row : 0) * a.ld_x;
-  auto load = [&](int c) {   // columns 16 c .. 16 c + 15, zeros past the last
-    Vec8<T> v[2];
+  Cols16<T> held[CH ? CH : 1];
+  Magnitude<T> most;
+  if constexpr (CH > 0) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) v[h] = load8_to<T, AL>(p + 16 * c + 8 * h, p + a.cols);
-    struct R { Vec8<T> v[2]; } r;
-    r.v[0] = v[0], r.v[1] = v[1];
-    return r;
-  };
-  float m = 0.f;
-  if (on)
-    for (int c = lane; c < a.chunks; c += a.lg) {
-      const auto r = load(c);
+    for (int h = 0; h < CH; ++h)
+      if (on && lane + h * a.lg < a.chunks) held[h] = load_cols16<T, AL>(p, lane + h * a.lg, a.cols);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) m = larger(m, fabsf(r.v[i >> 3].get(i & 7)));
-    }
-  for (int d = 1; d < min(a.lg, 64); d <<= 1) m = larger(m, __shfl_xor(m, d));
+    for (int h = 0; h < CH; ++h)
+      if (on && lane + h * a.lg < a.chunks) most.add(held[h]);
+  } else if (on) {
+    for (int c = lane; c < a.chunks; c += a.lg) most.add(load_cols16<T, AL>(p, c, a.cols));
+  }
+  unsigned m = most.bits();
+  for (int d = 1; d < min(a.lg, 64); d <<= 1) m = max(m, (unsigned)__shfl_xor((int)m, d));
   if (a.lg == 256) {   // (of every thread or none)
     if ((tid & 63) == 0) red[tid >> 6] = m;
     __syncthreads();
-    m = larger(larger(red[0], red[1]), larger(red[2], red[3]));
+    m = max(max(red[0], red[1]), max(red[2], red[3]));
   }
   if (!on) return;
-  const float s = scale8(m), inv = inverse8(s);
+  const float s = scale8(Magnitude<T>::value(m)), inv = inverse8(s);
   if (lane == 0) scales[row] = s;
-  for (int c = lane; c < a.chunks; c += a.lg) {
-    const auto r = load(c);
-    uint4 o;
-    unsigned* w = &o.x;
+  i4* out = reinterpret_cast<i4*>(values + row * a.ld_values);
+  if constexpr (CH > 0) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      unsigned b = 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int e = 4 * j + i;
-        const int q = s == s ? round8(r.v[e >> 3].get(e & 7), s, inv) : 0;
-        b |= (unsigned)(q & 255) << 8 * i;
+    for (int h = 0; h < CH; ++h)
+      if (lane + h * a.lg < a.chunks) {
+        bool again = false;
+        i4 q = round_most16(held[h], s, inv, again);
+        if (again) q = round_cols16(held[h], s, inv);
+        out[lane + h * a.lg] = q;
       }
-      w[j] = b;
-    }
-    *reinterpret_cast<uint4*>(values + row * a.ld_values + 16 * c) = o;
+  } else {
+    for (int c = lane; c < a.chunks; c += a.lg) out[c] = round_cols16(load_cols16<T, AL>(p, c, a.cols), s, inv);
   }
 }
 
@@ -91,20 +83,20 @@ __global__ void __launch_bounds__(256) unpack_rows_kernel(Rows8Args a, const int
 template <class T>
 __global__ void __launch_bounds__(256) pack_weights_kernel(const T* __restrict__ w, int n_in, int n_out, int64_t ld,
                                                            int8_t* __restrict__ values, float* __restrict__ scales) {
-  __shared__ float red[4][64];
+  __shared__ unsigned red[4][64];
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, tiles = (n_out + 63) / 64;
   const int64_t g = block_id() / tiles;
   const int col = block_id() % tiles * 64 + lane;
   const bool on = col < n_out;
   w += g * n_in * n_out + (on ? col : 0);
-  float m = 0.f;
+  unsigned m = 0;   // (magnitudes in the order of their bits: NaN above all)
   if (on)
-    for (int k = wv; k < n_in; k += 4) m = larger(m, fabsf(to_f32(w[(int64_t)k * n_out])));
+    for (int k = wv; k < n_in; k += 4) m = max(m, __float_as_uint(fabsf(to_f32(w[(int64_t)k * n_out]))));
   red[wv][lane] = m;
   __syncthreads();
-  m = larger(larger(red[0][lane], red[1][lane]), larger(red[2][lane], red[3][lane]));
+  m = max(max(red[0][lane], red[1][lane]), max(red[2][lane], red[3][lane]));
   if (!on) return;
-  const float s = scale8(m), inv = inverse8(s);
+  const float s = scale8(__uint_as_float(m)), inv = inverse8(s);
   if (wv == 0) scales[g * n_out + col] = s;
   values += (g * n_out + col) * ld;
   for (int64_t k0 = 16 * wv; k0 < n_in; k0 += 64) {
@@ -116,8 +108,8 @@ __global__ void __launch_bounds__(256) pack_weights_kernel(const T* __restrict__
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int64_t k = k0 + 4 * j + i;
-        const int q = k < n_in && s == s ? round8(to_f32(w[k * n_out]), s, inv) : 0;
-        b[j] |= (unsigned)(q & 255) << 8 * i;
+        const unsigned q = k < n_in && s == s ? round8(to_f32(w[k * n_out]), s, inv) : 0;
+        b[j] |= (q & 255) << 8 * i;
       }
     }
     *reinterpret_cast<uint4*>(values + k0) = o;
@@ -151,9 +143,14 @@ extern "C" mace_status mace_pack_rows(const mace_rows8_desc* desc, const void* x
     const int64_t blocks = ceil_div(d.n_rows, 256 / a.lg);
     if (!fits_grid(blocks)) return MACE_EUNSUPPORTED;
     const bool al = aligned16(x) && ((d.n_cols | d.ld_x) & 15) == 0;
-    auto f = al ? pack_rows_kernel<T, true> : pack_rows_kernel<T, false>;
-    f<<<grid_of(blocks), 256, 0, (hipStream_t)stream>>>(a, (const T*)x, (int8_t*)values, scales);
-    return launched();
+    auto run = [&](auto ch) {
+      constexpr int CH = decltype(ch)::value;
+      auto f = al ? pack_rows_kernel<T, true, CH> : pack_rows_kernel<T, false, CH>;
+      f<<<grid_of(blocks), 256, 0, (hipStream_t)stream>>>(a, (const T*)x, (int8_t*)values, scales);
+      return launched();
+    };
+    if (a.chunks <= a.lg) return run(Int<1>{});
+    return a.chunks <= 2 * a.lg ? run(Int<2>{}) : run(Int<0>{});
   });
 }
 

@@ -59,48 +59,63 @@ __device__ __forceinline__ void zero_rows(T* y, int64_t ld, int rows, int cols, 
   for (int i = tid; i < rows * cols; i += nt) y[(int64_t)(i / cols) * ld + i % cols] = (T)0.f;
 }
 
+// SiLU for results of 16 bits: v_exp_f32 and v_rcp_f32 as they are, off by at most 2^-24 |z| and
+// three units of FP32, in a third of activate's instructions (infinities: as there)
+__device__ __forceinline__ float silu16(float z) {
+  return z * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.44269502162933349609375f));
+}
+template <int ACT, bool FAST>
+__device__ __forceinline__ float activate_as(float z) {
+  if constexpr (FAST && ACT == MACE_ACT_SILU) return silu16(z);
+  return activate<ACT>(z);
+}
+
 // The epilogue of a block's product: y = act(value + b) + r, z = value + b where it is
 // wanted, of the run's rows and the columns from c0 on (y and z point there).
-// value(j, i): the product at vector j of tile row i, as lane_values orders them.
-template <class T, bool AL, class S, class F>
+// value(j, i, b): the product at vector j of tile row i, as lane_values orders them, and b.
+// AHEAD tile rows of residuals are requested before the first is used, FAST: silu16.
+template <class T, bool AL, class S, int AHEAD = 1, bool FAST = false, class F>
 __device__ __forceinline__ void linear_epilogue(const LinearArgs<T>& a, const RowRun& run, int c0, int cols, T* y, T* z,
                                                 int tid, F value) {
-  // a tile row's residual is requested before the row above is stored
-  constexpr int W = lane_width<T>, NV = lane_vectors<S::TN, W>;
+  constexpr int W = lane_width<T>, NV = lane_vectors<S::TN, W>, RING = AHEAD + 1 < S::TM ? AHEAD + 1 : S::TM;
   using V = typename Floats<W>::type;
+  typedef T tw __attribute__((ext_vector_type(W)));
   const int l = tid & 63, wv = tid >> 6;
   const int m0 = (wv / S::WN) * (S::BM / S::WM) + (l & 15), n0 = (wv % S::WN) * (S::BN / S::WN);
   const T* bias = a.bias ? a.bias + (int64_t)run.group * a.n_out + c0 : nullptr;
   const T* res = a.residual ? a.residual + run.row0 * a.ldr + c0 : nullptr;
   auto finish = [&](auto act) {
-    V bj[NV], rj[2][NV];
+    V bj[NV];
+    tw rj[RING][NV];   // (as they lie in memory: half the registers of 16-bit types)
     auto column = [&](int j) { return n0 + lane_column<W>(j, l); };
     auto count = [&](int j) { return AL ? W : min(W, cols - column(j)); };
     auto load_residual = [&](int i) {
 #pragma unroll
       for (int j = 0; j < NV; ++j)
         if (m0 + 16 * i < run.rows && column(j) < cols)
-          rj[i & 1][j] = read_n<W>(res + (int64_t)(m0 + 16 * i) * a.ldr + column(j), count(j), AL);
+          rj[i % RING][j] = read_raw<W>(res + (int64_t)(m0 + 16 * i) * a.ldr + column(j), count(j), AL);
     };
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       bj[j] = V{};
       if (bias && column(j) < cols) bj[j] = read_n<W>(bias + column(j), count(j), AL);
     }
-    if (res) load_residual(0);
+    if (res)
+#pragma unroll
+      for (int i = 0; i < RING - 1; ++i) load_residual(i);
 #pragma unroll
     for (int i = 0; i < S::TM; ++i) {
       const int64_t m = m0 + 16 * i;
-      if (res && i + 1 < S::TM) load_residual(i + 1);
+      if (res && i + RING - 1 < S::TM) load_residual(i + RING - 1);
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
-        V v = value(j, i) + bj[j];
+        V v = value(j, i, bj[j]);
         const int n = column(j);
         if (m >= run.rows || n >= cols) continue;
         if (z) store_n(z + m * a.ldz + n, v, count(j), AL);
 #pragma unroll
-        for (int q = 0; q < W; ++q) v[q] = activate<decltype(act)::value>(v[q]);
-        if (res) v += rj[i & 1][j];
+        for (int q = 0; q < W; ++q) v[q] = activate_as<decltype(act)::value, FAST>(v[q]);
+        if (res) v += __builtin_convertvector(rj[i % RING][j], V);
         store_n(y + m * a.ldy + n, v, count(j), AL);
       }
     }
