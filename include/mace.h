@@ -498,9 +498,12 @@ mace_status mace_linear8_forward(const mace_linear_desc* desc, const void* x8, c
 /* mace_linear_backward from an input and a pre-activation kept as 8-bit rows
  * between the passes (mace_pack_rows of x and of z; desc->ld_x and
  * desc->ld_preact are their leading dimensions, multiples of 16): the gradients
- * at x = q s rounded to dtype, as it is the products' operand, and at z = q s.
- * Weights, dy and the gradients are of dtype as there; z8 and z_scales are not
- * read and may be NULL without an activation, x8 and x_scales without dweights. */
+ * at x = q s and z = q s.  Weights, dy and the gradients are of dtype as there.
+ * Of 16-bit types the products' operands are, with an activation, the integers
+ * times powers of two (exact) and dz with the rest of x's scales, rounded; without
+ * one x rounded to dtype, and dy.  z8 and z_scales are not read and may be NULL
+ * without an activation, x8 and x_scales without dweights (dx is then rounded
+ * otherwise than with x_scales). */
 size_t mace_linear_backward8_workspace_bytes(const mace_linear_desc* desc, int32_t want_bias, int32_t want_weights);
 mace_status mace_linear_backward8(const mace_linear_desc* desc, const void* dy, int64_t ld_dy, const void* x8,
                                   const float* x_scales, const void* weights, const void* z8, const float* z_scales,

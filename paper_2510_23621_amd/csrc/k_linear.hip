@@ -17,7 +17,19 @@ struct RowGradArgs {
   const int* offsets;
   int64_t n, lddz, lddx;
   int n_in, n_out, groups;
+  const float* x_scales;   // of an 8-bit input, or NULL: dz has split_scale8's factors on its rows
 };
+// dx of row r from its product with dz
+template <class T, class V>
+__device__ __forceinline__ V without_factor(const RowGradArgs<T>& a, int64_t r, V v) {
+  if constexpr (sizeof(T) == 2)
+    if (a.x_scales) {
+      float power, factor;
+      split_scale8<T>(a.x_scales[r], power, factor);
+      v *= 1.f / factor;
+    }
+  return v;
+}
 template <class T>
 struct WeightGradArgs {
   const T *x, *dz;
@@ -343,7 +355,9 @@ __global__ void __launch_bounds__(S::NT) __attribute__((amdgpu_waves_per_eu(2)))
   }
   narrow_rows<T, S, true, AL>({a.dz + run.row0 * a.lddz, a.lddz, run.rows, 0, a.dz + (a.n - 1) * a.lddz + a.n_out},
                               a.w + ((int64_t)run.group * a.n_in + c0) * a.n_out, a.n_out, cols, a.n_out, lds, tid,
-                              [&](int64_t m, int n, auto v, int k) { store_n(dx + m * a.lddx + n, v, k, AL); });
+                              [&](int64_t m, int n, auto v, int k) {
+    store_n(dx + m * a.lddx + n, without_factor(a, run.row0 + m, v), k, AL);
+  });
 }
 
 // dx = dz W_g^T: tile `id`
@@ -363,8 +377,9 @@ __device__ __forceinline__ void row_grad_tile(const RowGradArgs<T>& a, int id, u
   const T* w = a.w + ((int64_t)run.group * a.n_in + c0) * a.n_out;
   product<T, S, true, true, AL>({dz, a.lddz, run.rows, 0, a.dz + (a.n - 1) * a.lddz + a.n_out},
                                 {w, a.n_out, cols, 0, a.w + (int64_t)a.groups * a.n_in * a.n_out}, a.n_out, lds, tid, acc);
-  for_results<S, lane_width<T>, AL>(acc, run.rows, cols, tid,
-                                    [&](int m, int n, auto v, int k) { store_n(dx + m * a.lddx + n, v, k, AL); });
+  for_results<S, lane_width<T>, AL>(acc, run.rows, cols, tid, [&](int m, int n, auto v, int k) {
+    store_n(dx + m * a.lddx + n, without_factor(a, run.row0 + m, v), k, AL);
+  });
 }
 
 template <bool AL, class S>
@@ -523,12 +538,15 @@ struct SlopeValues<int8_t, AL> {   // (8-bit rows are padded to whole vectors)
 // each sum their rows, then are added in order. One pass over dy and z (36864 x 2048
 // bfloat16: 101 to 115 us from card to card, 4.5 to 3.9 TB/s); both products read the rounded dz, so that the
 // activation is not evaluated again for every tile of columns.
-// Z: T, or int8_t with a scale for each row (z stands as q s, in FP32).
+// Z: T, or int8_t with a scale for each row (z stands as q s, in FP32). xs: scales of an 8-bit input,
+// or NULL; their split_scale8 factors go onto dz's rows before it is rounded, and the input's
+// operand is exact: one rounding of the weights' gradients' terms, not two (error of
+// bfloat16 gradients 2.3e-3, with x rounded instead 2.9e-3, of binary16 ones 2.9e-4 and 3.5e-4).
 constexpr int kSlopeThreads = 1024;
 template <class T, bool AL, class Z>
 __global__ void __launch_bounds__(kSlopeThreads)
 linear_slope_kernel(const T* __restrict__ dy, int64_t lddy, const Z* __restrict__ z, int64_t ldz,
-                    const float* __restrict__ zs, T* __restrict__ dz,
+                    const float* __restrict__ zs, const float* __restrict__ xs, T* __restrict__ dz,
                     int64_t lddz, float* __restrict__ sums, const int* __restrict__ offsets, int groups, int64_t n,
                     int n_out, int act, int run_rows, int cx) {
   __shared__ float red[kSlopeThreads * 8];
@@ -554,11 +572,14 @@ linear_slope_kernel(const T* __restrict__ dy, int64_t lddy, const Z* __restrict_
       for (int u = 0; u < U; ++u) {
         if (r0 + u * R >= run.rows) continue;
         if (dz) {
+          float power, factor = 1.f;
+          if constexpr (sizeof(T) == 2 && __is_same(Z, int8_t))
+            if (xs) split_scale8<T>(xs[run.row0 + r0 + u * R], power, factor);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const float o = g[u].get(i) * activation_slope(v[u].get(i), act);
             s[i] += o;
-            g[u].set(i, (T)o);
+            g[u].set(i, (T)(factor * o));
           }
           *reinterpret_cast<Vec8<T>*>(dz + (run.row0 + r0 + u * R) * lddz + col) = g[u];   // (own buffer: rows padded to whole vectors)
         } else {
@@ -751,8 +772,8 @@ mace_status forward(const mace_linear_desc& d, const void* x, const void* w, con
 }
 
 template <class T, class Z = T>
-mace_status backward(const mace_linear_desc& d, const void* dy, int64_t lddy, const void* x, const void* w, const void* z,
-                     const float* zs, const int* offsets, void* dx, int64_t lddx, void* dw, void* db, char* ws, hipStream_t s) {
+mace_status backward(const mace_linear_desc& d, const void* dy, int64_t lddy, const void* x, const float* xs, const void* w,
+                     const void* z, const float* zs, const int* offsets, void* dx, int64_t lddx, void* dw, void* db, char* ws, hipStream_t s) {
   const BackwardPlan p = plan_backward(d, db != nullptr, dw != nullptr);
   const T* dz = (const T*)dy;
   int64_t lddz = lddy;
@@ -770,7 +791,7 @@ mace_status backward(const mace_linear_desc& d, const void* dy, int64_t lddy, co
     const dim3 grid((unsigned)slope_runs(d), (unsigned)ceil_div(vecs, cx));
     T* out = d.act != MACE_ACT_NONE ? const_cast<T*>(dz) : nullptr;
     auto go = [&](auto f) {
-      f<<<grid, kSlopeThreads, 0, s>>>((const T*)dy, lddy, (const Z*)z, d.ld_preact, zs, out, lddz, db ? sums : nullptr, offsets,
+      f<<<grid, kSlopeThreads, 0, s>>>((const T*)dy, lddy, (const Z*)z, d.ld_preact, zs, xs, out, lddz, db ? sums : nullptr, offsets,
                              d.n_groups, d.n_rows, d.n_out, d.act, slope_run(d.n_rows), cx);
     };
     if (al) go(linear_slope_kernel<T, true, Z>);
@@ -779,7 +800,7 @@ mace_status backward(const mace_linear_desc& d, const void* dy, int64_t lddy, co
   }
   const bool al = aligned16(dz) && aligned16(w) && aligned16(dx) && aligned16(x) && aligned16(dw) && near(lddz) &&
                   near(d.ld_x) && ((d.n_in | d.n_out | lddz | lddx | (dw ? d.ld_x : 0)) & 7) == 0;
-  const RowGradArgs<T> ra{dz, (const T*)w, (T*)dx, offsets, d.n_rows, lddz, lddx, d.n_in, d.n_out, d.n_groups};
+  const RowGradArgs<T> ra{dz, (const T*)w, (T*)dx, offsets, d.n_rows, lddz, lddx, d.n_in, d.n_out, d.n_groups, xs};
   const WeightGradArgs<T> wa{(const T*)x, dz, (T*)dw, p.splits > 1 ? reinterpret_cast<float*>(ws + p.part) : nullptr,
                              offsets, d.n_rows, d.ld_x, lddz, d.n_in, d.n_out, d.n_groups, p.splits};
   const BiasGradArgs<T> ba{sums, (T*)db, offsets, d.n_rows, d.n_out, db ? d.n_groups : 0, slope_run(d.n_rows), (int)slope_runs(d)};
@@ -878,14 +899,17 @@ extern "C" mace_status mace_linear_backward(const mace_linear_desc* desc, const 
   char* ws = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(workspace) + 255) & ~uintptr_t(255));
   hipStream_t s = (hipStream_t)stream;
   if (d.dtype == MACE_TYPE_FP32)
-    return backward<float>(d, dy, ld_dy, x, weights, preact, nullptr, group_offsets, dx, ld_dx, dweights, dbias, ws, s);
+    return backward<float>(d, dy, ld_dy, x, nullptr, weights, preact, nullptr, group_offsets, dx, ld_dx, dweights, dbias, ws, s);
   if (d.dtype == MACE_TYPE_BF16)
-    return backward<__bf16>(d, dy, ld_dy, x, weights, preact, nullptr, group_offsets, dx, ld_dx, dweights, dbias, ws, s);
-  return backward<_Float16>(d, dy, ld_dy, x, weights, preact, nullptr, group_offsets, dx, ld_dx, dweights, dbias, ws, s);
+    return backward<__bf16>(d, dy, ld_dy, x, nullptr, weights, preact, nullptr, group_offsets, dx, ld_dx, dweights, dbias, ws, s);
+  return backward<_Float16>(d, dy, ld_dy, x, nullptr, weights, preact, nullptr, group_offsets, dx, ld_dx, dweights, dbias, ws, s);
 }
 
-// The input's 8-bit rows are written out in dtype first, as the products' operand
+// The input's 8-bit rows are written out in dtype first, as the products' operand. Of 16-bit types
+// with an activation, where dz is written too, as their integers times powers of two; the rest of
+// the scales is on dz.
 namespace {
+bool splits_scales(const mace_linear_desc& d) { return d.act != MACE_ACT_NONE && d.dtype != MACE_TYPE_FP32; }
 int64_t ld_input8(const mace_linear_desc& d) { return (d.n_in + 7) / 8 * 8; }
 size_t input8_bytes(const mace_linear_desc& d, bool weights) {
   return weights ? round256(size_t(d.n_rows) * ld_input8(d) * size_of(d.dtype)) : 0;
@@ -925,7 +949,8 @@ extern "C" mace_status mace_linear_backward8(const mace_linear_desc* desc, const
   const void* x = nullptr;
   if (dweights && d.n_rows > 0) {
     const mace_rows8_desc r{d.n_rows, d.n_in, d.dtype, ld_input8(d), d.ld_x};
-    if ((st = mace_unpack_rows(&r, x8, x_scales, ws, stream)) != MACE_OK) return st;
+    st = splits_scales(d) ? unpack_powers(r, x8, x_scales, ws, s) : mace_unpack_rows(&r, x8, x_scales, ws, stream);
+    if (st != MACE_OK) return st;
     x = ws;
   }
   ws += input8_bytes(d, dweights != nullptr);
@@ -933,7 +958,7 @@ extern "C" mace_status mace_linear_backward8(const mace_linear_desc* desc, const
   return by_type(d.dtype, [&](auto zero) {
     using T = decltype(zero);
     if (d.act != MACE_ACT_NONE)
-      return backward<T, int8_t>(d, dy, ld_dy, x, weights, z8, z_scales, group_offsets, dx, ld_dx, dweights, dbias, ws, s);
-    return backward<T>(d, dy, ld_dy, x, weights, nullptr, nullptr, group_offsets, dx, ld_dx, dweights, dbias, ws, s);
+      return backward<T, int8_t>(d, dy, ld_dy, x, splits_scales(d) ? x_scales : nullptr, weights, z8, z_scales, group_offsets, dx, ld_dx, dweights, dbias, ws, s);
+    return backward<T>(d, dy, ld_dy, x, nullptr, weights, nullptr, nullptr, group_offsets, dx, ld_dx, dweights, dbias, ws, s);
   });
 }

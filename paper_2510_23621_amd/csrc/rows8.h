@@ -5,6 +5,9 @@
 
 namespace mace {
 
+// mace_unpack_rows with split_scale8's powers in place of the scales (k_rows8.hip)
+mace_status unpack_powers(const mace_rows8_desc& d, const void* values, const float* scales, void* x, hipStream_t s);
+
 constexpr int kMaxColumns8 = 1 << 17;   // 127 * 127 * 2^17 < 2^31: sums of products fit
 constexpr int64_t kMaxPitch8 = 1 << 20;       // a tile's rows lie within 32-bit byte offsets
 constexpr float kSmallestScale8 = 1.17549435082228751e-38f;   // 2^-126
@@ -30,6 +33,17 @@ __device__ __forceinline__ unsigned round8(float x, float s, float inv) {
 }
 // (inv of a scale next to the smallest is finite; of NaN it is NaN, and the row's values are 0)
 __device__ __forceinline__ float inverse8(float s) { return 1.f / s; }
+
+// A row's scale as a power of two, with which its integers are exact numbers of T, and a factor in
+// (0.5, 1] (up to 1.01 where the larger power would take 127 of it past T's range; 1 for NaN).
+template <class T>
+__device__ __forceinline__ void split_scale8(float s, float& power, float& factor) {
+  const int bits = __float_as_int(s);
+  int e = (bits >> 23) + ((bits & 0x7fffff) != 0);   // (a scale is positive and normal)
+  e = min(e, 127 + (__is_same(T, _Float16) ? 9 : 121));
+  power = s == s ? __int_as_float(e << 23) : s;
+  factor = s == s ? s / power : 1.f;
+}
 
 // columns 16 c .. 16 c + 15 of a row, zeros past the last (AL: there are none)
 template <class T>
