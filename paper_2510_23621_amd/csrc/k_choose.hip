@@ -152,16 +152,16 @@ __device__ __forceinline__ bool take_groups(const ChooseArgs& a, Key (&key)[V], 
     const R t = value_of(c1);
     return c2 > none ? t + value_of(c2) : (c1 > none ? t : empty);
   };
-  // is the group's total among the top_groups largest
-  auto decide = [&](int g) {
+  // groups before g in the order of their totals, of those from h0 on in steps
+  auto better_than = [&](int g, int h0, int step) {
     const R mine = total[g];
     int better = 0;
-    for (int h = 0; h < a.groups; ++h) {
+    for (int h = h0; h < a.groups; h += step) {
       const R o = total[h];
       better += o > mine || (o == mine && h < g);
       near_tie |= h != g && fabsf((float)(o - mine)) <= __builtin_fmaf(fabsf((float)mine), 4.7683716e-7f, tol);
     }
-    return better < a.top_groups;
+    return better;
   };
   if (a.group_lanes) {   // whole lanes: their two best, joined over the group's lanes
     Key c1 = none, c2 = none;
@@ -170,24 +170,30 @@ __device__ __forceinline__ bool take_groups(const ChooseArgs& a, Key (&key)[V], 
       c2 = max_of(c2, min_of(c1, key[i]));
       c1 = max_of(c1, key[i]);
     }
-    auto join = [&](auto step) {
-      if constexpr (decltype(step)::value < LPR) {
-        Key a1, b1, a2, b2;
-        exchange<decltype(step)::value>(c1, a1, b1);
-        exchange<decltype(step)::value>(c2, a2, b2);
-        c1 = max_of(a1, b1);
-        c2 = max_of(min_of(a1, b1), max_of(a2, b2));
-      }
+    auto over_group = [&](auto join) {
+      if (LPR > 1 && a.group_lanes > 1) join(Int<1>{});
+      if (LPR > 2 && a.group_lanes > 2) join(Int<2>{});
+      if (LPR > 4 && a.group_lanes > 4) join(Int<4>{});
+      if (LPR > 8 && a.group_lanes > 8) join(Int<8>{});
+      if (LPR > 16 && a.group_lanes > 16) join(Int<16>{});
     };
-    if (a.group_lanes > 1) join(Int<1>{});
-    if (a.group_lanes > 2) join(Int<2>{});
-    if (a.group_lanes > 4) join(Int<4>{});
-    if (a.group_lanes > 8) join(Int<8>{});
-    if (a.group_lanes > 16) join(Int<16>{});
+    over_group([&](auto step) {
+      Key a1, b1, a2, b2;
+      exchange<decltype(step)::value>(c1, a1, b1);
+      exchange<decltype(step)::value>(c2, a2, b2);
+      c1 = max_of(a1, b1);
+      c2 = max_of(min_of(a1, b1), max_of(a2, b2));
+    });
     const int g = min(first * a.per_inverse >> 20, a.groups - 1);
     if (first == g * a.per) total[g] = total_of(c1, c2);
     __builtin_amdgcn_wave_barrier();
-    const bool taken = decide(g);
+    int better = better_than(g, lane & (a.group_lanes - 1), a.group_lanes);   // the group's lanes share the others
+    over_group([&](auto step) {
+      int x, y;
+      exchange<decltype(step)::value>(better, x, y);
+      better = x + y;
+    });
+    const bool taken = better < a.top_groups;
 #pragma unroll
     for (int i = 0; i < V; ++i) key[i] = taken ? key[i] : none;
   } else {
@@ -205,7 +211,7 @@ __device__ __forceinline__ bool take_groups(const ChooseArgs& a, Key (&key)[V], 
       total[g] = total_of(c1, c2);
     }
     __builtin_amdgcn_wave_barrier();
-    for (int g = lane; g < a.groups; g += LPR) sm.taken[row][g] = decide(g);
+    for (int g = lane; g < a.groups; g += LPR) sm.taken[row][g] = better_than(g, 0, 1) < a.top_groups;
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int i = 0; i < V; ++i) {

@@ -61,13 +61,22 @@ sort_kernel(Slots sl, int64_t slots, int64_t span, int E, int bits, const int* _
   };
   count(s0);
   if (gridDim.x > 1) {
-    // groups of threads over (block, bucket): partial sums of the blocks' counts
-    for (int i = tid; i < (int)gridDim.x * E1; i += kSortThreads) {
-      const int b = i / E1, k = i - b * E1, h = hist[i];
-      if (h) {
-        atomicAdd(&total[k], h);
-        if (b < (int)blockIdx.x) atomicAdd(&next[k], h);
+    // threads over (block, bucket): sums of the blocks' counts, eight loads in flight
+    const int all = gridDim.x * E1, mine = blockIdx.x * E1;   // (up to this block's counts: of earlier blocks)
+    for (int i0 = tid; i0 < all; i0 += 8 * kSortThreads) {
+      int h[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int i = i0 + u * kSortThreads;
+        h[u] = i < all ? hist[i] : 0;
       }
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (h[u]) {
+          const int i = i0 + u * kSortThreads, k = i % E1;
+          atomicAdd(&total[k], h[u]);
+          if (i < mine) atomicAdd(&next[k], h[u]);
+        }
     }
     __syncthreads();
   } else {

@@ -40,19 +40,18 @@ def _streamed(f):
     allocates belongs to the stream that uses it.  Refuses tensors that ask for
     a gradient: the result would have lost it without a word."""
     first = f.__code__.co_varnames[0]
+    packed = any("Rows8" in a or "Weights8" in a for a in f.__annotations__.values())   # (tuples of tensors)
 
     @wraps(f)
     def on(*args, stream=None, **kw):
         if torch.is_grad_enabled():
             for t in (*args, *kw.values()):
-                if getattr(t, "requires_grad", False) or isinstance(t, tuple) and any(getattr(u, "requires_grad", False)
-                                                                                      for u in t):
+                if getattr(t, "requires_grad", False) or packed and isinstance(t, tuple) and any(
+                        getattr(u, "requires_grad", False) for u in t):
                     raise ValueError(f"{f.__name__} records no gradients: call it under torch.no_grad() or on "
                                      "detached tensors")
         t = args[0] if args else kw[first]
-        if isinstance(t, tuple):   # (Rows8: the device of its values)
-            t = t[0]
-        device = t.get_device()   # (-1: a host tensor, which f refuses)
+        device = (t[0] if packed and isinstance(t, tuple) else t).get_device()   # (-1: a host tensor, which f refuses)
         if stream is not None:
             if stream.device.index != device:
                 raise ValueError(f"stream is of device {stream.device}, {first} of {device}")
@@ -524,8 +523,9 @@ def linear8(x, w: Weights8, bias=None, residual=None, *, offsets=None, act: str 
         d.ld_residual = _rows(residual, n, m, like, "residual")
     y = like.new_empty((n, m))
     lib = B.lib()
-    nbytes = 0 if x_scales is not None else lib.mace_linear8_workspace_bytes(d) or 1
-    ws = x.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
+    # (0 for sizes the library does not take: the call itself says which error; 256: nothing is kept in it)
+    nbytes = 0 if x_scales is not None else lib.mace_linear8_workspace_bytes(d)
+    ws = x.new_empty(nbytes, dtype=torch.uint8) if nbytes > 256 else None
     B._check(lib.mace_linear8_forward(d, x.data_ptr(), None if x_scales is None else x_scales.data_ptr(),
                                       values.data_ptr(), ld_w, w_scales.data_ptr(),
                                       None if bias is None else bias.data_ptr(),
