@@ -139,7 +139,7 @@ struct ChooseLds {
 };
 
 // Of a token's keys those outside its top_groups best groups become no_key. True: two
-// groups' totals differ by at most tol and a few units of themselves.
+// groups' totals differ by at most tol.
 template <class Key, int LPR, int V>
 __device__ __forceinline__ bool take_groups(const ChooseArgs& a, Key (&key)[V], float tol, int lane, int row, ChooseLds<LPR, V>& sm) {
   using R = decltype(value_of(Key{}));
@@ -159,7 +159,7 @@ __device__ __forceinline__ bool take_groups(const ChooseArgs& a, Key (&key)[V], 
     for (int h = h0; h < a.groups; h += step) {
       const R o = total[h];
       better += o > mine || (o == mine && h < g);
-      near_tie |= h != g && fabsf((float)(o - mine)) <= __builtin_fmaf(fabsf((float)mine), 4.7683716e-7f, tol);
+      near_tie |= h != g && fabsf((float)(o - mine)) <= tol;
     }
     return better;
   };
@@ -282,7 +282,8 @@ __device__ __noinline__ void choose_exact(ChooseArgs a, const T* logits, const f
 // Error of a score: the exponential is off by its argument's rounding, 2^-24 of |x - top| or
 // |x|, and a few units, the sum over experts by V + 6 more: ((D + 40) M) 2^-24 with D the row's
 // largest such argument and M = 1 / sum (or 1) the largest score there can be; s + b adds half a unit
-// of itself. Two keys may differ by twice that, two groups' totals by four times.
+// of itself. Two keys may differ by twice that, two groups' totals by four times, and by the
+// roundings of two sums.
 template <int LPR, int V>
 __device__ __forceinline__ bool choose_fast(const ChooseArgs& a, const float (&x)[V], const float (&b)[V], bool biased, float top,
                                             int lane, int row, bool& bad, ChooseLds<LPR, V>& sm) {
@@ -316,7 +317,13 @@ __device__ __forceinline__ bool choose_fast(const ChooseArgs& a, const float (&x
       scored[i] = key_of(on ? c : none);
     }
     tol = (fminf(__int_as_float(row_max<LPR>(arg)), 100.f) + 40.f) * unit * 1.1920929e-7f + 1e-36f;
-    if (a.groups > 1) near_tie = take_groups<int, LPR, V>(a, scored, 2 * tol, lane, row, sm);
+    if (a.groups > 1) {
+      int big = 0;   // a total is off by the roundings of its parts too, which may cancel
+#pragma unroll
+      for (int i = 0; i < V; ++i) big = max(big, scored[i] > kNoKey ? __float_as_int(fabsf(value_of(scored[i]))) : 0);
+      const float units = __int_as_float(row_max<LPR>(big)) * 4.7683716e-7f;
+      near_tie = take_groups<int, LPR, V>(a, scored, 2 * tol + units, lane, row, sm);
+    }
 #pragma unroll
     for (int i = 0; i < V; ++i)   // (without a bias the logits decide within the groups)
       key[i] = biased ? scored[i] : (scored[i] > kNoKey ? key[i] : kNoKey);

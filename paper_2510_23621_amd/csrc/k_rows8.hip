@@ -79,41 +79,48 @@ __global__ void __launch_bounds__(256) unpack_rows_kernel(Rows8Args a, const int
   store_n(x + row * a.ld_x + c, v, min(8, a.cols - c), AL);
 }
 
-// Weights: a block takes 64 output columns of a group, one a lane, its waves' rows
-// 16 at a time; the column's largest magnitude over all rows first.
+// Weights: a block takes 64 output columns of a group, one a lane, and its 16 waves the rows, 16 at
+// a time: the column's largest magnitude over all rows first, then the integers.
+constexpr int kPackThreads = 1024;
 template <class T>
-__global__ void __launch_bounds__(256) pack_weights_kernel(const T* __restrict__ w, int n_in, int n_out, int64_t ld,
-                                                           int8_t* __restrict__ values, float* __restrict__ scales) {
-  __shared__ unsigned red[4][64];
+__global__ void __launch_bounds__(kPackThreads) pack_weights_kernel(const T* __restrict__ w, int groups, int n_in, int n_out, int64_t ld,
+                                                                    int8_t* __restrict__ values, float* __restrict__ scales) {
+  constexpr int WAVES = kPackThreads / 64;
+  __shared__ unsigned red[WAVES][64];
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, tiles = (n_out + 63) / 64;
   const int64_t g = block_id() / tiles;
+  if (g >= groups) return;   // (a grid's last row of blocks is full)
   const int col = block_id() % tiles * 64 + lane;
   const bool on = col < n_out;
-  w += g * n_in * n_out + (on ? col : 0);
+  w += g * n_in * n_out + (on ? col : n_out - 1);
+  auto load = [&](int k0, float (&x)[16]) {   // rows k0 .. k0 + 15, zeros past the last
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = k0 + i < n_in ? to_f32(w[(int64_t)(k0 + i) * n_out]) : 0.f;
+  };
   unsigned m = 0;   // (magnitudes in the order of their bits: NaN above all)
-  if (on)
-    for (int k = wv; k < n_in; k += 4) m = max(m, __float_as_uint(fabsf(to_f32(w[(int64_t)k * n_out]))));
+  for (int k0 = 16 * wv; k0 < n_in; k0 += 16 * WAVES) {
+    float x[16];
+    load(k0, x);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) m = max(m, __float_as_uint(fabsf(x[i])));
+  }
   red[wv][lane] = m;
   __syncthreads();
-  m = max(max(red[0][lane], red[1][lane]), max(red[2][lane], red[3][lane]));
+#pragma unroll
+  for (int i = 0; i < WAVES; ++i) m = max(m, red[i][lane]);
   if (!on) return;
   const float s = scale8(__uint_as_float(m)), inv = inverse8(s);
   if (wv == 0) scales[g * n_out + col] = s;
   values += (g * n_out + col) * ld;
-  for (int64_t k0 = 16 * wv; k0 < n_in; k0 += 64) {
-    uint4 o;
-    unsigned* b = &o.x;
+  for (int k0 = 16 * wv; k0 < n_in; k0 += 16 * WAVES) {
+    float x[16];
+    unsigned q[16];
+    load(k0, x);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      b[j] = 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int64_t k = k0 + 4 * j + i;
-        const unsigned q = k < n_in && s == s ? round8(to_f32(w[k * n_out]), s, inv) : 0;
-        b[j] |= (q & 255) << 8 * i;
-      }
-    }
-    *reinterpret_cast<uint4*>(values + k0) = o;
+    for (int i = 0; i < 16; ++i) q[i] = round8(x[i], s, inv);
+    i4 o = lowest_bytes(q);
+    if (s != s) o = i4{0, 0, 0, 0};
+    *reinterpret_cast<i4*>(values + k0) = o;
   }
 }
 
@@ -191,7 +198,7 @@ extern "C" mace_status mace_pack_weights(int32_t n_groups, int32_t n_in, int32_t
     using T = decltype(zero);
     const int64_t blocks = n_groups * ceil_div(n_out, 64);
     if (!fits_grid(blocks)) return MACE_EUNSUPPORTED;
-    pack_weights_kernel<T><<<grid_of(blocks), 256, 0, (hipStream_t)stream>>>((const T*)weights, n_in, n_out, ld_values,
+    pack_weights_kernel<T><<<grid_of(blocks), kPackThreads, 0, (hipStream_t)stream>>>((const T*)weights, n_groups, n_in, n_out, ld_values,
                                                                             (int8_t*)values, scales);
     return launched();
   });

@@ -163,6 +163,15 @@ def test_scores_closer_than_their_roundings(scores, groups):
     check(x.expand(50, e).contiguous(), b, torch.randn(50, 8, generator=gen), 8, scores, groups, max(1, groups // 2))
 
 
+def test_groups_of_large_biases_that_cancel():
+    """Groups of two experts with biases c and -c: their totals are the scores' sums, which FP32 loses
+    (a unit of 2^20 is 2^-4), and FP64 keeps to 2^-32."""
+    x, _, dw = inputs(200, 16, 3, "fp32", 12)
+    b = torch.tensor([2.0 ** 20, -2.0 ** 20] * 8)
+    for scores in ("softmax", "sigmoid"):
+        check(x, b, dw, 3, scores, 8, 2)
+
+
 @pytest.mark.parametrize("spread", [30.0, 300.0, 3000.0])
 @pytest.mark.parametrize("normalise", [True, False])
 def test_large_logits(spread, normalise):

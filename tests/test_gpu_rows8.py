@@ -96,6 +96,19 @@ def test_pack_weights(g, k, m, dtype):
     assert p.n_in == k and not p.values[:, :, k:].any()
 
 
+def test_pack_weights_over_more_than_one_row_of_blocks():
+    """1024 groups of 2049 tiles of columns: more than 2^21 blocks."""
+    g, m = 1024, 131130
+    w = torch.zeros(g, 1, m, dtype=torch.float16, device="cuda")
+    w[-1] = torch.randn(1, m, device="cuda").half()
+    w[0, 0, 5] = 2
+    p = L.pack_weights(w)
+    x = w[-1, 0].double()
+    assert torch.equal(p.scales[-1].double(), (x.abs() / 127).float().clamp_min(2.0 ** -126).double())
+    assert torch.equal(p.values[-1, :, 0].double(), 127 * x.sign()) and not p.values[:, :, 1:].any()
+    assert p.values[0, 5, 0] == 127 and not p.values[1:-1].any()
+
+
 def offsets_of(sizes, tail=0):
     off = torch.tensor([0] + list(sizes)).cumsum(0)
     return off.tolist(), int(off[-1]) + tail
