@@ -273,10 +273,11 @@ SortPlan sort_plan(int64_t rows) {
   const int passes = (bits + 8) / 9;
   return {passes, (bits + passes - 1) / passes};
 }
-// Slots per segment: enough threads to fill the chip, few enough parts to join
+// Slots per segment: enough threads to fill the chip, few enough parts to join. 17,711 ids of 89 rows
+// 515 wide: 8 slots 32.7 us, 16 28.8, 32 33.5; 4,000 ids 128 wide: 8 slots 18.6, 16 20.2.
 int segment(const mace_embed_desc& d) {
-  const int64_t nv = ceil_div(d.width, d.dtype == MACE_TYPE_FP32 ? 4 : 8);
-  return (int)std::max<int64_t>(8, std::min<int64_t>(64, std::max(d.n_ids * nv / (1 << 19), d.n_ids / 8192)));
+  const int64_t nv = ceil_div(d.width, d.dtype == MACE_TYPE_FP32 ? 4 : 8), least = d.n_ids < 8192 ? 8 : 16;
+  return (int)std::max(least, std::min<int64_t>(64, std::max(d.n_ids * nv / (1 << 19), d.n_ids / 8192)));
 }
 
 struct BackwardPlan {
