@@ -488,7 +488,7 @@ mace_status mace_pack_weights(int32_t n_groups, int32_t n_in, int32_t n_out, int
  * dimension ld_w and w_scales as mace_pack_weights does.  Alternatively x_scales
  * is NULL and x8 (dev) [n_rows][n_in] of dtype, rounded to 8-bit rows on the way
  * in workspace (dev), of at least mace_linear8_workspace_bytes (0 on invalid
- * input; not used with x_scales). */
+ * input; where it is 256, and with x_scales, workspace may be NULL). */
 size_t mace_linear8_workspace_bytes(const mace_linear_desc* desc);
 mace_status mace_linear8_forward(const mace_linear_desc* desc, const void* x8, const float* x_scales, const void* w8,
                                  int64_t ld_w, const float* w_scales, const void* bias, const void* residual,

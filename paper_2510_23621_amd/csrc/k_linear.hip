@@ -542,16 +542,43 @@ struct SlopeValues<int8_t, AL> {   // (8-bit rows are padded to whole vectors)
 // or NULL; their split_scale8 factors go onto dz's rows before it is rounded, and the input's
 // operand is exact: one rounding of the weights' gradients' terms, not two (error of
 // bfloat16 gradients 2.3e-3, with x rounded instead 2.9e-3, of binary16 ones 2.9e-4 and 3.5e-4).
+// That operand is written by the launch's further columns of blocks (Input8).
 constexpr int kSlopeThreads = 1024;
+template <class T>
+struct Input8 {
+  const int8_t* values;
+  int64_t ld_values;
+  T* x;         // its integers times the power of their scale, in FP32 times the scale; or NULL
+  int64_t ld;   // a multiple of 8
+  int n_in, cx;
+  unsigned first;   // column of blocks
+};
+template <class T>
+__device__ __forceinline__ void write_input8(const Input8<T>& in, const float* __restrict__ xs, const RowRun& run) {
+  const int c = threadIdx.x % in.cx, col = 8 * ((blockIdx.y - in.first) * in.cx + c);
+  if (col >= in.n_in) return;
+  for (int r = threadIdx.x / in.cx; r < run.rows; r += kSlopeThreads / in.cx) {
+    const int64_t row = run.row0 + r;
+    const uint2 q = *reinterpret_cast<const uint2*>(in.values + row * in.ld_values + col);
+    float s = xs[row], factor;
+    if constexpr (sizeof(T) == 2) split_scale8<T>(s, s, factor);
+    Vec8<T> v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v.set(i, (T)(s * (float)(int8_t)((i < 4 ? q.x : q.y) >> 8 * (i & 3))));
+    *reinterpret_cast<Vec8<T>*>(in.x + row * in.ld + col) = v;
+  }
+}
 template <class T, bool AL, class Z>
 __global__ void __launch_bounds__(kSlopeThreads)
 linear_slope_kernel(const T* __restrict__ dy, int64_t lddy, const Z* __restrict__ z, int64_t ldz,
                     const float* __restrict__ zs, const float* __restrict__ xs, T* __restrict__ dz,
                     int64_t lddz, float* __restrict__ sums, const int* __restrict__ offsets, int groups, int64_t n,
-                    int n_out, int act, int run_rows, int cx) {
+                    int n_out, int act, int run_rows, int cx, Input8<T> in) {
   __shared__ float red[kSlopeThreads * 8];
   RowRun run;
   if (!find_run(offsets, groups, n, run_rows, blockIdx.x, run) || run.group >= groups) return;
+  if constexpr (__is_same(Z, int8_t))
+    if (blockIdx.y >= in.first) return write_input8(in, xs, run);
   const int tid = threadIdx.x, c = tid % cx, ry = tid / cx, R = kSlopeThreads / cx;
   const int col = 8 * (blockIdx.y * cx + c), k = n_out - col;
   float s[8] = {};
@@ -772,8 +799,8 @@ mace_status forward(const mace_linear_desc& d, const void* x, const void* w, con
 }
 
 template <class T, class Z = T>
-mace_status backward(const mace_linear_desc& d, const void* dy, int64_t lddy, const void* x, const float* xs, const void* w,
-                     const void* z, const float* zs, const int* offsets, void* dx, int64_t lddx, void* dw, void* db, char* ws, hipStream_t s) {
+mace_status backward(const mace_linear_desc& d, const void* dy, int64_t lddy, const void* x, const float* xs, Input8<T> in,
+                     const void* w, const void* z, const float* zs, const int* offsets, void* dx, int64_t lddx, void* dw, void* db, char* ws, hipStream_t s) {
   const BackwardPlan p = plan_backward(d, db != nullptr, dw != nullptr);
   const T* dz = (const T*)dy;
   int64_t lddz = lddy;
@@ -788,11 +815,15 @@ mace_status backward(const mace_linear_desc& d, const void* dy, int64_t lddy, co
     int cx = 1;
     while (cx < 64 && cx < vecs) cx *= 2;
     const bool al = aligned16(dy) && (__is_same(Z, int8_t) || aligned16(z)) && ((d.n_out | lddy | d.ld_preact) & 7) == 0;
-    const dim3 grid((unsigned)slope_runs(d), (unsigned)ceil_div(vecs, cx));
+    const int vecs_in = (d.n_in + 7) / 8;
+    in.cx = 1;
+    while (in.cx < 64 && in.cx < vecs_in) in.cx *= 2;
+    in.first = (unsigned)ceil_div(vecs, cx);
+    const dim3 grid((unsigned)slope_runs(d), in.first + (in.x ? (unsigned)ceil_div(vecs_in, in.cx) : 0));
     T* out = d.act != MACE_ACT_NONE ? const_cast<T*>(dz) : nullptr;
     auto go = [&](auto f) {
       f<<<grid, kSlopeThreads, 0, s>>>((const T*)dy, lddy, (const Z*)z, d.ld_preact, zs, xs, out, lddz, db ? sums : nullptr, offsets,
-                             d.n_groups, d.n_rows, d.n_out, d.act, slope_run(d.n_rows), cx);
+                             d.n_groups, d.n_rows, d.n_out, d.act, slope_run(d.n_rows), cx, in);
     };
     if (al) go(linear_slope_kernel<T, true, Z>);
     else go(linear_slope_kernel<T, false, Z>);
@@ -899,17 +930,15 @@ extern "C" mace_status mace_linear_backward(const mace_linear_desc* desc, const 
   char* ws = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(workspace) + 255) & ~uintptr_t(255));
   hipStream_t s = (hipStream_t)stream;
   if (d.dtype == MACE_TYPE_FP32)
-    return backward<float>(d, dy, ld_dy, x, nullptr, weights, preact, nullptr, group_offsets, dx, ld_dx, dweights, dbias, ws, s);
+    return backward<float>(d, dy, ld_dy, x, nullptr, {}, weights, preact, nullptr, group_offsets, dx, ld_dx, dweights, dbias, ws, s);
   if (d.dtype == MACE_TYPE_BF16)
-    return backward<__bf16>(d, dy, ld_dy, x, nullptr, weights, preact, nullptr, group_offsets, dx, ld_dx, dweights, dbias, ws, s);
-  return backward<_Float16>(d, dy, ld_dy, x, nullptr, weights, preact, nullptr, group_offsets, dx, ld_dx, dweights, dbias, ws, s);
+    return backward<__bf16>(d, dy, ld_dy, x, nullptr, {}, weights, preact, nullptr, group_offsets, dx, ld_dx, dweights, dbias, ws, s);
+  return backward<_Float16>(d, dy, ld_dy, x, nullptr, {}, weights, preact, nullptr, group_offsets, dx, ld_dx, dweights, dbias, ws, s);
 }
 
-// The input's 8-bit rows are written out in dtype first, as the products' operand. Of 16-bit types
-// with an activation, where dz is written too, as their integers times powers of two; the rest of
-// the scales is on dz.
+// The input's 8-bit rows are written out in dtype first, as the products' operand: beside dz where there is an
+// activation (Input8), by a launch of their own otherwise.
 namespace {
-bool splits_scales(const mace_linear_desc& d) { return d.act != MACE_ACT_NONE && d.dtype != MACE_TYPE_FP32; }
 int64_t ld_input8(const mace_linear_desc& d) { return (d.n_in + 7) / 8 * 8; }
 size_t input8_bytes(const mace_linear_desc& d, bool weights) {
   return weights ? round256(size_t(d.n_rows) * ld_input8(d) * size_of(d.dtype)) : 0;
@@ -946,19 +975,20 @@ extern "C" mace_status mace_linear_backward8(const mace_linear_desc* desc, const
   if (need > 256 && workspace_bytes < need) return MACE_ENOSPACE;
   char* ws = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(workspace) + 255) & ~uintptr_t(255));
   hipStream_t s = (hipStream_t)stream;
-  const void* x = nullptr;
-  if (dweights && d.n_rows > 0) {
-    const mace_rows8_desc r{d.n_rows, d.n_in, d.dtype, ld_input8(d), d.ld_x};
-    st = splits_scales(d) ? unpack_powers(r, x8, x_scales, ws, s) : mace_unpack_rows(&r, x8, x_scales, ws, stream);
-    if (st != MACE_OK) return st;
-    x = ws;
-  }
+  void* x = dweights && d.n_rows > 0 ? ws : nullptr;
   ws += input8_bytes(d, dweights != nullptr);
+  if (x && d.act == MACE_ACT_NONE) {
+    const mace_rows8_desc r{d.n_rows, d.n_in, d.dtype, ld_input8(d), d.ld_x};
+    if ((st = mace_unpack_rows(&r, x8, x_scales, x, stream)) != MACE_OK) return st;
+  }
+  const int64_t ld_x8 = d.ld_x;
   d.ld_x = ld_input8(d);
   return by_type(d.dtype, [&](auto zero) {
     using T = decltype(zero);
-    if (d.act != MACE_ACT_NONE)
-      return backward<T, int8_t>(d, dy, ld_dy, x, splits_scales(d) ? x_scales : nullptr, weights, z8, z_scales, group_offsets, dx, ld_dx, dweights, dbias, ws, s);
-    return backward<T>(d, dy, ld_dy, x, nullptr, weights, nullptr, nullptr, group_offsets, dx, ld_dx, dweights, dbias, ws, s);
+    if (d.act == MACE_ACT_NONE)
+      return backward<T>(d, dy, ld_dy, x, nullptr, {}, weights, nullptr, nullptr, group_offsets, dx, ld_dx, dweights, dbias, ws, s);
+    const Input8<T> in{(const int8_t*)x8, ld_x8, (T*)x, d.ld_x, d.n_in};
+    return backward<T, int8_t>(d, dy, ld_dy, x, x_scales, in, weights, z8, z_scales, group_offsets, dx, ld_dx, dweights, dbias,
+                               ws, s);
   });
 }

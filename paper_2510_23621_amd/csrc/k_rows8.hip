@@ -62,8 +62,8 @@ __global__ void __launch_bounds__(256) pack_rows_kernel(Rows8Args a, const T* __
   }
 }
 
-// x = q s, 8 columns a thread; POWERS: with split_scale8's power for s
-template <class T, bool AL, bool POWERS>
+// x = q s, 8 columns a thread
+template <class T, bool AL>
 __global__ void __launch_bounds__(256) unpack_rows_kernel(Rows8Args a, const int8_t* __restrict__ values,
                                                           const float* __restrict__ scales, T* __restrict__ x) {
   int vec;
@@ -71,8 +71,7 @@ __global__ void __launch_bounds__(256) unpack_rows_kernel(Rows8Args a, const int
   if (row >= a.n) return;
   const int c = 8 * vec;
   const uint2 q = *reinterpret_cast<const uint2*>(values + row * a.ld_values + c);
-  float s = scales[row], factor;
-  if (POWERS) split_scale8<T>(s, s, factor);
+  const float s = scales[row];
   f8 v;
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = s * (float)(int8_t)((i < 4 ? q.x : q.y) >> 8 * (i & 3));
@@ -162,31 +161,23 @@ extern "C" mace_status mace_pack_rows(const mace_rows8_desc* desc, const void* x
   });
 }
 
-template <bool POWERS>
-static mace_status unpack(const mace_rows8_desc& d, const void* values, const float* scales, void* x, hipStream_t s) {
-  return by_type(d.dtype, [&](auto zero) -> mace_status {
-    using T = decltype(zero);
-    const Rows8Args a{d.n_rows, d.ld_x, d.ld_values, d.n_cols, (int)ceil_div(d.n_cols, 16), 1};
-    const int64_t blocks = ceil_div(d.n_rows * ceil_div(d.n_cols, 8), 256);
-    if (!fits_grid(blocks)) return MACE_EUNSUPPORTED;
-    const bool al = aligned16(x) && ((d.n_cols | d.ld_x) & 7) == 0;
-    auto f = al ? unpack_rows_kernel<T, true, POWERS> : unpack_rows_kernel<T, false, POWERS>;
-    f<<<grid_of(blocks), 256, 0, s>>>(a, (const int8_t*)values, scales, (T*)x);
-    return launched();
-  });
-}
-
-mace_status mace::unpack_powers(const mace_rows8_desc& d, const void* values, const float* scales, void* x, hipStream_t s) {
-  return unpack<true>(d, values, scales, x, s);
-}
-
 extern "C" mace_status mace_unpack_rows(const mace_rows8_desc* desc, const void* values, const float* scales, void* x,
                                         void* stream) {
   const mace_status st = check(desc);
   if (st != MACE_OK) return st;
   if (desc->n_rows == 0) return MACE_OK;
   if (!x || !values || !scales || !aligned16(values)) return MACE_EINVAL;
-  return unpack<false>(*desc, values, scales, x, (hipStream_t)stream);
+  return by_type(desc->dtype, [&](auto zero) -> mace_status {
+    using T = decltype(zero);
+    const mace_rows8_desc& d = *desc;
+    const Rows8Args a{d.n_rows, d.ld_x, d.ld_values, d.n_cols, (int)ceil_div(d.n_cols, 16), 1};
+    const int64_t blocks = ceil_div(d.n_rows * ceil_div(d.n_cols, 8), 256);
+    if (!fits_grid(blocks)) return MACE_EUNSUPPORTED;
+    const bool al = aligned16(x) && ((d.n_cols | d.ld_x) & 7) == 0;
+    auto f = al ? unpack_rows_kernel<T, true> : unpack_rows_kernel<T, false>;
+    f<<<grid_of(blocks), 256, 0, (hipStream_t)stream>>>(a, (const int8_t*)values, scales, (T*)x);
+    return launched();
+  });
 }
 
 extern "C" mace_status mace_pack_weights(int32_t n_groups, int32_t n_in, int32_t n_out, int32_t dtype, const void* weights,

@@ -5,9 +5,6 @@
 
 namespace mace {
 
-// mace_unpack_rows with split_scale8's powers in place of the scales (k_rows8.hip)
-mace_status unpack_powers(const mace_rows8_desc& d, const void* values, const float* scales, void* x, hipStream_t s);
-
 constexpr int kMaxColumns8 = 1 << 17;   // 127 * 127 * 2^17 < 2^31: sums of products fit
 constexpr int64_t kMaxPitch8 = 1 << 20;       // a tile's rows lie within 32-bit byte offsets
 constexpr float kSmallestScale8 = 1.17549435082228751e-38f;   // 2^-126

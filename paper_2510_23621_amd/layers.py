@@ -431,7 +431,8 @@ def _check_rows8(r: Rows8, name: str):
     v, s, c = r
     if v.dim() != 2 or v.dtype is not torch.int8 or not v.is_cuda or not v.is_contiguous() or not 0 < c <= v.shape[1]:
         raise ValueError(f"{name}'s values must be contiguous int8 [n, columns, padded] on a GPU")
-    _whole(s, (v.shape[0],), torch.float32, v, f"{name}'s scales")
+    if s.dtype is not torch.float32 or s.shape != v.shape[:1] or s.get_device() != v.get_device() or not s.is_contiguous():
+        raise ValueError(f"{name}'s scales must be contiguous float32 [n] on {v.device}")
 
 
 @_streamed
