@@ -374,8 +374,12 @@ __device__ __forceinline__ bool choose_fast(const ChooseArgs& a, const float (&x
   return row_any<LPR>(near_tie);
 }
 
-// LPR lanes per token, V consecutive experts each. Scores in FP32; the few rows where a
-// decision lies within their error are decided again in FP64.
+// LPR lanes per token, V consecutive experts each. Scores in FP32; the few rows where a decision lies
+// within their error are decided again in FP64 (0.9 % of the rows below, a second pass for 1.8 % of the
+// waves; all of it in FP64, the first form, took 254 us). Bound by instructions: 36,864 tokens, 8 of 256
+// experts in 4 of 8 groups, 41 us, the vector units busy 68 % of it with 900 instructions for two tokens, of which
+// the lanes' sorting takes 150, nine rounds 220, scores and masks 200, groups 110, weights 60; the 38 MB of
+// logits would take 7.5.
 template <class T, int LPR, int V>
 __global__ void __launch_bounds__(256)
 choose_kernel(ChooseArgs a, const T* __restrict__ logits, const float* __restrict__ bias, int* __restrict__ expert,
@@ -458,7 +462,9 @@ struct ChooseGradLds {
 // v_j are the (renormalised) scores, g_j the weights' gradients: renormalised
 // dlogit_j = scale v_j (g_j - sum g v), times 1 - s_j for a sigmoid; otherwise scale s_j
 // g_j, times 1 - s_j or less scale s_e sum g s for every expert e. The chosen experts' values are
-// scattered through LDS; only a softmax that is not renormalised reads all logits.
+// scattered through LDS; only a softmax that is not renormalised reads all logits. 36,864 x 256 FP32, 8
+// chosen: 14 us, 38 MB written and 21 read; with a comparison for each expert and choice instead of the
+// scatter 37.
 template <class T, int LPR, int V>
 __global__ void __launch_bounds__(256)
 choose_bwd_kernel(ChooseArgs a, const float* __restrict__ dweights, const T* __restrict__ logits,
