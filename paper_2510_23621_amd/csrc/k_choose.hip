@@ -23,6 +23,14 @@ template <> __device__ __forceinline__ float lowest<float>() { return -3.4028234
 template <> __device__ __forceinline__ float lowest<__bf16>() { return -3.3895313892515355e38f; }
 template <> __device__ __forceinline__ float lowest<_Float16>() { return -65504.f; }
 
+// LDS written by some lanes of a wave, read by others: the hardware keeps a wave's order, and this the
+// compiler's
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // ------------------------------------------------------------------ lanes of a row
 // LPR consecutive lanes hold a token's row. Their sums, maxima and minima go
 // through the vector units' own exchanges (DPP, and swaps of half rows), without LDS.
@@ -126,13 +134,13 @@ struct ChooseShape {
 template <int LPR, int V>
 struct ChooseLds {
   using S = ChooseShape<LPR, V>;
-  union {
+  union {   // of one wave: the waves of a block do not wait for each other
     struct {
-      int key[(V + 1) * 256];     // each lane's keys, largest first, and none behind them
-      int index[(V + 1) * 256];   // their experts
+      int key[(V + 1) * 64];     // each lane's keys, largest first, and none behind them
+      int index[(V + 1) * 64];   // their experts
     } sorted;
-    double key[S::ROWS][LPR * V];   // (or integers)
-  };
+    double key[64 / LPR][LPR * V];   // (or integers)
+  } wave[4];
   double total[S::ROWS][S::G];   // (or floats)
   int taken[S::ROWS][S::G];
   int index[S::ROWS][S::K];   // the choice
@@ -186,7 +194,7 @@ __device__ __forceinline__ bool take_groups(const ChooseArgs& a, Key (&key)[V], 
     });
     const int g = min(first * a.per_inverse >> 20, a.groups - 1);
     if (first == g * a.per) total[g] = total_of(c1, c2);
-    __builtin_amdgcn_wave_barrier();
+    wave_sync();
     int better = better_than(g, lane & (a.group_lanes - 1), a.group_lanes);   // the group's lanes share the others
     over_group([&](auto step) {
       int x, y;
@@ -197,10 +205,10 @@ __device__ __forceinline__ bool take_groups(const ChooseArgs& a, Key (&key)[V], 
 #pragma unroll
     for (int i = 0; i < V; ++i) key[i] = taken ? key[i] : none;
   } else {
-    Key* keys = reinterpret_cast<Key*>(sm.key[row]);
+    Key* keys = reinterpret_cast<Key*>(sm.wave[threadIdx.x / 64].key[row % (64 / LPR)]);
 #pragma unroll
     for (int i = 0; i < V; ++i) keys[first + i] = key[i];
-    __builtin_amdgcn_wave_barrier();
+    wave_sync();
     for (int g = lane; g < a.groups; g += LPR) {
       Key c1 = none, c2 = none;
       for (int j = 0; j < a.per; ++j) {
@@ -210,16 +218,16 @@ __device__ __forceinline__ bool take_groups(const ChooseArgs& a, Key (&key)[V], 
       }
       total[g] = total_of(c1, c2);
     }
-    __builtin_amdgcn_wave_barrier();
+    wave_sync();
     for (int g = lane; g < a.groups; g += LPR) sm.taken[row][g] = better_than(g, 0, 1) < a.top_groups;
-    __builtin_amdgcn_wave_barrier();
+    wave_sync();
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const int g = min((first + i) * a.per_inverse >> 20, a.groups - 1);
       key[i] = sm.taken[row][g] ? key[i] : none;
     }
   }
-  __builtin_amdgcn_wave_barrier();
+  wave_sync();
   return near_tie;
 }
 
@@ -254,7 +262,7 @@ __device__ __noinline__ void choose_exact(ChooseArgs a, const T* logits, const f
       if (key[i] > none) key[i] = x[i];
   if (store)
     for (int j = lane; j < a.k; j += LPR) sm.index[row][j] = -1;
-  __builtin_amdgcn_wave_barrier();
+  wave_sync();
   for (int j = 0; j < a.k; ++j) {
     double best = key[0];
 #pragma unroll
@@ -272,7 +280,7 @@ __device__ __noinline__ void choose_exact(ChooseArgs a, const T* logits, const f
       if (first + i == e) key[i] = none;
     if (on && store && lane == 0) sm.index[row][j] = e;
   }
-  __builtin_amdgcn_wave_barrier();
+  wave_sync();
 }
 
 // The choice in FP32. Each lane sorts its keys; a round takes the largest head of the row's
@@ -340,18 +348,20 @@ __device__ __forceinline__ bool choose_fast(const ChooseArgs& a, const float (&x
       key[j] = max(k0, k1), key[j + 1] = min(k0, k1);
       index[j] = swap ? i1 : i0, index[j + 1] = swap ? i0 : i1;
     }
+  const int wl = threadIdx.x & 63;
+  auto& sorted = sm.wave[threadIdx.x / 64].sorted;
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    sm.sorted.key[256 * i + threadIdx.x] = key[i];
-    sm.sorted.index[256 * i + threadIdx.x] = index[i];
+    sorted.key[64 * i + wl] = key[i];
+    sorted.index[64 * i + wl] = index[i];
   }
-  sm.sorted.key[256 * V + threadIdx.x] = kNoKey;
+  sorted.key[64 * V + wl] = kNoKey;
   for (int j = lane; j < a.k; j += LPR) sm.index[row][j] = -1;
-  __builtin_amdgcn_wave_barrier();
-  int head = key[0], expert = index[0], at = threadIdx.x;
+  wave_sync();
+  int head = key[0], expert = index[0], at = wl;
   float before = __builtin_inff();
   // the row's lanes below this one
-  const unsigned long long below = ((1ull << lane) - 1) << (threadIdx.x & 63 & ~(LPR - 1));
+  const unsigned long long below = ((1ull << lane) - 1) << (wl & ~(LPR - 1));
   const int rounds = biased ? a.k + 1 : a.k;   // (one more, to see how near the next one came)
   for (int j = 0; j < rounds; ++j) {
     const int best = row_max<LPR>(head);
@@ -365,12 +375,12 @@ __device__ __forceinline__ bool choose_fast(const ChooseArgs& a, const float (&x
     }
     if (has && !(m & below)) {
       if (j < a.k) sm.index[row][j] = expert;
-      at += 256;
-      head = sm.sorted.key[at];
-      expert = sm.sorted.index[at];
+      at += 64;
+      head = sorted.key[at];
+      expert = sorted.index[at];
     }
   }
-  __builtin_amdgcn_wave_barrier();
+  wave_sync();
   return row_any<LPR>(near_tie);
 }
 
@@ -527,13 +537,13 @@ choose_bwd_kernel(ChooseArgs a, const float* __restrict__ dweights, const T* __r
   inner = row_sum<LPR>(inner);
 #pragma unroll
   for (int i = 0; i < V; ++i) sm.d[row][first + i] = 0.f;
-  __builtin_amdgcn_wave_barrier();
+  wave_sync();
   // an expert named twice gets both terms, in their order: seen by whose mark stayed
   bool twice = false;
 #pragma unroll
   for (int p = 0; p < P; ++p)
     if (e[p] >= 0) sm.place[row][e[p]] = lane + p * LPR;
-  __builtin_amdgcn_wave_barrier();
+  wave_sync();
 #pragma unroll
   for (int p = 0; p < P; ++p) {
     if (e[p] >= 0) twice |= sm.place[row][e[p]] != lane + p * LPR;
@@ -549,10 +559,10 @@ choose_bwd_kernel(ChooseArgs a, const float* __restrict__ dweights, const T* __r
     for (int p = 0; p < P; ++p)
       for (int j = 0; j < LPR; ++j) {
         if (lane == j && e[p] >= 0) sm.d[row][e[p]] += v[p];
-        __builtin_amdgcn_wave_barrier();
+        wave_sync();
       }
   }
-  __builtin_amdgcn_wave_barrier();
+  wave_sync();
   if (!live || first >= a.E) return;
   typedef T tv __attribute__((ext_vector_type(V)));
   tv out;

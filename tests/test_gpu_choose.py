@@ -163,6 +163,18 @@ def test_scores_closer_than_their_roundings(scores, groups):
     check(x.expand(50, e).contiguous(), b, torch.randn(50, 8, generator=gen), 8, scores, groups, max(1, groups // 2))
 
 
+@pytest.mark.parametrize("e,groups,top_groups", [(35, 5, 2), (120, 8, 3), (60, 12, 5), (511, 7, 3)])
+def test_rows_that_need_another_decision_among_others(e, groups, top_groups):
+    """Groups that are not whole lanes, every third token with scores that only FP64 tells apart: the
+    waves of a block take different ways and different times."""
+    gen = torch.Generator().manual_seed(e)
+    x = torch.randn(1500, e, generator=gen)
+    s = 1 / (1 + torch.exp(-x[0].double()))
+    b = (0.75 - s).float()
+    x[::3] = x[0]   # s + b = 0.75 up to the rounding of b
+    check(x, b, torch.randn(1500, 4, generator=gen), 4, "sigmoid", groups, top_groups)
+
+
 def test_groups_of_large_biases_that_cancel():
     """Groups of two experts with biases c and -c: their totals are the scores' sums, which FP32 loses
     (a unit of 2^20 is 2^-4), and FP64 keeps to 2^-32."""
