@@ -70,10 +70,15 @@ __global__ void __launch_bounds__(S::NT) linear8_kernel(Linear8Args<T> p) {
 constexpr int kThinRows = 16, kThinCols = 16, kThinLds = 56 << 10;
 // bytes from row to row: 16 more than a multiple of 128, so that eight rows' 16 bytes lie in all banks
 int thin_pitch(int n_in) { return (n_in + 127) / 128 * 128 + 16; }
-int thin_lds(int n_in) { return kThinRows * thin_pitch(n_in); }
+int thin_rows(int64_t n) {   // that a block holds: a power of two of them
+  int r = 1;
+  while (r < n && r < kThinRows) r *= 2;
+  return r;
+}
+int64_t thin_lds(const mace_linear_desc& d) { return (int64_t)thin_rows(d.n_rows) * thin_pitch(d.n_in); }
 
 template <class T, bool AL, bool PACKED>
-__global__ void __launch_bounds__(256) linear8_thin_kernel(Linear8Args<T> p, int n_in, int pitch) {
+__global__ void __launch_bounds__(256) linear8_thin_kernel(Linear8Args<T> p, int n_in, int pitch, int held) {
   extern __shared__ __align__(16) int8_t rows8[];
   __shared__ float scale[kThinRows];
   __shared__ unsigned red[4];
@@ -170,14 +175,15 @@ __global__ void __launch_bounds__(256) linear8_thin_kernel(Linear8Args<T> p, int
     if (t == 0) scale[row] = s;
   }
   __syncthreads();
-  // (rows past the run's are as LDS held them: integers, whose results are not stored)
+  // (rows past the run's are as LDS held them, or the last one's: integers, whose results are not stored)
+  const int8_t* xr = rows8 + min(i, held - 1) * pitch + 16 * g;
   i4 acc = {0, 0, 0, 0};
   for (int k = 64 * wv; k < k16; k += 256 * U) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int at = k + 256 * u;
       if (at < k16)
-        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(wr[u], *reinterpret_cast<const i4*>(rows8 + i * pitch + at + 16 * g), acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(wr[u], *reinterpret_cast<const i4*>(xr + at), acc, 0, 0, 0);
     }
     if (k + 256 * U < k16) load_weights(k + 256 * U);
   }
@@ -228,7 +234,7 @@ mace_status with_shape(int64_t rows, int64_t cols, int64_t groups, F f) {
 // against 9.8, 64 x 512 x 2048 (512) 7.4 against 8.9, 128 x 512 x 2048 (1024) 13.2 against 8.9.
 constexpr int kThinBlocks = 512;
 bool thin(const mace_linear_desc& d) {
-  return thin_lds(d.n_in) <= kThinLds && ceil_div(d.n_rows, kThinRows) * ceil_div(d.n_out, kThinCols) <= kThinBlocks;
+  return thin_lds(d) <= kThinLds && ceil_div(d.n_rows, kThinRows) * ceil_div(d.n_out, kThinCols) <= kThinBlocks;
 }
 template <class T>
 mace_status forward_thin(const mace_linear_desc& d, const Linear8Args<T>& p, bool packed, hipStream_t s) {
@@ -237,7 +243,7 @@ mace_status forward_thin(const mace_linear_desc& d, const Linear8Args<T>& p, boo
   const bool al = aligned16(p.a.x) && ((d.n_in | d.ld_x) & 15) == 0;
   auto f = packed ? linear8_thin_kernel<T, true, true>
                   : (al ? linear8_thin_kernel<T, true, false> : linear8_thin_kernel<T, false, false>);
-  f<<<grid_of(blocks), 256, thin_lds(d.n_in), s>>>(p, d.n_in, thin_pitch(d.n_in));
+  f<<<grid_of(blocks), 256, (unsigned)thin_lds(d), s>>>(p, d.n_in, thin_pitch(d.n_in), thin_rows(d.n_rows));
   return launched();
 }
 

@@ -158,6 +158,13 @@ def test_linear(n, k, m, dtype):
     check_linear(n, k, m, dtype, bias=False, residual=False)
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n,k,m", [(1, 50000, 40), (1, 8192, 1100), (2, 20001, 33), (3, 9000, 50), (7, 6100, 40), (9, 3000, 70),
+                                   (16, 3500, 30), (5, 60000, 20)])
+def test_linear_few_rows_of_long_sums(n, k, m, dtype):
+    check_linear(n, k, m, dtype, "silu")
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
 @pytest.mark.parametrize("sizes,tail", [([5], 0), ([0, 3, 0, 0, 70, 1], 0), ([0, 0], 9), ([64, 64, 128], 0), ([1] * 70 + [40], 11),
                                         ([129, 0, 257], 65), ([700, 3], 0)])
