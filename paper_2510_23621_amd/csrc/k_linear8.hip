@@ -100,15 +100,13 @@ __global__ void __launch_bounds__(256) linear8_thin_kernel(Linear8Args<T> p, int
   const int8_t* w = reinterpret_cast<const int8_t*>(a.w) + (w_row + min(i, cols - 1)) * 2 * p.ldw + 16 * g;
   constexpr int U = 8;   // steps of 64 products' indices in flight
   i4 wr[U];
-  auto load_weights = [&](int k) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int at = k + 256 * u;
-      wr[u] = i4{0, 0, 0, 0};
-      if (at + 16 * g < k16) wr[u] = *reinterpret_cast<const i4*>(w + at);
-    }
+  auto weights = [&](int at) {
+    i4 q = {0, 0, 0, 0};
+    if (at + 16 * g < k16) q = *reinterpret_cast<const i4*>(w + at);
+    return q;
   };
-  load_weights(64 * wv);
+#pragma unroll
+  for (int u = 0; u < U; ++u) wr[u] = weights(64 * wv + 256 * u);
   // what the epilogue adds, requested before the rows too
   const int n = 4 * g, count = min(4, cols - n);
   typedef T t4 __attribute__((ext_vector_type(4)));
@@ -182,10 +180,11 @@ __global__ void __launch_bounds__(256) linear8_thin_kernel(Linear8Args<T> p, int
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int at = k + 256 * u;
-      if (at < k16)
+      if (at < k16) {
         acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(wr[u], *reinterpret_cast<const i4*>(xr + at), acc, 0, 0, 0);
+        wr[u] = weights(at + 256 * U);
+      }
     }
-    if (k + 256 * U < k16) load_weights(k + 256 * U);
   }
   part[tid] = acc;
   __syncthreads();
