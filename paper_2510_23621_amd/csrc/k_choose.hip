@@ -146,8 +146,8 @@ struct ChooseLds {
   int index[S::ROWS][S::K];   // the choice
 };
 
-// Of a token's keys those outside its top_groups best groups become no_key. True: two
-// groups' totals differ by at most tol.
+// Of a token's keys those outside its top_groups best groups become no_key. True: two groups' totals
+// differ by at most tol and a few units of the largest of their parts, which may cancel.
 template <class Key, int LPR, int V>
 __device__ __forceinline__ bool take_groups(const ChooseArgs& a, Key (&key)[V], float tol, int lane, int row, ChooseLds<LPR, V>& sm) {
   using R = decltype(value_of(Key{}));
@@ -156,10 +156,14 @@ __device__ __forceinline__ bool take_groups(const ChooseArgs& a, Key (&key)[V], 
   const int first = lane * V;
   R* total = reinterpret_cast<R*>(sm.total[row]);
   bool near_tie = false;
+  float part = 0.f;
   auto total_of = [&](Key c1, Key c2) {
-    const R t = value_of(c1);
-    return c2 > none ? t + value_of(c2) : (c1 > none ? t : empty);
+    const R v1 = value_of(c1), v2 = value_of(c2);
+    if (c1 > none) part = fmaxf(part, fabsf((float)v1));
+    if (c2 > none) part = fmaxf(part, fabsf((float)v2));
+    return c2 > none ? v1 + v2 : (c1 > none ? v1 : empty);
   };
+  auto add_units = [&] { tol = __builtin_fmaf(__int_as_float(row_max<LPR>(__float_as_int(part))), 4.7683716e-7f, tol); };
   // groups before g in the order of their totals, of those from h0 on in steps
   auto better_than = [&](int g, int h0, int step) {
     const R mine = total[g];
@@ -193,7 +197,9 @@ __device__ __forceinline__ bool take_groups(const ChooseArgs& a, Key (&key)[V], 
       c2 = max_of(min_of(a1, b1), max_of(a2, b2));
     });
     const int g = min(first * a.per_inverse >> 20, a.groups - 1);
-    if (first == g * a.per) total[g] = total_of(c1, c2);
+    const R sum = total_of(c1, c2);
+    if (first == g * a.per) total[g] = sum;
+    add_units();
     wave_sync();
     int better = better_than(g, lane & (a.group_lanes - 1), a.group_lanes);   // the group's lanes share the others
     over_group([&](auto step) {
@@ -218,6 +224,7 @@ __device__ __forceinline__ bool take_groups(const ChooseArgs& a, Key (&key)[V], 
       }
       total[g] = total_of(c1, c2);
     }
+    add_units();
     wave_sync();
     for (int g = lane; g < a.groups; g += LPR) sm.taken[row][g] = better_than(g, 0, 1) < a.top_groups;
     wave_sync();
@@ -292,10 +299,10 @@ __device__ __noinline__ void choose_exact(ChooseArgs a, const T* logits, const f
 // largest such argument and M = 1 / sum (or 1) the largest score there can be; s + b adds half a unit
 // of itself. Two keys may differ by twice that, two groups' totals by four times, and by the
 // roundings of two sums.
-template <int LPR, int V>
+// b: the bias, -infinity for masked experts.
+template <bool SIGMOID, int LPR, int V>
 __device__ __forceinline__ bool choose_fast(const ChooseArgs& a, const float (&x)[V], const float (&b)[V], bool biased, float top,
                                             int lane, int row, bool& bad, ChooseLds<LPR, V>& sm) {
-  const float none = -__builtin_inff();
   constexpr float kLog2e = 1.44269502162933349609375f;
   int key[V];
   float tol = 0.f;
@@ -304,34 +311,31 @@ __device__ __forceinline__ bool choose_fast(const ChooseArgs& a, const float (&x
 #pragma unroll
     for (int i = 0; i < V; ++i) key[i] = key_of(x[i] + 0.f);
   if (biased || a.groups > 1) {   // (otherwise the logits decide, exactly)
+    const float base = top > -__builtin_inff() ? top : 0.f;
     float s[V], sum = 0.f;
     int arg = 0;   // of values that are not negative, in the order of their bits
 #pragma unroll
     for (int i = 0; i < V; ++i) {   // (masked: the argument is infinite, s 0)
-      const float d = a.sigmoid ? -x[i] : x[i] - top;
-      const float e = __builtin_amdgcn_exp2f(d * kLog2e);
-      s[i] = a.sigmoid ? __builtin_amdgcn_rcpf(1.f + e) : e;
+      const float d = SIGMOID ? x[i] : x[i] - base;
+      const float e = __builtin_amdgcn_exp2f(d * (SIGMOID ? -kLog2e : kLog2e));
+      s[i] = SIGMOID ? __builtin_amdgcn_rcpf(1.f + e) : e;
       sum += s[i];
       arg = max(arg, __float_as_int(fabsf(d)));
     }
     float unit = 1.f;
-    if (!a.sigmoid) unit = __builtin_amdgcn_rcpf(row_sum<LPR>(sum));
+    if constexpr (!SIGMOID) {
+      sum = row_sum<LPR>(sum);
+      unit = sum > 0.f ? __builtin_amdgcn_rcpf(sum) : 0.f;   // (nothing but masked experts)
+    }
     int scored[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const float c = __builtin_fmaf(s[i], unit, b[i]);
-      const bool on = x[i] > none;
-      bad |= on && c != c;
-      scored[i] = key_of(on ? c : none);
+      const float c = SIGMOID ? s[i] + b[i] : __builtin_fmaf(s[i], unit, b[i]);
+      bad |= c != c;
+      scored[i] = key_of(c);
     }
     tol = (fminf(__int_as_float(row_max<LPR>(arg)), 100.f) + 40.f) * unit * 1.1920929e-7f + 1e-36f;
-    if (a.groups > 1) {
-      int big = 0;   // a total is off by the roundings of its parts too, which may cancel
-#pragma unroll
-      for (int i = 0; i < V; ++i) big = max(big, scored[i] > kNoKey ? __float_as_int(fabsf(value_of(scored[i]))) : 0);
-      const float units = __int_as_float(row_max<LPR>(big)) * 4.7683716e-7f;
-      near_tie = take_groups<int, LPR, V>(a, scored, 2 * tol + units, lane, row, sm);
-    }
+    if (a.groups > 1) near_tie = take_groups<int, LPR, V>(a, scored, 2 * tol, lane, row, sm);
 #pragma unroll
     for (int i = 0; i < V; ++i)   // (without a bias the logits decide within the groups)
       key[i] = biased ? scored[i] : (scored[i] > kNoKey ? key[i] : kNoKey);
@@ -390,7 +394,7 @@ __device__ __forceinline__ bool choose_fast(const ChooseArgs& a, const float (&x
 // experts in 4 of 8 groups, 41 us, the vector units busy 68 % of it with 900 instructions for two tokens, of which
 // the lanes' sorting takes 150, nine rounds 220, scores and masks 200, groups 110, weights 60; the 38 MB of
 // logits would take 7.5.
-template <class T, int LPR, int V>
+template <class T, bool SIGMOID, int LPR, int V>
 __global__ void __launch_bounds__(256)
 choose_kernel(ChooseArgs a, const T* __restrict__ logits, const float* __restrict__ bias, int* __restrict__ expert,
               float* __restrict__ weights) {
@@ -408,23 +412,25 @@ choose_kernel(ChooseArgs a, const T* __restrict__ logits, const float* __restric
   for (int i = 0; i < V; ++i) b[i] = 0.f;
   if (bias) load_row<V>(bias, lane * V, a.E, 0.f, b);
   bool bad = false;
-  const float largest = a.sigmoid ? __builtin_inff() : 3.4028234663852886e38f;
+  constexpr float largest = SIGMOID ? __builtin_inff() : 3.4028234663852886e38f;
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     bad |= !(x[i] <= largest);
-    x[i] = x[i] > lowest<T>() ? x[i] : none;
+    const bool on = x[i] > lowest<T>();
+    x[i] = on ? x[i] : none;
+    b[i] = on ? b[i] : none;
   }
   float top = none;
-  if (!a.sigmoid) {
+  if constexpr (!SIGMOID) {
 #pragma unroll
     for (int i = 0; i < V; ++i) top = fmaxf(top, x[i]);
     top = row_max<LPR>(top);
   }
-  const bool again = choose_fast<LPR, V>(a, x, b, bias != nullptr, top, lane, row, bad, sm);
+  const bool again = choose_fast<SIGMOID, LPR, V>(a, x, b, bias != nullptr, top, lane, row, bad, sm);
   if (__any(again)) choose_exact<T, LPR, V>(a, logits + at * a.ld, bias, top, lane, row, again, sm);
   bad = row_any<LPR>(bad);
   float norm = 0.f;   // sum of exp(x - top) of the softmax
-  if (!a.sigmoid && !a.normalise) {
+  if (!SIGMOID && !a.normalise) {
 #pragma unroll
     for (int i = 0; i < V; ++i) norm += x[i] > none ? exp_minus(top - x[i]) : 0.f;
     norm = row_sum<LPR>(norm);
@@ -440,13 +446,13 @@ choose_kernel(ChooseArgs a, const T* __restrict__ logits, const float* __restric
     most = fmaxf(most, v[p]);
   }
   most = row_max<LPR>(most);
-  if (a.sigmoid) most = fminf(most, 0.f);
+  if (SIGMOID) most = fminf(most, 0.f);
 #pragma unroll
   for (int p = 0; p < P; ++p) {
     if (p * LPR >= a.k) break;
     if (!(v[p] > none)) v[p] = 0.f;
-    else if (a.normalise) v[p] = relative_score(v[p], most, a.sigmoid);
-    else v[p] = a.sigmoid ? sigmoid_of(v[p]) : exp_minus(top - v[p]) / norm;
+    else if (a.normalise) v[p] = relative_score(v[p], most, SIGMOID);
+    else v[p] = SIGMOID ? sigmoid_of(v[p]) : exp_minus(top - v[p]) / norm;
     total += v[p];
   }
   total = a.normalise ? row_sum<LPR>(total) : 1.f;
@@ -624,8 +630,8 @@ extern "C" mace_status mace_choose_forward(const mace_choose_desc* desc, const v
     return with_row(desc->n_experts, [&](auto lpr, auto v) {
       constexpr int LPR = decltype(lpr)::value, V = decltype(v)::value, rows = ChooseShape<LPR, V>::ROWS;
       const ChooseArgs a = args_of(*desc, V);
-      choose_kernel<T, LPR, V><<<grid_of((a.n + rows - 1) / rows), 256, 0, (hipStream_t)stream>>>(a, (const T*)logits, bias,
-                                                                                                 expert, weights);
+      auto f = a.sigmoid ? choose_kernel<T, true, LPR, V> : choose_kernel<T, false, LPR, V>;
+      f<<<grid_of((a.n + rows - 1) / rows), 256, 0, (hipStream_t)stream>>>(a, (const T*)logits, bias, expert, weights);
       return launched();
     });
   });
