@@ -391,9 +391,10 @@ __device__ __forceinline__ bool choose_fast(const ChooseArgs& a, const float (&x
 // LPR lanes per token, V consecutive experts each. Scores in FP32; the few rows where a decision lies
 // within their error are decided again in FP64 (0.9 % of the rows below, a second pass for 1.8 % of the
 // waves; all of it in FP64, the first form, took 254 us). Bound by instructions: 36,864 tokens, 8 of 256
-// experts in 4 of 8 groups, 41 us, the vector units busy 68 % of it with 900 instructions for two tokens, of which
-// the lanes' sorting takes 150, nine rounds 220, scores and masks 200, groups 110, weights 60; the 38 MB of
-// logits would take 7.5.
+// experts in 4 of 8 groups, 35.5 us, the vector units busy 68 % of it with 810 instructions for two tokens, of which
+// the lanes' sorting takes 150, nine rounds 220, scores and masks 200, groups 95, weights 60; the 38 MB of
+// logits would take 7.5. 16 lanes of 16 experts take 45 where 32 of 8 take 41, 64 of 4 48; one kernel for both
+// scores 41.
 template <class T, bool SIGMOID, int LPR, int V>
 __global__ void __launch_bounds__(256)
 choose_kernel(ChooseArgs a, const T* __restrict__ logits, const float* __restrict__ bias, int* __restrict__ expert,
