@@ -265,6 +265,8 @@ bool aligned(const mace_embed_desc& d, const void* a, const void* b) {
 size_t round256(size_t b) { return (b + 255) & ~size_t(255); }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// Slots a block of the sort takes at a time: 131,072 ids of 32,000 rows 131.5 us for the whole gradient, with 1024
+// 139.8 (more blocks' counts to read), with 4096 134.8 (fewer CUs); 262,144 ids of 2 rows 36.3, 35.5, 40.0.
 constexpr int kChunk = 2048;
 // Digits of the sort: ids and the number behind them, at most nine bits a pass.
 struct SortPlan {

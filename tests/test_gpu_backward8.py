@@ -152,6 +152,27 @@ def test_gradient_against_differences():
     assert (dx == 0).all()
 
 
+def test_offsets_beyond_32_bits():
+    """More than 2^31 elements of x8, of its 16-bit operand and of dx."""
+    n, k, m = (1 << 20) + 77, 2064, 24
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    x, z, dy = (torch.zeros(n, c, dtype=torch.bfloat16, device="cuda") for c in (k, m, m))
+    for t in (x, z, dy):
+        t[-50:] = torch.randn(50, t.shape[1], generator=gen, device="cuda").bfloat16()
+    w = (torch.randn(k, m, generator=gen, device="cuda") * k ** -0.5).bfloat16()
+    x8, z8 = L.pack_rows(x), L.pack_rows(z)
+    assert x8.values.numel() > 1 << 31
+    dx, dw, db = L.linear_backward8(dy, x8, w, z8, act="silu")
+    tail = [L.pack_rows(t[-50:].contiguous()) for t in (x, z)]
+    want = L.linear_backward8(dy[-50:].contiguous(), tail[0], w, tail[1], act="silu")
+    assert torch.equal(dx[-50:], want[0]) and not dx[:-50].any()
+    X, dz = stands_for(tail[0]), dy[-50:].cpu().double() * slope64(stands_for(tail[1]), "silu")
+    DW, mag = X.t() @ dz, X.abs().t() @ dz.abs()
+    u = U["bf16"]   # dz's rounding and the result's, and FP32 sums of 50 terms that are not zero
+    within(dw, DW, (u * (1 + 2 * u) + 64 * U32) * mag + u * DW.abs() + TINY["bf16"], "dw")
+    within(db, dz.sum(0), 100 * U32 * dz.abs().sum(0) + u * dz.sum(0).abs() * (1 + u), "db")
+
+
 def test_captured_beside_an_eager_graph():
     x, z, w, dy = (torch.randn(*s, device="cuda").bfloat16() for s in [(2000, 96), (2000, 64), (2, 96, 64), (2000, 64)])
     off = torch.tensor([0, 700, 1990], dtype=torch.int32, device="cuda")

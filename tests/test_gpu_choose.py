@@ -251,6 +251,24 @@ def test_experts_out_of_range_take_no_part():
 
 @pytest.mark.parametrize("scores", ["softmax", "sigmoid"])
 @pytest.mark.parametrize("normalise", [True, False])
+def test_an_expert_named_twice_gets_both_terms(scores, normalise):
+    """dlogits of sum_j g_j w_j by FP64 autograd, with the scores of the experts as named."""
+    gen = torch.Generator().manual_seed(11)
+    x, dw = torch.randn(33, 40, generator=gen), torch.randn(33, 6, generator=gen)
+    expert = torch.randint(0, 5, (33, 6), generator=gen, dtype=torch.int32)
+    expert[0] = 7
+    l = x.double().requires_grad_()
+    s = (torch.sigmoid(l) if scores == "sigmoid" else torch.softmax(l, 1)).gather(1, expert.long())
+    w = s / s.sum(1, keepdim=True) if normalise else s
+    (w * dw.double()).sum().backward()
+    got = L.choose_experts_backward(dw.cuda(), x.cuda(), expert.cuda(), scores=scores, normalise=normalise)
+    assert torch.equal(got, L.choose_experts_backward(dw.cuda(), x.cuda(), expert.cuda(), scores=scores, normalise=normalise))
+    size = (w.detach() * (dw.double().abs() + (w.detach() * dw.double().abs()).sum(1, keepdim=True))).sum(1, keepdim=True)
+    assert ((got.cpu().double() - l.grad).abs() <= 4 * (40 + 16 + 20) * U32 * size).all()
+
+
+@pytest.mark.parametrize("scores", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("normalise", [True, False])
 def test_gradient_against_differences(scores, normalise):
     """Central differences of sum(c w) along a random direction, with the experts held:
     h = 2^-7 leaves rounding (12 experts, 2^-24 * 40 / h) and truncation (h^2 / 6 times third
