@@ -104,6 +104,12 @@ def test_many_rows(n, n_in, n_out, sizes, dtype):
     case(n, n_in, n_out, dtype, "silu", sizes)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_short_sums_over_many_rows(dtype):
+    """dx as the form with weights in registers gives it (1026 runs of 512 rows, 64 columns)."""
+    case(525000, 64, 24, dtype, "silu")
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
 def test_same_as_the_layer_at_the_unpacked_input(dtype):
     """Without an activation it is linear_backward at the unpacked rows, bit for bit."""
