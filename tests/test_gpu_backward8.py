@@ -105,6 +105,14 @@ def test_many_rows(n, n_in, n_out, sizes, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("n,n_in,n_out,sizes", [(12288, 1024, 64, None), (12300, 1032, 72, None), (None, 1024, 64, [6000, 0, 6300]),
+                                                (1500, 1024, 1048, None)])
+def test_wide_tiles(n, n_in, n_out, sizes, dtype):
+    """dx, or dW, in 256 x 256 tiles."""
+    case(n, n_in, n_out, dtype, "gelu", sizes)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 def test_short_sums_over_many_rows(dtype):
     """dx as the form with weights in registers gives it (1026 runs of 512 rows, 64 columns)."""
     case(525000, 64, 24, dtype, "silu")
