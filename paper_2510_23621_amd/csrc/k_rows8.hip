@@ -18,7 +18,7 @@ struct Rows8Args {
 // lg lanes (a power of two up to a block) a row, 16 columns at a time: its largest magnitude, then its
 // integers. CH: chunks of columns that a lane holds between the two, 0: any number, read twice.
 // 36,864 x 2048 bfloat16: 44 to 46 us, 5.0 TB/s, a copy's rate; with an exact rounding of every column and the
-// rows read twice 60.
+// rows read twice, as those past 8192 columns are, 60.
 template <class T, bool AL, int CH>
 __global__ void __launch_bounds__(256) pack_rows_kernel(Rows8Args a, const T* __restrict__ x, int8_t* __restrict__ values,
                                                         float* __restrict__ scales) {
