@@ -190,9 +190,9 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(EmbedGradArgs a, const T
   flush(key == after);
 }
 
-// Runs that cross segments are joined by the block of the segment they begin in: blocks of
-// JS segments and cl lanes of four columns each. The JT / cl groups of lanes take a short run each; a long one's parts are shared among all groups, contiguous
-// ones each, and the groups' sums added in order.
+// Runs that cross segments are joined by the block of the segment they begin in: blocks of JS segments
+// and cl lanes of four columns each. The JT / cl groups of lanes take a short run each; a long one's
+// parts are shared among all groups, contiguous ones each, and the groups' sums added in order.
 constexpr int kShortRun = 8;
 template <class T, int JT, int JS>
 __global__ void __launch_bounds__(JT) embed_join_kernel(EmbedGradArgs a, int cl, int col_blocks, T* __restrict__ dtable) {
