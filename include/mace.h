@@ -500,8 +500,9 @@ mace_status mace_linear8_forward(const mace_linear_desc* desc, const void* x8, c
  * desc->ld_preact are their leading dimensions, multiples of 16): the gradients
  * at x = q s and z = q s.  Weights, dy and the gradients are of dtype as there.
  * Of 16-bit types the products' operands are, with an activation, the integers
- * times powers of two (exact) and dz with the rest of x's scales, rounded; without
- * one x rounded to dtype, and dy.  z8 and z_scales are not read and may be NULL
+ * times powers of two (exact) and dz with the rest of x's scales, rounded (in a row
+ * of more than 127 2^9 in binary16 or 127 2^121 in bfloat16 x rounded to dtype, infinite
+ * where that is, and dz); without an activation x rounded to dtype, and dy.  z8 and z_scales are not read and may be NULL
  * without an activation, x8 and x_scales without dweights (dx is then rounded
  * otherwise than with x_scales). */
 size_t mace_linear_backward8_workspace_bytes(const mace_linear_desc* desc, int32_t want_bias, int32_t want_weights);

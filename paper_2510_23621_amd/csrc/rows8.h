@@ -31,15 +31,15 @@ __device__ __forceinline__ unsigned round8(float x, float s, float inv) {
 // (inv of a scale next to the smallest is finite; of NaN it is NaN, and the row's values are 0)
 __device__ __forceinline__ float inverse8(float s) { return 1.f / s; }
 
-// A row's scale as a power of two, with which its integers are exact numbers of T, and a factor in
-// (0.5, 1] (up to 1.01 where the larger power would take 127 of it past T's range; 1 for NaN).
+// A row's scale as a power of two, with which its integers are exact numbers of T, and the rest, a
+// factor in (0.5, 1]. Where 127 of the power are beyond T's range (NaN too) the scale itself and 1: its
+// products with the integers are rounded to T, and what the factor multiplies stays as it is.
 template <class T>
 __device__ __forceinline__ void split_scale8(float s, float& power, float& factor) {
-  const int bits = __float_as_int(s);
-  int e = (bits >> 23) + ((bits & 0x7fffff) != 0);   // (a scale is positive and normal)
-  e = min(e, 127 + (__is_same(T, _Float16) ? 9 : 121));
-  power = s == s ? __int_as_float(e << 23) : s;
-  factor = s == s ? s / power : 1.f;
+  const int bits = __float_as_int(s), e = (bits >> 23) + ((bits & 0x7fffff) != 0);   // (a scale is positive and normal)
+  const bool exact = e <= 127 + (__is_same(T, _Float16) ? 9 : 121);
+  power = exact ? __int_as_float(e << 23) : s;
+  factor = exact ? s / power : 1.f;
 }
 
 // columns 16 c .. 16 c + 15 of a row, zeros past the last (AL: there are none)
