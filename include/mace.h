@@ -500,11 +500,12 @@ mace_status mace_linear8_forward(const mace_linear_desc* desc, const void* x8, c
  * desc->ld_preact are their leading dimensions, multiples of 16): the gradients
  * at x = q s and z = q s.  Weights, dy and the gradients are of dtype as there.
  * Of 16-bit types the products' operands are, with an activation, the integers
- * times powers of two (exact) and dz with the rest of x's scales, rounded (in a row
- * of more than 127 2^9 in binary16 or 127 2^121 in bfloat16 x rounded to dtype, infinite
- * where that is, and dz); without an activation x rounded to dtype, and dy.  z8 and z_scales are not read and may be NULL
- * without an activation, x8 and x_scales without dweights (dx is then rounded
- * otherwise than with x_scales). */
+ * times powers of two (exact) and dz with the rest of x's scales, rounded; but x
+ * rounded to dtype (infinite where that is) and dz in the rows of more than 127 2^9
+ * in binary16 or 127 2^121 in bfloat16, or with a scale of 2^-25 or less in binary16.
+ * Without an activation they are x rounded to dtype, and dy. z8 and z_scales are not
+ * read and may be NULL without an activation, x8 and x_scales without dweights (dx is
+ * then rounded otherwise than with x_scales). */
 size_t mace_linear_backward8_workspace_bytes(const mace_linear_desc* desc, int32_t want_bias, int32_t want_weights);
 mace_status mace_linear_backward8(const mace_linear_desc* desc, const void* dy, int64_t ld_dy, const void* x8,
                                   const float* x_scales, const void* weights, const void* z8, const float* z_scales,

@@ -98,3 +98,30 @@ def test_weights_gradient_of_largest_rows(dtype):
     x8 = L.pack_rows(x.cuda())
     assert (x8.scales.cpu() > big / 128).all()   # above the largest power of two whose 127-fold the type holds
     check(x8, dy, w, dtype, U[dtype] * stands_for(x8).abs())
+
+
+@pytest.mark.parametrize("n", [1, 4, 16])
+@pytest.mark.parametrize("size", [1e-7, 3e-7, 1e-6, 3e-6, 4e-6, 1e-5])
+def test_weights_gradient_of_smallest_binary16_rows(size, n):
+    """Rows down to binary16's smallest numbers. From scales of 2^-25 up the integers times a power
+    of two are exact; below, x is rounded to binary16: the numbers that the rows were packed from lie
+    within half a scale of q s, and the nearest number does at the most."""
+    gen = torch.Generator().manual_seed(3)
+    x = ((torch.rand(n, 60, generator=gen) - 0.5) * 2 * size).half()
+    x[:, 5] = size
+    dy = (2000 * torch.randn(n, 48, generator=gen)).half()
+    w = (torch.randn(60, 48, generator=gen) * 0.01).half()
+    x8 = L.pack_rows(x.cuda())
+    X, s = stands_for(x8), x8.scales.double().cpu()[:, None].expand(n, 60)
+    ex = torch.where(s > 2.0 ** -25, 0 * s, (s / 2 * (1 + 2.0 ** -20)).clamp_max(2.0 ** -25) + 2 * U32 * X.abs())
+    check(x8, dy, w, "fp16", ex)
+
+
+def test_rows_below_binary16():
+    """Rows of 1e-9 to 1e-12 packed from float32: x is zero in binary16, and dx and db what they are."""
+    gen = torch.Generator().manual_seed(4)
+    x = torch.randn(30, 40, generator=gen) * 10.0 ** -torch.linspace(9, 12, 30)[:, None]
+    dy = (2000 * torch.randn(30, 24, generator=gen)).half()
+    w = (torch.randn(40, 24, generator=gen) * 0.01).half()
+    x8 = L.pack_rows(x.cuda())
+    check(x8, dy, w, "fp16", torch.full((30, 40), 2.0 ** -25, dtype=torch.float64))
