@@ -14,6 +14,19 @@ struct Linear8Args {
   int64_t ldw;   // in pairs
 };
 
+// sum sx sw + b for an integer sum (below 2^31). Its product with sx stays within FP32 up to 2^96; in a row
+// with a larger scale (`large`) the smaller of the two scales comes first, so that no
+// product is out of range unless the last one is. (Scales in the order of their bits, NaN last.)
+constexpr float kLargeScale8 = 79228162514264337593543950336.f;   // 2^96
+__device__ __forceinline__ float scaled8(int sum, float sx, float sw, float b, bool large) {
+  float lo = sx, hi = sw;
+  if (large) {
+    lo = __int_as_float(min(__float_as_int(sx), __float_as_int(sw)));
+    hi = __int_as_float(max(__float_as_int(sx), __float_as_int(sw)));
+  }
+  return __builtin_fmaf((float)sum * lo, hi, b);
+}
+
 // y = act(sx sw (qx qw) + b) + r: exact integer sums on v_mfma_i32_16x16x64_i8, through the
 // tiles of the 16-bit layers, which move the same bytes per instruction. 36864 x 2048 x 2048 in eight groups to
 // bfloat16: 168 us bare (1.84 POP/s, where a library product of that size reaches 1.65 and a larger one
@@ -39,10 +52,20 @@ __global__ void __launch_bounds__(S::NT) linear8_kernel(Linear8Args<T> p) {
   f4 acc[S::TN][S::TM];
   const IntPair *x = reinterpret_cast<const IntPair*>(a.x) + run.row0 * a.ldx;
   const IntPair *w = reinterpret_cast<const IntPair*>(a.w) + w_row * p.ldw;
+  const int l = tid & 63, wv = tid >> 6;
+  // the wave's rows' scales, whether one is large: requested before the products, and two forms of the
+  // results (a branch for every row's values, or on scales requested after the products: 265 us where this takes 251)
+  constexpr int WR = S::BM / S::WM;
+  float row_scale[(WR + 63) / 64];
+#pragma unroll
+  for (int i = 0; i < (WR + 63) / 64; ++i)
+    row_scale[i] = p.xs[run.row0 + min(wv / S::WN * WR + min(64 * i + l, WR - 1), run.rows - 1)];
   tile_gemm_direct<IntPair, S, true, true>({x, a.ldx, run.rows, 0}, {w, p.ldw, cols, 0}, a.n_in, lds, tid, acc);
   constexpr int W = lane_width<T>, NV = lane_vectors<S::TN, W>;
-  const int l = tid & 63, wv = tid >> 6;
-  const int m0 = (wv / S::WN) * (S::BM / S::WM) + (l & 15), n0 = (wv % S::WN) * (S::BN / S::WN);
+  bool large = false;
+#pragma unroll
+  for (float s : row_scale) large |= !(s <= kLargeScale8);
+  const int m0 = (wv / S::WN) * WR + (l & 15), n0 = (wv % S::WN) * (S::BN / S::WN);
   using V = typename Floats<W>::type;
   float xs[S::TM];
   V ws[NV];
@@ -54,12 +77,16 @@ __global__ void __launch_bounds__(S::NT) linear8_kernel(Linear8Args<T> p) {
     ws[j] = V{};
     if (n < cols) ws[j] = read_n<W>(p.ws + w_row + n, min(W, cols - n), false);
   }
-  linear_epilogue<T, AL, S, sizeof(T) == 2 ? 4 : 2, sizeof(T) == 2>(a, run, c0, cols, y, (T*)nullptr, tid, [&](int j, int i, V b) {
-    V v = lane_values<W>(acc, j, i);
+  auto finish = [&](auto any_large) {
+    linear_epilogue<T, AL, S, sizeof(T) == 2 ? 4 : 2, sizeof(T) == 2>(a, run, c0, cols, y, (T*)nullptr, tid, [&](int j, int i, V b) {
+      V v = lane_values<W>(acc, j, i);
 #pragma unroll
-    for (int q = 0; q < W; ++q) v[q] = __builtin_fmaf((float)__float_as_int(v[q]) * xs[i], ws[j][q], b[q]);
-    return v;
-  });
+      for (int q = 0; q < W; ++q) v[q] = scaled8(__float_as_int(v[q]), xs[i], ws[j][q], b[q], any_large.value && !(xs[i] <= kLargeScale8));
+      return v;
+    });
+  };
+  if (__any(large)) finish(Int<1>{});
+  else finish(Int<0>{});
 }
 
 // Few rows: a block of four waves forms 16 x 16 results, each wave a quarter of K, added through LDS.
@@ -193,7 +220,7 @@ __global__ void __launch_bounds__(256) linear8_thin_kernel(Linear8Args<T> p, int
   f4 v;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    v[e] = __builtin_fmaf((float)acc[e] * scale[i], ws[e], bias[e]);
+    v[e] = scaled8(acc[e], scale[i], ws[e], bias[e], !(scale[i] <= kLargeScale8));
     v[e] = a.act == MACE_ACT_SILU ? activate_as<MACE_ACT_SILU, sizeof(T) == 2>(v[e])
                                   : (a.act == MACE_ACT_GELU ? activate<MACE_ACT_GELU>(v[e]) : v[e]);
   }
