@@ -458,10 +458,10 @@ mace_status mace_choose_backward(const mace_choose_desc* desc, const float* dwei
                                  const int32_t* expert, void* dlogits, int64_t ld_dlogits, void* stream);
 
 /* Rows of 8-bit integers: x_ij stands as q_ij s_i with s_i = max_j |x_ij| / 127
- * rounded to FP32 (at least 2^-126) and q_ij the integer nearest to x_ij / s_i
- * (the exact quotient; halves to the even one), -127 .. 127.  A row with a
- * non-finite element gets the scale NaN and zeros.  values (dev) int8
- * [n_rows][ld_values]: 16-byte aligned, ld_values a multiple of 16 and at least
+ * rounded to FP32 (at least 2^-126, and such that 127 s_i is finite) and q_ij the
+ * integer nearest to x_ij / s_i (the exact quotient; halves to the even one),
+ * -127 .. 127.  A row with a non-finite element gets the scale NaN and zeros.
+ * values (dev) int8 [n_rows][ld_values]: 16-byte aligned, ld_values a multiple of 16 and at least
  * n_cols, with zeros in the columns from n_cols to the next multiple of 16;
  * scales (dev) FP32 [n_rows].
  * mace_unpack_rows gives q s in FP32, rounded once to dtype.  n_rows <= 2^30,

@@ -9,10 +9,12 @@ constexpr int kMaxColumns8 = 1 << 17;   // 127 * 127 * 2^17 < 2^31: sums of prod
 constexpr int64_t kMaxPitch8 = 1 << 20;       // a tile's rows lie within 32-bit byte offsets
 constexpr float kSmallestScale8 = 1.17549435082228751e-38f;   // 2^-126
 
+constexpr float kLargestScale8 = 2.67938838901875044e+36f;   // 127 of the next number are infinite
+
 // Scale of a row whose largest magnitude is m; NaN for an infinite one and for NaN.
-// The division is IEEE's, so the scale is the rounded quotient.
+// The division is IEEE's, so the scale is the rounded quotient (of FP32's largest number the one below it).
 __device__ __forceinline__ float scale8(float m) {
-  return m < __builtin_inff() ? fmaxf(m / 127.f, kSmallestScale8) : __builtin_nanf("");
+  return m < __builtin_inff() ? fminf(fmaxf(m / 127.f, kSmallestScale8), kLargestScale8) : __builtin_nanf("");
 }
 
 // The integer nearest to x / s, halves to even, with inv about 1 / s. x inv + 1.5 2^23 rounds the
