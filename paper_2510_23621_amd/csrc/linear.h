@@ -23,16 +23,18 @@ __device__ __forceinline__ float normal_cdf(float z, float& e) {
   const float h = 0.5f * t * p * e;   // Phi(-|z|)
   return z > 0.f ? 1.f - h : h;
 }
+// act(z) = z gate(z)
+template <int ACT>
+__device__ __forceinline__ float gate(float z) {
+  // 1 / (1 + exp(-z)). exp_neg takes -88 at the least, and infinity not at all: above 88
+  // it is 1, below -88 (where z times it is under 2^-120) 0; -infinity times that is NaN, as with GELU
+  if constexpr (ACT == MACE_ACT_SILU) return z < -88.f ? 0.f : recip_ge1(1.f + exp_neg(fminf(z, 88.f)));
+  float e;
+  return normal_cdf(z, e);
+}
 template <int ACT>
 __device__ __forceinline__ float activate(float z) {
-  // z / (1 + exp(-z)). exp_neg takes -88 at the least, and infinity not at all: above 88
-  // the quotient is z, below -88 (where it is under 2^-120) z 0, NaN at -infinity as GELU
-  if constexpr (ACT == MACE_ACT_SILU) return z * (z < -88.f ? 0.f : recip_ge1(1.f + exp_neg(fminf(z, 88.f))));
-  if constexpr (ACT == MACE_ACT_GELU) {
-    float e;
-    return z * normal_cdf(z, e);
-  }
-  return z;
+  return ACT == MACE_ACT_NONE ? z : z * gate<ACT>(z);
 }
 // act'(z); beyond |z| = 88 the slopes are 0 and 1 to FP32, and z (1 - s) would
 // be inf 0 at an infinite z
@@ -59,21 +61,32 @@ __device__ __forceinline__ void zero_rows(T* y, int64_t ld, int rows, int cols, 
   for (int i = tid; i < rows * cols; i += nt) y[(int64_t)(i / cols) * ld + i % cols] = (T)0.f;
 }
 
-// SiLU for results of 16 bits: v_exp_f32 and v_rcp_f32 as they are, off by at most 2^-24 |z| and
-// three units of FP32, in a third of activate's instructions (infinities: as there)
-__device__ __forceinline__ float silu16(float z) {
-  return z * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.44269502162933349609375f));
+// SiLU's gate for results of 16 bits: v_exp_f32 and v_rcp_f32 as they are, in a third of gate's
+// instructions (infinities: as there). The exponent -z log2(e) is off by 1.3 units of 2^-24 of itself (the product's
+// rounding and the constant's), which e^-z / (1 + e^-z) <= 1 brings to at most 1.3 |z| 2^-24 of
+// the gate; exp2, the sum and the reciprocal add three units of FP32.
+__device__ __forceinline__ float gate16(float z) {
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.44269502162933349609375f));
+}
+template <int ACT, bool FAST>
+__device__ __forceinline__ float gate_as(float z) {
+  if constexpr (FAST && ACT == MACE_ACT_SILU) return gate16(z);
+  return gate<ACT>(z);
 }
 template <int ACT, bool FAST>
 __device__ __forceinline__ float activate_as(float z) {
-  if constexpr (FAST && ACT == MACE_ACT_SILU) return silu16(z);
-  return activate<ACT>(z);
+  return ACT == MACE_ACT_NONE ? z : z * gate_as<ACT, FAST>(z);
+}
+// act(z) + r: the last product and the sum are one operation wherever they stand
+template <int ACT, bool FAST>
+__device__ __forceinline__ float activate_add(float z, float r) {
+  return ACT == MACE_ACT_NONE ? z + r : __builtin_fmaf(z, gate_as<ACT, FAST>(z), r);
 }
 
 // The epilogue of a block's product: y = act(value + b) + r, z = value + b where it is
 // wanted, of the run's rows and the columns from c0 on (y and z point there).
 // value(j, i, b): the product at vector j of tile row i, as lane_values orders them, and b.
-// AHEAD tile rows of residuals are requested before the first is used, FAST: silu16.
+// AHEAD tile rows of residuals are requested before the first is used, FAST: gate16.
 template <class T, bool AL, class S, int AHEAD = 1, bool FAST = false, class F>
 __device__ __forceinline__ void linear_epilogue(const LinearArgs<T>& a, const RowRun& run, int c0, int cols, T* y, T* z,
                                                 int tid, F value) {
@@ -113,9 +126,14 @@ __device__ __forceinline__ void linear_epilogue(const LinearArgs<T>& a, const Ro
         const int n = column(j);
         if (m >= run.rows || n >= cols) continue;
         if (z) store_n(z + m * a.ldz + n, v, count(j), AL);
+        constexpr int ACT = decltype(act)::value;
+        if (res) {
 #pragma unroll
-        for (int q = 0; q < W; ++q) v[q] = activate_as<decltype(act)::value, FAST>(v[q]);
-        if (res) v += __builtin_convertvector(rj[i % RING][j], V);
+          for (int q = 0; q < W; ++q) v[q] = activate_add<ACT, FAST>(v[q], (float)rj[i % RING][j][q]);
+        } else {
+#pragma unroll
+          for (int q = 0; q < W; ++q) v[q] = activate_as<ACT, FAST>(v[q]);
+        }
         store_n(y + m * a.ldy + n, v, count(j), AL);
       }
     }
