@@ -96,15 +96,12 @@ __device__ __forceinline__ double value_of(double k) { return k; }
 __device__ __forceinline__ int no_key(int) { return kNoKey; }
 __device__ __forceinline__ double no_key(double) { return -__builtin_inff(); }
 
-// exp(-d) and 1 / (1 + exp(-x)) in either precision; NaN goes through
+// exp(-d) and 1 / (1 + exp(-x)); NaN goes through
 __device__ __forceinline__ float exp_minus(float d) { return d == d ? exp_neg(fminf(d, 200.f)) : d; }
-__device__ __forceinline__ double exp_minus(double d) { return exp(-d); }
 __device__ __forceinline__ float sigmoid_of(float x) { return x == x ? recip_ge1(1.f + exp_neg(fminf(x, 200.f))) : x; }
-__device__ __forceinline__ double sigmoid_of(double x) { return 1 / (1 + exp(-x)); }
 // A chosen expert's score over exp(m), m the largest chosen logit (of a sigmoid: at most 0), for
 // renormalised weights: no 0 / 0 where all scores underflow
-template <class R>
-__device__ __forceinline__ R relative_score(R x, R m, bool sigmoid) {
+__device__ __forceinline__ float relative_score(float x, float m, bool sigmoid) {
   if (!sigmoid) return exp_minus(m - x);
   return exp_minus(m - (x > 0 ? 0 : x)) / (1 + exp_minus(x > 0 ? x : -x));
 }
@@ -295,11 +292,15 @@ __device__ __noinline__ void choose_exact(ChooseArgs a, const T* logits, const f
 // lanes, of equal ones the first lane's, which holds the lower indices. True: a decision was
 // nearer than its error.
 //
-// Error of a score: the exponential is off by its argument's rounding, 2^-24 of |x - top| or
-// |x|, and a few units, the sum over experts by V + 6 more: ((D + 40) M) 2^-24 with D the row's
-// largest such argument and M = 1 / sum (or 1) the largest score there can be; s + b adds half a unit
-// of itself. Two keys may differ by twice that, two groups' totals by four times, and by the
-// roundings of two sums.
+// Error of a score, in units of 2^-24. Softmax: x - top, its product with the FP32 log2(e) and that constant
+// put 2.3 |d| of itself on e = exp(-|d|), d = x - top, and exp2 two: at most 0.9 + 2 of the largest e, which is 1,
+// for |d| e^-|d| <= 1 / e. Of the sum of n <= 512 scores that is 2.3 times the mean of |d| weighted with e, at
+// most 3.9 (511 experts at |d| = 4.9 beside the best), 2 more, V + 6 for its additions and 2 for the reciprocal: 27.
+// Together 30 times M = 1 / sum, the largest score there can be. Sigmoid: 1.3 |x| s (1 - s) <= 0.3
+// from the argument, and four from exp2, the sum and the reciprocal, with M = 1. The bound taken, (D + 40) M with D the
+// row's largest |d| or |x| up to 100, holds for both with room; infinite arguments (masks, places behind
+// the last expert) put D at its end. s + b adds half a unit of itself. Two keys may differ by twice the
+// bound, two groups' totals by four times, and by the roundings of two sums.
 // b: the bias, -infinity for masked experts.
 template <bool SIGMOID, int LPR, int V>
 __device__ __forceinline__ bool choose_fast(const ChooseArgs& a, const float (&x)[V], const float (&b)[V], bool biased, float top,
@@ -391,8 +392,9 @@ __device__ __forceinline__ bool choose_fast(const ChooseArgs& a, const float (&x
 
 // LPR lanes per token, V consecutive experts each. Scores in FP32; the few rows where a decision lies
 // within their error are decided again in FP64 (0.9 % of the rows below, a second pass for 1.8 % of the
-// waves; all of it in FP64, the first form, took 254 us). Bound by instructions: 36,864 tokens, 8 of 256
-// experts in 4 of 8 groups, 35.5 us, the vector units busy 68 % of it with 810 instructions for two tokens, of which
+// waves, and up to three times as many with masked experts or lanes that the experts do not fill, where the bound of
+// the error is at its end; all of it in FP64, the first form, took 254 us). Bound by instructions: 36,864 tokens, 8 of 256
+// experts in 4 of 8 groups, 35.2 us, the vector units busy 69 % of it with 810 instructions for two tokens, of which
 // the lanes' sorting takes 150, nine rounds 220, scores and masks 200, groups 95, weights 60; the 38 MB of
 // logits would take 7.5. 16 lanes of 16 experts take 45 where 32 of 8 take 41, 64 of 4 48; one kernel for both
 // scores 41.

@@ -119,9 +119,9 @@ __device__ __forceinline__ void zero_missing(const EmbedGradArgs& a, int block, 
 // the table; the parts of one that was begun before (0) or goes on behind (1; also where
 // it begins at the segment's first slot) go to part, for the join. The launch's first
 // blocks look for the rows that do not occur. No thread needs another, so that any width fills the waves. 131,072 rows
-// of 1024 bfloat16 into 32,000: 97 us, 265 MB read and 81 written; with 64 slots to a wave that walks
-// the columns 211 us, and 33 for the missing rows. Four rows in flight: eight 150 us for the whole
-// gradient against 143, sixteen 185.
+// of 1024 bfloat16 into 32,000: 97 us, 272 MB read and 83 written; with 64 slots to a wave that walks
+// the columns 211 us, and 33 for the missing rows. Four rows in flight: 125 us for the whole gradient (in a captured
+// graph, as at the rules below; its kernels one by one add up to 143), with two 124, eight 132, sixteen 165.
 template <class T, bool AL>
 __global__ void __launch_bounds__(256) embed_sum_kernel(EmbedGradArgs a, const T* __restrict__ dout, T* __restrict__ dtable) {
   constexpr int VE = kVecElems<T>, U = 4;
@@ -265,8 +265,8 @@ bool aligned(const mace_embed_desc& d, const void* a, const void* b) {
 size_t round256(size_t b) { return (b + 255) & ~size_t(255); }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Slots a block of the sort takes at a time: 131,072 ids of 32,000 rows 131.5 us for the whole gradient, with 1024
-// 139.8 (more blocks' counts to read), with 4096 134.8 (fewer CUs); 262,144 ids of 2 rows 36.3, 35.5, 40.0.
+// Slots a block of the sort takes at a time: 131,072 ids of 32,000 rows 125 us for the whole gradient, with 1024
+// 126 (more blocks' counts to read), with 4096 131 (fewer CUs); 262,144 ids of 2 rows 36.6, 35.5, 39.8.
 constexpr int kChunk = 2048;
 // Digits of the sort: ids and the number behind them, at most nine bits a pass.
 struct SortPlan {
@@ -280,7 +280,7 @@ SortPlan sort_plan(int64_t rows) {
   return {passes, (bits + passes - 1) / passes};
 }
 // Slots per segment: enough threads to fill the chip, few enough parts to join. 17,711 ids of 89 rows
-// 515 wide: 8 slots 32.7 us, 16 28.8, 32 33.5; 4,000 ids 128 wide: 8 slots 18.6, 16 20.2.
+// 515 wide: 8 slots 32.6 us, 16 28.1, 32 33.1; 4,000 ids 128 wide: 8 slots 17.3, 16 19.2.
 int segment(const mace_embed_desc& d) {
   const int64_t nv = ceil_div(d.width, d.dtype == MACE_TYPE_FP32 ? 4 : 8), least = d.n_ids < 8192 ? 8 : 16;
   return (int)std::max(least, std::min<int64_t>(64, std::max(d.n_ids * nv / (1 << 19), d.n_ids / 8192)));
@@ -321,7 +321,7 @@ BackwardPlan plan_backward(const mace_embed_desc& d) {
 using namespace mace;
 
 // Four vectors a thread from 16,384 blocks of one each on: 131,072 rows of 1024 bfloat16 (65,536)
-// 73 us against 84, 17,711 of 515 (4,497) 12.3 against 9.9.
+// 81 us against 90, 17,711 of 515 (4,497) 12.0 against 8.5.
 constexpr int64_t kManyBlocks = 1 << 14;
 
 extern "C" mace_status mace_embed_forward(const mace_embed_desc* desc, const void* table, const int32_t* ids, void* out,
@@ -377,7 +377,7 @@ extern "C" mace_status mace_embed_backward(const mace_embed_desc* desc, const vo
     const int64_t col_blocks = ceil_div(d.width, 4 * cl);
     const int64_t zero_blocks = ceil_div(d.n_rows, 256), blocks = zero_blocks + ceil_div(a.segments * a.nv, 256);
     // more lanes to a run where the average one is 128 parts or more to each group of the smaller
-    // block: 262,144 ids of 8 rows 797 wide 158 us against 184, 131,072 of 32,000 145 against 136
+    // block: 262,144 ids of 8 rows 797 wide 160 us against 184, 131,072 of 32,000 134 against 125
     const bool long_runs = a.segments / d.n_rows >= 128 * (256 / cl);
     const int64_t join_blocks = ceil_div(a.segments, long_runs ? 16 : 4) * col_blocks;
     if (!fits_grid(blocks) || !fits_grid(join_blocks)) return MACE_EUNSUPPORTED;

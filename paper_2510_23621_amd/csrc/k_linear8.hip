@@ -29,10 +29,10 @@ __device__ __forceinline__ float scaled8(int sum, float sx, float sw, float b, b
 
 // y = act(sx sw (qx qw) + b) + r: exact integer sums on v_mfma_i32_16x16x64_i8, through the
 // tiles of the 16-bit layers, which move the same bytes per instruction. 36864 x 2048 x 2048 in eight groups to
-// bfloat16: 168 us bare (1.84 POP/s, where a library product of that size reaches 1.65 and a larger one
-// 2.14), 239 with bias, SiLU and residual, whose 151 MB more and vector instructions come after the products: one
-// block per CU, and nothing to run beside. Tiles of 256 x 128 or 128 x 128, of which two blocks fit, take 215 to 282 bare.
-// Residuals four tile rows ahead: one ahead 254 us, all eight 338 (registers spill).
+// bfloat16, in a captured graph: 151 us bare (2.05 POP/s, where a library product of that size reaches 1.65 and a
+// larger one 2.14), 210 with bias, SiLU and residual, whose 151 MB more and vector instructions come after the products:
+// one block per CU, and nothing to run beside (one call at a time 235). Tiles of 128 x 128, of which two blocks fit, take
+// 189 and 250. Residuals four tile rows ahead: one ahead 217 us, all eight 213.
 template <class T, bool AL, class S>
 __global__ void __launch_bounds__(S::NT) linear8_kernel(Linear8Args<T> p) {
   __shared__ __align__(16) unsigned short lds[tile_lds<IntPair, S>];
@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(S::NT) linear8_kernel(Linear8Args<T> p) {
 // Few rows: a block of four waves forms 16 x 16 results, each wave a quarter of K, added through LDS.
 // The rows lie in LDS as integers over all of K; where they come as T the block rounds them itself
 // (no launch and no way through memory for them). The weights go straight to the matrix
-// instructions, requested before the rows. One row of 2048 bfloat16 on 2048 x 2048: 6.9 us, of
+// instructions, requested before the rows. One row of 2048 bfloat16 on 2048 x 2048: 6.0 to 7.2 us, of
 // which the weights' 4 MB take 0.8 at a copy's rate; the rest is the launch and three dependent trips to memory.
 constexpr int kThinRows = 16, kThinCols = 16, kThinLds = 56 << 10;
 // bytes from row to row: 16 more than a multiple of 128, so that eight rows' 16 bytes lie in all banks
@@ -247,8 +247,9 @@ using Mid = TileShape<128, 128, 2, 2, 64, 2, true>;
 using Small = TileShape<64, 64, 2, 2, 64, 4, true>;
 
 // Large from 192 blocks of its own on, of groups of 512 rows or more, Mid from 256: rows in 8 bits, SiLU and a
-// residual, 6144 x 2048 x 2048 (192 Large) 40 us against 52 as Mid, 4096 x 2048 x 2048 (128) 37.5 against 35.8;
-// 2048 x 2048 x 2048 (256 Mid) 19.5 against 22.2 as Small, 4096 x 512 x 512 (128) 9.2 against 6.1.
+// residual, 8192 x 2048 x 2048 (256 Large) 40 us against 44 as Mid, 6144 rows (192) 39.7 against 38.7, with K = 4096 57
+// against 60, 4096 rows (128) 35.8 against 24.4 (12288, a round and a half of Large, 71 against 66);
+// 2048 x 2048 x 2048 (256 Mid) 18.6 against 21.3 as Small, 4096 x 512 x 512 (128) 9.1 against 5.9.
 template <class F>
 mace_status with_shape(int64_t rows, int64_t cols, int64_t groups, F f) {
   if ((groups == 1 || rows / groups >= 512) && ceil_div(rows, 256) * ceil_div(cols, 256) >= 192) return f(Large{});
@@ -258,8 +259,8 @@ mace_status with_shape(int64_t rows, int64_t cols, int64_t groups, F f) {
 
 // The thin kernel up to two blocks per CU, where K fits LDS: rounding a block's rows again for every
 // 16 columns costs it more on larger launches. With rows in bfloat16 (the other way rounds them in a
-// launch of its own): 1 x 2048 x 2048 (128 blocks) 6.7 us against 11.4, 256 x 97 x 211 (224) 6.7
-// against 9.8, 64 x 512 x 2048 (512) 7.4 against 8.9, 128 x 512 x 2048 (1024) 13.2 against 8.9.
+// launch of its own): 1 x 2048 x 2048 (128 blocks) 6.0 us against 10.0, 256 x 97 x 211 (224) 6.5
+// against 8.8, 64 x 512 x 2048 (512) 7.4 against 7.6, 128 x 512 x 2048 (1024) 13.0 against 7.7.
 constexpr int kThinBlocks = 512;
 bool thin(const mace_linear_desc& d) {
   return thin_lds(d) <= kThinLds && ceil_div(d.n_rows, kThinRows) * ceil_div(d.n_out, kThinCols) <= kThinBlocks;

@@ -64,7 +64,7 @@ __global__ void __launch_bounds__(256) pack_rows_kernel(Rows8Args a, const T* __
   }
 }
 
-// x = q s, 8 columns a thread (36,864 x 2048 to bfloat16: 39 us, 5.8 TB/s)
+// x = q s, 8 columns a thread (36,864 x 2048 to bfloat16: 34 us, 6.6 TB/s)
 template <class T, bool AL>
 __global__ void __launch_bounds__(256) unpack_rows_kernel(Rows8Args a, const int8_t* __restrict__ values,
                                                           const float* __restrict__ scales, T* __restrict__ x) {

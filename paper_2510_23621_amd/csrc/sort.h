@@ -35,8 +35,8 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(Slots sl, int6
 // (earlier blocks from hist, earlier chunks and waves from their counts), and it ranks 64
 // slots at a time by matching buckets across its lanes. Integer counts only: the
 // order of the LDS additions does not matter. Up to one chunk the count is its own and
-// the sort one launch (96 slots 3.5 us, bound by the launch); 294,912 slots of 64
-// experts 14 us with the counting launch, 2^26 of 64 experts 470 us.
+// the sort one launch (96 slots 4 us, bound by the launch); 294,912 slots of 64
+// experts 12 to 14 us with the counting launch, 2^26 of 64 experts 470 us.
 // offsets [E + 1], or NULL: the first row of each bucket.
 template <class Slots, int kSortChunk>
 __global__ void __launch_bounds__(kSortThreads)
